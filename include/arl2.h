@@ -25,6 +25,9 @@
  *   arl2_hybrid_attn_fwd_fm  the readout pass that computes that query itself (fused feature map);
  *   arl2_gate_proj         the gate G = sigmoid(x W_g) of Eq. (6): headwise, one per token or element-wise.
  *
+ *   arl2_kv_append, arl2_kv_read, arl2_kv_attn_fwd   for layers that keep softmax over everything generated so far
+ *                          (Eq. (1)): a paged key/value cache held in 4 bits, and the attention that reads it.
+ *
  * Reading of the feature map: q and k arrive after RoPE, the learned 1x1 maps are
  * the identity, so phi is the L2 normalisation over the head dimension,
  * x / sqrt(sum x^2 + l2_eps), and V' = v.
@@ -264,6 +267,83 @@ size_t arl2_gdn_workspace_bytes(const arl2_desc *desc);
 arl2_status arl2_state_commit_gdn(const arl2_desc *desc,
                                   const void *k, const void *v,
                                   const float *alpha, const float *beta, float *S);
+
+/*
+ * ---- paged 4-bit key/value cache -----------------------------------------------------------------------
+ * The cache of a layer that keeps softmax (paper Eq. (1)): rows of Hkv stored heads, in pages of page_size tokens
+ * that a block table places anywhere in a pool, in 4 bits a feature and 8 more per 32 features: 68 bytes for a
+ * key row of 128 features, of which bf16 takes 256.  The pool is one array of arl2_kv_cache_bytes(desc) bytes, 16-byte aligned,
+ * whose layout is the library's own; bytes that no token was written to may hold anything.
+ *
+ * Format (the OCP microscaling format e2m1 with a power-of-two scale): 32 features of a token and head share
+ * an exponent e, the least one in [-120, 125] with max |x| <= 7 * 2^e, and each is stored as the nearest of
+ * 2^e * {0, 1/2, 1, 3/2, 2, 3, 4, 6} and their negatives (ties to the even code).  A group with a NaN or an
+ * infinity is stored as NaN.  The stored values are exact in bf16.
+ *
+ * Device-side indexes, int32, read when the kernels run (so a captured graph follows them):
+ *   block_table [B][max_pages]   page of the pool that holds tokens i * page_size .. + page_size - 1 of a stream.
+ *                                An entry outside [0, n_pages) holds no tokens: nothing is written there, zeros are
+ *                                read, attention does not see them (tokens that a sliding window dropped).
+ *                                Streams may share pages that are only read (a common prompt); if one call appends
+ *                                to the same place of a page twice, what is stored there is one of the two.
+ *   start, count, kv_len, q_len  [B] as described below.  Values beyond what the arrays hold are cut to it: count
+ *                                and q_len to [0, Lq], kv_len to [0, max_pages * page_size].
+ */
+typedef struct {
+    int32_t B;            /* streams, >= 1                                                       */
+    int32_t H;            /* query heads, a multiple of Hkv (query head h reads stored head      */
+                          /* h / (H / Hkv)); attention only                                      */
+    int32_t Hkv;          /* stored heads, >= 1                                                  */
+    int32_t Lq;           /* tokens per stream of the call's dense arrays, >= 1                  */
+    int32_t D;            /* head dimension: 64 or 128                                           */
+    int32_t page_size;    /* tokens per page: 16, 32, 64, 128 or 256                             */
+    int32_t n_pages;      /* pages of the pool, >= 1                                             */
+    int32_t max_pages;    /* block table entries per stream, >= 1; max_pages * page_size <= 2^30 */
+    int32_t causal;       /* attention: 0 every stored token is seen; 1 see arl2_kv_attn_fwd     */
+    float sm_scale;       /* attention: logit scale; 0 selects 1/sqrt(D)                         */
+    void *workspace;      /* attention: device scratch, >= arl2_kv_workspace_bytes               */
+    size_t workspace_bytes;
+    void *stream;         /* hipStream_t; NULL is the default stream                             */
+} arl2_kv_desc;
+
+/* Bytes of the pool, and the scratch that arl2_kv_attn_fwd takes for this descriptor (0: none is needed; it depends on the sizes
+ * alone, not on kv_len).  Both return 0 for an invalid descriptor. */
+size_t arl2_kv_cache_bytes(const arl2_kv_desc *desc);
+size_t arl2_kv_workspace_bytes(const arl2_kv_desc *desc);
+
+/*
+ * Writes new rows into the cache: token i < count[b] of stream b goes to position start[b] + i, over what was there.
+ *   k, v      device bf16 [B][Lq][Hkv][D]; rows from count[b] on are not read.
+ *   rope_cos, rope_sin   device fp32 [max_pages * page_size][D/2], 16-byte aligned, indexed by position: the key's pair
+ *             (k[2i], k[2i+1]) is rotated by that angle (computed in fp64, rounded once to fp32) before it is
+ *             stored.  Both NULL: no rotation.  Values are never rotated.
+ *   start     device int32 [B].       count   device int32 [B], or NULL: Lq for all.
+ *   cache     the pool.  Tokens outside [0, max_pages * page_size) and pages outside the pool are skipped; every
+ *             other byte of the pool keeps its value.
+ */
+arl2_status arl2_kv_append(const arl2_kv_desc *desc, const void *k, const void *v,
+                           const float *rope_cos, const float *rope_sin,
+                           const int32_t *block_table, const int32_t *start, const int32_t *count, void *cache);
+
+/*
+ * Gives the values that stored rows stand for: k, v [B][Lq][Hkv][D] bf16, token i < count[b] from position start[b] + i.
+ * Rows from count[b] on are left as they were; a row without a place in the cache is zero.
+ */
+arl2_status arl2_kv_read(const arl2_kv_desc *desc, const void *cache,
+                         const int32_t *block_table, const int32_t *start, const int32_t *count, void *k, void *v);
+
+/*
+ * out_i = softmax_j(sm_scale * q_i.K_j) V_j over the stored tokens j < kv_len[b] of the stream, for its query tokens
+ * i < q_len[b].  desc->causal: query i stands at position kv_len[b] - q_len[b] + i and sees the tokens up to it (the queries are
+ * the last tokens stored).  A query that sees no token gives zeros.
+ *   q         device bf16 [B][Lq][H][D]; rows from q_len[b] on are not read.  A row with a NaN or an infinity gives NaN.
+ *   kv_len    device int32 [B].       q_len   device int32 [B], or NULL: Lq for all.
+ *   out       device bf16 [B][Lq][H][D]; rows from q_len[b] on are left as they were.  Must not overlap an input.
+ * fp32 accumulation, softmax statistics and joins of the key axis, which is divided the same way for the same descriptor:
+ * results are bit-identical from run to run.  Uses desc->workspace; calls that overlap in time need one each.
+ */
+arl2_status arl2_kv_attn_fwd(const arl2_kv_desc *desc, const void *q, const void *cache,
+                             const int32_t *block_table, const int32_t *kv_len, const int32_t *q_len, void *out);
 
 const char *arl2_status_string(arl2_status s);
 

@@ -29,6 +29,7 @@ ARL2_GATE_PER_HEAD, ARL2_GATE_PER_ELEMENT, ARL2_GATE_PER_TOKEN = 0, 1, 2
 EXPORTS = ["arl2_workspace_bytes", "arl2_hybrid_attn_fwd", "arl2_state_commit", "arl2_state_commit_delta",
            "arl2_static_scratch_bytes", "arl2_state_commit_static", "arl2_state_commit_fm",
            "arl2_gdn_workspace_bytes", "arl2_state_commit_gdn", "arl2_hybrid_attn_fwd_ex", "arl2_hybrid_attn_fwd_fm", "arl2_feature_map", "arl2_gate_proj",
+           "arl2_kv_cache_bytes", "arl2_kv_workspace_bytes", "arl2_kv_append", "arl2_kv_read", "arl2_kv_attn_fwd",
            "arl2_status_string", "arl2_last_error", "arl2_version"]
 
 
@@ -38,6 +39,13 @@ class arl2_desc(ctypes.Structure):
                 ("g_dtype", ctypes.c_int32), ("sm_scale", ctypes.c_float), ("l2_eps", ctypes.c_float),
                 ("g_mode", ctypes.c_int32), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
                 ("stream", ctypes.c_void_p)]
+
+
+class arl2_kv_desc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("Lq", ctypes.c_int32),
+                ("D", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32), ("causal", ctypes.c_int32), ("sm_scale", ctypes.c_float),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)]
 
 
 class Arl2Error(RuntimeError):
@@ -106,6 +114,17 @@ def load_library() -> ctypes.CDLL:
         lib.arl2_gdn_workspace_bytes.restype = ctypes.c_size_t
         lib.arl2_state_commit_gdn.argtypes = [dp, vp, vp, vp, vp, vp]
         lib.arl2_state_commit_gdn.restype = ctypes.c_int
+        kdp = ctypes.POINTER(arl2_kv_desc)
+        lib.arl2_kv_cache_bytes.argtypes = [kdp]
+        lib.arl2_kv_cache_bytes.restype = ctypes.c_size_t
+        lib.arl2_kv_workspace_bytes.argtypes = [kdp]
+        lib.arl2_kv_workspace_bytes.restype = ctypes.c_size_t
+        lib.arl2_kv_append.argtypes = [kdp] + [vp] * 8
+        lib.arl2_kv_append.restype = ctypes.c_int
+        lib.arl2_kv_read.argtypes = [kdp] + [vp] * 6
+        lib.arl2_kv_read.restype = ctypes.c_int
+        lib.arl2_kv_attn_fwd.argtypes = [kdp] + [vp] * 6
+        lib.arl2_kv_attn_fwd.restype = ctypes.c_int
         lib.arl2_status_string.argtypes = [ctypes.c_int]
         lib.arl2_status_string.restype = ctypes.c_char_p
         lib.arl2_last_error.argtypes = []
@@ -395,6 +414,105 @@ def arl2_state_commit_gdn(k: torch.Tensor, v: torch.Tensor, alpha: torch.Tensor,
         _dev(alpha, "alpha", (B, L, H), torch.float32), _dev(beta, "beta", (B, L, H), torch.float32),
         _dev(S, "S", (B, H, D, D), torch.float32))
     _check(st)
+
+
+# ---- paged 4-bit key/value cache
+
+def _kv_token_bytes(D: int) -> int:
+    """Stored bytes of a token and head, key and value: 4 bits a feature and a scale byte for 32 of them."""
+    return 2 * (D // 2 + D // 32)
+
+
+def alloc_kv_cache(n_pages: int, heads: int, page_size: int, D: int, device="cuda") -> torch.Tensor:
+    """A pool of pages for ``heads`` stored heads of ``D`` features: uint8 [n_pages, heads, page_size, bytes of a token and head]
+    (the last two dimensions say how much a page holds, not where a token lies in it).  Not initialised: it need not be."""
+    return torch.empty((n_pages, heads, page_size, _kv_token_bytes(D)), dtype=torch.uint8, device=device)
+
+
+def _kv_desc(B, H, Hkv, Lq, D, page_size, n_pages, max_pages, causal=False, sm_scale=0.0,
+             workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> arl2_kv_desc:
+    return arl2_kv_desc(B, H, Hkv, Lq, D, page_size, n_pages, max_pages, 1 if causal else 0, sm_scale,
+                        _dev(workspace, "workspace"), 0 if workspace is None else workspace.nbytes,
+                        _current_stream() if stream is None else stream)
+
+
+def arl2_kv_workspace_bytes(B: int, H: int, Hkv: int, Lq: int, D: int, page_size: int, max_pages: int) -> int:
+    """Device scratch bytes that arl2_kv_attn_fwd needs for these sizes (0: none)."""
+    d = _kv_desc(B, H, Hkv, Lq, D, page_size, 1, max_pages, stream=0)
+    return int(load_library().arl2_kv_workspace_bytes(ctypes.byref(d)))
+
+
+def alloc_kv_workspace(B: int, H: int, Hkv: int, Lq: int, D: int, page_size: int, max_pages: int, device="cuda") -> Optional[torch.Tensor]:
+    """Convenience: a torch buffer of arl2_kv_workspace_bytes() bytes, or None where none is needed."""
+    n = arl2_kv_workspace_bytes(B, H, Hkv, Lq, D, page_size, max_pages)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def _kv_sizes(cache: torch.Tensor, block_table: torch.Tensor, B: int, Hkv: Optional[int], D: int) -> tuple:
+    """n_pages, stored heads, page size and table width, from a pool and a block table that fit rows of D features."""
+    if cache.dim() != 4 or cache.dtype != torch.uint8 or cache.shape[3] != _kv_token_bytes(D):
+        raise ValueError(f"cache must be uint8 [n_pages, heads, page_size, {_kv_token_bytes(D)}] for {D} features")
+    if Hkv is not None and cache.shape[1] != Hkv:
+        raise ValueError(f"cache holds {cache.shape[1]} heads, expected {Hkv}")
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError(f"block_table must be [{B}, max_pages]")
+    return cache.shape[0], cache.shape[1], cache.shape[2], block_table.shape[1]
+
+
+def _one_device(*tensors) -> None:
+    """The kernels run on the current device, whose memory all tensors have to be."""
+    here = {t.device for t in tensors if t is not None}
+    if len(here) > 1 or (torch.cuda.is_initialized() and next(iter(here)).index != torch.cuda.current_device()):
+        raise ValueError(f"all tensors must be on the current device, got {sorted(map(str, here))}")
+
+
+def arl2_kv_append(k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, start: torch.Tensor, *,
+                   count: Optional[torch.Tensor] = None, rope_cos: Optional[torch.Tensor] = None,
+                   rope_sin: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> None:
+    """Rotates (with tables [max_pages * page_size, D/2] by position) and quantises k, v [B, L, heads, D] bf16 into ``cache`` (see
+    ``alloc_kv_cache``): token i < count[b] (None: L) of stream b to position start[b] + i of the pages block_table [B, max_pages]."""
+    if k.dim() != 4:
+        raise ValueError("k must be [B, L, heads, D]")
+    B, L, Hkv, D = k.shape
+    n_pages, _, page, width = _kv_sizes(cache, block_table, B, Hkv, D)
+    ptrs = (_dev(k, "k", None, torch.bfloat16), _dev(v, "v", (B, L, Hkv, D), torch.bfloat16),
+            _dev(rope_cos, "rope_cos", (width * page, D // 2), torch.float32), _dev(rope_sin, "rope_sin", (width * page, D // 2), torch.float32),
+            _dev(block_table, "block_table", None, torch.int32), _dev(start, "start", (B,), torch.int32),
+            _dev(count, "count", (B,), torch.int32), _dev(cache, "cache"))
+    _one_device(k, v, rope_cos, rope_sin, block_table, start, count, cache)
+    d = _kv_desc(B, Hkv, Hkv, L, D, page, n_pages, width, stream=stream)
+    _check(load_library().arl2_kv_append(ctypes.byref(d), *ptrs))
+
+
+def arl2_kv_read(cache: torch.Tensor, block_table: torch.Tensor, start: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *,
+                 count: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> None:
+    """The values of stored rows into k, v [B, L, heads, D] bf16: token i < count[b] (None: L) from position start[b] + i."""
+    if k.dim() != 4:
+        raise ValueError("k must be [B, L, heads, D]")
+    B, L, Hkv, D = k.shape
+    n_pages, _, page, width = _kv_sizes(cache, block_table, B, Hkv, D)
+    ptrs = (_dev(cache, "cache"), _dev(block_table, "block_table", None, torch.int32), _dev(start, "start", (B,), torch.int32),
+            _dev(count, "count", (B,), torch.int32), _dev(k, "k", None, torch.bfloat16), _dev(v, "v", (B, L, Hkv, D), torch.bfloat16))
+    _one_device(cache, block_table, start, count, k, v)
+    d = _kv_desc(B, Hkv, Hkv, L, D, page, n_pages, width, stream=stream)
+    _check(load_library().arl2_kv_read(ctypes.byref(d), *ptrs))
+
+
+def arl2_kv_attn_fwd(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor, out: torch.Tensor, *,
+                     q_len: Optional[torch.Tensor] = None, causal: bool = False, sm_scale: float = 0.0,
+                     workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> None:
+    """Softmax attention of q [B, L, H, D] bf16 over the kv_len[b] stored tokens of each stream into ``out``, H a multiple of the
+    stored heads; ``causal``: the q_len[b] (None: L) queries are the last tokens stored and see those up to their own.  ``workspace``:
+    of ``arl2_kv_workspace_bytes`` (``alloc_kv_workspace``), one for each call in flight."""
+    if q.dim() != 4:
+        raise ValueError("q must be [B, L, H, D]")
+    B, L, H, D = q.shape
+    n_pages, Hkv, page, width = _kv_sizes(cache, block_table, B, None, D)
+    ptrs = (_dev(q, "q", None, torch.bfloat16), _dev(cache, "cache"), _dev(block_table, "block_table", None, torch.int32),
+            _dev(kv_len, "kv_len", (B,), torch.int32), _dev(q_len, "q_len", (B,), torch.int32), _dev(out, "out", (B, L, H, D), torch.bfloat16))
+    _one_device(q, cache, block_table, kv_len, q_len, out, workspace)
+    d = _kv_desc(B, H, Hkv, L, D, page, n_pages, width, causal, sm_scale, workspace, stream)
+    _check(load_library().arl2_kv_attn_fwd(ctypes.byref(d), *ptrs))
 
 
 def arl2_version() -> int:

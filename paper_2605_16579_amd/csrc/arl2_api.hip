@@ -81,6 +81,74 @@ size_t commit_workspace_of(const arl2_desc *d, int nsplit)
 size_t commit_workspace(const arl2_desc *d) { return commit_workspace_of(d, arl2::commit_delta_max_nsplit(d->B, d->H, d->Lq)); }
 size_t commit_workspace_plain(const arl2_desc *d) { return commit_workspace_of(d, arl2::commit_nsplit(d->B, d->H, d->Lq)); }
 
+// ---- paged 4-bit key/value cache
+
+arl2_status check_kv_desc(const arl2_kv_desc *d)
+{
+    if (d == nullptr) return fail(ARL2_ERR_INVALID_ARG, "desc is NULL");
+    if (d->B < 1 || d->Hkv < 1 || d->Lq < 1 || d->n_pages < 1 || d->max_pages < 1)
+        return fail(ARL2_ERR_INVALID_ARG, "B, Hkv, Lq, n_pages and max_pages must all be >= 1");
+    if (d->D != 64 && d->D != 128) return fail(ARL2_ERR_UNSUPPORTED, "D must be 64 or 128");
+    if (d->page_size < 16 || d->page_size > 256 || (d->page_size & (d->page_size - 1)))
+        return fail(ARL2_ERR_UNSUPPORTED, "page_size must be 16, 32, 64, 128 or 256");
+    if ((double)d->max_pages * d->page_size > 1073741824.0)
+        return fail(ARL2_ERR_UNSUPPORTED, "max_pages * page_size must stay below 2^30");
+    if ((double)d->B * d->Lq > 2.0e9 || (double)d->B * d->Hkv > 1.0e6 || (double)d->n_pages * d->Hkv > 2.0e9)
+        return fail(ARL2_ERR_UNSUPPORTED, "problem too large (B*Lq and n_pages*Hkv must stay below 2e9, B*Hkv below 1e6)");
+    return ARL2_OK;
+}
+
+// The same with what attention needs beyond it.
+arl2_status check_kv_attn_desc(const arl2_kv_desc *d)
+{
+    const arl2_status st = check_kv_desc(d);
+    if (st != ARL2_OK) return st;
+    if (d->H < 1 || d->H % d->Hkv) return fail(ARL2_ERR_INVALID_ARG, "H must be a positive multiple of Hkv");
+    if (d->causal != 0 && d->causal != 1) return fail(ARL2_ERR_INVALID_ARG, "causal must be 0 or 1");
+    if (!(d->sm_scale >= 0.f) || d->sm_scale > FLT_MAX) return fail(ARL2_ERR_INVALID_ARG, "sm_scale must be finite and >= 0 (0 selects the default)");
+    if ((double)d->B * d->H > 1.0e6 || (double)d->Lq * d->H > 2.0e9)
+        return fail(ARL2_ERR_UNSUPPORTED, "problem too large (B*H must stay below 1e6, Lq*H below 2e9)");
+    return ARL2_OK;
+}
+
+arl2::KvPool kv_pool(const arl2_kv_desc *d)
+{
+    arl2::KvPool p;
+    p.shift = 0;
+    while ((1 << p.shift) < d->page_size) ++p.shift;
+    p.heads = d->Hkv;
+    p.n_pages = d->n_pages;
+    p.max_pages = d->max_pages;
+    return p;
+}
+size_t kv_rows_bytes(const arl2_kv_desc *d, int heads) { return (size_t)d->B * d->Lq * heads * d->D * 2; }
+size_t kv_table_bytes(const arl2_kv_desc *d) { return (size_t)d->B * d->max_pages * sizeof(int32_t); }
+arl2::KvAttnPlan kv_plan(const arl2_kv_desc *d) { return arl2::kv_attn_plan(d->B, d->Lq, d->H / d->Hkv, kv_pool(d), d->D); }
+
+struct Range { const void *p; size_t n; };
+
+// Does `out` share a byte with one of the inputs?
+template <int N>
+bool overlaps_any(Range out, const Range (&in)[N])
+{
+    for (const Range &r : in)
+        if (overlaps(out.p, out.n, r.p, r.n)) return true;
+    return false;
+}
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// The kernels give a thread to 8 features of four tokens.
+bool kv_rows_fit(const arl2_kv_desc *d) { return (double)d->B * d->Hkv * ((d->Lq + 3.0) / 4 + 1) * (d->D / 8) <= 2147483000.0; }
+
+arl2::KvRowsArgs kv_rows_args(const arl2_kv_desc *d, const int32_t *table, const int32_t *start, const int32_t *count)
+{
+    arl2::KvRowsArgs a = {};
+    a.table = table; a.start = start; a.count = count;
+    a.pool = kv_pool(d);
+    a.B = d->B; a.L = d->Lq; a.D = d->D;
+    return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -435,6 +503,100 @@ arl2_status arl2_state_commit_static(const arl2_desc *desc, const void *k, const
     d.workspace = ptr;
     d.workspace_bytes = kStaticScratchBytes;
     return commit_common(&d, k, v, gate, nullptr, false, S);
+}
+
+// ---- paged 4-bit key/value cache ----------------------------------------------------------------------
+size_t arl2_kv_cache_bytes(const arl2_kv_desc *desc)
+{
+    return check_kv_desc(desc) == ARL2_OK ? arl2::kv_pool_bytes(kv_pool(desc), desc->D) : 0;
+}
+
+size_t arl2_kv_workspace_bytes(const arl2_kv_desc *desc)
+{
+    return check_kv_attn_desc(desc) == ARL2_OK ? kv_plan(desc).bytes : 0;
+}
+
+arl2_status arl2_kv_append(const arl2_kv_desc *desc, const void *k, const void *v, const float *rope_cos, const float *rope_sin,
+                           const int32_t *block_table, const int32_t *start, const int32_t *count, void *cache)
+{
+    const arl2_status st = check_kv_desc(desc);
+    if (st != ARL2_OK) return st;
+    if (!k || !v || !block_table || !start || !cache)
+        return fail(ARL2_ERR_INVALID_ARG, "k, v, block_table, start and cache must not be NULL");
+    if ((rope_cos == nullptr) != (rope_sin == nullptr))
+        return fail(ARL2_ERR_INVALID_ARG, "rope_cos and rope_sin must be given together");
+    if (!aligned16(k) || !aligned16(v) || !aligned16(cache) || !aligned16(rope_cos) || !aligned16(rope_sin))
+        return fail(ARL2_ERR_INVALID_ARG, "k, v, cache, rope_cos and rope_sin must be 16-byte aligned");
+    if (!aligned4(block_table) || !aligned4(start) || !aligned4(count))
+        return fail(ARL2_ERR_INVALID_ARG, "block_table, start and count must be 4-byte aligned");
+    if (!kv_rows_fit(desc)) return fail(ARL2_ERR_UNSUPPORTED, "problem too large (B * Hkv * Lq * D must stay below 2^36)");
+    const size_t rows = kv_rows_bytes(desc, desc->Hkv), lens = desc->B * sizeof(int32_t);
+    const size_t rope = (size_t)desc->max_pages * desc->page_size * (desc->D / 2) * sizeof(float);
+    const Range in[] = {{k, rows}, {v, rows}, {rope_cos, rope}, {rope_sin, rope}, {block_table, kv_table_bytes(desc)}, {start, lens}, {count, lens}};
+    if (overlaps_any({cache, arl2_kv_cache_bytes(desc)}, in)) return fail(ARL2_ERR_INVALID_ARG, "the cache must not overlap an input");
+
+    arl2::KvRowsArgs a = kv_rows_args(desc, block_table, start, count);
+    a.k = k; a.v = v; a.cs = rope_cos; a.sn = rope_sin; a.cache = cache;
+    const hipError_t e = arl2::launch_kv_append(a, reinterpret_cast<hipStream_t>(desc->stream));
+    if (e != hipSuccess) return fail(ARL2_ERR_DEVICE, "append launch failed: %s", hipGetErrorString(e));
+    return ARL2_OK;
+}
+
+arl2_status arl2_kv_read(const arl2_kv_desc *desc, const void *cache, const int32_t *block_table, const int32_t *start, const int32_t *count,
+                         void *k, void *v)
+{
+    const arl2_status st = check_kv_desc(desc);
+    if (st != ARL2_OK) return st;
+    if (!k || !v || !block_table || !start || !cache)
+        return fail(ARL2_ERR_INVALID_ARG, "cache, block_table, start, k and v must not be NULL");
+    if (!aligned16(k) || !aligned16(v) || !aligned16(cache)) return fail(ARL2_ERR_INVALID_ARG, "cache, k and v must be 16-byte aligned");
+    if (!aligned4(block_table) || !aligned4(start) || !aligned4(count))
+        return fail(ARL2_ERR_INVALID_ARG, "block_table, start and count must be 4-byte aligned");
+    if (!kv_rows_fit(desc)) return fail(ARL2_ERR_UNSUPPORTED, "problem too large (B * Hkv * Lq * D must stay below 2^36)");
+    const size_t rows = kv_rows_bytes(desc, desc->Hkv), lens = desc->B * sizeof(int32_t);
+    const Range in[] = {{cache, arl2_kv_cache_bytes(desc)}, {block_table, kv_table_bytes(desc)}, {start, lens}, {count, lens}};
+    if (overlaps_any({k, rows}, in) || overlaps_any({v, rows}, in) || overlaps(k, rows, v, rows))
+        return fail(ARL2_ERR_INVALID_ARG, "k and v must overlap neither an input nor each other");
+
+    arl2::KvRowsArgs a = kv_rows_args(desc, block_table, start, count);
+    a.cache = const_cast<void *>(cache); a.k_out = k; a.v_out = v;
+    const hipError_t e = arl2::launch_kv_read(a, reinterpret_cast<hipStream_t>(desc->stream));
+    if (e != hipSuccess) return fail(ARL2_ERR_DEVICE, "read launch failed: %s", hipGetErrorString(e));
+    return ARL2_OK;
+}
+
+arl2_status arl2_kv_attn_fwd(const arl2_kv_desc *desc, const void *q, const void *cache, const int32_t *block_table, const int32_t *kv_len,
+                             const int32_t *q_len, void *out)
+{
+    const arl2_status st = check_kv_attn_desc(desc);
+    if (st != ARL2_OK) return st;
+    if (!q || !cache || !block_table || !kv_len || !out)
+        return fail(ARL2_ERR_INVALID_ARG, "q, cache, block_table, kv_len and out must not be NULL");
+    if (!aligned16(q) || !aligned16(cache) || !aligned16(out)) return fail(ARL2_ERR_INVALID_ARG, "q, cache and out must be 16-byte aligned");
+    if (!aligned4(block_table) || !aligned4(kv_len) || !aligned4(q_len))
+        return fail(ARL2_ERR_INVALID_ARG, "block_table, kv_len and q_len must be 4-byte aligned");
+    const arl2::KvAttnPlan plan = kv_plan(desc);
+    if ((double)plan.units * plan.nsplit > 2147483000.0 || (double)plan.units * plan.tile_rows > 2147483000.0)
+        return fail(ARL2_ERR_UNSUPPORTED, "problem too large for one launch");
+    if (plan.bytes > 0 && (desc->workspace == nullptr || desc->workspace_bytes < plan.bytes))
+        return fail(ARL2_ERR_WORKSPACE, "workspace is NULL or smaller than arl2_kv_workspace_bytes()");
+    if (!aligned16(desc->workspace)) return fail(ARL2_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    const size_t rows = kv_rows_bytes(desc, desc->H), lens = desc->B * sizeof(int32_t);
+    const Range in[] = {{q, rows}, {cache, arl2_kv_cache_bytes(desc)}, {block_table, kv_table_bytes(desc)}, {kv_len, lens}, {q_len, lens}};
+    const Range ws = {desc->workspace, plan.bytes};
+    if (overlaps_any({out, rows}, in)) return fail(ARL2_ERR_INVALID_ARG, "out must not overlap an input");
+    if (overlaps_any(ws, in) || overlaps(ws.p, ws.n, out, rows))
+        return fail(ARL2_ERR_INVALID_ARG, "the workspace must overlap neither an input nor out");
+
+    arl2::KvAttnArgs a = {};
+    a.q = q; a.cache = cache; a.table = block_table; a.kv_len = kv_len; a.q_len = q_len; a.out = out;
+    a.pool = kv_pool(desc);
+    a.B = desc->B; a.H = desc->H; a.Lq = desc->Lq; a.D = desc->D; a.G = desc->H / desc->Hkv;
+    a.causal = desc->causal;
+    a.scale_log2 = (desc->sm_scale > 0.f ? desc->sm_scale : 1.0f / sqrtf((float)desc->D)) * 1.4426950408889634f;
+    const hipError_t e = arl2::launch_kv_attn(a, plan, desc->workspace, reinterpret_cast<hipStream_t>(desc->stream));
+    if (e != hipSuccess) return fail(ARL2_ERR_DEVICE, "attention launch failed: %s", hipGetErrorString(e));
+    return ARL2_OK;
 }
 
 const char *arl2_status_string(arl2_status s)

@@ -11,6 +11,8 @@
 #include <type_traits>
 #include <utility>
 
+#include "arl2_kv_layout.h"
+
 namespace arl2 {
 
 typedef __bf16 bf16_t;
@@ -103,6 +105,43 @@ struct GdnArgs {
     float l2_eps;
 };
 
+// Rows of the paged 4-bit cache: append (k, v in, cache written) and read (cache in, k_out, v_out written).
+struct KvRowsArgs {
+    const void *k, *v;     // [B][L][heads][D] bf16
+    void *k_out, *v_out;   // likewise
+    void *cache;
+    const float *cs, *sn;  // [positions][D/2] rotation tables of the keys, or both nullptr
+    const int32_t *table;  // [B][max_pages]
+    const int32_t *start;  // [B]
+    const int32_t *count;  // [B], or nullptr: L for all
+    KvPool pool;
+    int B, L, D;
+};
+
+struct KvAttnArgs {
+    const void *q;         // [B][Lq][H][D] bf16
+    const void *cache;
+    const int32_t *table;  // [B][max_pages]
+    const int32_t *kv_len; // [B]
+    const int32_t *q_len;  // [B], or nullptr: Lq for all
+    void *out;             // [B][Lq][H][D] bf16
+    float *part_o, *part_ml;   // partial results [unit][split][tile_rows][D], and their maximum and sum
+    KvPool pool;
+    int B, H, Lq, D;
+    int G;                 // query heads per stored head
+    int causal;
+    int n_tiles, nsplit, chunk, tile_rows;     // from the plan
+    float scale_log2;      // sm_scale * log2(e)
+};
+
+// How a call of attention over the cache is divided: query tiles per (stream, stored head), splits of `chunk` tokens each.
+struct KvAttnPlan {
+    long long n_tiles, units;     // units: B * stored heads * n_tiles
+    int nsplit, chunk, tile_rows;
+    size_t o_bytes, bytes;        // of the workspace: the partial outputs, all
+};
+KvAttnPlan kv_attn_plan(int B, int Lq, int G, const KvPool &pool, int D);
+
 // Token splits of the bf16 commit for a problem size, and the most that the delta rule takes: they also size the workspace.
 int commit_nsplit(int B, int H, int L);
 int commit_delta_max_nsplit(int B, int H, int L);
@@ -118,6 +157,10 @@ hipError_t launch_commit_reduce_bf16(const CommitArgs &a, hipStream_t stream);
 hipError_t launch_commit_gdn_bf16(const GdnArgs &a, hipStream_t stream);
 hipError_t launch_feature_map_bf16(const FmapArgs &a, hipStream_t stream);
 hipError_t launch_gate_proj_bf16(const GateArgs &a, hipStream_t stream);
+
+hipError_t launch_kv_append(const KvRowsArgs &a, hipStream_t stream);
+hipError_t launch_kv_read(const KvRowsArgs &a, hipStream_t stream);
+hipError_t launch_kv_attn(KvAttnArgs a, const KvAttnPlan &p, void *workspace, hipStream_t stream);
 
 // Workspace of the token-sequential commit (per-block transition maps).
 size_t gdn_workspace_bytes(int B, int H, int L, int D);
