@@ -93,6 +93,7 @@ arl2_status check_kv_desc(const arl2_kv_desc *d)
         return fail(ARL2_ERR_UNSUPPORTED, "page_size must be 16, 32, 64, 128 or 256");
     if ((double)d->max_pages * d->page_size > 1073741824.0)
         return fail(ARL2_ERR_UNSUPPORTED, "max_pages * page_size must stay below 2^30");
+    if ((double)d->Hkv * d->page_size * (d->D + d->D / 16) > 4294967295.0) return fail(ARL2_ERR_UNSUPPORTED, "a page must stay below 4 GiB");
     if ((double)d->B * d->Lq > 2.0e9 || (double)d->B * d->Hkv > 1.0e6 || (double)d->n_pages * d->Hkv > 2.0e9)
         return fail(ARL2_ERR_UNSUPPORTED, "problem too large (B*Lq and n_pages*Hkv must stay below 2e9, B*Hkv below 1e6)");
     return ARL2_OK;

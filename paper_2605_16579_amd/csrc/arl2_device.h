@@ -137,6 +137,7 @@ struct KvAttnArgs {
 // How a call of attention over the cache is divided: query tiles per (stream, stored head), splits of `chunk` tokens each.
 struct KvAttnPlan {
     long long n_tiles, units;     // units: B * stored heads * n_tiles
+    int tiled;                    // by the kernel of many rows per workgroup
     int nsplit, chunk, tile_rows;
     size_t o_bytes, bytes;        // of the workspace: the partial outputs, all
 };

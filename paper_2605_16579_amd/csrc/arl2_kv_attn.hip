@@ -1,73 +1,14 @@
 // Attention over the paged 4-bit key/value cache (gfx950):
 //   out_i = sum_j softmax_j(sm_scale * q_i.K_j) V_j      over the stored tokens j of the stream, all or (causal) up to query i
-#include "arl2_device.h"
+#include "arl2_kv_attn.h"
 
 #include <limits.h>
 
 namespace arl2 {
 namespace {
 
-typedef __attribute__((ext_vector_type(6))) uint32_t u32x6;
-typedef __attribute__((ext_vector_type(8))) int i32x8;
-typedef __attribute__((ext_vector_type(32))) __bf16 bf16x32;
-typedef __attribute__((ext_vector_type(32))) float f32x32;
-
 constexpr int kRows = 32;        // query rows of a workgroup
-constexpr int kKeys = 32;        // keys of a block
 constexpr int kWaves = 4;
-constexpr int kParts = 3;        // of a query feature
-
-// What one workgroup's query rows may see.  A row is a (query token, query head of the stored head's group).
-struct Span {
-    int klen, qn;        // stored tokens of the stream, its query tokens
-    int rows;            // query rows there are
-    __device__ __forceinline__ int limit(int row, const KvAttnArgs &a) const
-    {
-        return a.causal ? kv_clamp(klen - qn + row / a.G + 1, klen) : klen;
-    }
-};
-__device__ __forceinline__ Span span_of(const KvAttnArgs &a, int b)
-{
-    Span s;
-    s.klen = kv_clamp(a.kv_len[b], kv_capacity(a.pool));
-    s.qn = a.q_len != nullptr ? kv_clamp(a.q_len[b], a.Lq) : a.Lq;
-    s.rows = s.qn * a.G;
-    return s;
-}
-
-// Query features as B operands: lane (c, hh) has features 64 s + 32 hh .. + 31 of row c, as e2m1-scaled parts.
-template <int D>
-struct Query {
-    static constexpr int STEPS = D / 64;
-    u32x6 part[STEPS][kParts];
-    uint32_t scale[STEPS];           // byte p: of part p
-    __device__ __forceinline__ void load(const bf16_t *row, bool there)
-    {
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            union { u32x4 u[4]; bf16x32 v; } x;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x.u[i] = there ? *(const u32x4 *)(row + 64 * s + 8 * i) : u32x4{0, 0, 0, 0};
-            uint32_t m = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) m = max(m, max(x.u[i][j] << 16 & 0x7fffffffu, x.u[i][j] & 0x7fff0000u));
-            const bool finite = m < 0x7f800000u;
-            const int e = finite ? max((int)(m >> 23) - 2, 27) : 127;      // largest magnitude in [4, 8) 2^(e - 127)
-            scale[s] = (uint32_t)e | (uint32_t)(e - 4) << 8 | (uint32_t)(e - 8) << 16;
-            if (!finite) scale[s] |= 255u;
-#pragma unroll
-            for (int p = 0; p < kParts; ++p) {
-                const float unit = __uint_as_float((uint32_t)(e - 4 * p) << 23);
-                part[s][p] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x.v, unit);
-                const f32x32 taken = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(part[s][p], unit);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) x.v[j] = to_bf16((float)x.v[j] - taken[j]);
-            }
-        }
-    }
-};
 
 // One block of 32 stored tokens in registers.
 template <int D>
@@ -107,16 +48,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_stream_kernel(KvAttnArgs a)
     Query<D> q;
     q.load((const bf16_t *)a.q + q_row + 32 * hh, row_there);
 
-    // Keys are dealt to the rows of the first product so that the logits of lane (c, hh) belong to keys 16 hh .. 16 hh + 15 in
-    // order: accumulator r of half-wave hh is row 8 (r / 4) + 4 hh + r % 4.
-    const int key_of_row = 16 * ((c >> 2) & 1) + 8 * (c >> 4) + 4 * ((c >> 3) & 1) + (c & 3);
+    // Keys are dealt to the rows of the first product so that the logits of lane (c, hh) belong to keys 16 hh .. 16 hh + 15 of the
+    // block in order: accumulator r of half-wave hh is row 8 (r / 4) + 4 hh + r % 4.
+    const int row_key = 16 * ((c >> 2) & 1) + 8 * (c >> 4) + 4 * ((c >> 3) & 1) + (c & 3);
     const int32_t *table = a.table + (size_t)b * a.pool.max_pages;
     const unsigned char *pool = (const unsigned char *)a.cache;
     const int shift = a.pool.shift, in_page = (1 << shift) - 1;
     auto head = [&](int page) { return pool + kv_head_offset(a.pool, D, page < 0 ? 0 : page, h); };
     auto load = [&](Block<D> &x, int key0, int page_k, int page_v) {
         const unsigned char *kb = head(page_k), *vb = head(page_v);
-        const int tk = (key0 + key_of_row) & in_page, tv = (key0 + 16 * hh) & in_page;
+        const int tk = (key0 + row_key) & in_page, tv = (key0 + 16 * hh) & in_page;
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) x.k[s] = *(const u32x4 *)(kb + kv_key_codes(tk, 32 * s + 16 * hh, D));
         if constexpr (D == 128) x.ks = *(const uint32_t *)(kb + kv_key_scales(shift, tk, 0, D)) >> (8 * hh);
@@ -202,8 +143,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_stream_kernel(KvAttnArgs a)
                 uint32_t w[8];
                 static_for<0, 8>([&](auto j_) {
                     constexpr int j = decltype(j_)::value, t = 8 * u + j;
-                    const float sc = __uint_as_float(((x.vs[s][t >> 2] >> (8 * (t & 3))) & 255u) << 23);
-                    w[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.v[s][t >> 2], sc, t & 3));
+                    w[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.v[s][t >> 2], scale_operand<(t & 3)>(x.vs[s][t >> 2]), t & 3));
                 });
                 union { u32x4 u; bf16x8 v; } even, odd;
 #pragma unroll
@@ -223,7 +163,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_stream_kernel(KvAttnArgs a)
         Block<D> x, y;
         auto pages = [&](int blk, int &pk, int &pv) {
             const int key0 = kbeg + blk * kKeys;
-            pk = kv_page(a.pool, table, key0 + key_of_row);
+            pk = kv_page(a.pool, table, key0 + row_key);
             pv = kv_page(a.pool, table, key0 + 16 * hh);
         };
         int pk = 0, pv = 0;
@@ -319,9 +259,9 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a)
     const int unit = blockIdx.x / a.tile_rows, rr = blockIdx.x % a.tile_rows;
     const int qt = unit % a.n_tiles, bh = unit / a.n_tiles, h = bh % a.pool.heads, b = bh / a.pool.heads;
     const Span sp = span_of(a, b);
-    const int row0 = qt * kRows, row = row0 + rr;
+    const int row0 = qt * a.tile_rows, row = row0 + rr;
     if (row >= sp.rows) return;
-    const int lim_max = sp.limit(min(row0 + kRows, sp.rows) - 1, a);
+    const int lim_max = sp.limit(min(row0 + a.tile_rows, sp.rows) - 1, a);
     if (lim_max <= a.chunk) return;                    // written by the one workgroup that saw it all
     const int n = (lim_max + a.chunk - 1) / a.chunk;
     const int g = threadIdx.x / LANES, d = 4 * (threadIdx.x % LANES);
@@ -367,24 +307,34 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a)
 
 }  // namespace
 
-// Splits of the key axis: the tokens of one and their number, from the sizes alone.
 KvAttnPlan kv_attn_plan(int B, int Lq, int G, const KvPool &pool, int D)
 {
-    KvAttnPlan p;
-    const long long rows = (long long)Lq * G;
-    const long long tiles = (rows + kRows - 1) / kRows;
-    const long long cap = kv_capacity(pool);
-    const long long units = (long long)B * pool.heads * tiles;
-    p.tile_rows = (int)(rows < kRows ? rows : kRows);
+    KvAttnPlan p = {};
+    const long long rows = (long long)Lq * G, cap = kv_capacity(pool), heads = (long long)B * pool.heads;
+    p.tiled = rows > 64;
+    p.tile_rows = p.tiled ? kTileRows : (int)(rows < kRows ? rows : kRows);
+    p.n_tiles = (rows + p.tile_rows - 1) / p.tile_rows;
+    p.units = heads * p.n_tiles;
     long long chunk = 256;
-    while (chunk < 2048 && units * ((cap + chunk - 1) / chunk) > 1024) chunk *= 2;
-    if (units >= 1024) chunk = cap;
+    if (p.tiled) {
+        // the fewest rounds of one workgroup per CU, each split paying for its partial results
+        double best = 1e30;
+        for (int s = 1; s <= 32; ++s) {
+            const long long tokens = ((cap + s - 1) / s + 255) / 256 * 256;
+            const long long n = (cap + tokens - 1) / tokens;
+            const double rounds = (double)((p.units * n + kNumCu - 1) / kNumCu);
+            const double us = rounds * (tokens / 64 * 1.4 + 8) + (n > 1 ? 5 + (double)heads * rows * n * D * 8 / 4.5e6 : 0);
+            if (us < best) { best = us; chunk = tokens; }
+        }
+    } else {
+        while (chunk < 2048 && p.units * ((cap + chunk - 1) / chunk) > 1024) chunk *= 2;
+        if (p.units >= 1024) chunk = cap;
+    }
     p.nsplit = (int)((cap + chunk - 1) / chunk);
     p.chunk = (int)chunk;
-    p.n_tiles = tiles;
-    p.units = units;
-    p.o_bytes = p.nsplit > 1 ? (size_t)units * p.nsplit * p.tile_rows * D * sizeof(float) : 0;
-    p.bytes = p.nsplit > 1 ? p.o_bytes + (size_t)units * p.nsplit * p.tile_rows * 2 * sizeof(float) : 0;
+    const size_t slots = (size_t)p.units * p.nsplit * p.tile_rows;
+    p.o_bytes = p.nsplit > 1 ? slots * D * sizeof(float) : 0;
+    p.bytes = p.nsplit > 1 ? p.o_bytes + slots * 2 * sizeof(float) : 0;
     return p;
 }
 
@@ -397,7 +347,7 @@ hipError_t launch_kv_attn(KvAttnArgs a, const KvAttnPlan &p, void *workspace, hi
     a.part_o = (float *)workspace;
     a.part_ml = (float *)((unsigned char *)workspace + p.o_bytes);
     const dim3 grid((unsigned)(p.units * p.nsplit)), block(64 * kWaves);
-    hipError_t e = a.D == 128 ? launch_kernel(kv_stream_kernel<128>, grid, block, stream, a) : launch_kernel(kv_stream_kernel<64>, grid, block, stream, a);
+    hipError_t e = p.tiled ? launch_kv_tile(a, grid.x, stream) : a.D == 128 ? launch_kernel(kv_stream_kernel<128>, grid, block, stream, a) : launch_kernel(kv_stream_kernel<64>, grid, block, stream, a);
     if (e != hipSuccess || p.nsplit == 1) return e;
     const dim3 jgrid((unsigned)(p.units * p.tile_rows));
     return a.D == 128 ? launch_kernel(kv_join_kernel<128>, jgrid, dim3(256), stream, a) : launch_kernel(kv_join_kernel<64>, jgrid, dim3(256), stream, a);

@@ -153,7 +153,8 @@ def test_refusals_of_the_descriptor(A):
     for call in (_append, _read, _attn):
         for bad in (dict(B=0), dict(Hkv=0), dict(Lq=0), dict(Lq=-3), dict(n_pages=0), dict(max_pages=0)):
             assert call(A, _desc(A, **bad)) == 1, (call, bad)
-        for bad in (dict(D=96), dict(D=256), dict(page_size=8), dict(page_size=48), dict(page_size=512), dict(max_pages=2 ** 25), dict(B=10 ** 6), dict(n_pages=2 ** 31 - 1)):
+        for bad in (dict(D=96), dict(D=256), dict(page_size=8), dict(page_size=48), dict(page_size=512), dict(max_pages=2 ** 25), dict(B=10 ** 6), dict(n_pages=2 ** 31 - 1),
+                    dict(B=1, Hkv=130000, H=130000, page_size=256)):
             assert call(A, _desc(A, **bad)) == 2, (call, bad)
     for bad in (dict(H=0), dict(H=7), dict(causal=2), dict(sm_scale=-1.0), dict(sm_scale=float("nan")), dict(sm_scale=float("inf"))):
         assert _attn(A, _desc(A, **bad)) == 1, bad
