@@ -130,7 +130,7 @@ struct KvAttnArgs {
     int B, H, Lq, D;
     int G;                 // query heads per stored head
     int causal;
-    int n_tiles, nsplit, chunk, tile_rows;     // from the plan
+    int units, n_tiles, nsplit, chunk, tile_rows;     // from the plan
     float scale_log2;      // sm_scale * log2(e)
 };
 

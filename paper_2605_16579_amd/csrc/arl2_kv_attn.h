@@ -66,6 +66,16 @@ struct Query {
     }
 };
 
+// The first n bytes of a word, n any number; and its bytes of 255.
+__device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u; }
+__device__ __forceinline__ uint32_t bytes_255(uint32_t w)
+{
+    uint32_t x = w & (w >> 4) & 0x0f0f0f0fu;
+    x &= x >> 2 & 0x03030303u;
+    x &= x >> 1 & 0x01010101u;
+    return x * 255u;
+}
+
 // Scale byte b of a word as a conversion's scale operand, of which only the exponent bits count (measured for every exponent, with
 // sign and mantissa bits set): the other bytes' bits need not be cleared.
 template <int b>

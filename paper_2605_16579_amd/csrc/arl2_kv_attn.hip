@@ -4,71 +4,118 @@
 
 #include <limits.h>
 
+#include <algorithm>
+
 namespace arl2 {
 namespace {
 
 constexpr int kRows = 32;        // query rows of a workgroup
 constexpr int kWaves = 4;
+constexpr int kSlots = 3 * kNumCu;     // workgroups that run at a time
 
-// One block of 32 stored tokens in registers.
+// LDS of a wavefront: a ring of blocks of 32 tokens as they are stored, per 16-token group key codes [16-byte piece of a row][token],
+// value codes, key scales, value scales.
 template <int D>
-struct Block {
-    static constexpr int STEPS = D / 64;
-    u32x4 k[STEPS];          // lane (c, hh): key row i = c, features 64 s + 32 hh .. + 31
-    uint32_t ks;             // the row's scales from feature 32 hh on
-    u32x4 v[STEPS], vs[STEPS];     // feature pair 32 x + c, tokens 16 hh .. + 15: codes, and scales of the pair's group
-    int page;                // of tokens 16 hh .. + 15, or -1
+struct Stream {
+    static constexpr int STEPS = D / 64, OB = D / 32;
+    static constexpr int CODES = 16 * D / 2, SCALES = 16 * D / 32;         // of a group: keys', and values'
+    static constexpr int GROUP = 2 * CODES + 2 * SCALES, BLOCK = 2 * GROUP;
+    static constexpr int STAGES = 3, AHEAD = STAGES - 1;                   // blocks on their way while one is worked on
+    static constexpr int LOADS = D == 128 ? 6 : 4;                         // instructions per block
+    static constexpr int ENDING = kRows * (64 + 4) * 4;                    // outputs on their way to the join: 64 features of 32 rows, 128 of 16
+    static constexpr int RING = STAGES * BLOCK > ENDING ? STAGES * BLOCK : ENDING;
 };
 
-template <int D>
-__global__ __launch_bounds__(64 * kWaves, 2) void kv_stream_kernel(KvAttnArgs a)
+// Waits until at most n of this wavefront's requests of LOADS loads each are on their way.
+template <int LOADS>
+__device__ __forceinline__ void wait_requests(int n)
 {
-    constexpr int STEPS = D / 64, OB = D / 32;
-    __shared__ __attribute__((aligned(16))) float sm_o[kWaves][kRows][D + 4];
+    if (n >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * LOADS) : "memory");
+    else if (n == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
+    else if (n == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+template <int D>
+__global__ __launch_bounds__(64 * kWaves, 3) void kv_stream_kernel(KvAttnArgs a)
+{
+    using C = Stream<D>;
+    constexpr int STEPS = C::STEPS, OB = C::OB, KS = D / 16;
+    __shared__ __attribute__((aligned(16))) unsigned char ring[kWaves][C::RING];
     __shared__ float sm_ml[kWaves][2][kRows];
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, hh = lane >> 5;
-    uint32_t id = blockIdx.x;
-    const int split = id % a.nsplit;
-    const int unit = id / a.nsplit;
-    const int qt = unit % a.n_tiles, bh = unit / a.n_tiles, h = bh % a.pool.heads, b = bh / a.pool.heads;
+    // All first splits, then all second ones, ..: consecutive workgroups go to different XCDs, and the later splits are empty for
+    // the shorter streams.  Query tiles of one stored head stay on one XCD where the heads divide evenly.
+    const int split = (int)blockIdx.x / a.units, u = (int)blockIdx.x % a.units;
+    const bool by_xcd = a.n_tiles > 1 && a.units / a.n_tiles % kNumXcd == 0;
+    const int qt = (by_xcd ? u / kNumXcd : u) % a.n_tiles, bh = by_xcd ? u / kNumXcd / a.n_tiles * kNumXcd + u % kNumXcd : u / a.n_tiles;
+    const int h = bh % a.pool.heads, b = bh / a.pool.heads, unit = bh * a.n_tiles + qt;
+    const int kbeg = split * a.chunk;
+
+    // ---- blocks: wavefront w takes blocks w, w + kWaves, .. of the split, straight into its ring
+    // (the block table, like the lengths, is read through the scalar cache: a vector load's wait would wait for the copies too)
+    typedef const __attribute__((address_space(4))) int32_t *scalar_ptr;
+    const scalar_ptr table = (scalar_ptr)(uintptr_t)(a.table + (size_t)b * a.pool.max_pages);
+    const int shift = a.pool.shift, in_page = (1 << shift) - 1, capacity = kv_capacity(a.pool);
+    const unsigned char *head_base = (const unsigned char *)a.cache + (size_t)h * kv_head_bytes(shift, D);
+    const uint32_t page_bytes = (uint32_t)a.pool.heads * (uint32_t)kv_head_bytes(shift, D);
+    unsigned char *mine = ring[wave];
+    const uint32_t lds0 = lds_address(mine);
+    auto key_of = [&](int m) { return kbeg + (wave + kWaves * m) * kKeys; };        // first key of the wavefront's block m
+    auto page_of = [&](int pos) -> int {          // kv_page, for a position that is not negative
+        const int e = table[min(pos >> shift, a.pool.max_pages - 1)];
+        return pos < capacity && (uint32_t)e < (uint32_t)a.pool.n_pages ? e : -1;
+    };
+    int page[2];                                  // of the two groups of the next block to request
+    uint32_t placed = 0;                          // whether the groups of the blocks requested have one, two bits each, the last block lowest
+    auto lookup = [&](int m) {
+        page[0] = page_of(key_of(m));
+        page[1] = page_of(key_of(m) + 16);
+    };
+    const uint32_t codes_at = D == 128 ? (lane & 15) * (D / 2) + 16 * (lane >> 4)                        // keys (D = 64: and values)
+                                       : lane < 32 ? (lane & 15) * (D / 2) + 16 * (lane >> 4) : 16 * (lane - 32) + ((D / 2) << shift);
+    const uint32_t scales_at = (D << shift) + (lane < D / 32 ? 16 * lane : 16 * (lane - D / 32) + ((D / 32) << shift));
+    auto request = [&](int m) {                   // `page` holds the block's
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+            const __amdgpu_buffer_rsrc_t rsrc = make_rsrc(head_base + (uint64_t)(uint32_t)max(page[g], 0) * page_bytes, (uint32_t)kv_head_bytes(shift, D));
+            const uint32_t t = (uint32_t)(key_of(m) + 16 * g) & in_page, dst = lds0 + m % C::STAGES * C::BLOCK + g * C::GROUP;
+            load_to_lds(rsrc, codes_at + t * (D / 2), dst);
+            if constexpr (D == 128) load_to_lds(rsrc, 16 * lane + ((D / 2) << shift) + t * (D / 2), dst + C::CODES);
+            if (lane < D / 16) load_to_lds(rsrc, scales_at + t * (D / 32), dst + 2 * C::CODES);
+        }
+        placed = placed << 2 | (page[0] >= 0 ? 1u : 0u) | (page[1] >= 0 ? 2u : 0u);
+    };
+    if (split == 0) lookup(0);           // (beside the lengths; later splits are often empty and first see whether they are)
+
     const Span sp = span_of(a, b);
-    const int row0 = qt * kRows;
+    const int row0 = qt * a.tile_rows;
     if (row0 >= sp.rows) return;
-    const int n_rows = min(kRows, sp.rows - row0);
+    const int n_rows = min(a.tile_rows, sp.rows - row0);
     const int lim_min = sp.limit(row0, a), lim_max = sp.limit(row0 + n_rows - 1, a);
-    const int kbeg = split * a.chunk, kend = min(lim_max, kbeg + a.chunk);
+    const int kend = min(lim_max, kbeg + a.chunk);
     if (kbeg >= kend && split > 0) return;
     const bool whole = lim_max <= a.chunk;                    // this workgroup sees all that its rows see
+    if (split > 0) lookup(0);
+    const int n_blocks = (kend - kbeg + kKeys - 1) / kKeys, n = (n_blocks - wave + kWaves - 1) / kWaves;      // of the split, of the wavefront
+    for (int m = 0; m < C::AHEAD; ++m) {
+        if (m < n) {
+            request(m);
+            lookup(m + 1);
+        } else {
+            placed <<= 2;
+        }
+    }
 
     const int row = row0 + c;
     const bool row_there = c < n_rows;
     const int lim = row_there ? sp.limit(row, a) : sp.klen;
     const size_t q_row = (((size_t)b * a.Lq + row / a.G) * a.H + (size_t)h * a.G + row % a.G) * D;
-    Query<D> q;
-    q.load((const bf16_t *)a.q + q_row + 32 * hh, row_there);
-
-    // Keys are dealt to the rows of the first product so that the logits of lane (c, hh) belong to keys 16 hh .. 16 hh + 15 of the
-    // block in order: accumulator r of half-wave hh is row 8 (r / 4) + 4 hh + r % 4.
-    const int row_key = 16 * ((c >> 2) & 1) + 8 * (c >> 4) + 4 * ((c >> 3) & 1) + (c & 3);
-    const int32_t *table = a.table + (size_t)b * a.pool.max_pages;
-    const unsigned char *pool = (const unsigned char *)a.cache;
-    const int shift = a.pool.shift, in_page = (1 << shift) - 1;
-    auto head = [&](int page) { return pool + kv_head_offset(a.pool, D, page < 0 ? 0 : page, h); };
-    auto load = [&](Block<D> &x, int key0, int page_k, int page_v) {
-        const unsigned char *kb = head(page_k), *vb = head(page_v);
-        const int tk = (key0 + row_key) & in_page, tv = (key0 + 16 * hh) & in_page;
+    // k-step t of the first product takes features (D / 2) hh + 8 t .. + 7 in half-wave hh, for the keys as they lie in a row
+    bf16x8 qf[KS];
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) x.k[s] = *(const u32x4 *)(kb + kv_key_codes(tk, 32 * s + 16 * hh, D));
-        if constexpr (D == 128) x.ks = *(const uint32_t *)(kb + kv_key_scales(shift, tk, 0, D)) >> (8 * hh);
-        else x.ks = *(const uint16_t *)(kb + kv_key_scales(shift, tk, 0, D)) >> (8 * hh);
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            x.v[s] = *(const u32x4 *)(vb + kv_value_codes(shift, tv, 32 * s + c, D));
-            x.vs[s] = *(const u32x4 *)(vb + kv_value_scales(shift, tv, 2 * s + (c >> 4), D));
-        }
-        x.page = page_v;
-    };
+    for (int t = 0; t < KS; ++t) qf[t] = row_there ? *(const bf16x8 *)((const bf16_t *)a.q + q_row + (D / 2) * hh + 8 * t) : bf16x8{};
 
     f32x16 o[OB];                // O^T: block 2 s + e holds features 64 s + 2 i + e, i the accumulator's row
 #pragma unroll
@@ -76,48 +123,83 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_stream_kernel(KvAttnArgs a)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;
+    const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
     int nan_key[STEPS];          // first key with a NaN value among those that not all rows see
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) nan_key[s] = INT_MAX;
 
-    auto process = [&](Block<D> &x, int key0, auto masked_) {
-        constexpr bool MASKED = decltype(masked_)::value;
-        f32x16 s_acc = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-        static_for<0, STEPS>([&](auto s_) {
-            constexpr int s = decltype(s_)::value;
-            const i32x8 ka = {(int)x.k[s][0], (int)x.k[s][1], (int)x.k[s][2], (int)x.k[s][3], 0, 0, 0, 0};
-            static_for<0, kParts>([&](auto p_) {
-                constexpr int p = decltype(p_)::value;
-                const u32x6 w = q.part[s][p];
-                const i32x8 qb = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], (int)w[4], (int)w[5], 0, 0};
-                s_acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qb, s_acc, 4, 2, 2 * s, (int)x.ks, p, (int)q.scale[s]);
+#pragma unroll 1
+    for (int m = 0; m < n; ++m) {
+        if (m + C::AHEAD < n) {
+            request(m + C::AHEAD);
+            lookup(m + C::AHEAD + 1);
+        } else {
+            placed <<= 2;
+        }
+        wait_requests<C::LOADS>(min(n - 1 - m, C::AHEAD));
+        const unsigned char *blk = mine + m % C::STAGES * C::BLOCK;
+        const int key0 = key_of(m);
+        const uint32_t groups = placed >> (2 * C::AHEAD) & 3u;
+
+        // ---- logits: row c of the product is key c, so that accumulator r of half-wave hh is key 8 (r / 4) + 4 hh + r % 4
+        u32x4 kf[STEPS];                                       // codes of features (D / 2) hh ..
+        const unsigned char *kg = blk + (c >> 4) * C::GROUP;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) kf[s] = *(const u32x4 *)(kg + (STEPS * hh + s) * 256 + (c & 15) * 16);
+        uint32_t ks;                                           // their scales
+        if constexpr (D == 128) ks = *(const uint16_t *)(kg + 2 * C::CODES + 4 * (c & 15) + 2 * hh);
+        else ks = kg[2 * C::CODES + 2 * (c & 15) + hh];
+        // value codes and scales of the same keys: feature pair 32 s + c, tokens 16 u + 8 x + 4 hh ..
+        uint32_t vc[STEPS][2][2], vs[STEPS][2][2];
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    vc[s][u][x] = *(const uint32_t *)(blk + u * C::GROUP + C::CODES + (32 * s + c) * 16 + 8 * x + 4 * hh);
+                    vs[s][u][x] = *(const uint32_t *)(blk + u * C::GROUP + 2 * C::CODES + C::SCALES + (2 * s + (c >> 4)) * 16 + 8 * x + 4 * hh);
+                }
+        f32x16 s_acc = zero;
+        static_for<0, KS>([&](auto t_) {
+            constexpr int t = decltype(t_)::value;
+            union { uint32_t u[4]; bf16x8 v; } x;
+            static_for<0, 4>([&](auto i_) {
+                constexpr int i = decltype(i_)::value;
+                x.u[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(kf[t >> 2][t & 3], scale_operand<(t >> 2)>(ks), i));
             });
+            s_acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.v, qf[t], s_acc, 0, 0, 0);
         });
-        if constexpr (MASKED) {
-            const int left = (x.page < 0 ? 0 : lim) - (key0 + 16 * hh);
+        if (__builtin_expect(key0 + kKeys > min(lim_min, kend) || groups != 3u, 0)) {
+            const int left = min(lim, kend) - (key0 + 4 * hh);
+            const int left0 = groups & 1u ? left : INT_MIN, left1 = groups & 2u ? left : INT_MIN;
 #pragma unroll
             for (int r = 0; r < 16; ++r)
-                if (r >= left) s_acc[r] = -INFINITY;
+                if (8 * (r >> 2) + (r & 3) >= (r < 8 ? left0 : left1)) s_acc[r] = -INFINITY;
             // values that no row of the workgroup sees are not to reach the product, whatever they are; a NaN among those that
             // some see goes to these rows alone, at the end
-            const int left_v = (x.page < 0 ? 0 : lim_max) - (key0 + 16 * hh), left_all = lim_min - (key0 + 16 * hh);
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s)
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int t = 0; t < 16; ++t) {
-                    const uint32_t byte = 255u << (8 * (t & 3));
-                    const bool nan = (x.vs[s][t >> 2] & byte) == byte;
-                    if (t >= left_v || (nan && t >= left_all)) {
-                        x.v[s][t >> 2] &= ~byte;
-                        x.vs[s][t >> 2] = (x.vs[s][t >> 2] & ~byte) | (byte & 0x7f7f7f7fu);
-                        if (t < left_v) nan_key[s] = min(nan_key[s], key0 + 16 * hh + t);
+                for (int x = 0; x < 2; ++x) {
+                    const int key = key0 + 16 * u + 8 * x + 4 * hh;
+                    const uint32_t seen = first_bytes((groups >> u & 1u ? kend : 0) - key), by_all = first_bytes(lim_min - key);
+#pragma unroll
+                    for (int s = 0; s < STEPS; ++s) {
+                        const uint32_t nan = bytes_255(vs[s][u][x]) & ~by_all, gone = ~seen | nan;
+                        if ((nan & seen) != 0) nan_key[s] = min(nan_key[s], key + (__ffs(nan & seen) - 1) / 8);
+                        vc[s][u][x] &= ~gone;
+                        vs[s][u][x] = (vs[s][u][x] & ~gone) | (gone & 0x7f7f7f7fu);
                     }
                 }
         }
+
+        // ---- softmax
         float mx = s_acc[0];
 #pragma unroll
         for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s_acc[r]);
-        mx = xhalf_max(mx) * a.scale_log2;
+        const auto other = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);      // both half-waves'
+        mx = fmaxf(__uint_as_float(other[0]), __uint_as_float(other[1])) * a.scale_log2;
         const float m_new = fmaxf(m_run, mx);
         const float m_ref = fmaxf(m_new, -FLT_MAX);
         if (__any(m_new > m_run)) {
@@ -136,14 +218,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_stream_kernel(KvAttnArgs a)
             l_run += p;
             pf[r >> 3][r & 7] = to_bf16(p);
         }
+
+        // ---- output
         static_for<0, STEPS>([&](auto s_) {
             constexpr int s = decltype(s_)::value;
             static_for<0, 2>([&](auto u_) {
                 constexpr int u = decltype(u_)::value;
                 uint32_t w[8];
                 static_for<0, 8>([&](auto j_) {
-                    constexpr int j = decltype(j_)::value, t = 8 * u + j;
-                    w[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x.v[s][t >> 2], scale_operand<(t & 3)>(x.vs[s][t >> 2]), t & 3));
+                    constexpr int j = decltype(j_)::value;
+                    w[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vc[s][u][j >> 2], scale_operand<(j & 3)>(vs[s][u][j >> 2]), j & 3));
                 });
                 union { u32x4 u; bf16x8 v; } even, odd;
 #pragma unroll
@@ -155,38 +239,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_stream_kernel(KvAttnArgs a)
                 o[2 * s + 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(odd.v, pf[u], o[2 * s + 1], 0, 0, 0);
             });
         });
-    };
-
-    {
-        const int n_blocks = (kend - kbeg + kKeys - 1) / kKeys;
-        int blk = wave;
-        Block<D> x, y;
-        auto pages = [&](int blk, int &pk, int &pv) {
-            const int key0 = kbeg + blk * kKeys;
-            pk = kv_page(a.pool, table, key0 + row_key);
-            pv = kv_page(a.pool, table, key0 + 16 * hh);
-        };
-        int pk = 0, pv = 0;
-        if (blk < n_blocks) {
-            pages(blk, pk, pv);
-            load(x, kbeg + blk * kKeys, pk, pv);
-            pages(blk + kWaves, pk, pv);
-        }
-        while (blk < n_blocks) {
-            const int next = blk + kWaves;
-            if (next < n_blocks) {
-                load(y, kbeg + next * kKeys, pk, pv);
-                pages(next + kWaves, pk, pv);
-            }
-            const int key0 = kbeg + blk * kKeys;
-            if (key0 + kKeys > lim_min || __any(x.page < 0)) process(x, key0, std::true_type{});
-            else process(x, key0, std::false_type{});
-            x = y;
-            blk = next;
-        }
     }
 
     // ---- the wavefronts' results, each relative to its own maximum
+    if (n > 0) {             // zero times the query row: NaN where it is not finite, which logits of -inf alone would not show
+        f32x16 nil = zero;
+#pragma unroll
+        for (int t = 0; t < KS; ++t) nil = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf16x8{}, qf[t], nil, 0, 0, 0);
+        l_run += nil[0];
+    }
     l_run = xhalf_sum(l_run);
     bool any_nan = false;
 #pragma unroll
@@ -207,44 +268,64 @@ __global__ __launch_bounds__(64 * kWaves, 2) void kv_stream_kernel(KvAttnArgs a)
         sm_ml[wave][0][c] = m_run;
         sm_ml[wave][1][c] = l_run;
     }
-    if (c < n_rows) {
+    // The outputs take the ring's place (nothing is on its way into it any more): up to 16 rows at once, more 64 features at a time.
+    auto put = [&](int orw, int first) {
+        if (row_there) {
+            static_for<0, STEPS>([&](auto s_) {
+                constexpr int s = decltype(s_)::value;
+                if (first < 0 || first == 64 * s) {
+                    float *dst = (float *)mine + c * orw + (first < 0 ? 64 * s : 0);
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
+                    for (int g = 0; g < 4; ++g)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int i = 8 * (r >> 2) + 4 * hh + (r & 3);
-                *(f32x2 *)&sm_o[wave][c][64 * s + 2 * i] = f32x2{o[2 * s][r], o[2 * s + 1][r]};
-            }
-    }
-    __syncthreads();
-    constexpr int PER = D / 4;                         // 16-byte pieces of a row
-    for (int e = tid; e < n_rows * PER; e += 64 * kWaves) {
-        const int rr = e / PER, d = 4 * (e % PER);
-        float m = sm_ml[0][0][rr];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sm_ml[w][0][rr]);
-        const float m_ref = fmaxf(m, -FLT_MAX);
-        f32x4 sum = {0, 0, 0, 0};
-        float l = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float f = __builtin_amdgcn_exp2f(sm_ml[w][0][rr] - m_ref);
-            const f32x4 y = *(const f32x4 *)&sm_o[w][rr][d];
-            l = fmaf(sm_ml[w][1][rr], f, l);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] = fmaf(y[i], f, sum[i]);
+                        for (int i = 0; i < 2; ++i)
+                            *(f32x4 *)(dst + 16 * g + 8 * hh + 4 * i) = f32x4{o[2 * s][4 * g + 2 * i], o[2 * s + 1][4 * g + 2 * i], o[2 * s][4 * g + 2 * i + 1], o[2 * s + 1][4 * g + 2 * i + 1]};
+                }
+            });
         }
-        if (whole) {
-            const float inv = l == 0.f ? 0.f : 1.f / l;          // a row that sees nothing is zero
-            const int orow = row0 + rr;
-            bf16x4 y;
+        __syncthreads();
+    };
+    auto join = [&](int orw, int first, int pieces) {  // 16-byte pieces of a row
+        for (int e = tid; e < n_rows * pieces; e += 64 * kWaves) {
+            const int rr = e / pieces, d = 4 * (e % pieces);
+            float mw[kWaves], m = -INFINITY, l = 0.f;
+            f32x4 y[kWaves], sum = {0, 0, 0, 0};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = to_bf16(sum[i] * inv);
-            *(bf16x4 *)((bf16_t *)a.out + (((size_t)b * a.Lq + orow / a.G) * a.H + (size_t)h * a.G + orow % a.G) * D + d) = y;
-        } else {
-            const size_t slot = ((size_t)unit * a.nsplit + split) * a.tile_rows + rr;
-            *(f32x4 *)(a.part_o + slot * D + d) = sum;
-            if (d == 0) *(f32x2 *)(a.part_ml + slot * 2) = f32x2{m, l};
+            for (int w = 0; w < kWaves; ++w) {
+                mw[w] = sm_ml[w][0][rr];
+                y[w] = *(const f32x4 *)((const float *)ring[w] + rr * orw + d);
+                m = fmaxf(m, mw[w]);
+            }
+            const float m_ref = fmaxf(m, -FLT_MAX);
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = __builtin_amdgcn_exp2f(mw[w] - m_ref);
+                l = fmaf(sm_ml[w][1][rr], f, l);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[i] = fmaf(y[w][i], f, sum[i]);
+            }
+            if (whole) {
+                const float inv = l == 0.f ? 0.f : 1.f / l;          // a row that sees nothing is zero
+                const int orow = row0 + rr;
+                bf16x4 z;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[i] = to_bf16(sum[i] * inv);
+                *(bf16x4 *)((bf16_t *)a.out + (((size_t)b * a.Lq + orow / a.G) * a.H + (size_t)h * a.G + orow % a.G) * D + first + d) = z;
+            } else {
+                const size_t slot = ((size_t)unit * a.nsplit + split) * a.tile_rows + rr;
+                *(f32x4 *)(a.part_o + slot * D + first + d) = sum;
+                if (first + d == 0) *(f32x2 *)(a.part_ml + slot * 2) = f32x2{m, l};
+            }
+        }
+    };
+    if (D == 64 || n_rows <= 16) {
+        put(D + 4, -1);
+        join(D + 4, 0, D / 4);
+    } else {
+        for (int f = 0; f < D; f += 64) {
+            if (f > 0) __syncthreads();
+            put(64 + 4, f);
+            join(64 + 4, f, 16);
         }
     }
 }
@@ -267,15 +348,32 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a)
     const int g = threadIdx.x / LANES, d = 4 * (threadIdx.x % LANES);
     float m = -INFINITY, l = 0.f;
     f32x4 sum = {0, 0, 0, 0};
-    for (int s = g; s < n; s += GROUPS) {
-        const size_t slot = ((size_t)unit * a.nsplit + s) * a.tile_rows + rr;
-        const f32x2 ml = *(const f32x2 *)(a.part_ml + slot * 2);
-        const f32x4 y = *(const f32x4 *)(a.part_o + slot * D + d);
-        const float m_new = fmaxf(m, ml[0]), m_ref = fmaxf(m_new, -FLT_MAX);
-        const float f0 = __builtin_amdgcn_exp2f(m - m_ref), f1 = __builtin_amdgcn_exp2f(ml[0] - m_ref);
-        l = l * f0 + ml[1] * f1;
+    constexpr int AT_ONCE = 4;
+    for (int s0 = g; s0 < n; s0 += GROUPS * AT_ONCE) {
+        f32x2 ml[AT_ONCE];
+        f32x4 y[AT_ONCE];
+        float m_new = m;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] = sum[i] * f0 + y[i] * f1;
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int s = s0 + GROUPS * k;
+            const size_t slot = ((size_t)unit * a.nsplit + min(s, n - 1)) * a.tile_rows + rr;
+            ml[k] = *(const f32x2 *)(a.part_ml + slot * 2);
+            y[k] = *(const f32x4 *)(a.part_o + slot * D + d);
+            if (s >= n) ml[k] = f32x2{-INFINITY, 0.f}, y[k] = f32x4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) m_new = fmaxf(m_new, ml[k][0]);
+        const float m_ref = fmaxf(m_new, -FLT_MAX), f0 = __builtin_amdgcn_exp2f(m - m_ref);
+        l *= f0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i] *= f0;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const float f1 = __builtin_amdgcn_exp2f(ml[k][0] - m_ref);
+            l = fmaf(ml[k][1], f1, l);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = fmaf(y[k][i], f1, sum[i]);
+        }
         m = m_new;
     }
     *(f32x4 *)&sm_o[g][d] = sum;
@@ -327,8 +425,9 @@ KvAttnPlan kv_attn_plan(int B, int Lq, int G, const KvPool &pool, int D)
             if (us < best) { best = us; chunk = tokens; }
         }
     } else {
-        while (chunk < 2048 && p.units * ((cap + chunk - 1) / chunk) > 1024) chunk *= 2;
-        if (p.units >= 1024) chunk = cap;
+        const long long one_round = (cap * p.units + kSlots - 1) / kSlots;
+        chunk = B == 1 ? one_round : std::min(one_round, std::max(1024LL, cap / 8));
+        chunk = (std::max(chunk, 256LL) + 127) / 128 * 128;
     }
     p.nsplit = (int)((cap + chunk - 1) / chunk);
     p.chunk = (int)chunk;
@@ -341,6 +440,7 @@ KvAttnPlan kv_attn_plan(int B, int Lq, int G, const KvPool &pool, int D)
 hipError_t launch_kv_attn(KvAttnArgs a, const KvAttnPlan &p, void *workspace, hipStream_t stream)
 {
     a.n_tiles = (int)p.n_tiles;
+    a.units = (int)p.units;
     a.nsplit = p.nsplit;
     a.chunk = p.chunk;
     a.tile_rows = p.tile_rows;

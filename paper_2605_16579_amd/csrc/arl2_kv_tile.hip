@@ -27,9 +27,6 @@ struct Tile {
     static_assert(PVN % RING == 0, "the fragment ring runs across slots");
 };
 
-// The first n bytes of a word, n any number.
-__device__ __forceinline__ uint32_t first_bytes(int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u; }
-
 // Workgroup barrier after all but the last N of this wavefront's loads into LDS have arrived, and all but the last M of its LDS
 // operations, which end in the order they were issued in.
 template <int N, int M = 0>
@@ -131,10 +128,7 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
         for (int i = 0; i < C::T / 4; ++i) {
             const int key = (tile0 + tile) * kTile + 16 * vg + 8 * (vx + i) + 4 * hv;
             const uint32_t seen = first_bytes((ok ? kend : 0) - key), by_all = first_bytes(lim_min - key);
-            uint32_t nan = vs[i] & (vs[i] >> 4) & 0x0f0f0f0fu;       // bytes of 255
-            nan &= nan >> 2 & 0x03030303u;
-            nan &= nan >> 1 & 0x01010101u;
-            nan = nan * 255u & ~by_all;
+            const uint32_t nan = bytes_255(vs[i]) & ~by_all;
             if ((nan & seen) != 0) atomicMin(&nan_key[dp >> 4], key + (__ffs(nan & seen) - 1) / 8);
             const uint32_t gone = ~seen | nan;
             vc[i] &= ~gone;
