@@ -471,6 +471,8 @@ def arl2_kv_append(k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, block_
                    rope_sin: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> None:
     """Rotates (with tables [max_pages * page_size, D/2] by position) and quantises k, v [B, L, heads, D] bf16 into ``cache`` (see
     ``alloc_kv_cache``): token i < count[b] (None: L) of stream b to position start[b] + i of the pages block_table [B, max_pages]."""
+    if _plain_call("arl2_kv_append", b"Pyyrrbinc", 0.0, 0.0, stream, None, k, v, rope_cos, rope_sin, block_table, start, count, cache):
+        return
     if k.dim() != 4:
         raise ValueError("k must be [B, L, heads, D]")
     B, L, Hkv, D = k.shape
@@ -487,6 +489,8 @@ def arl2_kv_append(k: torch.Tensor, v: torch.Tensor, cache: torch.Tensor, block_
 def arl2_kv_read(cache: torch.Tensor, block_table: torch.Tensor, start: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *,
                  count: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> None:
     """The values of stored rows into k, v [B, L, heads, D] bf16: token i < count[b] (None: L) from position start[b] + i."""
+    if _plain_call("arl2_kv_read", b"Pcbinyy", 0.0, 0.0, stream, None, cache, block_table, start, count, k, v):
+        return
     if k.dim() != 4:
         raise ValueError("k must be [B, L, heads, D]")
     B, L, Hkv, D = k.shape
@@ -504,6 +508,8 @@ def arl2_kv_attn_fwd(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Te
     """Softmax attention of q [B, L, H, D] bf16 over the kv_len[b] stored tokens of each stream into ``out``, H a multiple of the
     stored heads; ``causal``: the q_len[b] (None: L) queries are the last tokens stored and see those up to their own.  ``workspace``:
     of ``arl2_kv_workspace_bytes`` (``alloc_kv_workspace``), one for each call in flight."""
+    if _plain_call("arl2_kv_attn_fwd", b"Pxcbinx", sm_scale, 1.0 if causal else 0.0, stream, workspace, q, cache, block_table, kv_len, q_len, out):
+        return
     if q.dim() != 4:
         raise ValueError("q must be [B, L, H, D]")
     B, L, H, D = q.shape

@@ -8,8 +8,13 @@
 //   q  [B][Lq][H][D], the inputs' type (the first tensor, which names the sizes and the type)      k  [B][Lkv][H][D], likewise
 //   S  [B][H][D][D] fp32    W  [H][D][D], the inputs' type    r  [Lq][D/2] fp32    a  [B][H] fp32    t  [B][Lq][H] fp32
 //   g  [B][Lq][H], [B][Lq] or [B][Lq][H][D], fp32 or bf16: sets the descriptor's gate mode and type
+// Calls on the paged cache begin with P and take `causal` in the place of l2_eps; their descriptor is arl2_kv_desc, all of their tensors
+// are on the current device, and a letter is
+//   c  the pool, uint8 [n_pages][Hkv][page_size][bytes of a token]      b  [B][max_pages] int32
+//   x  [B][Lq][H][D] bf16     y  [B][Lq][Hkv][D] bf16    r  [max_pages page_size][D/2] fp32    i, n  [B] int32 (n or None)
 // Measured: a call of the smallest size took 7 us to issue through ctypes, of them 3.5 in the library and the runtime.
 #include <Python.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/arl2.h"
@@ -81,18 +86,61 @@ bool check(Checked &c, char kind, PyObject *o, int i)
     return ok;
 }
 
-int invoke(void *f, const arl2_desc *d, const void *const *p, int n)
+// The same for calls on the paged cache; the arrays that name the sizes may come after others.
+bool check_kv(arl2_kv_desc &d, const char *kinds, PyObject *const *args, int n, const void **p)
+{
+    const at::Tensor *t[kMaxTensors] = {}, *rows = nullptr, *pool = nullptr, *table = nullptr;
+    int device = -1;
+    for (int i = 0; i < n; ++i) {
+        if (args[i] == Py_None) {
+            if (kinds[i] != 'n' && kinds[i] != 'r') return false;
+            continue;
+        }
+        if ((t[i] = plain(args[i])) == nullptr) return false;
+        if (device < 0) device = t[i]->get_device();
+        if (t[i]->get_device() != device) return false;
+        if ((kinds[i] == 'x' || kinds[i] == 'y') && rows == nullptr) rows = t[i];
+        if (kinds[i] == 'c') pool = t[i];
+        if (kinds[i] == 'b') table = t[i];
+    }
+    if (rows == nullptr || pool == nullptr || table == nullptr || rows->dim() != 4 || pool->dim() != 4 || table->dim() != 2) return false;
+    if (device != (int)c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice().index()) return false;
+    for (const at::Tensor *x : {rows, pool, table})
+        for (int64_t m : x->sizes())
+            if (m > INT32_MAX) return false;
+    const int64_t B = rows->size(0), L = rows->size(1), H = rows->size(2), D = rows->size(3), Hkv = pool->size(1), cap = table->size(1) * pool->size(2);
+    d.B = (int32_t)B; d.Lq = (int32_t)L; d.H = (int32_t)H; d.D = (int32_t)D;
+    d.n_pages = (int32_t)pool->size(0); d.Hkv = (int32_t)Hkv; d.page_size = (int32_t)pool->size(2); d.max_pages = (int32_t)table->size(1);
+    for (int i = 0; i < n; ++i) {
+        if (t[i] == nullptr) continue;
+        const at::ScalarType type = t[i]->scalar_type();
+        bool ok = false;
+        switch (kinds[i]) {
+        case 'c': ok = type == at::kByte && pool->size(3) == 2 * (D / 2 + D / 32); break;
+        case 'b': ok = type == at::kInt && table->size(0) == B; break;
+        case 'x': ok = type == at::kBFloat16 && is_shape(*t[i], {B, L, H, D}); break;
+        case 'y': ok = type == at::kBFloat16 && is_shape(*t[i], {B, L, Hkv, D}); break;
+        case 'r': ok = type == at::kFloat && is_shape(*t[i], {cap, D / 2}); break;
+        case 'i': case 'n': ok = type == at::kInt && is_shape(*t[i], {B}); break;
+        }
+        if (!ok) return false;
+        p[i] = t[i]->data_ptr();
+    }
+    return true;
+}
+
+int invoke(void *f, const void *d, const void *const *p, int n)
 {
     typedef const void *P;
     switch (n) {
-    case 3: return ((int (*)(const arl2_desc *, P, P, P))f)(d, p[0], p[1], p[2]);
-    case 4: return ((int (*)(const arl2_desc *, P, P, P, P))f)(d, p[0], p[1], p[2], p[3]);
-    case 5: return ((int (*)(const arl2_desc *, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4]);
-    case 6: return ((int (*)(const arl2_desc *, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5]);
-    case 7: return ((int (*)(const arl2_desc *, P, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5], p[6]);
-    case 8: return ((int (*)(const arl2_desc *, P, P, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]);
+    case 3: return ((int (*)(P, P, P, P))f)(d, p[0], p[1], p[2]);
+    case 4: return ((int (*)(P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3]);
+    case 5: return ((int (*)(P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4]);
+    case 6: return ((int (*)(P, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5]);
+    case 7: return ((int (*)(P, P, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5], p[6]);
+    case 8: return ((int (*)(P, P, P, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]);
     case 10:
-        return ((int (*)(const arl2_desc *, P, P, P, P, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9]);
+        return ((int (*)(P, P, P, P, P, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9]);
     }
     return -1;
 }
@@ -100,9 +148,11 @@ int invoke(void *f, const arl2_desc *d, const void *const *p, int n)
 PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
 {
     constexpr Py_ssize_t kFixed = 6;
-    if (nargs <= kFixed || !PyBytes_CheckExact(args[1]) || PyBytes_GET_SIZE(args[1]) != nargs - kFixed || nargs - kFixed > kMaxTensors) Py_RETURN_NONE;
+    if (nargs <= kFixed || !PyBytes_CheckExact(args[1]) || nargs - kFixed > kMaxTensors) Py_RETURN_NONE;
     const int n = (int)(nargs - kFixed);
     const char *kinds = PyBytes_AS_STRING(args[1]);
+    const bool kv = kinds[0] == 'P';
+    if (PyBytes_GET_SIZE(args[1]) != n + kv) Py_RETURN_NONE;
     void *f = PyLong_AsVoidPtr(args[0]);
     const double sm_scale = PyFloat_AsDouble(args[2]), l2_eps = PyFloat_AsDouble(args[3]);
     void *stream = PyLong_Check(args[4]) ? PyLong_AsVoidPtr(args[4]) : nullptr;
@@ -111,24 +161,40 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         Py_RETURN_NONE;
     }
     Checked c;
+    arl2_kv_desc kd{};
+    void *workspace = nullptr;
+    size_t workspace_bytes = 0;
     try {
-        for (int i = 0; i < n; ++i)
-            if (!check(c, kinds[i], args[kFixed + i], i)) Py_RETURN_NONE;
+        if (kv) {
+            if (!check_kv(kd, kinds + 1, args + kFixed, n, c.p)) Py_RETURN_NONE;
+        } else {
+            for (int i = 0; i < n; ++i)
+                if (!check(c, kinds[i], args[kFixed + i], i)) Py_RETURN_NONE;
+        }
         if (args[5] != Py_None) {
             const at::Tensor *w = plain(args[5]);
-            if (w == nullptr) Py_RETURN_NONE;
-            c.d.workspace = w->data_ptr();
-            c.d.workspace_bytes = w->nbytes();
+            if (w == nullptr || (kv && w->get_device() != THPVariable_Unpack(args[kFixed]).get_device())) Py_RETURN_NONE;
+            workspace = w->data_ptr();
+            workspace_bytes = w->nbytes();
         }
     } catch (...) {                           // a tensor without storage, or of a layout that has no such notion
         Py_RETURN_NONE;
     }
+    if (kv) {
+        kd.sm_scale = (float)sm_scale;
+        kd.causal = l2_eps != 0.0;
+        kd.workspace = workspace;
+        kd.workspace_bytes = workspace_bytes;
+        kd.stream = stream;
+    }
     c.d.sm_scale = (float)sm_scale;
     c.d.l2_eps = (float)l2_eps;
+    c.d.workspace = workspace;
+    c.d.workspace_bytes = workspace_bytes;
     c.d.stream = stream;
     int st;
     Py_BEGIN_ALLOW_THREADS
-    st = invoke(f, &c.d, c.p, n);
+    st = invoke(f, kv ? (const void *)&kd : &c.d, c.p, n);
     Py_END_ALLOW_THREADS
     if (st < 0) Py_RETURN_NONE;
     return PyLong_FromLong(st);

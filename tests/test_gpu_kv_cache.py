@@ -427,3 +427,58 @@ def test_a_chunk_goes_from_the_softmax_cache_into_the_linear_memory(A, oracle):
         table[:, :c * L // page] = -1                                   # whole pages of what the state now holds
         pool.set_table(table)
     assert (cos == pool.cos).all() and (sin == pool.sin).all()
+
+
+# ---- the binding's two ways
+
+class Checked(torch.Tensor):
+    """A tensor that is no plain torch.Tensor: a call with it is marshalled in Python."""
+
+
+def test_compiled_and_checked_calls_agree(A, monkeypatch):
+    from paper_2605_16579_amd import binding
+    seen, host_call = [], binding._host_call
+
+    def recorded(*args):
+        seen.append(host_call(*args))
+        return seen[-1]
+
+    monkeypatch.setattr(binding, "_host_call", recorded)
+    B, Hkv, H, L, D, page, width = 2, 2, 6, 5, 64, 32, 20
+    table = torch.randperm(B * width).view(B, width).int().cuda()
+    k, v = (R.bf16_normal((B, L, Hkv, D), i).cuda() for i in range(2))
+    q, start, count, lens = R.bf16_normal((B, L, H, D), 3).cuda(), R.ints([0, 600]), R.ints([5, 3]), R.ints([5, 603])
+    cs, sn = torch.rand(width * page, D // 2, device="cuda"), torch.rand(width * page, D // 2, device="cuda")
+    ws = A.alloc_kv_workspace(B, H, Hkv, L, D, page, width)
+    assert ws is not None
+
+    def run(wrap, **kw):
+        cache = torch.zeros((B * width, Hkv, page, 68), dtype=torch.uint8, device="cuda")
+        out, rk, rv = torch.zeros_like(q), torch.zeros_like(k), torch.zeros_like(v)
+        for f in (lambda: A.arl2_kv_append(wrap(k), v, cache, table, start, count=count, rope_cos=cs, rope_sin=sn, **kw),
+                  lambda: A.arl2_kv_read(cache, table, start, wrap(rk), rv, count=count, **kw),
+                  lambda: A.arl2_kv_attn_fwd(wrap(q), cache, table, lens, out, q_len=count, causal=True, sm_scale=0.2, workspace=ws, **kw)):
+            f()
+        torch.cuda.synchronize()
+        return cache, out, rk, rv
+
+    plain = run(lambda t: t)
+    assert seen == [0, 0, 0]
+    seen.clear()
+    checked = run(lambda t: t.as_subclass(Checked))
+    assert seen == [None] * 3
+    on_stream = run(lambda t: t, stream=torch.cuda.current_stream().cuda_stream)
+    for a, b, c in zip(plain, checked, on_stream):
+        assert torch.equal(a, b) and torch.equal(a, c) and a.any()
+    # what the compiled way does not take is refused by the other
+    cache = plain[0]
+    for bad in (dict(cache=cache[:, :1].contiguous()), dict(cache=cache.int()), dict(table=table[:1]), dict(start=start.long()), dict(start=R.ints([1])),
+                dict(k=k.float()), dict(v=v[:, :2].contiguous()), dict(cs=cs[:-1]), dict(start=start.cpu()), dict(k=k.transpose(1, 2))):
+        a = dict(k=k, v=v, cache=cache, table=table, start=start, cs=cs)
+        a.update(bad)
+        seen.clear()
+        with pytest.raises((ValueError, TypeError)):
+            A.arl2_kv_append(a["k"], a["v"], a["cache"], a["table"], a["start"], rope_cos=a["cs"], rope_sin=sn)
+        assert seen == [None], bad
+    with pytest.raises(A.Arl2Error, match="workspace"):
+        A.arl2_kv_attn_fwd(q, cache, table, lens, torch.empty_like(q), workspace=ws[:-16])
