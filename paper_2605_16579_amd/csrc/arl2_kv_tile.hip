@@ -44,10 +44,11 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
     __shared__ int nan_key[D / 32];      // first key with a NaN value among those that not all rows see
 
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c = lane & 31, hh = lane >> 5;
-    const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
-    // the last query tile first: of causal rows it sees the most
-    const int qt = a.n_tiles - 1 - id % a.n_tiles;
-    const int split = id / a.n_tiles % a.nsplit, bh = id / a.n_tiles / a.nsplit, h = bh % a.pool.heads, b = bh / a.pool.heads;
+    // The last query tiles first: of causal rows they see the most.  Heads innermost, so that every XCD has work of every stream
+    // (a stored head of 4000 tokens is 0.5 MB: that several L2s read it costs less than an idle XCD).
+    const int heads = a.units / a.n_tiles, bh = (int)blockIdx.x % heads;
+    const int split = (int)blockIdx.x / heads % a.nsplit, qt = a.n_tiles - 1 - (int)blockIdx.x / heads / a.nsplit;
+    const int h = bh % a.pool.heads, b = bh / a.pool.heads;
     const Span sp = span_of(a, b);
     const int row0 = qt * a.tile_rows;
     if (row0 >= sp.rows) return;
