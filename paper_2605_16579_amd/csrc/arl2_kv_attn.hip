@@ -330,33 +330,20 @@ __global__ __launch_bounds__(64 * kWaves, 3) void kv_stream_kernel(KvAttnArgs a)
     }
 }
 
-// Joins a row's partial results, in the order of the splits within each of 8 groups and then of the groups.
+// Adds the partial results of splits `first`, first + step, .. (up to n) of a row into (m, l, sum): four features from d on, four
+// splits at a time, whose loads do not wait for one another.
 template <int D>
-__global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a)
+__device__ __forceinline__ void add_splits(const KvAttnArgs &a, size_t slot0, int first, int step, int n, int d, float &m, float &l, f32x4 &sum)
 {
-    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
-    __shared__ __attribute__((aligned(16))) float sm_o[GROUPS][D];
-    __shared__ float sm_ml[GROUPS][2];
-    const int unit = blockIdx.x / a.tile_rows, rr = blockIdx.x % a.tile_rows;
-    const int qt = unit % a.n_tiles, bh = unit / a.n_tiles, h = bh % a.pool.heads, b = bh / a.pool.heads;
-    const Span sp = span_of(a, b);
-    const int row0 = qt * a.tile_rows, row = row0 + rr;
-    if (row >= sp.rows) return;
-    const int lim_max = sp.limit(min(row0 + a.tile_rows, sp.rows) - 1, a);
-    if (lim_max <= a.chunk) return;                    // written by the one workgroup that saw it all
-    const int n = (lim_max + a.chunk - 1) / a.chunk;
-    const int g = threadIdx.x / LANES, d = 4 * (threadIdx.x % LANES);
-    float m = -INFINITY, l = 0.f;
-    f32x4 sum = {0, 0, 0, 0};
     constexpr int AT_ONCE = 4;
-    for (int s0 = g; s0 < n; s0 += GROUPS * AT_ONCE) {
+    for (int s0 = first; s0 < n; s0 += step * AT_ONCE) {
         f32x2 ml[AT_ONCE];
         f32x4 y[AT_ONCE];
         float m_new = m;
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
-            const int s = s0 + GROUPS * k;
-            const size_t slot = ((size_t)unit * a.nsplit + min(s, n - 1)) * a.tile_rows + rr;
+            const int s = s0 + step * k;
+            const size_t slot = slot0 + (size_t)min(s, n - 1) * a.tile_rows;
             ml[k] = *(const f32x2 *)(a.part_ml + slot * 2);
             y[k] = *(const f32x4 *)(a.part_o + slot * D + d);
             if (s >= n) ml[k] = f32x2{-INFINITY, 0.f}, y[k] = f32x4{0, 0, 0, 0};
@@ -376,31 +363,67 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a)
         }
         m = m_new;
     }
-    *(f32x4 *)&sm_o[g][d] = sum;
-    if (d == 0) {
-        sm_ml[g][0] = m;
-        sm_ml[g][1] = l;
-    }
-    __syncthreads();
-    if (g > 0) return;
-    m = sm_ml[0][0];
+}
+
+// Joins the partial results of rows that more than one workgroup worked on.  Up to kFewSplits splits: D / 4 lanes to a row, in the
+// order of the splits.  More: a workgroup to a row, 1024 / D splits side by side, then these in order.
+// In us, 32768 rows of 2 splits 13 and 53 with a workgroup to a row; 32 rows of 94 splits 5.
+constexpr int kFewSplits = 8;
+template <int D, bool FEW>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a)
+{
+    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+    const int g = threadIdx.x / LANES, d = 4 * (threadIdx.x % LANES);
+    const int per_unit = FEW ? (a.tile_rows + GROUPS - 1) / GROUPS : a.tile_rows;
+    const int unit = blockIdx.x / per_unit, rr = FEW ? (int)(blockIdx.x % per_unit) * GROUPS + g : blockIdx.x % per_unit;
+    const int qt = unit % a.n_tiles, bh = unit / a.n_tiles, h = bh % a.pool.heads, b = bh / a.pool.heads;
+    const Span sp = span_of(a, b);
+    const int row0 = qt * a.tile_rows, row = row0 + rr;
+    if (rr >= a.tile_rows || row >= sp.rows) return;
+    const int lim_max = sp.limit(min(row0 + a.tile_rows, sp.rows) - 1, a);
+    if (lim_max <= a.chunk) return;                    // written by the one workgroup that saw it all
+    const int n = (lim_max + a.chunk - 1) / a.chunk;
+    const size_t slot0 = (size_t)unit * a.nsplit * a.tile_rows + rr;
+    float m = -INFINITY, l = 0.f;
+    f32x4 sum = {0, 0, 0, 0};
+    add_splits<D>(a, slot0, FEW ? 0 : g, FEW ? 1 : GROUPS, n, d, m, l, sum);
+    if constexpr (!FEW) {
+        __shared__ __attribute__((aligned(16))) float sm_o[GROUPS][D];
+        __shared__ float sm_ml[GROUPS][2];
+        *(f32x4 *)&sm_o[g][d] = sum;
+        if (d == 0) {
+            sm_ml[g][0] = m;
+            sm_ml[g][1] = l;
+        }
+        __syncthreads();
+        if (g > 0) return;
+        m = sm_ml[0][0];
 #pragma unroll
-    for (int i = 1; i < GROUPS; ++i) m = fmaxf(m, sm_ml[i][0]);
-    const float m_ref = fmaxf(m, -FLT_MAX);
-    sum = f32x4{0, 0, 0, 0};
-    l = 0.f;
+        for (int i = 1; i < GROUPS; ++i) m = fmaxf(m, sm_ml[i][0]);
+        const float m_ref = fmaxf(m, -FLT_MAX);
+        sum = f32x4{0, 0, 0, 0};
+        l = 0.f;
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
-        const float f = __builtin_amdgcn_exp2f(sm_ml[i][0] - m_ref);
-        l = fmaf(sm_ml[i][1], f, l);
+        for (int i = 0; i < GROUPS; ++i) {
+            const float f = __builtin_amdgcn_exp2f(sm_ml[i][0] - m_ref);
+            l = fmaf(sm_ml[i][1], f, l);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[j] = fmaf(sm_o[i][d + j], f, sum[j]);
+            for (int j = 0; j < 4; ++j) sum[j] = fmaf(sm_o[i][d + j], f, sum[j]);
+        }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     bf16x4 y;
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = to_bf16(sum[i] * inv);
     *(bf16x4 *)((bf16_t *)a.out + (((size_t)b * a.Lq + row / a.G) * a.H + (size_t)h * a.G + row % a.G) * D + d) = y;
+}
+
+template <int D>
+hipError_t launch_join(const KvAttnArgs &a, hipStream_t stream)
+{
+    constexpr int GROUPS = 1024 / D;
+    if (a.nsplit > kFewSplits) return launch_kernel(kv_join_kernel<D, false>, dim3((unsigned)a.units * a.tile_rows), dim3(256), stream, a);
+    return launch_kernel(kv_join_kernel<D, true>, dim3((unsigned)a.units * ((a.tile_rows + GROUPS - 1) / GROUPS)), dim3(256), stream, a);
 }
 
 }  // namespace
@@ -415,13 +438,12 @@ KvAttnPlan kv_attn_plan(int B, int Lq, int G, const KvPool &pool, int D)
     p.units = heads * p.n_tiles;
     long long chunk = 256;
     if (p.tiled) {
-        // the fewest rounds of one workgroup per CU, each split paying for its partial results
         double best = 1e30;
-        for (int s = 1; s <= 32; ++s) {
-            const long long tokens = ((cap + s - 1) / s + 255) / 256 * 256;
-            const long long n = (cap + tokens - 1) / tokens;
+        for (int n = 1; n <= 64; ++n) {
+            const long long tokens = std::max((cap + n - 1) / n + 63, 256LL) / 64 * 64;
+            if (n > 1 && (cap + tokens - 1) / tokens < n) continue;
             const double rounds = (double)((p.units * n + kNumCu - 1) / kNumCu);
-            const double us = rounds * (tokens / 64 * 1.4 + 8) + (n > 1 ? 5 + (double)heads * rows * n * D * 8 / 4.5e6 : 0);
+            const double us = rounds * (tokens / 64 * (D == 128 ? 1.42 : 1.0) + 7) + (n > 1 ? 5 + (double)heads * rows * n * D * 8 / 4.5e6 : 0);
             if (us < best) { best = us; chunk = tokens; }
         }
     } else {
@@ -449,8 +471,7 @@ hipError_t launch_kv_attn(KvAttnArgs a, const KvAttnPlan &p, void *workspace, hi
     const dim3 grid((unsigned)(p.units * p.nsplit)), block(64 * kWaves);
     hipError_t e = p.tiled ? launch_kv_tile(a, grid.x, stream) : a.D == 128 ? launch_kernel(kv_stream_kernel<128>, grid, block, stream, a) : launch_kernel(kv_stream_kernel<64>, grid, block, stream, a);
     if (e != hipSuccess || p.nsplit == 1) return e;
-    const dim3 jgrid((unsigned)(p.units * p.tile_rows));
-    return a.D == 128 ? launch_kernel(kv_join_kernel<128>, jgrid, dim3(256), stream, a) : launch_kernel(kv_join_kernel<64>, jgrid, dim3(256), stream, a);
+    return a.D == 128 ? launch_join<128>(a, stream) : launch_join<64>(a, stream);
 }
 
 }  // namespace arl2
