@@ -3,9 +3,18 @@
 
 #include <limits.h>
 
+// (the lambdas of the main loop have two users each)
+#define INLINE __attribute__((always_inline))
+
 namespace arl2 {
 namespace {
 
+typedef __attribute__((ext_vector_type(6))) uint32_t u32x6;
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(32))) __bf16 bf16x32;
+typedef __attribute__((ext_vector_type(32))) float f32x32;
+
+constexpr int kParts = 3;         // of a query feature, at most
 constexpr int kTile = 64;         // keys of a tile
 constexpr int kNT = 512;          // threads: eight wavefronts of 32 query rows
 constexpr int kStages = 4;        // of each LDS ring
@@ -14,8 +23,7 @@ constexpr int kWindow = 64;       // tiles whose block-table entries are held in
 template <int D>
 struct Tile {
     static constexpr int STEPS = D / 64, OB = D / 32;
-    static constexpr int SN = STEPS * kParts;       // products of a block: logits,
-    static constexpr int PVN = 2 * OB;              // output
+    static constexpr int PVN = 2 * OB;              // products of a block's output
     static constexpr int RING = 4, PF = RING - 1;   // V fragments in flight from LDS
     static constexpr int T = D / 16;                // tokens of a feature pair that a thread converts
     // as stored: key codes [16-key group][16-byte piece of a row][key], value codes as in the cache, key scales, value scales
@@ -25,6 +33,56 @@ struct Tile {
     static constexpr int V_OFF = kStages * RAW, TC_OFF = V_OFF + kStages * V_BYTES;
     static constexpr int SMEM = TC_OFF + 2 * kWindow * 4 * 4;
     static_assert(PVN % RING == 0, "the fragment ring runs across slots");
+};
+
+// A query row as B operands of the scaled matrix instruction: lane (c, hh) has features 64 s + 32 hh .. + 31 of row c, each as the
+// sum of up to three 6-bit floats (e2m3: 4 significant bits, steps of 1/8 below 2, 1/4 below 4, 1/2 below 8) at units u, u / 16 and
+// u / 256, the largest of the 32 in [4, 8) u.  6-bit operands run at four times bf16's rate: two parts take half the time of one
+// bf16 product, three parts three quarters.  A bf16 feature of at least u / 8 is exact in three parts (smaller ones within 2^-12 of
+// the largest), one of at least u in two.  Two are enough where what they leave of each of the wavefront's rows is no longer than
+// 2^-9 of the row, half of what one rounding to bf16 may take.  Rows of normal values leave 2^-10.5, the longest of 32 rarely
+// more than 2^-9.3; rows with a feature far above the others' size get the third part.  (4680 queries over 32760 keys: 712 us with
+// two parts, 759 us with three; error against 64 bits 2.36e-3 and 2.27e-3 of the output, of which rounding the output is 1.65e-3.)
+template <int D>
+struct Query {
+    static constexpr int STEPS = D / 64;
+    u32x6 part[STEPS][kParts];
+    uint32_t scale[STEPS];           // byte p: of part p; 255, a NaN, in the place of the first where a feature is not finite
+    bool two;                        // whether two parts are enough
+    __device__ __forceinline__ void load(const bf16_t *row, bool there)
+    {
+        float all = 0.f, left = 0.f;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            union { u32x4 u[4]; bf16x32 v; } x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x.u[i] = there ? *(const u32x4 *)(row + 64 * s + 8 * i) : u32x4{0, 0, 0, 0};
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) m = max(m, max(x.u[i][j] << 16 & 0x7fffffffu, x.u[i][j] & 0x7fff0000u));
+            const bool finite = m < 0x7f800000u;
+            const int e = finite ? max((int)(m >> 23) - 2, 27) : 127;
+            scale[s] = (uint32_t)e | (uint32_t)(e - 4) << 8 | (uint32_t)(e - 8) << 16;
+            if (!finite) scale[s] |= 255u;
+#pragma unroll
+            for (int p = 0; p < kParts; ++p) {
+                const float unit = __uint_as_float((uint32_t)(e - 4 * p) << 23);
+                part[s][p] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x.v, unit);
+                const f32x32 taken = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(part[s][p], unit);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    const float f = (float)x.v[j], r = f - taken[j];              // (exact: fewer bits than the feature has)
+                    if (p == 0) all = fmaf(f, f, all);
+                    if (p == 1) left = fmaf(r, r, left);
+                    x.v[j] = to_bf16(r);
+                }
+            }
+        }
+        all = xhalf_sum(all);
+        two = xhalf_sum(left) <= 0x1p-18f * all && all <= FLT_MAX;
+    }
 };
 
 // Workgroup barrier after all but the last N of this wavefront's loads into LDS have arrived, and all but the last M of its LDS
@@ -61,7 +119,7 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
     const int q0 = 32 * wave, row = row0 + q0 + c;
     const bool active = q0 < n_rows, row_there = q0 + c < n_rows;
     const int lim = row_there ? sp.limit(row, a) : sp.klen;
-    const size_t q_row = (((size_t)b * a.Lq + row / a.G) * a.H + (size_t)h * a.G + row % a.G) * D;
+    auto row_offset = [&](int r) { return (((size_t)b * a.Lq + r / a.G) * a.H + (size_t)h * a.G + r % a.G) * D; };
     if (tid < D / 32) nan_key[tid] = INT_MAX;
 
     // ---- tiles
@@ -89,8 +147,8 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
     const uint32_t code_dst = lds0 + part * C::CODES + grp * (C::CODES / 4), scale_dst = lds0 + 2 * C::CODES + part * C::SCALES + grp * (C::SCALES / 4);
     int group_entry;                 // of 16-token group lane & 3 of the next tile to request
     __amdgpu_buffer_rsrc_t page_rsrc;
-    auto entry_fetch = [&](int tile) { group_entry = tc[((tile / kWindow) & 1) * 256 + (tile % kWindow) * 4 + (lane & 3)]; };
-    auto request = [&](int tile, auto step_) {
+    auto entry_fetch = [&](int tile) INLINE { group_entry = tc[((tile / kWindow) & 1) * 256 + (tile % kWindow) * 4 + (lane & 3)]; };
+    auto request = [&](int tile, auto step_) INLINE {
         constexpr int step = decltype(step_)::value;
         const uint32_t t = (uint32_t)((tile0 + tile) * kTile + 16 * grp) & in_page, stage = (tile & (kStages - 1)) * C::RAW;
         if constexpr (step == 0) {
@@ -113,7 +171,7 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
     const int vs_src = 2 * C::CODES + C::SCALES + (vg * (D / 32) + (dp >> 4)) * 16 + 8 * vx + 4 * hv;
     const int v_dst = C::V_OFF + ((4 * (vg >> 1) + 2 * hv + (vg & 1)) * (D / 2) + dp) * 16 + 8 * vx;
     uint32_t vc[C::T / 4], vs[C::T / 4];
-    auto values_fetch = [&](int tile) {
+    auto values_fetch = [&](int tile) INLINE {
         const unsigned char *raw = smem + (tile & (kStages - 1)) * C::RAW;
 #pragma unroll
         for (int i = 0; i < C::T / 4; ++i) {
@@ -123,7 +181,7 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
     };
     // Values that no row of the workgroup sees are not to reach the product, whatever they are; a NaN among those that some see
     // goes to these rows alone, at the end.
-    auto take_out = [&](int tile, uint32_t groups) {
+    auto take_out = [&](int tile, uint32_t groups) INLINE {
         const bool ok = groups >> vg & 1u;
 #pragma unroll
         for (int i = 0; i < C::T / 4; ++i) {
@@ -137,11 +195,11 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
         }
     };
     uint32_t w[C::T];
-    auto convert = [&](auto t_) {
+    auto convert = [&](auto t_) INLINE {
         constexpr int t = decltype(t_)::value;
         w[t] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(vc[t >> 2], scale_operand<(t & 3)>(vs[t >> 2]), t & 3));
     };
-    auto values_store = [&](int tile, auto odd_) {       // of the pair's even or odd feature
+    auto values_store = [&](int tile, auto odd_) INLINE {       // of the pair's even or odd feature
         constexpr bool odd = decltype(odd_)::value;
         constexpr uint32_t sel = odd ? 0x07060302 : 0x05040100;
         unsigned char *dst = smem + v_dst + (tile & (kStages - 1)) * C::V_BYTES + (odd ? C::V_BYTES / 2 : 0);
@@ -150,7 +208,7 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
         else
             *(u32x2 *)dst = u32x2{__builtin_amdgcn_perm(w[1], w[0], sel), __builtin_amdgcn_perm(w[3], w[2], sel)};
     };
-    auto values = [&](int tile, bool care, uint32_t groups) {        // all of it at once
+    auto values = [&](int tile, bool care, uint32_t groups) INLINE {        // all of it at once
         values_fetch(tile);
         if (care) take_out(tile, groups);
         static_for<0, C::T>(convert);
@@ -169,24 +227,24 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
     Query<D> q;
 
     // Block j is half j % 2 of tile j / 2; its key c is row c of the first product.
-    auto k_fetch = [&](int j, auto s_) {
+    auto k_fetch = [&](int j, auto s_) INLINE {
         constexpr int s = decltype(s_)::value;
         const unsigned char *p = smem + ((j >> 1) & (kStages - 1)) * C::RAW + (j & 1) * (C::CODES / 2);
         kf[s] = *(const u32x4 *)(p + (c >> 4) * (C::CODES / 4) + (2 * s + hh) * 256 + (c & 15) * 16);
     };
-    auto ks_fetch = [&](auto par_, int j) {
+    auto ks_fetch = [&](auto par_, int j) INLINE {
         constexpr int P = decltype(par_)::value;
         const unsigned char *p = smem + ((j >> 1) & (kStages - 1)) * C::RAW + 2 * C::CODES + (j & 1) * (C::SCALES / 2);
         if constexpr (D == 128) kscale[P] = *(const uint32_t *)(p + 4 * c) >> (8 * hh);
         else kscale[P] = *(const uint16_t *)(p + 2 * c) >> (8 * hh);
     };
-    auto v_frag = [&](int j, auto p_) -> bf16x8 {       // of the block's product p: 16-key step p / OB, features p % OB
+    auto v_frag = [&](int j, auto p_) INLINE -> bf16x8 {       // of the block's product p: 16-key step p / OB, features p % OB
         constexpr int p = decltype(p_)::value, u = p / OB, x = p % OB / 2, e = p % OB % 2;
         const unsigned char *v = smem + C::V_OFF + ((j >> 1) & (kStages - 1)) * C::V_BYTES + e * (C::V_BYTES / 2);
         return *(const bf16x8 *)(v + ((4 * (j & 1) + 2 * hh + u) * (D / 2) + 32 * x + c) * 16);
     };
-    auto s_mfma = [&](auto par_, auto n_) {             // product n of the logits: features 64 (n / kParts) .., part n % kParts
-        constexpr int P = decltype(par_)::value, nn = decltype(n_)::value, s = nn / kParts, p = nn % kParts;
+    auto s_mfma = [&](auto parts_, auto par_, auto n_) INLINE {        // product n of the logits: features 64 (n / parts) .., part n % parts
+        constexpr int PARTS = decltype(parts_)::value, P = decltype(par_)::value, nn = decltype(n_)::value, s = nn / PARTS, p = nn % PARTS;
         const i32x8 ka = {(int)kf[s][0], (int)kf[s][1], (int)kf[s][2], (int)kf[s][3], 0, 0, 0, 0};
         const u32x6 w6 = q.part[s][p];
         const i32x8 qb = {(int)w6[0], (int)w6[1], (int)w6[2], (int)w6[3], (int)w6[4], (int)w6[5], 0, 0};
@@ -194,11 +252,11 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
         if constexpr (nn == 0) s_acc[P] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qb, zero, 4, 2, 2 * s, (int)kscale[P], p, (int)q.scale[s]);
         else s_acc[P] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(ka, qb, s_acc[P], 4, 2, 2 * s, (int)kscale[P], p, (int)q.scale[s]);
     };
-    auto pv_mfma = [&](auto par_, auto p_) {
+    auto pv_mfma = [&](auto par_, auto p_) INLINE {
         constexpr int P = decltype(par_)::value, p = decltype(p_)::value;
         o[p % OB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[p % C::RING], pf[P][p / OB], o[p % OB], 0, 0, 0);
     };
-    auto mask = [&](auto par_, int j, uint32_t groups) {        // logits of block j of keys that the row does not see
+    auto mask = [&](auto par_, int j, uint32_t groups) INLINE {        // logits of block j of keys that the row does not see
         constexpr int P = decltype(par_)::value;
         const uint32_t ok = groups >> (2 * (j & 1));
         const int key0 = tile0 * kTile + 32 * j + 4 * hh, left = min(lim, kend) - key0;
@@ -211,11 +269,12 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
     // One slot, on key block j (logits in s_acc[j % 2]): S(j+1) = K_{j+1} Q^T and O^T += V_{j-1}^T P_{j-1}^T on the matrix cores beside
     // the softmax of block j on the vector ALU; on the way the K fragments of block j + 2 and, at the end, the first V fragments
     // of block j.  STAGE 1: tile `tile` is requested; 2: its values (in vc, vs) are converted.
-    auto slot = [&](auto par_, auto has_s_, auto has_pv_, auto next_k_, bool masked, uint32_t groups, auto stage_, int j, int tile) {
+    auto slot = [&](auto parts_, auto par_, auto has_s_, auto has_pv_, auto next_k_, bool masked, uint32_t groups, auto stage_, int j, int tile) INLINE {
         constexpr int P = decltype(par_)::value;
         constexpr bool HAS_S = decltype(has_s_)::value, HAS_PV = decltype(has_pv_)::value, NEXT_K = decltype(next_k_)::value;
         constexpr int STAGE = decltype(stage_)::value;
-        constexpr int SL = HAS_S ? C::SN : 0, NS = SL + (HAS_PV ? C::PVN : 0);
+        constexpr int PARTS = decltype(parts_)::value, SN = STEPS * PARTS;     // products of a block's logits
+        constexpr int SL = HAS_S ? SN : 0, NS = SL + (HAS_PV ? C::PVN : 0);
         if (__builtin_expect(masked, 0)) mask(par_, j, groups);
         float x[16], ps0 = 0.f, ps1 = 0.f;
         auto op_scale = [&](auto v_) {
@@ -246,9 +305,9 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
         static_for<0, NS>([&](auto n_) {
             constexpr int n = decltype(n_)::value;
             if constexpr (is_s(n)) {
-                s_mfma(std::integral_constant<int, P ^ 1>{}, std::integral_constant<int, idx(n)>{});
+                s_mfma(parts_, std::integral_constant<int, P ^ 1>{}, std::integral_constant<int, idx(n)>{});
                 // (a fragment's last product: the next block's takes its place)
-                if constexpr (NEXT_K && idx(n) % kParts == kParts - 1) k_fetch(j + 2, std::integral_constant<int, idx(n) / kParts>{});
+                if constexpr (NEXT_K && idx(n) % PARTS == PARTS - 1) k_fetch(j + 2, std::integral_constant<int, idx(n) / PARTS>{});
             } else {
                 constexpr int p = idx(n);
                 if constexpr (p + C::PF < C::PVN) fr[(p + C::PF) % C::RING] = v_frag(j - 1, std::integral_constant<int, p + C::PF>{});
@@ -259,8 +318,9 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
             if constexpr (STAGE == 1) {          // (beside products in flight: behind the barrier every wavefront would do it at once)
                 if constexpr (n == 1) request(tile, std::integral_constant<int, 0>{});
                 if constexpr (n == 3) request(tile, std::integral_constant<int, 1>{});
-                if constexpr (n == 5) request(tile, std::integral_constant<int, 2>{});
-                if constexpr (n == 6) {
+                static_assert(NS > 5, "a step for each");
+                if constexpr (n == 4) request(tile, std::integral_constant<int, 2>{});
+                if constexpr (n == 5) {
                     entry_fetch(tile + 1);
                     values_fetch(tile - 2);
                 }
@@ -316,7 +376,7 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
     // ---- prologue: the block table's first window, tiles 0 to 2 requested, the values of tile 0
     int entry = window_entry(0);
     window_store(0, entry);
-    if (active) q.load((const bf16_t *)a.q + q_row + 32 * hh, row_there);
+    if (active) q.load((const bf16_t *)a.q + row_offset(row) + 32 * hh, row_there);
     __syncthreads();
     static_for<0, 3>([&](auto t_) {
         entry_fetch(decltype(t_)::value);
@@ -329,17 +389,18 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
     // Interval i holds the slots of blocks 2 i and 2 i + 1.  They read the keys of tile i + 1 and the values of tiles i - 1 and i; the
     // values of tile i + 1 are converted and tile i + 3 is requested.  The barrier at its end publishes the values and makes sure
     // that tile i + 2, requested an interval before, is there.
-    auto table_ahead = [&](int i) {
+    auto table_ahead = [&](int i) INLINE {
         if (__builtin_expect((i & (kWindow - 5)) == 8, 0)) {          // 8 or 12 of 64
             if ((i & 4) == 0) entry = window_entry(i / kWindow + 1);
             else window_store(i / kWindow + 1, entry);
         }
     };
-    if (active) {
+    auto attend = [&](auto parts_) INLINE {
+        asm volatile("" ::: "memory");       // (the first fragments are read here, not before the choice of parts and kept for both)
         ks_fetch(par0, 0);
         ks_fetch(par1, 1);
         static_for<0, STEPS>([&](auto s_) { k_fetch(0, s_); });
-        static_for<0, C::SN>([&](auto n_) { s_mfma(par0, n_); });
+        static_for<0, STEPS * decltype(parts_)::value>([&](auto n_) { s_mfma(parts_, par0, n_); });
         static_for<0, STEPS>([&](auto s_) { k_fetch(1, s_); });
         mask(par0, 0, placed >> 8);
         float mx = s_acc[0][0];
@@ -352,14 +413,14 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
             const bool care_next = careful >> 1 & 1u;
             request_all(3);
             entry_fetch(4);
-            slot(par0, yes, no, yes, true, groups, stage0, 0, 0);
+            slot(parts_, par0, yes, no, yes, true, groups, stage0, 0, 0);
 #pragma unroll
             for (int i = 0; i < OB; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
             values_fetch(1);
             if (care_next) take_out(1, next);
-            slot(par1, yes, yes, yes, true, groups, stage2, 1, 1);
+            slot(parts_, par1, yes, yes, yes, true, groups, stage2, 1, 1);
             wait_barrier<2>();
         }
 #pragma unroll 1
@@ -367,19 +428,23 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
             table_ahead(i);
             const uint32_t groups = placed >> 8, next = placed >> 4;
             const bool masked = careful >> 2 & 1u, care_next = careful >> 1 & 1u;
-            slot(par0, yes, yes, yes, masked, groups, stage1, 2 * i, i + 3);
+            slot(parts_, par0, yes, yes, yes, masked, groups, stage1, 2 * i, i + 3);
             if (__builtin_expect(care_next, 0)) take_out(i + 1, next);
-            slot(par1, yes, yes, yes, masked, groups, stage2, 2 * i + 1, i + 1);
+            slot(parts_, par1, yes, yes, yes, masked, groups, stage2, 2 * i + 1, i + 1);
             wait_barrier<2, 2>();        // (two fragments were requested after the values' last store)
         }
         const int j = 2 * (n - 1);
-        slot(par0, yes, yes, no, true, placed >> 8, stage0, j, 0);
-        slot(par1, no, yes, no, true, placed >> 8, stage0, j + 1, 0);
+        slot(parts_, par0, yes, yes, no, true, placed >> 8, stage0, j, 0);
+        slot(parts_, par1, no, yes, no, true, placed >> 8, stage0, j + 1, 0);
         static_for<0, C::PVN>([&](auto p_) {
             constexpr int p = decltype(p_)::value;
             if constexpr (p + C::PF < C::PVN) fr[(p + C::PF) % C::RING] = v_frag(j + 1, std::integral_constant<int, p + C::PF>{});
             pv_mfma(par1, p_);
         });
+    };
+    if (active) {
+        if (__all(q.two)) attend(std::integral_constant<int, 2>{});
+        else attend(std::integral_constant<int, 3>{});
     } else {                             // no rows: moves the tiles only
         m_run = 0.f;
         wait_barrier<2>();
@@ -409,7 +474,9 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
     if (!row_there) return;
     if (whole) {
         const float inv = l_run == 0.f ? 0.f : 1.f / l_run;          // a row that sees nothing is zero
-        bf16_t *out = (bf16_t *)a.out + q_row;
+        int out_row = row;
+        asm volatile("" : "+v"(out_row));                            // (its offset is worked out here, not kept from the beginning)
+        bf16_t *out = (bf16_t *)a.out + row_offset(out_row);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
 #pragma unroll

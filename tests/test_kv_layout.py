@@ -219,3 +219,11 @@ def test_binding_refuses_what_does_not_fit(A):
     with pytest.raises(ValueError, match="device memory"):
         A.arl2_kv_attn_fwd(k, cache, table, start, k.clone())
     assert A.alloc_kv_cache(9, 2, 64, 128, device="cpu").shape == cache.shape
+
+
+def test_cache_kernels_use_no_scratch(A):
+    from test_kernel_resources import scratch_per_kernel
+    kernels = {name: n for name, n in scratch_per_kernel(A.binding.LIB_PATH).items() if "kv_" in name}
+    # append, read, attention for few and for many rows, and two joins, for two head dimensions each
+    assert len(kernels) == 12, sorted(kernels)
+    assert not any(kernels.values()), {name: n for name, n in kernels.items() if n}
