@@ -139,7 +139,7 @@ bool overlaps_any(Range out, const Range (&in)[N])
 bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // The kernels give a thread to 8 features of four tokens.
-bool kv_rows_fit(const arl2_kv_desc *d) { return (double)d->B * d->Hkv * ((d->Lq + 3.0) / 4 + 1) * (d->D / 8) <= 2147483000.0; }
+bool kv_rows_fit(const arl2_kv_desc *d) { return (double)d->B * d->Hkv * ((d->Lq + 15.0) / 16 + 1) * (d->D / 2) <= 2147483000.0; }
 
 arl2::KvRowsArgs kv_rows_args(const arl2_kv_desc *d, const int32_t *table, const int32_t *start, const int32_t *count)
 {

@@ -12,8 +12,10 @@
 // The conversion to e2m1 is the hardware's (round to nearest even, saturating).
 //
 // One thread: 8 features of four tokens at positions 4 m .. 4 m + 3, keys and values: 16-byte loads, a row by D / 8 consecutive
-// lanes, the group's maximum by two exchanges between four lanes.  The four tokens of a value pair are one 4-byte store (they are
-// neighbours in the cache); where the call has only some of the four tokens they are stored byte by byte.
+// lanes, the group's maximum by two exchanges between four lanes.  Four neighbouring threads groups make a 16-token group; the
+// heads of a group follow one another, so that a workgroup's heads find the rotation tables in its CU's cache.  The four tokens of
+// a value pair are one 4-byte store (they are neighbours in the cache), at D = 128 the whole group's 16 tokens one 16-byte store after
+// an exchange between lanes; where the call has only some of the tokens they are stored byte by byte.
 #include "arl2_device.h"
 
 namespace arl2 {
@@ -72,6 +74,22 @@ __device__ __forceinline__ u32x4 transpose_bytes(u32x4 x)
     return r;
 }
 
+// Words I and J become (I's lower and J's lower half-wave, I's upper and J's upper one); the same with every 16 lanes and the next.
+template <int I, int J>
+__device__ __forceinline__ void swap32(u32x4 &x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(x[I], x[J], false, false);
+    x[I] = r[0];
+    x[J] = r[1];
+}
+template <int I, int J>
+__device__ __forceinline__ void swap16(u32x4 &x)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(x[I], x[J], false, false);
+    x[I] = r[0];
+    x[J] = r[1];
+}
+
 // What a thread works on.
 struct Item {
     int b, h, chunk;        // stream, head, 8-feature chunk
@@ -92,15 +110,16 @@ __device__ __forceinline__ bool item_of(const KvRowsArgs &a, Item &it)
     const uint32_t id = blockIdx.x * kThreads + threadIdx.x;
     it.chunk = id % CPR;
     uint32_t rest = id / CPR;
-    const uint32_t quads = (uint32_t)(a.L + 3) / 4 + 1;
-    const uint32_t quad = rest % quads;
-    rest /= quads;
+    const uint32_t quad = rest & 3, groups = (uint32_t)(a.L + 15) / 16 + 1;
+    rest >>= 2;
     it.h = rest % a.pool.heads;
-    it.b = rest / a.pool.heads;
+    rest /= a.pool.heads;
+    const uint32_t group = rest % groups;
+    it.b = rest / groups;
     if (it.b >= a.B) return false;
     it.first = a.start[it.b];
     it.count = a.count != nullptr ? kv_clamp(a.count[it.b], a.L) : a.L;
-    it.pos = ((it.first >> 2) + quad) * 4;                 // (a negative position has no page)
+    it.pos = ((it.first >> 4) + group) * 16 + 4 * quad;    // (a negative position has no page)
     if (!it.has_any()) return false;
     it.page = kv_page(a.pool, a.table + (size_t)it.b * a.pool.max_pages, it.pos);
     return true;
@@ -110,10 +129,8 @@ template <int D>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvRowsArgs a)
 {
     Item it;
-    // (the four lanes of a group have the same page and leave together)
-    if (!item_of<D>(a, it) || it.page < 0) return;
+    if (!item_of<D>(a, it)) return;
     const int shift = a.pool.shift, t = (int)it.pos & ((1 << shift) - 1), H = a.pool.heads;
-    unsigned char *base = (unsigned char *)a.cache + kv_head_offset(a.pool, D, it.page, it.h);
     u32x4 kx[4], vx[4];
     f32x4 cs[4], sn[4];
 #pragma unroll
@@ -123,11 +140,16 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvRowsArgs a)
         const size_t off = it.row(i, a.L, H) * D + 8 * it.chunk;
         kx[i] = *(const u32x4 *)((const bf16_t *)a.k + off);
         vx[i] = *(const u32x4 *)((const bf16_t *)a.v + off);
-        if (a.cs != nullptr) {
+        if (a.cs != nullptr && it.pos + i >= 0 && it.pos + i < kv_capacity(a.pool)) {       // (the tables' rows)
             cs[i] = *(const f32x4 *)(a.cs + (size_t)(it.pos + i) * (D / 2) + 4 * it.chunk);
             sn[i] = *(const f32x4 *)(a.sn + (size_t)(it.pos + i) * (D / 2) + 4 * it.chunk);
         }
     }
+    // The rows are on their way before the page is known to exist: they are there in any case.  The four lanes of a group have the same
+    // page and leave together.
+    asm volatile("" ::: "memory");
+    if (it.page < 0) return;
+    unsigned char *base = (unsigned char *)a.cache + kv_head_offset(a.pool, D, it.page, it.h);
     u32x4 vcodes;
     uint32_t vscale[4];
 #pragma unroll
@@ -154,9 +176,19 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(KvRowsArgs a)
         }
     }
     if (it.has_all()) {
-        const u32x4 r = transpose_bytes(vcodes);
+        u32x4 r = transpose_bytes(vcodes);
+        if (D == 128 && __popcll(__ballot(true)) == kWave) {
+            // The wavefront has all of a 16-token group.  Lane 16 q + i holds tokens 4 q .. of feature pairs 4 i + j in word j; after the
+            // exchange it holds all tokens of pair 4 i + q.
+            swap32<0, 2>(r);
+            swap32<1, 3>(r);
+            swap16<0, 1>(r);
+            swap16<2, 3>(r);
+            *(u32x4 *)(base + kv_value_codes(shift, t & ~15, 4 * it.chunk + ((threadIdx.x >> 4) & 3), D)) = r;
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) *(uint32_t *)(base + kv_value_codes(shift, t, 4 * it.chunk + j, D)) = r[j];
+            for (int j = 0; j < 4; ++j) *(uint32_t *)(base + kv_value_codes(shift, t, 4 * it.chunk + j, D)) = r[j];
+        }
         if ((it.chunk & 3) == 0)
             *(uint32_t *)(base + kv_value_scales(shift, t, it.chunk >> 2, D)) = vscale[0] | vscale[1] << 8 | vscale[2] << 16 | vscale[3] << 24;
         return;
@@ -202,7 +234,7 @@ __global__ __launch_bounds__(kThreads) void kv_read_kernel(KvRowsArgs a)
 
 unsigned row_groups(const KvRowsArgs &a, int D)
 {
-    const long long n = (long long)a.B * a.pool.heads * ((a.L + 3) / 4 + 1) * (D / 8);
+    const long long n = (long long)a.B * a.pool.heads * ((a.L + 15) / 16 + 1) * 4 * (D / 8);
     return (unsigned)((n + kThreads - 1) / kThreads);
 }
 
