@@ -133,7 +133,7 @@ def stack_report(A, W, torch, dev, layers=30, hybrid_layers=22, chunks=7, reps=5
     }
 
 
-def stack_execute(A, W, torch, dev, layers=30, hybrid_layers=22, chunks=7, pool=3):
+def stack_execute(A, W, torch, dev, layers=30, hybrid_layers=22, chunks=7, pool=3, kv_cache="bf16"):
     """The same stack, executed: for each of `chunks` chunks the chunk's keys and values are appended to the
     KV cache of every softmax layer, then `passes` readout passes run through all layers in order (a hybrid
     layer reads its own fixed-size state, a softmax layer attends to its cache, current chunk included), then
@@ -141,7 +141,8 @@ def stack_execute(A, W, torch, dev, layers=30, hybrid_layers=22, chunks=7, pool=
     whole rollout back to back on one stream between two events; peak device memory is what torch's allocator
     reports for the caches, states and workspace of the stack (inputs and outputs are allocated before the
     measurement starts and excluded).  Inputs are synthetic: a pool of `pool` pre-drawn (q, k, v, g) sets is
-    cycled over layer passes, there is no model between the layers."""
+    cycled over layer passes, there is no model between the layers.  `kv_cache` "4bit": the softmax layers keep
+    the paged 4-bit cache (arl2_kv_append, arl2_kv_attn_fwd) instead of a dense bf16 one."""
     w = W.WORKLOADS["wan_layer"]
     P, L = w.passes, w.L
     sets = [tuple(t.to(dev) for t in W.pass_inputs(w, 100 + i, 0)) for i in range(pool)]
@@ -154,8 +155,16 @@ def stack_execute(A, W, torch, dev, layers=30, hybrid_layers=22, chunks=7, pool=
         torch.cuda.synchronize()
         torch.cuda.reset_peak_memory_stats()
         base = torch.cuda.memory_allocated()
-        caches = [(torch.empty((w.B, chunks * L, w.H, w.D), dtype=torch.bfloat16, device=dev),
-                   torch.empty((w.B, chunks * L, w.H, w.D), dtype=torch.bfloat16, device=dev)) for _ in range(n_soft)]
+        if kv_cache == "4bit":
+            page = 64
+            per_stream = (chunks * L + page - 1) // page
+            caches = [A.alloc_kv_cache(w.B * per_stream, w.H, page, w.D, device=dev) for _ in range(n_soft)]
+            table = torch.arange(w.B * per_stream, dtype=torch.int32, device=dev).view(w.B, per_stream)
+            lens = [torch.full((w.B,), c * L, dtype=torch.int32, device=dev) for c in range(chunks + 1)]
+            kv_ws = A.alloc_kv_workspace(w.B, w.H, w.H, L, w.D, page, per_stream, device=dev)
+        else:
+            caches = [(torch.empty((w.B, chunks * L, w.H, w.D), dtype=torch.bfloat16, device=dev),
+                       torch.empty((w.B, chunks * L, w.H, w.D), dtype=torch.bfloat16, device=dev)) for _ in range(n_soft)]
         states = [torch.zeros((w.B, w.H, w.D, w.D), dtype=torch.float32, device=dev) for _ in range(n_hybrid)]
         ws = A.alloc_workspace(w.B, w.H, L, w.D, torch.bfloat16, device=dev) if n_hybrid else None
         e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
@@ -164,14 +173,19 @@ def stack_execute(A, W, torch, dev, layers=30, hybrid_layers=22, chunks=7, pool=
         e0.record()
         for c in range(chunks):
             kc, vc, gate = cleans[c % pool]
-            for (ck, cv) in caches:                                  # cache growth: this chunk's K, V appended
-                ck[:, c * L:(c + 1) * L].copy_(kc)
-                cv[:, c * L:(c + 1) * L].copy_(vc)
+            for cache in caches:                                     # cache growth: this chunk's K, V appended
+                if kv_cache == "4bit":
+                    A.arl2_kv_append(kc, vc, cache, table, lens[c])
+                else:
+                    cache[0][:, c * L:(c + 1) * L].copy_(kc)
+                    cache[1][:, c * L:(c + 1) * L].copy_(vc)
             for p in range(P):
                 for l in range(layers):
                     q, k, v, g = sets[(c + p + l) % pool]
                     if l < n_hybrid:
                         A.arl2_hybrid_attn_fwd(q, k, v, states[l], g, out)
+                    elif kv_cache == "4bit":
+                        A.arl2_kv_attn_fwd(q, caches[l - n_hybrid], table, lens[c + 1], out, workspace=kv_ws)
                     else:
                         ck, cv = caches[l - n_hybrid]
                         A.arl2_hybrid_attn_fwd(q, ck[:, :(c + 1) * L], cv[:, :(c + 1) * L], None, None, out)
@@ -270,6 +284,8 @@ def main() -> int:
     ap.add_argument("--stack-report", action="store_true",
                     help="instead of the bench line: attention time and memory of a 30-layer stack over a "
                          "21-latent-frame rollout (7 chunks), 22 hybrid + 8 softmax-KV layers vs 30 softmax-KV layers")
+    ap.add_argument("--kv-cache", choices=("bf16", "4bit"), default="bf16",
+                    help="with --stack-report --execute: what the softmax layers keep their keys and values in")
     ap.add_argument("--execute", action="store_true",
                     help="with --stack-report: also run the whole rollout of both stacks for real (KV caches allocated and "
                          "appended to per chunk, every layer pass launched), time it end to end and report peak memory")
@@ -307,7 +323,7 @@ def main() -> int:
     if args.stack_report:
         rep = stack_report(A, W, torch, dev)
         if args.execute:
-            ex = stack_execute(A, W, torch, dev)
+            ex = stack_execute(A, W, torch, dev, kv_cache=args.kv_cache)
             rep["executed"] = ex
             rep["executed_over_weighted_sum"] = {
                 "hybrid_stack": ex["hybrid_stack"]["attention_ms"] / rep["hybrid_stack"]["attention_ms"],

@@ -36,13 +36,13 @@ struct Tile {
 };
 
 // A query row as B operands of the scaled matrix instruction: lane (c, hh) has features 64 s + 32 hh .. + 31 of row c, each as the
-// sum of up to three 6-bit floats (e2m3: 4 significant bits, steps of 1/8 below 2, 1/4 below 4, 1/2 below 8) at units u, u / 16 and
-// u / 256, the largest of the 32 in [4, 8) u.  6-bit operands run at four times bf16's rate: two parts take half the time of one
-// bf16 product, three parts three quarters.  A bf16 feature of at least u / 8 is exact in three parts (smaller ones within 2^-12 of
-// the largest), one of at least u in two.  Two are enough where what they leave of each of the wavefront's rows is no longer than
-// 2^-9 of the row, half of what one rounding to bf16 may take.  Rows of normal values leave 2^-10.5, the longest of 32 rarely
-// more than 2^-9.3; rows with a feature far above the others' size get the third part.  (4680 queries over 32760 keys: 712 us with
-// two parts, 759 us with three; error against 64 bits 2.36e-3 and 2.27e-3 of the output, of which rounding the output is 1.65e-3.)
+// sum of up to three 6-bit floats (e2m3: 4 significant bits, steps of 1/8 below 2, 1/4 below 4, 1/2 up to 7.5) at units u, u / 32 and
+// u / 256, the largest of the 32 in (3.75, 7.5] u.  6-bit operands run at four times bf16's rate: two parts take half the time of
+// one bf16 product, three parts three quarters.  Three parts are within 2^-12 u of a bf16 feature and exact from u / 8 on; two are
+// exact from u / 2 on (but for 2^-6 u where the first leaves just half a step of 1/2).  Two are enough where what they leave of each
+// of the wavefront's rows is no longer than 2^-9 of the row, half of what one rounding to bf16 may take.  Rows of normal values
+// leave 2^-10.9, the longest of 32 rarely more than 2^-9.1; rows with a feature far above the others' size get the third part.
+// (4680 queries over 32760 keys: 712 us with two parts, 759 us with three on one card.)
 template <int D>
 struct Query {
     static constexpr int STEPS = D / 64;
@@ -63,12 +63,12 @@ struct Query {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) m = max(m, max(x.u[i][j] << 16 & 0x7fffffffu, x.u[i][j] & 0x7fff0000u));
             const bool finite = m < 0x7f800000u;
-            const int e = finite ? max((int)(m >> 23) - 2, 27) : 127;
-            scale[s] = (uint32_t)e | (uint32_t)(e - 4) << 8 | (uint32_t)(e - 8) << 16;
+            const int e = finite ? max((int)((m + 0xfffffu) >> 23) - 2, 27) : 127;       // one more from above 7.5 on
+            scale[s] = (uint32_t)e | (uint32_t)(e - 5) << 8 | (uint32_t)(e - 8) << 16;
             if (!finite) scale[s] |= 255u;
 #pragma unroll
             for (int p = 0; p < kParts; ++p) {
-                const float unit = __uint_as_float((uint32_t)(e - 4 * p) << 23);
+                const float unit = __uint_as_float((uint32_t)(e - (p == 0 ? 0 : p == 1 ? 5 : 8)) << 23);
                 part[s][p] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x.v, unit);
                 const f32x32 taken = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(part[s][p], unit);
 #pragma unroll

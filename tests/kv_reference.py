@@ -41,15 +41,16 @@ def attend(q, k, v, limit, scale, seen=None):
     """One stream: q [n, H, D], k, v [T, Hkv, D] (float64), query i sees keys j < limit[i] (and seen[j]).
 
     Returns the outputs [n, H, D] and how far a kernel may be from them, for a kernel that rounds probabilities and outputs to bf16
-    (2^-8 relative each), takes a query row to within 2^-12 of the largest of each 32 features, feature by feature, or to within
+    (2^-8 relative each), takes a query row to within 1.07 * 2^-12 of the largest of each 32 features, feature by feature, or to within
     2^-9 of its length (see below) and otherwise computes in fp32:
 
       |error| <= 2^-8 (sum_j p_j |v_j| + |out|)  +  2 dl sum_j p_j |v_j|,
-      dl, the error of a logit: scale * max(sum_d 2^-12 amax_32(q) |k_d|, 2^-9 |q| |k|)  +  2^-18 (1 + |largest logit|)
+      dl, the error of a logit: scale * max(sum_d 1.07 * 2^-12 amax_32(q) |k_d|, 2^-9 |q| |k|)  +  2^-18 (1 + |largest logit|)
       (fp32: sums of up to 128 products, a scaling, and an exponential's argument, each a few 2^-24 of the operands)
 
-    A query feature is taken as three 6-bit floats (4 significant bits, steps of 1/2 at most below 8) at units u, u/16, u/256
-    with the largest magnitude in [4, 8) u: what is left after the third is at most half its largest step, 2^-10 u <= 2^-12 amax.
+    A query feature is taken as three 6-bit floats (4 significant bits, steps of 1/2 at most below 8) at units u, u/32, u/256
+    with the largest magnitude in (3.75, 7.5] u: the first leaves at most half its largest step, u/4, the second of that (up to
+    7.5 units) u/64, the third at most half its largest step, 2^-10 u <= 2^-12 * 1.07 amax; 1.07 is in the factor of the sum below.
     The third is left out only where the two leave no more than 2^-9 of the row's length, in the Euclidean norm: the error of its
     product with a key is then at most 2^-9 |q| |k| by Cauchy and Schwarz.
     """
@@ -78,7 +79,7 @@ def attend(q, k, v, limit, scale, seen=None):
         mag = p @ np.abs(v0)
         amax = np.abs(q[:, h]).reshape(n, D // 32, 32).max(-1).repeat(32, -1)
         k0 = np.where(np.isnan(kk), 0.0, kk)
-        by_feature, by_length = 2.0 ** -12 * (amax @ np.abs(k0).max(0, initial=0.0)), 2.0 ** -9 * np.linalg.norm(q[:, h], axis=-1) * np.linalg.norm(k0, axis=-1).max(initial=0.0)
+        by_feature, by_length = 1.07 * 2.0 ** -12 * (amax @ np.abs(k0).max(0, initial=0.0)), 2.0 ** -9 * np.linalg.norm(q[:, h], axis=-1) * np.linalg.norm(k0, axis=-1).max(initial=0.0)
         dl = scale * np.maximum(by_feature, by_length) + 2.0 ** -18 * (1 + np.abs(np.where(see, logit, 0.0)).max(-1, initial=0.0))
         bound[:, h] = 2.0 ** -8 * (mag + np.abs(o)) * 1.01 + 2 * dl[:, None] * mag + 2.0 ** -120
     return out, bound

@@ -482,3 +482,12 @@ def test_compiled_and_checked_calls_agree(A, monkeypatch):
         assert seen == [None], bad
     with pytest.raises(A.Arl2Error, match="workspace"):
         A.arl2_kv_attn_fwd(q, cache, table, lens, torch.empty_like(q), workspace=ws[:-16])
+
+
+def test_bench_runs_the_stack_on_the_cache(A):
+    import bench
+    dev = torch.device("cuda:0")
+    dense, four = (bench.stack_execute(A, W, torch, dev, layers=4, hybrid_layers=2, chunks=2, kv_cache=c) for c in ("bf16", "4bit"))
+    assert four["softmax_stack"]["readout_calls"] == dense["softmax_stack"]["readout_calls"]
+    # 136 bytes of a stored token and head where bf16 takes 512; the workspace is shared by the layers
+    assert four["softmax_stack"]["peak_memory_bytes"] < 0.5 * dense["softmax_stack"]["peak_memory_bytes"]
