@@ -1,5 +1,17 @@
 // Attention over the paged 4-bit key/value cache (gfx950):
 //   out_i = sum_j softmax_j(sm_scale * q_i.K_j) V_j      over the stored tokens j of the stream, all or (causal) up to query i
+//
+// Here: the kernel for few query rows (single tokens, drafts: up to 64 rows of a stored head), the join of what several workgroups
+// found for the same rows, and the choice between this kernel and that of arl2_kv_tile.hip.
+//
+// Few rows: reading the cache is all there is to do (136 bytes of a token and head at D = 128 against 2 D multiplications).  Workgroups
+// of four wavefronts take 32 rows (columns of the matrix products; one is as good as 32) and a split of the tokens.  A wavefront
+// works alone on every fourth block of 32 tokens: it copies blocks straight into an LDS ring of its own, two ahead of the one it is
+// on, and waits on nothing but its own loads.  13 KB per wavefront, three workgroups per CU: 104 KB of a CU on their way.  Keys and values are
+// converted to bf16, in which they are exact.  At the end the wavefronts' results, each with its own maximum and sum, are added.
+// Measured: 131001 tokens of 8 stored heads, 32 query heads: 33 us (4.3 TB/s; a copy of 1 GiB moves 4.85 TB/s) and 5 us for the
+// join; 64 streams of 1 to 8192 tokens 31 us, of which a workgroup's fixed part (lengths, table, first blocks, ending: 5 us) and
+// splits that turn out empty are most.  Two workgroups per CU with a block more ahead: 38.5 and 39.6 us instead of 38.4 and 35.2 in all.
 #include "arl2_kv_attn.h"
 
 #include <limits.h>
@@ -367,7 +379,7 @@ __device__ __forceinline__ void add_splits(const KvAttnArgs &a, size_t slot0, in
 
 // Joins the partial results of rows that more than one workgroup worked on.  Up to kFewSplits splits: D / 4 lanes to a row, in the
 // order of the splits.  More: a workgroup to a row, 1024 / D splits side by side, then these in order.
-// In us, 32768 rows of 2 splits 13 and 53 with a workgroup to a row; 32 rows of 94 splits 5.
+// Whole calls, lanes and workgroups to a row: 18720 rows of 3 splits 103 and 119 us, 2048 of up to 8 34.6 and 35.4 us.
 constexpr int kFewSplits = 8;
 template <int D, bool FEW>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttnArgs a)
@@ -428,6 +440,14 @@ hipError_t launch_join(const KvAttnArgs &a, hipStream_t stream)
 
 }  // namespace
 
+//
+// The kernel.  In us, few rows and many: 12 heads x 128 over 32760 tokens 64 rows 37 and 36, 96 rows 48 and 38; 8 streams x 8 heads over 4096,
+// causal, 64 rows 28 and 27, 96 rows 32 and 29; 64 x 8 over 1024 64 rows 36 and 40, 96 rows 49 and 44; x 64, 16 x 12 over 2000 64 rows 25 and 31,
+// 96 rows 34 and 32.  (Where either finds few workgroups the first stays ahead: 12 heads over 4680, 256 rows 27 and 32.)
+// Many rows: the splits that the measured cost of a tile, of a workgroup's ends and of partial results make the cheapest; e.g. 12 heads,
+// 1560 rows over 10920: 1 to 6 splits 236, 143, 110, 152, 133, 122 us; 4680 rows over 4680: 119 without, 146 with two.
+// Few rows: one round of workgroups; with several streams, whose lengths the host does not know, at most an eighth of the table's length or
+// 1024 tokens (64 streams of 1 to 8192 tokens: 512, 1024, 1408, 2048 tokens 39, 36.5, 36, 44 us).
 KvAttnPlan kv_attn_plan(int B, int Lq, int G, const KvPool &pool, int D)
 {
     KvAttnPlan p = {};

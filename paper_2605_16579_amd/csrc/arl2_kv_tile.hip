@@ -1,4 +1,29 @@
-// Attention over the paged 4-bit key/value cache for many query rows (gfx950).
+// Attention over the paged 4-bit key/value cache for many query rows (gfx950): chunks and prompts, from 65 rows on.
+//
+// A row is a (query token, query head of the stored head's group).  A workgroup has 256 of them, eight wavefronts 32 each, and walks
+// over its tokens in tiles of 64, everything transposed:
+//   S^T[key][row] = K[key][:] . Q[row][:]      keys as they are stored, 4 bits with a scale per 32 features: operands of the scaled
+//                                              matrix instruction as they lie; queries as sums of 6-bit floats (`Query`)
+//   O^T[d][row]  += V^T[d][key] . P^T[key][row]     values as bf16, in which they are exact; probabilities rounded to bf16 (2^-9 on the
+//                                              average of the result's size, as in every product of bf16 matrices)
+// Values cannot go into the scaled instruction: its scales belong to 32 terms of a sum, which runs over tokens here, and the cache
+// scales values per token so that single tokens can be appended.  So they are converted, once per workgroup and tile (28 vector
+// instructions per thread), into an LDS tile that the second product reads in 16-byte pieces without bank conflicts.
+//
+// Tiles come straight from memory into LDS as they are stored (8.7 KB; a bf16 tile is 32 KB), requested three intervals before their
+// values are converted; the block table's entries pass through LDS as well.  Per tile a wavefront requests one of eight pieces.  Waits
+// count this wavefront's loads, one barrier per tile publishes them all.  What belongs to a request is spread over the first steps
+// of a slot, beside products in flight: behind the barrier all eight wavefronts did it at once (682 -> 646 us on zeros).
+//
+// The unit of the schedule is a slot, the softmax of one 32-key block beside the first product of the next block and the second
+// product of the previous one.  Softmax: probabilities relative to a running maximum that starts as the first block's and is
+// raised only where a lane's share of a block's sum shows that a logit passed it by about 2^7; then the block is done again.
+// Masks (the last tile, causal rows' ends, groups without a page) are branches around the slots, not variants of them: two variants
+// in one loop doubled the accumulators (344 bytes of scratch).
+//
+// What bounds it: vector instructions and the power of the matrix cores together.  12 heads x 128, 4680 queries over 32760 keys: 677
+// to 726 us by card (942 GFLOP: 1.30 to 1.39 PFLOP/s), on zeros, where power does not bound it, 629 us; the matrix instructions alone
+// would take 390 us.  The bf16 readout over a dense bf16 cache takes 760 to 818 us on the same cards.
 #include "arl2_kv_attn.h"
 
 #include <limits.h>

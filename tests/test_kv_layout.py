@@ -159,6 +159,8 @@ def test_refusals_of_the_descriptor(A):
     for bad in (dict(H=0), dict(H=7), dict(causal=2), dict(sm_scale=-1.0), dict(sm_scale=float("nan")), dict(sm_scale=float("inf"))):
         assert _attn(A, _desc(A, **bad)) == 1, bad
     assert _attn(A, _desc(A, H=2 * 600000)) == 2
+    huge = _desc(A, B=90000, H=10, Hkv=1, Lq=20000, max_pages=2 ** 22, page_size=256)
+    assert _attn(A, huge) == 2 and lib.arl2_kv_workspace_bytes(ctypes.byref(huge)) == 0
     assert _append(A, _desc(A, B=1000, Hkv=900, Lq=10 ** 6)) == 2 and _read(A, _desc(A, B=1000, Hkv=900, Lq=10 ** 6)) == 2
     assert lib.arl2_kv_append(None, *PTR) == 1 and lib.arl2_kv_read(None, *PTR[:6]) == 1 and lib.arl2_kv_attn_fwd(None, *PTR[:6]) == 1
     assert lib.arl2_kv_cache_bytes(ctypes.byref(_desc(A))) == 9 * 2 * 64 * 136
