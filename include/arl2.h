@@ -285,7 +285,7 @@ arl2_status arl2_state_commit_gdn(const arl2_desc *desc,
  *                                An entry outside [0, n_pages) holds no tokens: nothing is written there, zeros are
  *                                read, attention does not see them (tokens that a sliding window dropped).
  *                                Streams may share pages that are only read (a common prompt); if one call appends
- *                                to the same place of a page twice, what is stored there is one of the two.
+ *                                different rows to the same place of a page, what is stored there may mix their bytes.
  *   start, count, kv_len, q_len  [B] as described below.  Values beyond what the arrays hold are cut to it: count
  *                                and q_len to [0, Lq], kv_len to [0, max_pages * page_size].
  */
@@ -336,7 +336,8 @@ arl2_status arl2_kv_read(const arl2_kv_desc *desc, const void *cache,
  * out_i = softmax_j(sm_scale * q_i.K_j) V_j over the stored tokens j < kv_len[b] of the stream, for its query tokens
  * i < q_len[b].  desc->causal: query i stands at position kv_len[b] - q_len[b] + i and sees the tokens up to it (the queries are
  * the last tokens stored).  A query that sees no token gives zeros.
- *   q         device bf16 [B][Lq][H][D]; rows from q_len[b] on are not read.  A row with a NaN or an infinity gives NaN.
+ *   q         device bf16 [B][Lq][H][D]; rows from q_len[b] on are not read.  A row with a NaN or an infinity gives NaN
+ *             if it sees a token.
  *   kv_len    device int32 [B].       q_len   device int32 [B], or NULL: Lq for all.
  *   out       device bf16 [B][Lq][H][D]; rows from q_len[b] on are left as they were.  Must not overlap an input.
  * fp32 accumulation, softmax statistics and joins of the key axis, which is divided the same way for the same descriptor:

@@ -135,6 +135,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void kv_stream_kernel(KvAttnArgs a)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[i][r] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;
+    bool sees = false;           // whether the row sees one of the wavefront's tokens (this half-wave's of them)
     const f32x16 zero = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
     int nan_key[STEPS];          // first key with a NaN value among those that not all rows see
 #pragma unroll
@@ -185,6 +186,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void kv_stream_kernel(KvAttnArgs a)
         if (__builtin_expect(key0 + kKeys > min(lim_min, kend) || groups != 3u, 0)) {
             const int left = min(lim, kend) - (key0 + 4 * hh);
             const int left0 = groups & 1u ? left : INT_MIN, left1 = groups & 2u ? left : INT_MIN;
+            sees |= left0 > 0 || left1 > 16;
 #pragma unroll
             for (int r = 0; r < 16; ++r)
                 if (8 * (r >> 2) + (r & 3) >= (r < 8 ? left0 : left1)) s_acc[r] = -INFINITY;
@@ -204,6 +206,8 @@ __global__ __launch_bounds__(64 * kWaves, 3) void kv_stream_kernel(KvAttnArgs a)
                         vs[s][u][x] = (vs[s][u][x] & ~gone) | (gone & 0x7f7f7f7fu);
                     }
                 }
+        } else {
+            sees = true;
         }
 
         // ---- softmax
@@ -258,7 +262,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void kv_stream_kernel(KvAttnArgs a)
         f32x16 nil = zero;
 #pragma unroll
         for (int t = 0; t < KS; ++t) nil = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bf16x8{}, qf[t], nil, 0, 0, 0);
-        l_run += nil[0];
+        if (sees) l_run += nil[0];       // (a row that sees nothing is zero, whatever it holds)
     }
     l_run = xhalf_sum(l_run);
     bool any_nan = false;
@@ -440,7 +444,7 @@ hipError_t launch_join(const KvAttnArgs &a, hipStream_t stream)
 
 }  // namespace
 
-//
+// How a call is divided, from its sizes alone.
 // The kernel.  In us, few rows and many: 12 heads x 128 over 32760 tokens 64 rows 37 and 36, 96 rows 48 and 38; 8 streams x 8 heads over 4096,
 // causal, 64 rows 28 and 27, 96 rows 32 and 29; 64 x 8 over 1024 64 rows 36 and 40, 96 rows 49 and 44; x 64, 16 x 12 over 2000 64 rows 25 and 31,
 // 96 rows 34 and 32.  (Where either finds few workgroups the first stays ahead: 12 heads over 4680, 256 rows 27 and 32.)

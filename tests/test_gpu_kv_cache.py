@@ -176,6 +176,41 @@ def test_long_and_short_streams_in_one_call(A, D, L, G, causal):
     R.check_attention(A, pool, R.bf16_normal((4, L, G, D), 1), lens, [L, min(L, 2), L, L], causal)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("D,Hkv,splits", [(64, 8, 1), (128, 8, 1), (64, 4, 2)])
+def test_many_rows_over_long_caches(A, D, Hkv, splits, causal):
+    """Workgroups that walk over more tiles than one or two portions of the block table hold, past pages that were dropped."""
+    G, L, page, T = 32, 250, 16, 9003
+    pool = R.Paged(A, 1, Hkv, D, page, T)
+    pool.fill_with([T])
+    table = pool.table.copy()
+    for at in (4095, 4096, 4544, 8191, 8192, 8992):                          # pages that end and begin portions, or lie about them
+        table[0, at // page] = -1
+    pool.set_table(table)
+    slots = A.arl2_kv_workspace_bytes(1, G * Hkv, Hkv, L, D, page, pool.width) // (4 * (D + 2))
+    assert slots == (0 if splits == 1 else Hkv * -(-G * L // 256) * 256 * splits)
+    q = R.bf16_normal((1, L, G * Hkv, D), 3)
+    out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+    ws = A.alloc_kv_workspace(1, G * Hkv, Hkv, L, D, page, pool.width)
+    A.arl2_kv_attn_fwd(q.cuda(), pool.cache, pool.table_dev, R.ints([T]), out, causal=causal, workspace=ws)
+    got = out.float().cpu().numpy().astype(np.float64)[0]
+    limit = [T - L + i + 1 if causal else T for i in range(L)]
+    for h in (0, G + 7, G * Hkv - 1):
+        one = slice(h // G, h // G + 1)
+        ref, bound = R.attend(q[0, :, h:h + 1].double().numpy(), pool.k[0, :T, one], pool.v[0, :T, one], limit, D ** -0.5, pool.seen(0)[:T])
+        off = np.abs(got[:, h:h + 1] - ref)
+        assert (off <= bound).all(), (h, np.argwhere(~(off <= bound))[:4])
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("B,L", [(200, 1), (70, 66)])
+def test_many_streams(A, B, L, causal):
+    lens = [(37 * b) % 131 for b in range(B)]
+    pool = R.Paged(A, B, 1, 64, 16, 130)
+    pool.fill_with(lens)
+    R.check_attention(A, pool, R.bf16_normal((B, L, 1, 64), 1), lens, [(5 * b) % (L + 1) for b in range(B)], causal)
+
+
 def test_lengths_beyond_the_table_are_cut(A):
     pool = R.Paged(A, 3, 1, 128, 16, 48)
     pool.fill_with([48, 48, 48])
@@ -225,6 +260,26 @@ def test_queries_that_are_not_finite_give_nan(A, L):
     want = torch.zeros(1, L, 2, 128, dtype=torch.bool)
     want[0, 0, 0] = want[0, 1, 1] = want[0, L - 1, 0] = True
     assert torch.equal(nan, want)
+
+
+@pytest.mark.parametrize("L", [3, 300])
+@pytest.mark.parametrize("tokens", [0, 20, 600])
+def test_queries_that_are_not_finite_and_see_nothing_give_zeros(A, tokens, L):
+    pool = R.Paged(A, 2, 1, 128, 16, 640)
+    pool.fill_with([tokens, 640])
+    table = pool.table.copy()
+    table[0] = -1                                                            # stream 0: every page dropped
+    table[1, 1:] = -1
+    pool.set_table(table)
+    q = R.bf16_normal((2, L, 2, 128), 1)
+    q[:, 0, 0, 5], q[:, 1, 1, 127], q[:, 2, 0, 64] = float("nan"), float("inf"), -float("inf")
+    out = R.check_attention(A, pool, q, [tokens, 640])
+    assert (out[0] == 0).all() and out[1].isnan().any()
+    # causal, more queries than tokens: the first queries see nothing
+    pool = R.Paged(A, 1, 1, 128, 16, 640)
+    pool.fill_with([2])
+    out = R.check_attention(A, pool, q[:1], [min(2, L - 2)], causal=True)
+    assert (out[0, :2] == 0).all()
 
 
 @pytest.mark.parametrize("L", [5, 300])
