@@ -16,6 +16,10 @@
 // heads of a group follow one another, so that a workgroup's heads find the rotation tables in its CU's cache.  The four tokens of
 // a value pair are one 4-byte store (they are neighbours in the cache), at D = 128 the whole group's 16 tokens one 16-byte store after
 // an exchange between lanes; where the call has only some of the tokens they are stored byte by byte.
+//
+// What bounds them: memory, and the loads that wait for one another (lengths, then rows and page, then stores).  4680 tokens of 12
+// heads x 128: append 12.2 us (38.7 MB: 3.2 TB/s), read 9.2 us (36.4 MB: 3.9 TB/s); reading 4 x 1560 tokens 11.4 us (48.5 MB: 4.3 TB/s);
+// a copy of 1 GiB moves 4.85 TB/s.  One token of 16 streams: 4.7 and 3.2 us, which is launch and latency.
 #include "arl2_device.h"
 
 namespace arl2 {
