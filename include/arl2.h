@@ -342,7 +342,8 @@ arl2_status arl2_kv_read(const arl2_kv_desc *desc, const void *cache,
  *   out       device bf16 [B][Lq][H][D]; rows from q_len[b] on are left as they were.  Must not overlap an input.
  * fp32 accumulation, softmax statistics and joins of the key axis, which is divided the same way for the same descriptor:
  * results are bit-identical from run to run.  Probabilities are rounded to bf16 for the second product, and with more than 64
- * query rows (Lq * H / Hkv) a query row may be taken to within 2^-9 of its length, half of what rounding it to bf16 may have taken.
+ * query rows (Lq * H / Hkv) a query row may be taken to within 2^-9 of its length, half of what rounding it to bf16 may have taken, or
+ * a feature to within 2^-112, whichever is more.
  * Uses desc->workspace; calls that overlap in time need one each.
  */
 arl2_status arl2_kv_attn_fwd(const arl2_kv_desc *desc, const void *q, const void *cache,

@@ -68,6 +68,8 @@ struct Tile {
 // of the wavefront's rows is no longer than 2^-9 of the row, half of what one rounding to bf16 may take.  Rows of normal values
 // leave 2^-10.9, the longest of 32 rarely more than 2^-9.1; rows with a feature far above the others' size get the third part.
 // (4680 queries over 32760 keys: 712 us with two parts, 759 us with three on one card.)
+// That is decided from sums of squares in fp32, out of whose range they fall for features below 2^-63 and rows from 2^64 on: a row shorter
+// than 2^-30 or longer than 2^64 keeps three parts.  u is 2^-100 at least, where three parts are within 2^-112 of a feature.
 template <int D>
 struct Query {
     static constexpr int STEPS = D / 64;
@@ -91,6 +93,7 @@ struct Query {
             const int e = finite ? max((int)((m + 0xfffffu) >> 23) - 2, 27) : 127;       // one more from above 7.5 on
             scale[s] = (uint32_t)e | (uint32_t)(e - 5) << 8 | (uint32_t)(e - 8) << 16;
             if (!finite) scale[s] |= 255u;
+            left += m != 0 ? 0x1p-78f : 0.f;      // (above 2^-18 of the squares of a row shorter than 2^-30; nothing beside those of others)
 #pragma unroll
             for (int p = 0; p < kParts; ++p) {
                 const float unit = __uint_as_float((uint32_t)(e - (p == 0 ? 0 : p == 1 ? 5 : 8)) << 23);

@@ -1,0 +1,40 @@
+"""What attention over the 4-bit cache makes of a query row: of any size that bf16 has, and of that row alone."""
+import pytest
+import torch
+
+import kv_checks as C
+import kv_reference as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def A():
+    import paper_2605_16579_amd as A
+    A.load_library()
+    return A
+
+
+def one_feature_rows(L, H, D, seed):
+    """Rows of one feature of 4.25 among small ones: its first 6-bit part leaves half a step and its second part half of one of its own,
+    2^-8.1 of the row, so that it takes a third."""
+    q = R.bf16_normal((1, L, H, D), seed, 0.02)
+    for i in range(L):
+        for h in range(H):
+            q[0, i, h, (7 * i + 3 * h) % D] = 4.25 * (-1) ** i
+    return q
+
+
+@pytest.mark.parametrize("L,G", [(64, 1), (65, 1), (40, 3)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("power", [-106, -98, -90, -76, -62, -31, 0, 40, 62, 100])
+def test_rows_of_every_size(A, D, L, G, power):
+    """(Logits are the same for every power: sm_scale is its reciprocal.)"""
+    pool = R.Paged(A, 1, 1, D, 64, 300)
+    pool.fill_with([300])
+    q = (one_feature_rows(L, G, D, 1).float() * 2.0 ** power).bfloat16()
+    C.check(A, pool, q, [300], sm_scale=2.0 ** (1 - power))
+    # without the one feature, and rows of zeros among them
+    q = (R.bf16_normal((1, L, G, D), 2).float() * 2.0 ** power).bfloat16()
+    q[0, 3:40:5] = 0.0
+    C.check(A, pool, q, [300], causal=True, sm_scale=2.0 ** -(power + 3))
