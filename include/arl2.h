@@ -343,7 +343,7 @@ arl2_status arl2_kv_read(const arl2_kv_desc *desc, const void *cache,
  * fp32 accumulation, softmax statistics and joins of the key axis, which is divided the same way for the same descriptor:
  * results are bit-identical from run to run.  Probabilities are rounded to bf16 for the second product, and with more than 64
  * query rows (Lq * H / Hkv) a query row may be taken to within 2^-9 of its length, half of what rounding it to bf16 may have taken, or
- * a feature to within 2^-112, whichever is more.
+ * a feature to within 2^-112, whichever is more.  What the other queries of the call hold does not change a bit of a query's output.
  * Uses desc->workspace; calls that overlap in time need one each.
  */
 arl2_status arl2_kv_attn_fwd(const arl2_kv_desc *desc, const void *q, const void *cache,

@@ -64,9 +64,10 @@ struct Tile {
 // sum of up to three 6-bit floats (e2m3: 4 significant bits, steps of 1/8 below 2, 1/4 below 4, 1/2 up to 7.5) at units u, u / 32 and
 // u / 256, the largest of the 32 in (3.75, 7.5] u.  6-bit operands run at four times bf16's rate: two parts take half the time of
 // one bf16 product, three parts three quarters.  Three parts are within 2^-12 u of a bf16 feature and exact from u / 8 on; two are
-// exact from u / 2 on (but for 2^-6 u where the first leaves just half a step of 1/2).  Two are enough where what they leave of each
-// of the wavefront's rows is no longer than 2^-9 of the row, half of what one rounding to bf16 may take.  Rows of normal values
-// leave 2^-10.9, the longest of 32 rarely more than 2^-9.1; rows with a feature far above the others' size get the third part.
+// exact from u / 2 on (but for 2^-6 u where the first leaves just half a step of 1/2).  Two are enough where what they leave of
+// the row is no longer than 2^-9 of it, half of what one rounding to bf16 may take; a wavefront spares the third product where all its
+// rows have enough.  Rows of normal values leave 2^-10.9, the longest of 32 rarely more than 2^-9.1; rows with a feature far above the
+// others' size get the third part.
 // (4680 queries over 32760 keys: 712 us with two parts, 759 us with three on one card.)
 // That is decided from sums of squares in fp32, out of whose range they fall for features below 2^-63 and rows from 2^64 on: a row shorter
 // than 2^-30 or longer than 2^64 keeps three parts.  u is 2^-100 at least, where three parts are within 2^-112 of a feature.
@@ -75,7 +76,7 @@ struct Query {
     static constexpr int STEPS = D / 64;
     u32x6 part[STEPS][kParts];
     uint32_t scale[STEPS];           // byte p: of part p; 255, a NaN, in the place of the first where a feature is not finite
-    bool two;                        // whether two parts are enough
+    bool two;                        // whether two parts are enough; the third is then zero
     __device__ __forceinline__ void load(const bf16_t *row, bool there)
     {
         float all = 0.f, left = 0.f;
@@ -110,6 +111,11 @@ struct Query {
         }
         all = xhalf_sum(all);
         two = xhalf_sum(left) <= 0x1p-18f * all && all <= FLT_MAX;
+        // (if another row of the wavefront needs the third part, this one's is zero: its result is the same in whatever company)
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int i = 0; i < 6; ++i) part[s][2][i] = two ? 0u : part[s][2][i];
     }
 };
 
@@ -368,7 +374,8 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
         });
         if constexpr (!HAS_PV)
             static_for<0, C::PF>([&](auto p_) { fr[decltype(p_)::value] = v_frag(j, p_); });
-        // Rarely a logit exceeded the running maximum by more than the threshold: raise it, rescale, redo the block.
+        // Rarely a logit exceeded the running maximum by more than the threshold: raise it, rescale, redo the block.  Rows of the wavefront
+        // without need keep their maximum and find the same probabilities and sums again, bit for bit.
         ps0 += ps1;
         if (__builtin_expect(__any(!(ps0 < 4096.0f)), 0)) {
             // (a use on this path too: the products of block j + 1 would otherwise be moved behind the branch, away from the softmax)
@@ -376,19 +383,21 @@ __global__ __launch_bounds__(kNT, 2) void kv_tile_kernel(KvAttnArgs a)
             float mx = s_acc[P][0];
             static_for<1, 16>([&](auto r_) { mx = fmaxf(mx, s_acc[P][decltype(r_)::value]); });
             mx = xhalf_max(mx) * a.scale_log2;
-            const float m_new = fmaxf(m_run, mx);
+            const bool need = xhalf_max(ps0 < 4096.0f ? 0.f : 1.f) > 0.f;
+            const float m_new = need ? fmaxf(m_run, mx) : m_run;
             const float alpha = m_new == m_run ? 1.0f : __builtin_amdgcn_exp2f(m_run - m_new);
             m_run = m_new;
             l_run *= alpha;
             if constexpr (HAS_PV)
                 static_for<0, OB>([&](auto i_) { static_for<0, 16>([&](auto r_) { o[decltype(i_)::value][decltype(r_)::value] *= alpha; }); });
-            ps0 = 0.f;
+            ps0 = ps1 = 0.f;
             static_for<0, 16>([&](auto r_) {
                 constexpr int r = decltype(r_)::value;
                 const float p = __builtin_amdgcn_exp2f(fmaf(s_acc[P][r], a.scale_log2, -m_run));
-                ps0 += p;
+                (r & 1 ? ps1 : ps0) += p;
                 pf[P][r >> 3][r & 7] = to_bf16(p);
             });
+            ps0 += ps1;
         }
         l_run += ps0;
     };

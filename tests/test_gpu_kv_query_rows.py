@@ -38,3 +38,27 @@ def test_rows_of_every_size(A, D, L, G, power):
     q = (R.bf16_normal((1, L, G, D), 2).float() * 2.0 ** power).bfloat16()
     q[0, 3:40:5] = 0.0
     C.check(A, pool, q, [300], causal=True, sm_scale=2.0 ** -(power + 3))
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("L,G", [(9, 2), (100, 2), (70, 4), (300, 1)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_row_depends_on_itself_alone(A, D, L, G, causal):
+    """A query that is changed changes no other: neither those of other tokens, earlier causal ones above all, nor of other heads."""
+    pool = R.Paged(A, 1, 2, D, 32, 900)
+    pool.fill_with([900], std=1.5)
+    q = R.bf16_normal((1, L, 2 * G, D), 4)
+    out = torch.full((5,) + tuple(q.shape[1:]), 7.0, dtype=torch.bfloat16, device="cuda")
+    ws = A.alloc_kv_workspace(1, 2 * G, 2, L, D, 32, pool.width)
+    changed = torch.zeros((L, 2 * G), dtype=torch.bool)
+    for i in range(5, L, 16):
+        changed[i, i // 16 % (2 * G)] = True
+    for n, row in enumerate((None, one_feature_rows(1, 1, D, 3)[0, 0, 0], 40.0, float("nan"), 0.0)):
+        x = q.clone()
+        if n > 0:
+            x[0, changed] = row if n == 1 else x[0, changed] * row
+        A.arl2_kv_attn_fwd(x.cuda(), pool.cache, pool.table_dev, R.ints([900]), out[n:n + 1], causal=causal, workspace=ws)
+    out = out.cpu().view(torch.int16)
+    for n in range(1, 5):
+        assert torch.equal(out[n][~changed], out[0][~changed]), n
+        assert not torch.equal(out[n][changed], out[0][changed]), n
