@@ -98,7 +98,13 @@ struct Query {
 #pragma unroll
             for (int p = 0; p < kParts; ++p) {
                 const float unit = __uint_as_float((uint32_t)(e - (p == 0 ? 0 : p == 1 ? 5 : 8)) << 23);
-                part[s][p] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x.v, unit);
+                bf16x32 from = x.v;
+                // (features whose nearest 6-bit float is 2^128, beyond fp32: cut to the one below, which leaves up to 7.5 of the second's units)
+                if (p == 0 && __builtin_expect(__any(m > 0x7f700000u), 0)) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) from[j] = to_bf16(fminf(fmaxf((float)from[j], -0x1.ep127f), 0x1.ep127f));
+                }
+                part[s][p] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(from, unit);
                 const f32x32 taken = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(part[s][p], unit);
 #pragma unroll
                 for (int j = 0; j < 32; ++j) {

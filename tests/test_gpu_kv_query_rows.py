@@ -62,3 +62,15 @@ def test_a_row_depends_on_itself_alone(A, D, L, G, causal):
     for n in range(1, 5):
         assert torch.equal(out[n][~changed], out[0][~changed]), n
         assert not torch.equal(out[n][changed], out[0][changed]), n
+
+
+@pytest.mark.parametrize("L,G", [(64, 1), (65, 1), (33, 4)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_the_largest_features(A, D, L, G):
+    """Features next to the largest of bf16, whose nearest 6-bit float is 2^128."""
+    pool = R.Paged(A, 1, 1, D, 64, 300)
+    pool.fill_with([300], std=2.0 ** -9)
+    q = (R.bf16_normal((1, L, G, D), 1).float().clamp(-3, 3) * 2.0 ** 124).bfloat16()
+    for i in range(L):
+        q[0, i, :, i % D] = (-1) ** i * (255 - i % 16) * 2.0 ** 120
+    C.check(A, pool, q, [300], sm_scale=2.0 ** -118)
