@@ -38,12 +38,12 @@ struct Stream {
     static constexpr int RING = STAGES * BLOCK > ENDING ? STAGES * BLOCK : ENDING;
 };
 
-// Waits until at most n of this wavefront's requests of LOADS loads each are on their way.
+// Waits until at most n of this wavefront's requests of LOADS loads each are on their way, n <= 2.
 template <int LOADS>
 __device__ __forceinline__ void wait_requests(int n)
 {
-    if (n >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * LOADS) : "memory");
-    else if (n == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
+    static_assert(2 * LOADS <= 63, "vmcnt has 6 bits");
+    if (n == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * LOADS) : "memory");
     else if (n == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LOADS) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
@@ -149,6 +149,7 @@ __global__ __launch_bounds__(64 * kWaves, 3) void kv_stream_kernel(KvAttnArgs a)
         } else {
             placed <<= 2;
         }
+        static_assert(C::AHEAD == 2, "the counts that wait_requests knows");
         wait_requests<C::LOADS>(min(n - 1 - m, C::AHEAD));
         const unsigned char *blk = mine + m % C::STAGES * C::BLOCK;
         const int key0 = key_of(m);
