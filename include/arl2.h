@@ -300,7 +300,7 @@ typedef struct {
     int32_t n_pages;      /* pages of the pool, >= 1                                             */
     int32_t max_pages;    /* block table entries per stream, >= 1; max_pages * page_size <= 2^30 */
     int32_t causal;       /* attention: 0 every stored token is seen; 1 see arl2_kv_attn_fwd     */
-    float sm_scale;       /* attention: logit scale; 0 selects 1/sqrt(D)                         */
+    float sm_scale;       /* attention: logit scale, at most 2^127; 0 selects 1/sqrt(D)          */
     void *workspace;      /* attention: device scratch, >= arl2_kv_workspace_bytes               */
     size_t workspace_bytes;
     void *stream;         /* hipStream_t; NULL is the default stream                             */
@@ -340,6 +340,7 @@ arl2_status arl2_kv_read(const arl2_kv_desc *desc, const void *cache,
  *             if it sees a token.
  *   kv_len    device int32 [B].       q_len   device int32 [B], or NULL: Lq for all.
  *   out       device bf16 [B][Lq][H][D]; rows from q_len[b] on are left as they were.  Must not overlap an input.
+ * Products q_i.K_j and logits have to lie in fp32's range, +-2^127.
  * fp32 accumulation, softmax statistics and joins of the key axis, which is divided the same way for the same descriptor:
  * results are bit-identical from run to run.  Probabilities are rounded to bf16 for the second product, and with more than 64
  * query rows (Lq * H / Hkv) a query row may be taken to within 2^-9 of its length, half of what rounding it to bf16 may have taken, or

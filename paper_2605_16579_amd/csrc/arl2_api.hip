@@ -106,7 +106,8 @@ arl2_status check_kv_attn_desc(const arl2_kv_desc *d)
     if (st != ARL2_OK) return st;
     if (d->H < 1 || d->H % d->Hkv) return fail(ARL2_ERR_INVALID_ARG, "H must be a positive multiple of Hkv");
     if (d->causal != 0 && d->causal != 1) return fail(ARL2_ERR_INVALID_ARG, "causal must be 0 or 1");
-    if (!(d->sm_scale >= 0.f) || d->sm_scale > FLT_MAX) return fail(ARL2_ERR_INVALID_ARG, "sm_scale must be finite and >= 0 (0 selects the default)");
+    // (the kernels multiply by sm_scale * log2(e), which is to be finite too)
+    if (!(d->sm_scale >= 0.f) || d->sm_scale > 0x1p127f) return fail(ARL2_ERR_INVALID_ARG, "sm_scale must be >= 0 (0 selects the default) and at most 2^127");
     if ((double)d->B * d->H > 1.0e6 || (double)d->Lq * d->H > 2.0e9 || (double)d->B * d->H * d->Lq > 68719476736.0)
         return fail(ARL2_ERR_UNSUPPORTED, "problem too large (B*H must stay below 1e6, Lq*H below 2e9, B*H*Lq below 2^36)");
     return ARL2_OK;

@@ -74,3 +74,11 @@ def test_the_largest_features(A, D, L, G):
     for i in range(L):
         q[0, i, :, i % D] = (-1) ** i * (255 - i % 16) * 2.0 ** 120
     C.check(A, pool, q, [300], sm_scale=2.0 ** -118)
+
+
+@pytest.mark.parametrize("L", [1, 64, 65])
+def test_the_largest_scale(A, L):
+    pool = R.Paged(A, 1, 1, 128, 64, 300)
+    pool.fill_with([300], std=2.0 ** -40)
+    q = (R.bf16_normal((1, L, 1, 128), 2).float() * 2.0 ** -90).bfloat16()
+    C.check(A, pool, q, [300], sm_scale=2.0 ** 127)
