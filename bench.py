@@ -75,14 +75,15 @@ def cpu_baseline(w, passes_inputs, clean, S0, steps, rule="plain", rule_inputs=N
     }
 
 
-def stack_report(A, W, torch, dev, layers=30, hybrid_layers=22, chunks=7, reps=5):
+def stack_report(A, W, torch, dev, layers=30, hybrid_layers=22, chunks=7, reps=5, kv_cache="bf16"):
     """Attention-only time and memory of a full layer stack over a 7-chunk (21 latent frame) rollout.
     Every layer pass is one arl2_hybrid_attn_fwd call at the Wan-2.1-1.3B layer shape: hybrid layers
     read the fixed-size state; softmax layers attend to a KV cache that holds c chunks at chunk c
     (S = NULL, Lkv = c * 4680).  Layer passes of one kind and one cache length cost the same, so each
     distinct call is timed on its own (median of `reps` batches of back-to-back calls) and the stack total is the
     weighted sum: a cross-check of the executed rollout (stack_execute), which is the measurement.  Inputs are
-    synthetic and there is no model between the layers."""
+    synthetic and there is no model between the layers.  `kv_cache` "4bit": the cache is the paged 4-bit one and a softmax layer's
+    pass one arl2_kv_attn_fwd call."""
     w = W.WORKLOADS["wan_layer"]
     P = w.passes
     q, k, v, g = (t.to(dev) for t in W.pass_inputs(w, 0, 0))
@@ -93,6 +94,14 @@ def stack_report(A, W, torch, dev, layers=30, hybrid_layers=22, chunks=7, reps=5
     A.arl2_state_commit(kc, vc, gate, S, ws)
     kv_k = W.normal(1, w, (w.B, chunks * w.L, w.H, w.D), 101).to(dev)
     kv_v = W.normal(1, w, (w.B, chunks * w.L, w.H, w.D), 102).to(dev)
+    if kv_cache == "4bit":
+        page = 64
+        per_stream = (chunks * w.L + page - 1) // page
+        pages = A.alloc_kv_cache(w.B * per_stream, w.H, page, w.D, device=dev)
+        table = torch.arange(w.B * per_stream, dtype=torch.int32, device=dev).view(w.B, per_stream)
+        lens = [torch.full((w.B,), c * w.L, dtype=torch.int32, device=dev) for c in range(chunks + 1)]
+        kv_ws = A.alloc_kv_workspace(w.B, w.H, w.H, w.L, w.D, page, per_stream, device=dev)
+        A.arl2_kv_append(kv_k, kv_v, pages, table, lens[0])
 
     def timed(fn, batch=32):
         """Milliseconds per call: `batch` back-to-back calls between two events (as the calls run in a stack), median of `reps`."""
@@ -111,17 +120,24 @@ def stack_report(A, W, torch, dev, layers=30, hybrid_layers=22, chunks=7, reps=5
 
     t_hybrid = timed(lambda: A.arl2_hybrid_attn_fwd(q, k, v, S, g, out))
     t_commit = timed(lambda: A.arl2_state_commit(kc, vc, gate, S, ws))
-    t_kv = [timed(lambda c=c: A.arl2_hybrid_attn_fwd(q, kv_k[:, :c * w.L], kv_v[:, :c * w.L], None, None, out))
-            for c in range(1, chunks + 1)]
+    def softmax_pass(c):
+        if kv_cache == "4bit":
+            A.arl2_kv_attn_fwd(q, pages, table, lens[c], out, workspace=kv_ws)
+        else:
+            A.arl2_hybrid_attn_fwd(q, kv_k[:, :c * w.L], kv_v[:, :c * w.L], None, None, out)
+
+    t_kv = [timed(lambda c=c: softmax_pass(c)) for c in range(1, chunks + 1)]
     sm_layers = layers - hybrid_layers
     hybrid_ms = sum(P * (hybrid_layers * t_hybrid + sm_layers * t_kv[c]) + hybrid_layers * t_commit for c in range(chunks))
     softmax_ms = sum(P * layers * t_kv[c] for c in range(chunks))
     tok_bytes = w.B * w.H * w.D * 2
-    kv_layer_bytes = 2 * chunks * w.L * tok_bytes                      # K and V cache of one softmax layer at full length
+    # K and V cache of one softmax layer at full length
+    kv_layer_bytes = pages.nbytes if kv_cache == "4bit" else 2 * chunks * w.L * tok_bytes
     state_bytes = w.B * w.H * w.D * w.D * 4
     return {
         "report": "attention time and memory of a %d-layer stack over %d chunks of %d tokens, %d readout passes per chunk"
                   % (layers, chunks, w.L, P),
+        "kv_cache": kv_cache,
         "hybrid_stack": {"layers": "%d hybrid + %d softmax-KV" % (hybrid_layers, sm_layers), "attention_ms": hybrid_ms,
                          "memory_bytes": hybrid_layers * state_bytes + sm_layers * kv_layer_bytes},
         "softmax_stack": {"layers": "%d softmax-KV" % layers, "attention_ms": softmax_ms,
@@ -285,7 +301,7 @@ def main() -> int:
                     help="instead of the bench line: attention time and memory of a 30-layer stack over a "
                          "21-latent-frame rollout (7 chunks), 22 hybrid + 8 softmax-KV layers vs 30 softmax-KV layers")
     ap.add_argument("--kv-cache", choices=("bf16", "4bit"), default="bf16",
-                    help="with --stack-report --execute: what the softmax layers keep their keys and values in")
+                    help="with --stack-report: what the softmax layers keep their keys and values in")
     ap.add_argument("--execute", action="store_true",
                     help="with --stack-report: also run the whole rollout of both stacks for real (KV caches allocated and "
                          "appended to per chunk, every layer pass launched), time it end to end and report peak memory")
@@ -293,6 +309,8 @@ def main() -> int:
                     help="run only a plain device copy of 256 MiB (5 times): the reference for scaling the "
                          "FETCH_SIZE / WRITE_SIZE counters of a rocprofv3 --pmc run")
     args = ap.parse_args()
+    if args.kv_cache != "bf16" and not args.stack_report:
+        ap.error("--kv-cache belongs to --stack-report")
     if args.gpus != 1 or int(os.environ.get("WORLD_SIZE", "1")) != 1:
         print("bench.py: this build runs on ONE GPU (heads and streams are independent, so the step "
               "shards without any exchange); --gpus must be 1", file=sys.stderr)
@@ -321,7 +339,7 @@ def main() -> int:
     w = W.WORKLOADS[args.workload]
     io_bytes = 2 if w.io_dtype == "bf16" else 4
     if args.stack_report:
-        rep = stack_report(A, W, torch, dev)
+        rep = stack_report(A, W, torch, dev, kv_cache=args.kv_cache)
         if args.execute:
             ex = stack_execute(A, W, torch, dev, kv_cache=args.kv_cache)
             rep["executed"] = ex
