@@ -276,7 +276,7 @@ arl2_status arl2_state_commit_gdn(const arl2_desc *desc,
  * whose layout is the library's own; bytes that no token was written to may hold anything.
  *
  * Format (the OCP microscaling format e2m1 with a power-of-two scale): 32 features of a token and head share
- * an exponent e, the least one in [-120, 125] with max |x| <= 7 * 2^e, and each is stored as the nearest of
+ * an exponent e, the least one in [-120, 125] with max |x| <= 7 * 2^e (125 beyond), and each is stored as the nearest of
  * 2^e * {0, 1/2, 1, 3/2, 2, 3, 4, 6} and their negatives (ties to the even code).  A group with a NaN or an
  * infinity is stored as NaN.  The stored values are exact in bf16.
  *
@@ -345,6 +345,10 @@ arl2_status arl2_kv_read(const arl2_kv_desc *desc, const void *cache,
  * results are bit-identical from run to run.  Probabilities are rounded to bf16 for the second product, and with more than 64
  * query rows (Lq * H / Hkv) a query row may be taken to within 2^-9 of its length, half of what rounding it to bf16 may have taken, or
  * a feature to within 2^-112, whichever is more.  What the other queries of the call hold does not change a bit of a query's output.
+ * That division goes by max_pages * page_size, the longest history that the table could hold; parts beyond kv_len are left empty.  Where
+ * histories are far shorter, fewer workgroups share them: 1560 queries of 12 heads over 10920 tokens took 99 us with a table of
+ * that width and 215 with one four or twelve times as wide, single tokens of 16 streams of 8192 tokens 35, 42 and 74 us with tables of
+ * 8192, 32768 and 131072.
  * Uses desc->workspace; calls that overlap in time need one each.
  */
 arl2_status arl2_kv_attn_fwd(const arl2_kv_desc *desc, const void *q, const void *cache,

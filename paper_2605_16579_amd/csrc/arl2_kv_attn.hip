@@ -10,7 +10,7 @@
 // on, and waits on nothing but its own loads.  13 KB per wavefront, three workgroups per CU: 104 KB of a CU on their way.  Keys and values are
 // converted to bf16, in which they are exact.  At the end the wavefronts' results, each with its own maximum and sum, are added.
 // Measured: 131001 tokens of 8 stored heads, 32 query heads: 33 us (4.3 TB/s; a copy of 1 GiB moves 4.85 TB/s) and 5 us for the
-// join; 64 streams of 1 to 8192 tokens 31 us, of which a workgroup's fixed part (lengths, table, first blocks, ending: 5 us) and
+// join; 64 streams of 1 to 7122 tokens 31 us, of which a workgroup's fixed part (lengths, table, first blocks, ending: 5 us) and
 // splits that turn out empty are most.  Two workgroups per CU with a block more ahead: 38.5 and 39.6 us instead of 38.4 and 35.2 in all.
 #include "arl2_kv_attn.h"
 
@@ -23,7 +23,7 @@ namespace {
 
 constexpr int kRows = 32;        // query rows of a workgroup
 constexpr int kWaves = 4;
-constexpr int kSlots = 3 * kNumCu;     // workgroups that run at a time
+constexpr int kSlots = 3 * kNumCu;     // workgroups that run at a time at D = 128 (D = 64: four of them find room on a CU; divided alike)
 
 // LDS of a wavefront: a ring of blocks of 32 tokens as they are stored, per 16-token group key codes [16-byte piece of a row][token],
 // value codes, key scales, value scales.
@@ -452,7 +452,8 @@ hipError_t launch_join(const KvAttnArgs &a, hipStream_t stream)
 // Many rows: the splits that the measured cost of a tile, of a workgroup's ends and of partial results make the cheapest; e.g. 12 heads,
 // 1560 rows over 10920: 1 to 6 splits 236, 143, 110, 152, 133, 122 us; 4680 rows over 4680: 119 without, 146 with two.
 // Few rows: one round of workgroups; with several streams, whose lengths the host does not know, at most an eighth of the table's length or
-// 1024 tokens (64 streams of 1 to 8192 tokens: 512, 1024, 1408, 2048 tokens 39, 36.5, 36, 44 us).
+// 1024 tokens (64 streams of 1 to 7122 tokens, a table for 7136: 512, 1024, 1408, 2048 tokens 39, 36.5, 36, 44 us).
+// Both go by what the table could hold, and many rows by all of it for every row, causal or not.
 KvAttnPlan kv_attn_plan(int B, int Lq, int G, const KvPool &pool, int D)
 {
     KvAttnPlan p = {};

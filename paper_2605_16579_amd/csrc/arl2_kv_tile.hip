@@ -8,7 +8,8 @@
 //                                              average of the result's size, as in every product of bf16 matrices)
 // Values cannot go into the scaled instruction: its scales belong to 32 terms of a sum, which runs over tokens here, and the cache
 // scales values per token so that single tokens can be appended.  So they are converted, once per workgroup and tile (28 vector
-// instructions per thread), into an LDS tile that the second product reads in 16-byte pieces without bank conflicts.
+// instructions per thread), into an LDS tile that the second product reads in 16-byte pieces without bank conflicts.  The codes are read
+// 4 bytes a lane, 16 apart, with conflicts: the 11.2 M cycles counted in the launch below are 6 for each of these 1.87 M reads.
 //
 // Tiles come straight from memory into LDS as they are stored (8.7 KB; a bf16 tile is 32 KB), requested three intervals before their
 // values are converted; the block table's entries pass through LDS as well.  Per tile a wavefront requests one of eight pieces.  Waits
@@ -23,7 +24,8 @@
 //
 // What bounds it: vector instructions and the power of the matrix cores together.  12 heads x 128, 4680 queries over 32760 keys: 677
 // to 726 us by card (942 GFLOP: 1.30 to 1.39 PFLOP/s), on zeros, where power does not bound it, 629 us; the matrix instructions alone
-// would take 390 us.  The bf16 readout over a dense bf16 cache takes 760 to 818 us on the same cards.
+// would take 390 us.  The bf16 readout over a dense bf16 cache takes 760 to 818 us on the same cards.  24 heads x 64, as many operations:
+// 1032 us (0.91 PFLOP/s), with as many exponentials for half the products.
 #include "arl2_kv_attn.h"
 
 #include <limits.h>
