@@ -63,8 +63,11 @@ def expected(q, k, v, limit, scale, seen=None):
     # sum_j of c_j^2, of which each term's vector has its length and the sum at most both, and of c_j with |v - out| <= |v| + |out|
     square = 2.0 ** -16 * (p ** 2 @ v ** 2)
     spread = d ** 2 * (p ** 2 @ v ** 2 - 2 * out * (p ** 2 @ v) + (p ** 2).sum(-1, keepdims=True) * out ** 2)
-    both = np.square(np.sqrt(square) + np.sqrt(np.maximum(spread, 0.0)))
-    return p, out, both, (2.0 ** -8 + d) * (p @ np.abs(v)) + d * np.abs(out)
+    # What was summed up to a running maximum is lost where a later one is 2^126 times as much; many rows raise theirs where a block's
+    # probabilities add up to 2^12.
+    gone = 2.0 ** -114 * (see @ np.abs(v))
+    both = np.square(np.sqrt(square) + np.sqrt(np.maximum(spread, 0.0)) + gone)
+    return p, out, both, (2.0 ** -8 + d) * (p @ np.abs(v)) + d * np.abs(out) + gone
 
 
 def misses(got, out, square, total):
