@@ -28,6 +28,10 @@
  *   arl2_kv_append, arl2_kv_read, arl2_kv_attn_fwd   for layers that keep softmax over everything generated so far
  *                          (Eq. (1)): a paged key/value cache held in 4 bits, and the attention that reads it.
  *
+ *   arl2_scan_fwd, arl2_scan_bwd   the linear branch as a causal recurrence over tokens (Eq. (4) without the correction term,
+ *                          every token reading the state that it leaves), and its gradients;
+ *   arl2_rope_fwd, arl2_rope_bwd   queries and keys normalised and rotated by positions on several axes, and the gradients.
+ *
  * Reading of the feature map: q and k arrive after RoPE, the learned 1x1 maps are
  * the identity, so phi is the L2 normalisation over the head dimension,
  * x / sqrt(sum x^2 + l2_eps), and V' = v.
@@ -353,6 +357,104 @@ arl2_status arl2_kv_read(const arl2_kv_desc *desc, const void *cache,
  */
 arl2_status arl2_kv_attn_fwd(const arl2_kv_desc *desc, const void *q, const void *cache,
                              const int32_t *block_table, const int32_t *kv_len, const int32_t *q_len, void *out);
+
+/*
+ * ---- the linear branch as a causal recurrence ---------------------------------------------------------------
+ * For t = 1..len of every stream and head, k'_t = L2Norm(k_t), q'_t = L2Norm(q_t) (Eq. (3)) or the rows as they are,
+ *     S_t = exp(log_alpha_t) S_{t-1} + k'_t^T v_t,        out_t = q'_t S_t:
+ * Eq. (4) with beta = 1 and without the delta-correction term, token by token, and Eq. (5) with the state that a token leaves
+ * instead of a state that its chunk shares: what a causal model trains on and generates with.
+ */
+typedef struct {
+    int32_t B, H, L, D;   /* streams, heads, tokens: >= 1; D: 64 or 128.  L*H*D must stay below 2^30                    */
+    int32_t raw_rows;     /* 0: rows of q and k are divided by sqrt(|row|^2 + l2_eps); 1: they are taken as they are   */
+    float l2_eps;         /* 0 selects 1e-6                                                                            */
+    void *workspace;      /* device scratch, >= arl2_scan_workspace_bytes or arl2_scan_bwd_workspace_bytes, 16-byte     */
+    size_t workspace_bytes;  /* aligned; one for each call in flight                                                   */
+    void *stream;         /* hipStream_t; NULL is the default stream                                                   */
+} arl2_scan_desc;
+
+/* Scratch of the two calls (it depends on the sizes alone; 0: none is needed, or the descriptor is invalid). */
+size_t arl2_scan_workspace_bytes(const arl2_scan_desc *desc);
+size_t arl2_scan_bwd_workspace_bytes(const arl2_scan_desc *desc);
+
+/*
+ *   q, k, v   device bf16 [B][L][H][D].
+ *   log_alpha device fp32 [B][L][H]: natural logarithms of the gates, in [-inf, 0].  -inf (and what is below -2839) is a gate of zero: the state
+ *             begins anew with that token.  Values above 0 are taken as 0.  NULL: all gates are one.
+ *   seq_len   device int32 [B], read when the kernels run, cut to [0, L], or NULL: L for all.  Rows from seq_len[b] on are not read,
+ *             and left as they were in what is written.
+ *   S0        device fp32 [B][H][D][D], the state before the first token; NULL: zeros.
+ *   out       device bf16 [B][L][H][D]; must not overlap an input.
+ *   S         device fp32 [B][H][D][D], the state after the last token (S0 where there is none); NULL: it is not wanted.  May be S0 itself
+ *             (the state is updated in place), else it must not overlap an input.
+ * States, decays and sums are fp32 (a block's decays come from sums in fp64).  On the matrix cores the state and the rows that enter it are taken
+ * as two bf16 parts (to 2^-17 of each value), and products q'.k' within a block of 64 tokens are rounded to bf16 once.
+ * Up to 8 tokens are computed in fp32 throughout, with the state read and written once.  A NaN or an infinity in
+ * a row reaches outputs of the 64 tokens, counted from the first, that it lies in and of later ones, not of earlier blocks.  Deterministic.
+ */
+arl2_status arl2_scan_fwd(const arl2_scan_desc *desc, const void *q, const void *k, const void *v, const float *log_alpha,
+                          const int32_t *seq_len, const float *S0, void *out, float *S);
+
+/*
+ * Gradients of arl2_scan_fwd's arguments, of those that are given:
+ *   dout      device bf16 [B][L][H][D], gradient of out.
+ *   dS        device fp32 [B][H][D][D], gradient of the last state; NULL: zeros.
+ *   dq, dk, dv  device bf16 [B][L][H][D], written (through the normalisation where there is one).
+ *   dlog_alpha  device fp32 [B][L][H], written: the gradient of log_alpha as if it had no upper limit; zero at a gate of zero.  NULL: it is not wanted.
+ *   dS0       device fp32 [B][H][D][D], written; NULL: it is not wanted.  May be dS itself.
+ * What is written must overlap neither an input (dS0 and dS apart) nor what else is written.  Deterministic.
+ */
+arl2_status arl2_scan_bwd(const arl2_scan_desc *desc, const void *q, const void *k, const void *v, const float *log_alpha,
+                          const int32_t *seq_len, const float *S0, const void *dout, const float *dS,
+                          void *dq, void *dk, void *dv, float *dlog_alpha, float *dS0);
+
+/*
+ * ---- rotary positions on several axes -------------------------------------------------------------------------
+ * Rows of queries and keys as attention and the linear branch take them: y = R(pos) (w . x / sqrt(mean(x^2) + norm_eps)).
+ * The features of a head are D / 2 pairs; axis a turns the next axis_pairs[a] of them, its pair i by the angle
+ * pos[a] * theta[a]^(-i / axis_pairs[a]):  (x0, x1) -> (x0 cos - x1 sin, x0 sin + x1 cos).  Pairs beyond the axes' are not turned.
+ */
+typedef enum { ARL2_NORM_NONE = 0, ARL2_NORM_HEAD = 1, ARL2_NORM_ROW = 2 } arl2_norm_mode;
+
+typedef struct {
+    int32_t B, H, L, D;   /* streams, query heads, tokens: >= 1; D: 64 or 128                                          */
+    int32_t Hk;           /* key heads, >= 0 (0: there are no keys, their arrays are NULL); (H + Hk) * D <= 24576       */
+    int32_t io_dtype;     /* arl2_dtype of rows, weights and gradients of rows                                        */
+    int32_t norm;         /* arl2_norm_mode: the mean over a head's features, over all features of a token's          */
+                          /* queries (and of its keys), or no norm and no weights                                    */
+    int32_t halves;       /* pairs are 0: features (2i, 2i + 1), 1: features (i, i + D / 2)                           */
+    int32_t pos_per_stream;  /* pos is 0: [L][n_axes], 1: [B][L][n_axes]                                              */
+    int32_t n_axes;       /* 1 to 4                                                                                  */
+    int32_t axis_pairs[4];   /* each >= 1, together <= D / 2                                                          */
+    double theta[4];      /* > 0; 0 selects 10000                                                                    */
+    float norm_eps;       /* 0 selects 1e-6                                                                          */
+    void *workspace;      /* arl2_rope_bwd with weights' gradients: >= arl2_rope_workspace_bytes, 16-byte aligned     */
+    size_t workspace_bytes;
+    void *stream;         /* hipStream_t; NULL is the default stream                                                 */
+} arl2_rope_desc;
+
+size_t arl2_rope_workspace_bytes(const arl2_rope_desc *desc);
+
+/*
+ *   q, k      device, io_dtype [B][L][H][D] and [B][L][Hk][D].
+ *   wq, wk    device, io_dtype: [D] and [D] (ARL2_NORM_HEAD, shared by the heads), [H*D] and [Hk*D] (ARL2_NORM_ROW); NULL: ones.
+ *   pos       device int32, any values: angles are computed in fp64.
+ *   seq_len   device int32 [B], or NULL: L for all.  Rows from seq_len[b] on are not read, and left as they were in what is written.
+ *   yq, yk    device, like q and k.  yq may be q and yk may be k (in place); else they must overlap neither an input nor each other.
+ * fp32 arithmetic, one rounding to io_dtype.
+ */
+arl2_status arl2_rope_fwd(const arl2_rope_desc *desc, const void *q, const void *k, const void *wq, const void *wk,
+                          const int32_t *pos, const int32_t *seq_len, void *yq, void *yk);
+
+/*
+ * Gradients: dyq, dyk of yq, yk are given; dq, dk are written (they may be dyq and dyk), and the weights' gradients dwq, dwk, fp32, summed over the tokens
+ * that there are (and over the heads: ARL2_NORM_HEAD), each where it is not NULL and the rows have a norm.  Without a norm q and k are not read and may be NULL.
+ * Deterministic.
+ */
+arl2_status arl2_rope_bwd(const arl2_rope_desc *desc, const void *q, const void *k, const void *wq, const void *wk,
+                          const int32_t *pos, const int32_t *seq_len, const void *dyq, const void *dyk,
+                          void *dq, void *dk, float *dwq, float *dwk);
 
 const char *arl2_status_string(arl2_status s);
 

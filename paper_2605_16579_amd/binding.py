@@ -25,11 +25,14 @@ HOST_FOR = f"Python {sys.version_info[0]}.{sys.version_info[1]}, torch {torch.__
 ARL2_OK, ARL2_ERR_INVALID_ARG, ARL2_ERR_UNSUPPORTED, ARL2_ERR_WORKSPACE, ARL2_ERR_DEVICE = range(5)
 ARL2_F32, ARL2_BF16 = 0, 1
 ARL2_GATE_PER_HEAD, ARL2_GATE_PER_ELEMENT, ARL2_GATE_PER_TOKEN = 0, 1, 2
+ARL2_NORM_NONE, ARL2_NORM_HEAD, ARL2_NORM_ROW = 0, 1, 2
 
 EXPORTS = ["arl2_workspace_bytes", "arl2_hybrid_attn_fwd", "arl2_state_commit", "arl2_state_commit_delta",
            "arl2_static_scratch_bytes", "arl2_state_commit_static", "arl2_state_commit_fm",
            "arl2_gdn_workspace_bytes", "arl2_state_commit_gdn", "arl2_hybrid_attn_fwd_ex", "arl2_hybrid_attn_fwd_fm", "arl2_feature_map", "arl2_gate_proj",
            "arl2_kv_cache_bytes", "arl2_kv_workspace_bytes", "arl2_kv_append", "arl2_kv_read", "arl2_kv_attn_fwd",
+           "arl2_scan_workspace_bytes", "arl2_scan_bwd_workspace_bytes", "arl2_scan_fwd", "arl2_scan_bwd",
+           "arl2_rope_workspace_bytes", "arl2_rope_fwd", "arl2_rope_bwd",
            "arl2_status_string", "arl2_last_error", "arl2_version"]
 
 
@@ -45,6 +48,18 @@ class arl2_kv_desc(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("Lq", ctypes.c_int32),
                 ("D", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
                 ("max_pages", ctypes.c_int32), ("causal", ctypes.c_int32), ("sm_scale", ctypes.c_float),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)]
+
+
+class arl2_scan_desc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("L", ctypes.c_int32), ("D", ctypes.c_int32), ("raw_rows", ctypes.c_int32),
+                ("l2_eps", ctypes.c_float), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)]
+
+
+class arl2_rope_desc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("L", ctypes.c_int32), ("D", ctypes.c_int32), ("Hk", ctypes.c_int32),
+                ("io_dtype", ctypes.c_int32), ("norm", ctypes.c_int32), ("halves", ctypes.c_int32), ("pos_per_stream", ctypes.c_int32),
+                ("n_axes", ctypes.c_int32), ("axis_pairs", ctypes.c_int32 * 4), ("theta", ctypes.c_double * 4), ("norm_eps", ctypes.c_float),
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)]
 
 
@@ -125,6 +140,13 @@ def load_library() -> ctypes.CDLL:
         lib.arl2_kv_read.restype = ctypes.c_int
         lib.arl2_kv_attn_fwd.argtypes = [kdp] + [vp] * 6
         lib.arl2_kv_attn_fwd.restype = ctypes.c_int
+        for desc, names in ((arl2_scan_desc, {"arl2_scan_fwd": 8, "arl2_scan_bwd": 13}), (arl2_rope_desc, {"arl2_rope_fwd": 8, "arl2_rope_bwd": 12})):
+            for name, pointers in names.items():
+                getattr(lib, name).argtypes = [ctypes.POINTER(desc)] + [vp] * pointers
+                getattr(lib, name).restype = ctypes.c_int
+        for desc, name in ((arl2_scan_desc, "arl2_scan_workspace_bytes"), (arl2_scan_desc, "arl2_scan_bwd_workspace_bytes"), (arl2_rope_desc, "arl2_rope_workspace_bytes")):
+            getattr(lib, name).argtypes = [ctypes.POINTER(desc)]
+            getattr(lib, name).restype = ctypes.c_size_t
         lib.arl2_status_string.argtypes = [ctypes.c_int]
         lib.arl2_status_string.restype = ctypes.c_char_p
         lib.arl2_last_error.argtypes = []
@@ -519,6 +541,141 @@ def arl2_kv_attn_fwd(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Te
     _one_device(q, cache, block_table, kv_len, q_len, out, workspace)
     d = _kv_desc(B, H, Hkv, L, D, page, n_pages, width, causal, sm_scale, workspace, stream)
     _check(load_library().arl2_kv_attn_fwd(ctypes.byref(d), *ptrs))
+
+
+# ---- the linear branch as a causal recurrence
+
+def _scan_desc(B, H, L, D, normalise=True, l2_eps=0.0, workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> arl2_scan_desc:
+    return arl2_scan_desc(B, H, L, D, 0 if normalise else 1, l2_eps, _dev(workspace, "workspace"), 0 if workspace is None else workspace.nbytes,
+                          _current_stream() if stream is None else stream)
+
+
+def arl2_scan_workspace_bytes(B: int, H: int, L: int, D: int) -> int:
+    """Device scratch bytes that arl2_scan_fwd needs for these sizes (0: none)."""
+    return int(load_library().arl2_scan_workspace_bytes(ctypes.byref(_scan_desc(B, H, L, D, stream=0))))
+
+
+def arl2_scan_bwd_workspace_bytes(B: int, H: int, L: int, D: int) -> int:
+    """Device scratch bytes that arl2_scan_bwd needs for these sizes."""
+    return int(load_library().arl2_scan_bwd_workspace_bytes(ctypes.byref(_scan_desc(B, H, L, D, stream=0))))
+
+
+def alloc_scan_workspace(B: int, H: int, L: int, D: int, backward: bool = False, device="cuda") -> Optional[torch.Tensor]:
+    """Convenience: a torch buffer for arl2_scan_fwd (or arl2_scan_bwd) of these sizes, or None where none is needed."""
+    n = arl2_scan_bwd_workspace_bytes(B, H, L, D) if backward else arl2_scan_workspace_bytes(B, H, L, D)
+    return torch.empty(n, dtype=torch.uint8, device=device) if n else None
+
+
+def arl2_scan_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_alpha: Optional[torch.Tensor], S0: Optional[torch.Tensor],
+                  out: torch.Tensor, S: Optional[torch.Tensor], *, seq_len: Optional[torch.Tensor] = None, normalise: bool = True,
+                  l2_eps: float = 0.0, workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> None:
+    """S_t = exp(log_alpha_t) S_{t-1} + k'_t^T v_t, out_t = q'_t S_t for the first seq_len[b] (None: all) tokens of q, k, v [B, L, H, D] bf16;
+    k', q': L2-normalised, or (``normalise`` false) as they are.  log_alpha [B, L, H] fp32 (None: zeros); S0 (None: zeros) and S (None: not
+    wanted) [B, H, D, D] fp32, may be the same.  ``workspace``: of ``alloc_scan_workspace``, one for each call in flight."""
+    if _plain_call("arl2_scan_fwd", b"CqqqtnSqS", 0.0 if normalise else 1.0, l2_eps, stream, workspace, q, k, v, log_alpha, seq_len, S0, out, S):
+        return
+    if q.dim() != 4:
+        raise ValueError("q must be [B, L, H, D]")
+    B, L, H, D = q.shape
+    bf16, state = torch.bfloat16, (B, H, D, D)
+    ptrs = (_dev(q, "q", None, bf16), _dev(k, "k", q.shape, bf16), _dev(v, "v", q.shape, bf16), _dev(log_alpha, "log_alpha", (B, L, H), torch.float32),
+            _dev(seq_len, "seq_len", (B,), torch.int32), _dev(S0, "S0", state, torch.float32), _dev(out, "out", q.shape, bf16), _dev(S, "S", state, torch.float32))
+    _one_device(q, k, v, log_alpha, seq_len, S0, out, S, workspace)
+    d = _scan_desc(B, H, L, D, normalise, l2_eps, workspace, stream)
+    _check(load_library().arl2_scan_fwd(ctypes.byref(d), *ptrs))
+
+
+def arl2_scan_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_alpha: Optional[torch.Tensor], S0: Optional[torch.Tensor],
+                  dout: torch.Tensor, dS: Optional[torch.Tensor], dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor,
+                  dlog_alpha: Optional[torch.Tensor], dS0: Optional[torch.Tensor], *, seq_len: Optional[torch.Tensor] = None, normalise: bool = True,
+                  l2_eps: float = 0.0, workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> None:
+    """Gradients of ``arl2_scan_fwd``: from dout [B, L, H, D] bf16 and dS [B, H, D, D] fp32 (None: zeros) into dq, dk, dv [B, L, H, D] bf16,
+    dlog_alpha [B, L, H] fp32 and dS0 [B, H, D, D] fp32 (None: not wanted).  ``workspace``: of ``alloc_scan_workspace(..., backward=True)``."""
+    if _plain_call("arl2_scan_bwd", b"CqqqtnSqSqqqtS", 0.0 if normalise else 1.0, l2_eps, stream, workspace,
+                   q, k, v, log_alpha, seq_len, S0, dout, dS, dq, dk, dv, dlog_alpha, dS0):
+        return
+    if q.dim() != 4:
+        raise ValueError("q must be [B, L, H, D]")
+    B, L, H, D = q.shape
+    bf16, gates, state = torch.bfloat16, (B, L, H), (B, H, D, D)
+    ptrs = (_dev(q, "q", None, bf16), _dev(k, "k", q.shape, bf16), _dev(v, "v", q.shape, bf16), _dev(log_alpha, "log_alpha", gates, torch.float32),
+            _dev(seq_len, "seq_len", (B,), torch.int32), _dev(S0, "S0", state, torch.float32), _dev(dout, "dout", q.shape, bf16), _dev(dS, "dS", state, torch.float32),
+            _dev(dq, "dq", q.shape, bf16), _dev(dk, "dk", q.shape, bf16), _dev(dv, "dv", q.shape, bf16), _dev(dlog_alpha, "dlog_alpha", gates, torch.float32),
+            _dev(dS0, "dS0", state, torch.float32))
+    _one_device(q, k, v, log_alpha, seq_len, S0, dout, dS, dq, dk, dv, dlog_alpha, dS0, workspace)
+    d = _scan_desc(B, H, L, D, normalise, l2_eps, workspace, stream)
+    _check(load_library().arl2_scan_bwd(ctypes.byref(d), *ptrs))
+
+
+# ---- rotary positions on several axes
+
+_NORMS = {"none": ARL2_NORM_NONE, "head": ARL2_NORM_HEAD, "row": ARL2_NORM_ROW}
+
+
+def _rope_desc(B, H, L, D, Hk, io_dtype=ARL2_BF16, norm="none", halves=False, pos_per_stream=False, axis_pairs=(1,), theta=None, norm_eps=0.0,
+               workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> arl2_rope_desc:
+    theta = [0.0] * len(axis_pairs) if theta is None else theta
+    if norm not in _NORMS:
+        raise ValueError(f"norm must be one of {sorted(_NORMS)}")
+    if not 1 <= len(axis_pairs) <= 4 or len(theta) != len(axis_pairs):
+        raise ValueError("axis_pairs must name 1 to 4 axes, and theta as many")
+    return arl2_rope_desc(B, H, L, D, Hk, io_dtype, _NORMS[norm], 1 if halves else 0, 1 if pos_per_stream else 0, len(axis_pairs),
+                          (ctypes.c_int32 * 4)(*axis_pairs), (ctypes.c_double * 4)(*theta), norm_eps, _dev(workspace, "workspace"),
+                          0 if workspace is None else workspace.nbytes, _current_stream() if stream is None else stream)
+
+
+def arl2_rope_workspace_bytes(B: int, H: int, Hk: int, L: int, D: int) -> int:
+    """Device scratch bytes that arl2_rope_bwd needs where weights' gradients are wanted."""
+    return int(load_library().arl2_rope_workspace_bytes(ctypes.byref(_rope_desc(B, H, L, D, Hk, stream=0))))
+
+
+def alloc_rope_workspace(B: int, H: int, Hk: int, L: int, D: int, device="cuda") -> torch.Tensor:
+    """Convenience: a torch buffer of arl2_rope_workspace_bytes() bytes."""
+    return torch.empty(max(arl2_rope_workspace_bytes(B, H, Hk, L, D), 16), dtype=torch.uint8, device=device)
+
+
+def _rope_call(rows, keys, wq, wk, pos, seq_len, norm, axis_pairs, kw):
+    """The descriptor of a call on query rows and key rows (or None) of these kinds, and what the other arrays must look like."""
+    if rows.dim() != 4 or (keys is not None and keys.dim() != 4):
+        raise ValueError("queries and keys must be [B, L, heads, D]")
+    B, L, H, D = rows.shape
+    Hk = 0 if keys is None else keys.shape[2]
+    width = (lambda heads: (D,)) if norm == "head" else (lambda heads: (heads * D,))
+    n = len(axis_pairs)
+    per_stream = pos.dim() == 3
+    d = _rope_desc(B, H, L, D, Hk, _dtype_code(rows), norm, pos_per_stream=per_stream, axis_pairs=axis_pairs, **kw)
+    like_q, like_k = ((B, L, H, D), rows.dtype), ((B, L, Hk, D), rows.dtype)
+    fixed = (_dev(wq, "wq", width(H), rows.dtype), _dev(wk, "wk", width(Hk), rows.dtype),
+             _dev(pos, "pos", (B, L, n) if per_stream else (L, n), torch.int32), _dev(seq_len, "seq_len", (B,), torch.int32))
+    return d, like_q, like_k, width(H), width(Hk), fixed
+
+
+def arl2_rope_fwd(q: torch.Tensor, k: Optional[torch.Tensor], wq: Optional[torch.Tensor], wk: Optional[torch.Tensor], pos: torch.Tensor,
+                  yq: torch.Tensor, yk: Optional[torch.Tensor], *, axis_pairs, theta=None, halves: bool = False, norm: str = "none",
+                  norm_eps: float = 0.0, seq_len: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> None:
+    """yq, yk (may be q, k) = the rows of q [B, L, H, D] and k [B, L, Hk, D] (or None) over their root mean square of a head's features ("head",
+    weights [D]), of a token's row ("row", weights [H * D] and [Hk * D]) or as they are ("none"), times the weights (None: ones), rotated by
+    pos [L, axes] or [B, L, axes] int32: ``axis_pairs`` pairs of features by each axis with frequencies theta^(-i / pairs) (None, 0: 10000);
+    pairs are neighbours, or (``halves``) features i and i + D / 2.  fp32 or bf16."""
+    d, like_q, like_k, _, _, (pwq, pwk, ppos, plen) = _rope_call(q, k, wq, wk, pos, seq_len, norm, axis_pairs,
+                                                                 dict(theta=theta, halves=halves, norm_eps=norm_eps, stream=stream))
+    ptrs = (_dev(q, "q", *like_q), _dev(k, "k", *like_k), pwq, pwk, ppos, plen, _dev(yq, "yq", *like_q), _dev(yk, "yk", *like_k))
+    _one_device(q, k, wq, wk, pos, seq_len, yq, yk)
+    _check(load_library().arl2_rope_fwd(ctypes.byref(d), *ptrs))
+
+
+def arl2_rope_bwd(q: Optional[torch.Tensor], k: Optional[torch.Tensor], wq: Optional[torch.Tensor], wk: Optional[torch.Tensor], pos: torch.Tensor,
+                  dyq: torch.Tensor, dyk: Optional[torch.Tensor], dq: torch.Tensor, dk: Optional[torch.Tensor], dwq: Optional[torch.Tensor],
+                  dwk: Optional[torch.Tensor], *, axis_pairs, theta=None, halves: bool = False, norm: str = "none", norm_eps: float = 0.0,
+                  seq_len: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> None:
+    """Gradients of ``arl2_rope_fwd``: from dyq, dyk into dq, dk (may be dyq, dyk) and, fp32, the weights' dwq, dwk (None: not wanted), which
+    take a ``workspace`` of ``alloc_rope_workspace``.  q and k may be None where ``norm`` is "none"."""
+    d, like_q, like_k, of_q, of_k, (pwq, pwk, ppos, plen) = _rope_call(dyq, dyk, wq, wk, pos, seq_len, norm, axis_pairs,
+                                                                       dict(theta=theta, halves=halves, norm_eps=norm_eps, workspace=workspace, stream=stream))
+    ptrs = (_dev(q, "q", *like_q), _dev(k, "k", *like_k), pwq, pwk, ppos, plen, _dev(dyq, "dyq", *like_q), _dev(dyk, "dyk", *like_k),
+            _dev(dq, "dq", *like_q), _dev(dk, "dk", *like_k), _dev(dwq, "dwq", of_q, torch.float32), _dev(dwk, "dwk", of_k, torch.float32))
+    _one_device(q, k, wq, wk, pos, seq_len, dyq, dyk, dq, dk, dwq, dwk, workspace)
+    _check(load_library().arl2_rope_bwd(ctypes.byref(d), *ptrs))
 
 
 def arl2_version() -> int:

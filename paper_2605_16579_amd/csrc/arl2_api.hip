@@ -2,10 +2,14 @@
 // gfx950 kernels, error reporting.  Nothing here allocates device memory or synchronises.
 #include "../../include/arl2.h"
 #include "arl2_device.h"
+#include "arl2_rope.h"
+#include "arl2_scan.h"
 
 #include <atomic>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 
 namespace {
 
@@ -148,6 +152,99 @@ arl2::KvRowsArgs kv_rows_args(const arl2_kv_desc *d, const int32_t *table, const
     a.table = table; a.start = start; a.count = count;
     a.pool = kv_pool(d);
     a.B = d->B; a.L = d->Lq; a.D = d->D;
+    return a;
+}
+
+// ---- the causal recurrence
+
+arl2_status check_scan_desc(const arl2_scan_desc *d)
+{
+    if (d == nullptr) return fail(ARL2_ERR_INVALID_ARG, "desc is NULL");
+    if (d->B < 1 || d->H < 1 || d->L < 1) return fail(ARL2_ERR_INVALID_ARG, "B, H and L must all be >= 1");
+    if (d->D != 64 && d->D != 128) return fail(ARL2_ERR_UNSUPPORTED, "D must be 64 or 128");
+    if (d->raw_rows != 0 && d->raw_rows != 1) return fail(ARL2_ERR_INVALID_ARG, "raw_rows must be 0 or 1");
+    if (!(d->l2_eps >= 0.f)) return fail(ARL2_ERR_INVALID_ARG, "l2_eps must be >= 0 (0 selects the default)");
+    // A stream's rows are addressed with 32-bit byte offsets, which may point 64 rows past the last.
+    if ((double)d->L * d->H * d->D >= 1073741824.0 || 64.0 * d->H * d->D >= 1073741824.0)
+        return fail(ARL2_ERR_UNSUPPORTED, "problem too large (L*H*D and 64*H*D must stay below 2^30)");
+    if ((double)d->B * d->H > 1.0e6 || (double)d->B * d->H * ((d->L + 63.0) / 64) * 3 > 2147483000.0)
+        return fail(ARL2_ERR_UNSUPPORTED, "problem too large (B*H must stay below 1e6, B*H*L below 2^35)");
+    return ARL2_OK;
+}
+size_t scan_rows_bytes(const arl2_scan_desc *d) { return (size_t)d->B * d->L * d->H * d->D * 2; }
+size_t scan_gate_bytes(const arl2_scan_desc *d) { return (size_t)d->B * d->L * d->H * sizeof(float); }
+size_t scan_state_bytes(const arl2_scan_desc *d) { return (size_t)d->B * d->H * d->D * d->D * sizeof(float); }
+arl2::ScanArgs scan_args(const arl2_scan_desc *d, const void *q, const void *k, const void *v, const float *log_alpha, const int32_t *seq_len, const float *S0)
+{
+    arl2::ScanArgs a = {};
+    a.q = q; a.k = k; a.v = v; a.la = log_alpha; a.len = seq_len; a.S0 = S0;
+    a.workspace = d->workspace;
+    a.B = d->B; a.H = d->H; a.L = d->L; a.D = d->D;
+    a.normalise = !d->raw_rows;
+    a.eps = d->l2_eps > 0.f ? d->l2_eps : 1e-6f;
+    return a;
+}
+
+// ---- rotary positions
+
+arl2_status check_rope_desc(const arl2_rope_desc *d)
+{
+    if (d == nullptr) return fail(ARL2_ERR_INVALID_ARG, "desc is NULL");
+    if (d->B < 1 || d->H < 1 || d->L < 1 || d->Hk < 0) return fail(ARL2_ERR_INVALID_ARG, "B, H and L must all be >= 1, Hk >= 0");
+    if (d->D != 64 && d->D != 128) return fail(ARL2_ERR_UNSUPPORTED, "D must be 64 or 128");
+    if (d->io_dtype != ARL2_F32 && d->io_dtype != ARL2_BF16) return fail(ARL2_ERR_INVALID_ARG, "io_dtype is not an arl2_dtype");
+    if (d->norm != ARL2_NORM_NONE && d->norm != ARL2_NORM_HEAD && d->norm != ARL2_NORM_ROW) return fail(ARL2_ERR_INVALID_ARG, "norm is not an arl2_norm_mode");
+    if ((d->halves != 0 && d->halves != 1) || (d->pos_per_stream != 0 && d->pos_per_stream != 1))
+        return fail(ARL2_ERR_INVALID_ARG, "halves and pos_per_stream must be 0 or 1");
+    if (d->n_axes < 1 || d->n_axes > 4) return fail(ARL2_ERR_INVALID_ARG, "n_axes must be 1 to 4");
+    long long pairs = 0;
+    for (int a = 0; a < d->n_axes; ++a) {
+        if (d->axis_pairs[a] < 1) return fail(ARL2_ERR_INVALID_ARG, "axis_pairs must be >= 1");
+        if (!(d->theta[a] >= 0.0) || d->theta[a] > 1e30 || (d->theta[a] > 0.0 && d->theta[a] < 1e-3))
+            return fail(ARL2_ERR_INVALID_ARG, "theta must lie in [1e-3, 1e30] (0 selects the default)");
+        pairs += d->axis_pairs[a];
+    }
+    if (pairs > d->D / 2) return fail(ARL2_ERR_INVALID_ARG, "axis_pairs must be D / 2 at most together");
+    if (!(d->norm_eps >= 0.f)) return fail(ARL2_ERR_INVALID_ARG, "norm_eps must be >= 0 (0 selects the default)");
+    if (((double)d->H + d->Hk) * (d->D / 16) > arl2::kRopeMostUnits) return fail(ARL2_ERR_UNSUPPORTED, "(H + Hk) * D must be 24576 at most");
+    if ((double)d->B * d->L > 2.0e9) return fail(ARL2_ERR_UNSUPPORTED, "problem too large (B*L must stay below 2e9)");
+    return ARL2_OK;
+}
+size_t rope_rows_bytes(const arl2_rope_desc *d, int heads) { return (size_t)d->B * d->L * heads * d->D * elem_bytes(d->io_dtype); }
+size_t rope_weight_bytes(const arl2_rope_desc *d, int heads) { return (size_t)(d->norm == ARL2_NORM_HEAD ? 1 : heads) * d->D * elem_bytes(d->io_dtype); }
+size_t rope_pos_bytes(const arl2_rope_desc *d) { return (size_t)(d->pos_per_stream ? d->B : 1) * d->L * d->n_axes * sizeof(int32_t); }
+
+// What both directions check; `keys`: the arrays of keys' rows, which are there exactly where there are keys.
+arl2_status check_rope_call(const arl2_rope_desc *d, std::initializer_list<const void *> keys, const void *wq, const void *wk, const int32_t *pos, const int32_t *seq_len)
+{
+    const arl2_status st = check_rope_desc(d);
+    if (st != ARL2_OK) return st;
+    for (const void *k : keys)
+        if ((k != nullptr) != (d->Hk > 0)) return fail(ARL2_ERR_INVALID_ARG, "keys must be given exactly where Hk > 0");
+    if (pos == nullptr) return fail(ARL2_ERR_INVALID_ARG, "pos must not be NULL");
+    if ((wq || wk) && d->norm == ARL2_NORM_NONE) return fail(ARL2_ERR_INVALID_ARG, "rows without a norm have no weights");
+    if (wk && d->Hk == 0) return fail(ARL2_ERR_INVALID_ARG, "wk must be NULL where there are no keys");
+    if (!aligned16(wq) || !aligned16(wk)) return fail(ARL2_ERR_INVALID_ARG, "wq and wk must be 16-byte aligned");
+    if (!aligned4(pos) || !aligned4(seq_len)) return fail(ARL2_ERR_INVALID_ARG, "pos and seq_len must be 4-byte aligned");
+    return ARL2_OK;
+}
+
+arl2::RopeArgs rope_args(const arl2_rope_desc *d, const void *q, const void *k, const void *wq, const void *wk, const int32_t *pos, const int32_t *seq_len)
+{
+    arl2::RopeArgs a = {};
+    a.x[0] = q; a.x[1] = k; a.w[0] = wq; a.w[1] = wk; a.pos = pos; a.len = seq_len;
+    a.B = d->B; a.L = d->L; a.D = d->D; a.heads[0] = d->H; a.heads[1] = d->Hk;
+    a.axes = d->n_axes; a.pos_per_stream = d->pos_per_stream; a.halves = d->halves;
+    a.norm = d->norm == ARL2_NORM_NONE ? arl2::kNormNone : d->norm == ARL2_NORM_HEAD ? arl2::kNormHead : arl2::kNormRow;
+    a.f32 = d->io_dtype == ARL2_F32;
+    a.eps = d->norm_eps > 0.f ? d->norm_eps : 1e-6f;
+    for (int x = 0; x < d->n_axes; ++x) {
+        const double theta = d->theta[x] > 0.0 ? d->theta[x] : 10000.0;
+        for (int i = 0; i < d->axis_pairs[x]; ++i, ++a.pairs) {
+            a.axis[a.pairs] = (uint8_t)x;
+            a.turns[a.pairs] = std::pow(theta, -(double)i / d->axis_pairs[x]) * 0.15915494309189535;      // 1 / 2 pi
+        }
+    }
     return a;
 }
 
@@ -598,6 +695,145 @@ arl2_status arl2_kv_attn_fwd(const arl2_kv_desc *desc, const void *q, const void
     a.scale_log2 = (desc->sm_scale > 0.f ? desc->sm_scale : 1.0f / sqrtf((float)desc->D)) * 1.4426950408889634f;
     const hipError_t e = arl2::launch_kv_attn(a, plan, desc->workspace, reinterpret_cast<hipStream_t>(desc->stream));
     if (e != hipSuccess) return fail(ARL2_ERR_DEVICE, "attention launch failed: %s", hipGetErrorString(e));
+    return ARL2_OK;
+}
+
+// ---- the causal recurrence ----------------------------------------------------------------------------
+size_t arl2_scan_workspace_bytes(const arl2_scan_desc *desc)
+{
+    return check_scan_desc(desc) == ARL2_OK ? arl2::scan_plan(desc->B, desc->H, desc->L, desc->D, false).bytes : 0;
+}
+
+size_t arl2_scan_bwd_workspace_bytes(const arl2_scan_desc *desc)
+{
+    return check_scan_desc(desc) == ARL2_OK ? arl2::scan_plan(desc->B, desc->H, desc->L, desc->D, true).bytes : 0;
+}
+
+arl2_status arl2_scan_fwd(const arl2_scan_desc *desc, const void *q, const void *k, const void *v, const float *log_alpha,
+                          const int32_t *seq_len, const float *S0, void *out, float *S)
+{
+    const arl2_status st = check_scan_desc(desc);
+    if (st != ARL2_OK) return st;
+    if (!q || !k || !v || !out) return fail(ARL2_ERR_INVALID_ARG, "q, k, v and out must not be NULL");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(S0) || !aligned16(S))
+        return fail(ARL2_ERR_INVALID_ARG, "q, k, v, S0, out and S must be 16-byte aligned");
+    if (!aligned4(log_alpha) || !aligned4(seq_len)) return fail(ARL2_ERR_INVALID_ARG, "log_alpha and seq_len must be 4-byte aligned");
+    const arl2::ScanPlan plan = arl2::scan_plan(desc->B, desc->H, desc->L, desc->D, false);
+    if (plan.bytes > 0 && (desc->workspace == nullptr || desc->workspace_bytes < plan.bytes))
+        return fail(ARL2_ERR_WORKSPACE, "workspace is NULL or smaller than arl2_scan_workspace_bytes()");
+    if (!aligned16(desc->workspace)) return fail(ARL2_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    const size_t rows = scan_rows_bytes(desc), gates = scan_gate_bytes(desc), state = scan_state_bytes(desc), lens = desc->B * sizeof(int32_t);
+    const Range ws = {desc->workspace, plan.bytes};
+    const Range in[] = {{q, rows}, {k, rows}, {v, rows}, {log_alpha, gates}, {seq_len, lens}, {S0, state}};
+    const Range in_but_S0[] = {{q, rows}, {k, rows}, {v, rows}, {log_alpha, gates}, {seq_len, lens}, {S == S0 ? nullptr : S0, state}};
+    if (overlaps_any({out, rows}, in) || overlaps_any({S, state}, in_but_S0) || overlaps(out, rows, S, state))
+        return fail(ARL2_ERR_INVALID_ARG, "out and S must overlap neither an input nor each other (S may be S0)");
+    if (overlaps_any(ws, in) || overlaps(ws.p, ws.n, out, rows) || overlaps(ws.p, ws.n, S, state))
+        return fail(ARL2_ERR_INVALID_ARG, "the workspace must overlap no other argument");
+
+    arl2::ScanArgs a = scan_args(desc, q, k, v, log_alpha, seq_len, S0);
+    a.out = out; a.S = S;
+    const hipError_t e = arl2::launch_scan_fwd(a, plan, reinterpret_cast<hipStream_t>(desc->stream));
+    if (e != hipSuccess) return fail(ARL2_ERR_DEVICE, "scan launch failed: %s", hipGetErrorString(e));
+    return ARL2_OK;
+}
+
+arl2_status arl2_scan_bwd(const arl2_scan_desc *desc, const void *q, const void *k, const void *v, const float *log_alpha,
+                          const int32_t *seq_len, const float *S0, const void *dout, const float *dS,
+                          void *dq, void *dk, void *dv, float *dlog_alpha, float *dS0)
+{
+    const arl2_status st = check_scan_desc(desc);
+    if (st != ARL2_OK) return st;
+    if (!q || !k || !v || !dout || !dq || !dk || !dv) return fail(ARL2_ERR_INVALID_ARG, "q, k, v, dout, dq, dk and dv must not be NULL");
+    for (const void *p : {q, k, v, dout, (const void *)dq, (const void *)dk, (const void *)dv, (const void *)S0, (const void *)dS, (const void *)dS0})
+        if (!aligned16(p)) return fail(ARL2_ERR_INVALID_ARG, "rows, states and their gradients must be 16-byte aligned");
+    if (!aligned4(log_alpha) || !aligned4(seq_len) || !aligned4(dlog_alpha))
+        return fail(ARL2_ERR_INVALID_ARG, "log_alpha, dlog_alpha and seq_len must be 4-byte aligned");
+    if (dlog_alpha != nullptr && log_alpha == nullptr) return fail(ARL2_ERR_INVALID_ARG, "dlog_alpha is of a log_alpha that is NULL");
+    const arl2::ScanPlan plan = arl2::scan_plan(desc->B, desc->H, desc->L, desc->D, true);
+    if (desc->workspace == nullptr || desc->workspace_bytes < plan.bytes)
+        return fail(ARL2_ERR_WORKSPACE, "workspace is NULL or smaller than arl2_scan_bwd_workspace_bytes()");
+    if (!aligned16(desc->workspace)) return fail(ARL2_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    const size_t rows = scan_rows_bytes(desc), gates = scan_gate_bytes(desc), state = scan_state_bytes(desc), lens = desc->B * sizeof(int32_t);
+    const Range in[] = {{q, rows}, {k, rows}, {v, rows}, {log_alpha, gates}, {seq_len, lens}, {S0, state}, {dout, rows}, {dS, state}};
+    const Range made[] = {{dq, rows}, {dk, rows}, {dv, rows}, {dlog_alpha, gates}, {dS0, state}, {desc->workspace, plan.bytes}};
+    for (const Range &m : made) {
+        for (const Range &i : in)
+            if (overlaps(m.p, m.n, i.p, i.n) && !(m.p == dS0 && i.p == dS && dS0 == dS))
+                return fail(ARL2_ERR_INVALID_ARG, "gradients and the workspace must not overlap an input (dS0 may be dS)");
+        for (const Range &o : made)
+            if (&o != &m && overlaps(m.p, m.n, o.p, o.n)) return fail(ARL2_ERR_INVALID_ARG, "gradients and the workspace must not overlap each other");
+    }
+
+    arl2::ScanArgs a = scan_args(desc, q, k, v, log_alpha, seq_len, S0);
+    a.dout = dout; a.dS = dS; a.dq = dq; a.dk = dk; a.dv = dv; a.dla = dlog_alpha; a.dS0 = dS0;
+    const hipError_t e = arl2::launch_scan_bwd(a, plan, reinterpret_cast<hipStream_t>(desc->stream));
+    if (e != hipSuccess) return fail(ARL2_ERR_DEVICE, "scan gradient launch failed: %s", hipGetErrorString(e));
+    return ARL2_OK;
+}
+
+// ---- rotary positions ---------------------------------------------------------------------------------
+size_t arl2_rope_workspace_bytes(const arl2_rope_desc *desc)
+{
+    return check_rope_desc(desc) == ARL2_OK ? arl2::rope_workspace_bytes(desc->B, desc->L, desc->D, desc->H + desc->Hk) : 0;
+}
+
+arl2_status arl2_rope_fwd(const arl2_rope_desc *desc, const void *q, const void *k, const void *wq, const void *wk,
+                          const int32_t *pos, const int32_t *seq_len, void *yq, void *yk)
+{
+    const arl2_status st = check_rope_call(desc, {k, yk}, wq, wk, pos, seq_len);
+    if (st != ARL2_OK) return st;
+    if (!q || !yq) return fail(ARL2_ERR_INVALID_ARG, "q and yq must not be NULL");
+    for (const void *p : {q, k, (const void *)yq, (const void *)yk})
+        if (!aligned16(p)) return fail(ARL2_ERR_INVALID_ARG, "rows must be 16-byte aligned");
+    const size_t nq = rope_rows_bytes(desc, desc->H), nk = rope_rows_bytes(desc, desc->Hk);
+    const Range fixed[] = {{wq, rope_weight_bytes(desc, desc->H)}, {wk, rope_weight_bytes(desc, desc->Hk)}, {pos, rope_pos_bytes(desc)}, {seq_len, desc->B * sizeof(int32_t)}};
+    if (overlaps_any({yq, nq}, fixed) || overlaps_any({yk, nk}, fixed) || overlaps(yq, nq, yk, nk) || overlaps(yq, nq, k, nk) || overlaps(yk, nk, q, nq) ||
+        (yq != q && overlaps(yq, nq, q, nq)) || (yk != k && overlaps(yk, nk, k, nk)))
+        return fail(ARL2_ERR_INVALID_ARG, "yq and yk must overlap neither an input nor each other (yq may be q, yk may be k)");
+
+    arl2::RopeArgs a = rope_args(desc, q, k, wq, wk, pos, seq_len);
+    a.y[0] = yq; a.y[1] = yk;
+    const hipError_t e = arl2::launch_rope(a, reinterpret_cast<hipStream_t>(desc->stream));
+    if (e != hipSuccess) return fail(ARL2_ERR_DEVICE, "rotation launch failed: %s", hipGetErrorString(e));
+    return ARL2_OK;
+}
+
+arl2_status arl2_rope_bwd(const arl2_rope_desc *desc, const void *q, const void *k, const void *wq, const void *wk,
+                          const int32_t *pos, const int32_t *seq_len, const void *dyq, const void *dyk,
+                          void *dq, void *dk, float *dwq, float *dwk)
+{
+    const arl2_status st = check_rope_call(desc, {dyk, dk}, wq, wk, pos, seq_len);
+    if (st != ARL2_OK) return st;
+    if (!dyq || !dq) return fail(ARL2_ERR_INVALID_ARG, "dyq and dq must not be NULL");
+    const bool norm = desc->norm != ARL2_NORM_NONE;
+    if (norm && (!q || (desc->Hk > 0 && !k))) return fail(ARL2_ERR_INVALID_ARG, "q and k must not be NULL where rows have a norm");
+    if ((dwq || dwk) && !norm) return fail(ARL2_ERR_INVALID_ARG, "rows without a norm have no weights and no gradients of weights");
+    if (dwk && desc->Hk == 0) return fail(ARL2_ERR_INVALID_ARG, "dwk must be NULL where there are no keys");
+    for (const void *p : {q, k, dyq, dyk, (const void *)dq, (const void *)dk})
+        if (!aligned16(p)) return fail(ARL2_ERR_INVALID_ARG, "rows must be 16-byte aligned");
+    if (!aligned4(dwq) || !aligned4(dwk)) return fail(ARL2_ERR_INVALID_ARG, "dwq and dwk must be 4-byte aligned");
+    const size_t need = dwq || dwk ? arl2_rope_workspace_bytes(desc) : 0;
+    if (need > 0 && (desc->workspace == nullptr || desc->workspace_bytes < need))
+        return fail(ARL2_ERR_WORKSPACE, "workspace is NULL or smaller than arl2_rope_workspace_bytes()");
+    if (!aligned16(desc->workspace)) return fail(ARL2_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    const size_t nq = rope_rows_bytes(desc, desc->H), nk = rope_rows_bytes(desc, desc->Hk), w = sizeof(float);
+    const size_t elem = elem_bytes(desc->io_dtype);
+    const Range in[] = {{norm ? q : nullptr, nq}, {norm ? k : nullptr, nk}, {wq, rope_weight_bytes(desc, desc->H)}, {wk, rope_weight_bytes(desc, desc->Hk)},
+                        {pos, rope_pos_bytes(desc)}, {seq_len, desc->B * sizeof(int32_t)}, {dyq, nq}, {dyk, nk}};
+    const Range made[] = {{dq, nq}, {dk, nk}, {dwq, rope_weight_bytes(desc, desc->H) / elem * w}, {dwk, rope_weight_bytes(desc, desc->Hk) / elem * w}, {desc->workspace, need}};
+    for (const Range &m : made) {
+        for (const Range &i : in)
+            if (overlaps(m.p, m.n, i.p, i.n) && !(m.p == dq && i.p == dyq && dq == dyq) && !(m.p == dk && i.p == dyk && dk == dyk))
+                return fail(ARL2_ERR_INVALID_ARG, "gradients and the workspace must not overlap an input (dq may be dyq, dk may be dyk)");
+        for (const Range &o : made)
+            if (&o != &m && overlaps(m.p, m.n, o.p, o.n)) return fail(ARL2_ERR_INVALID_ARG, "gradients and the workspace must not overlap each other");
+    }
+
+    arl2::RopeArgs a = rope_args(desc, q, k, wq, wk, pos, seq_len);
+    a.dy[0] = dyq; a.dy[1] = dyk; a.y[0] = dq; a.y[1] = dk; a.dw[0] = dwq; a.dw[1] = dwk; a.part = (float *)desc->workspace;
+    const hipError_t e = arl2::launch_rope_bwd(a, reinterpret_cast<hipStream_t>(desc->stream));
+    if (e != hipSuccess) return fail(ARL2_ERR_DEVICE, "rotation gradient launch failed: %s", hipGetErrorString(e));
     return ARL2_OK;
 }
 

@@ -12,6 +12,9 @@
 // are on the current device, and a letter is
 //   c  the pool, uint8 [n_pages][Hkv][page_size][bytes of a token]      b  [B][max_pages] int32
 //   x  [B][Lq][H][D] bf16     y  [B][Lq][Hkv][D] bf16    r  [max_pages page_size][D/2] fp32    i, n  [B] int32 (n or None)
+// Calls of the recurrence begin with C and take `raw_rows` in the place of sm_scale; their descriptor is arl2_scan_desc, all of their tensors are on
+// the current device, and a letter is
+//   q  [B][L][H][D] bf16 (the first names the sizes)     t  [B][L][H] fp32 or None     S  [B][H][D][D] fp32 or None     n  [B] int32 or None
 // Measured: a call of the smallest size took 7 us to issue through ctypes, of them 3.5 in the library and the runtime.
 #include <Python.h>
 #include <c10/core/impl/VirtualGuardImpl.h>
@@ -21,7 +24,7 @@
 
 namespace {
 
-constexpr int kMaxTensors = 10;
+constexpr int kMaxTensors = 13;
 
 struct Checked {
     arl2_desc d{};
@@ -129,6 +132,39 @@ bool check_kv(arl2_kv_desc &d, const char *kinds, PyObject *const *args, int n, 
     return true;
 }
 
+// The same for calls of the recurrence.
+bool check_scan(arl2_scan_desc &d, const char *kinds, PyObject *const *args, int n, const void **p)
+{
+    int64_t B = 0, L = 0, H = 0, D = 0;
+    const int device = (int)c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice().index();
+    for (int i = 0; i < n; ++i) {
+        if (args[i] == Py_None) {
+            if (kinds[i] == 'q') return false;
+            continue;
+        }
+        const at::Tensor *t = plain(args[i]);
+        if (t == nullptr || t->get_device() != device) return false;
+        if (i == 0) {
+            if (t->dim() != 4) return false;
+            for (int64_t m : t->sizes())
+                if (m > INT32_MAX) return false;
+            B = t->size(0); L = t->size(1); H = t->size(2); D = t->size(3);
+            d.B = (int32_t)B; d.L = (int32_t)L; d.H = (int32_t)H; d.D = (int32_t)D;
+        }
+        const at::ScalarType type = t->scalar_type();
+        bool ok = false;
+        switch (kinds[i]) {
+        case 'q': ok = type == at::kBFloat16 && is_shape(*t, {B, L, H, D}); break;
+        case 't': ok = type == at::kFloat && is_shape(*t, {B, L, H}); break;
+        case 'S': ok = type == at::kFloat && is_shape(*t, {B, H, D, D}); break;
+        case 'n': ok = type == at::kInt && is_shape(*t, {B}); break;
+        }
+        if (!ok) return false;
+        p[i] = t->data_ptr();
+    }
+    return true;
+}
+
 int invoke(void *f, const void *d, const void *const *p, int n)
 {
     typedef const void *P;
@@ -141,6 +177,8 @@ int invoke(void *f, const void *d, const void *const *p, int n)
     case 8: return ((int (*)(P, P, P, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]);
     case 10:
         return ((int (*)(P, P, P, P, P, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9]);
+    case 13:
+        return ((int (*)(P, P, P, P, P, P, P, P, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11], p[12]);
     }
     return -1;
 }
@@ -151,8 +189,8 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     if (nargs <= kFixed || !PyBytes_CheckExact(args[1]) || nargs - kFixed > kMaxTensors) Py_RETURN_NONE;
     const int n = (int)(nargs - kFixed);
     const char *kinds = PyBytes_AS_STRING(args[1]);
-    const bool kv = kinds[0] == 'P';
-    if (PyBytes_GET_SIZE(args[1]) != n + kv) Py_RETURN_NONE;
+    const bool kv = kinds[0] == 'P', scan = kinds[0] == 'C';
+    if (PyBytes_GET_SIZE(args[1]) != n + (kv || scan)) Py_RETURN_NONE;
     void *f = PyLong_AsVoidPtr(args[0]);
     const double sm_scale = PyFloat_AsDouble(args[2]), l2_eps = PyFloat_AsDouble(args[3]);
     void *stream = PyLong_Check(args[4]) ? PyLong_AsVoidPtr(args[4]) : nullptr;
@@ -162,18 +200,21 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     }
     Checked c;
     arl2_kv_desc kd{};
+    arl2_scan_desc sd{};
     void *workspace = nullptr;
     size_t workspace_bytes = 0;
     try {
         if (kv) {
             if (!check_kv(kd, kinds + 1, args + kFixed, n, c.p)) Py_RETURN_NONE;
+        } else if (scan) {
+            if (!check_scan(sd, kinds + 1, args + kFixed, n, c.p)) Py_RETURN_NONE;
         } else {
             for (int i = 0; i < n; ++i)
                 if (!check(c, kinds[i], args[kFixed + i], i)) Py_RETURN_NONE;
         }
         if (args[5] != Py_None) {
             const at::Tensor *w = plain(args[5]);
-            if (w == nullptr || (kv && w->get_device() != THPVariable_Unpack(args[kFixed]).get_device())) Py_RETURN_NONE;
+            if (w == nullptr || ((kv || scan) && w->get_device() != THPVariable_Unpack(args[kFixed]).get_device())) Py_RETURN_NONE;
             workspace = w->data_ptr();
             workspace_bytes = w->nbytes();
         }
@@ -187,6 +228,13 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         kd.workspace_bytes = workspace_bytes;
         kd.stream = stream;
     }
+    if (scan) {
+        sd.raw_rows = sm_scale != 0.0;
+        sd.l2_eps = (float)l2_eps;
+        sd.workspace = workspace;
+        sd.workspace_bytes = workspace_bytes;
+        sd.stream = stream;
+    }
     c.d.sm_scale = (float)sm_scale;
     c.d.l2_eps = (float)l2_eps;
     c.d.workspace = workspace;
@@ -194,7 +242,7 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     c.d.stream = stream;
     int st;
     Py_BEGIN_ALLOW_THREADS
-    st = invoke(f, kv ? (const void *)&kd : &c.d, c.p, n);
+    st = invoke(f, kv ? (const void *)&kd : scan ? (const void *)&sd : &c.d, c.p, n);
     Py_END_ALLOW_THREADS
     if (st < 0) Py_RETURN_NONE;
     return PyLong_FromLong(st);

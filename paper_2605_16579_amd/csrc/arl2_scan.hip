@@ -1,0 +1,683 @@
+// The linear branch as a causal recurrence over tokens, and its gradients (gfx950).  Per (stream, head), k' and q' the normalised rows:
+//
+//   S_t = a_t S_{t-1} + k'_t^T v_t        out_t = q'_t S_t
+//   G_t = a_{t+1} G_{t+1} + q'_t^T dout_t        dq'_t = S_t dout_t    dk'_t = G_t v_t    dv_t = G_t^T k'_t    dS0 = a_1 G_1
+//   E_t = a_t <S_{t-1}, G_t> = E_{t+1} + q'_t . dq'_t - k'_t . dk'_t,  the gradient of log a_t;    E_{L+1} = <S_L, dS>
+//
+// All four row results are one walk over blocks of 64 tokens.  With c_t the sum of log2 a over the block's tokens up to t, rows
+// X that ask, rows Y and Z that make the state, T the state that the block begins with (r_t = 2^(c_t), w_s = 2^(c_end - c_s)):
+//   row_t = r_t X_t T + sum_{s <= t} 2^(c_t - c_s) (X_t . Y_s) Z_s,        T <- 2^(c_end) T + sum_s w_s Y_s^T Z_s
+//   out: X, Y, Z = q', k', v        dq': dout, v, k', the state transposed
+//   and backwards in time (r and w change places, s >= t):    dv: k', q', dout        dk': v, dout, q', the state transposed
+#include "arl2_device.h"
+#include "arl2_scan.h"
+
+namespace arl2 {
+namespace {
+
+constexpr int kBlock = 64;                    // tokens
+constexpr int kStepTokens = 8;
+constexpr double kLog2e = 1.4426950408889634;
+
+enum Mode { kOut, kDq, kDk, kDv, kSum, kSumBack };       // the last two make states and no rows
+
+// One call's arrays in the workspace: states [B*H][nseg + 1][D][D], the way forth (state i: what segment i begins with) and back
+// (state i: the gradient of what segment i - 1 ends with), the segments' decays, and q'.dq', k'.dk' [B*H][L].
+struct Work {
+    float *forth, *back, *decay_forth, *decay_back, *qq, *kk;
+    int nseg, seg;
+};
+
+template <int D>
+struct Cfg {
+    static constexpr int NW = D / 32;                     // wavefronts, each with 32 columns of the state
+    static constexpr int NT = 64 * NW;
+    static constexpr int LPR = D / 8;                     // lanes to a row of 16-byte pieces
+    // Rows 32 bytes further than their length: four rows' 32-byte pieces of a transposing read lie in different banks, and so do
+    // eight rows' 16-byte pieces.
+    static constexpr int ROW = 2 * D + 32;
+    static constexpr int MAT = kBlock * ROW;
+    static constexpr int PROW = 2 * kBlock + 16;
+    static constexpr int PMAT = kBlock * PROW;
+};
+
+// The exponents c_t of a block as whole and fractional parts: differences of parts lose nothing, however far c runs, and a gate of
+// zero is 2^-4096 (which a block's other gates cannot bring back).
+struct Scalars {
+    float whole[2][kBlock], frac[2][kBlock], first[2][kBlock], last[2][kBlock], total[2];     // of two blocks in turn
+    float sx[kBlock], sy[kBlock], ww[kBlock];             // 1 / |X row|, 1 / |Y or Z row|, weights of the rows in the state
+    float red[4][kBlock][2];
+};
+
+__device__ __forceinline__ int tokens_of(const ScanArgs &a, int b)
+{
+    if (a.len == nullptr) return a.L;
+    return min(max(a.len[b], 0), a.L);
+}
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_add(double x)
+{
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xf, false);
+    return x + __builtin_bit_cast(double, ((unsigned long long)hi << 32) | lo);
+}
+// Sum over the lanes up to this one.
+__device__ __forceinline__ double wave_prefix(double x)
+{
+    x = dpp_add<0x111, 0xf>(x);        // row_shr 1, 2, 4, 8
+    x = dpp_add<0x112, 0xf>(x);
+    x = dpp_add<0x114, 0xf>(x);
+    x = dpp_add<0x118, 0xf>(x);
+    x = dpp_add<0x142, 0xa>(x);        // row_bcast 15 to rows 1 and 3, 31 to rows 2 and 3
+    return dpp_add<0x143, 0xc>(x);
+}
+
+__device__ __forceinline__ double log2_gate(float la)
+{
+    double x = (double)la * kLog2e;
+    x = x > 0.0 ? 0.0 : x;
+    return x < -4096.0 ? -4096.0 : x;                     // (a NaN stays one)
+}
+
+// Two fp32 values as two bf16 each, hi + lo to 2^-17 of them.
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t &hi, uint32_t &lo)
+{
+    const bf16x2 h = {to_bf16(x), to_bf16(y)};
+    hi = __builtin_bit_cast(uint32_t, h);
+    const bf16x2 l = {to_bf16(x - __uint_as_float(hi << 16)), to_bf16(y - __uint_as_float(hi & 0xffff0000u))};
+    lo = __builtin_bit_cast(uint32_t, l);
+}
+__device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mfma(u32x4 a, bf16x8 b, f32x16 c) { return mfma(__builtin_bit_cast(bf16x8, a), b, c); }
+
+template <int D, int MODE>
+struct Walk {
+    using C = Cfg<D>;
+    static constexpr bool REV = MODE == kDk || MODE == kDv || MODE == kSumBack;
+    static constexpr bool ROWS = MODE != kSum && MODE != kSumBack;
+    static constexpr bool TRANSPOSED = MODE == kDq || MODE == kDk;
+    static constexpr bool GRAD = MODE == kDq || MODE == kDk;      // the normalisation's gradient at the end
+    static constexpr bool SPLIT = MODE != kOut;                   // products of rows in two parts: their sums with q and k meet in E
+    static constexpr int LDS_ROWS = (ROWS ? 3 : 2) * C::MAT + (ROWS ? (SPLIT ? 2 : 1) * C::PMAT : 0);
+
+    // `lds`: LDS_ROWS bytes.  Segment `seg` of (stream, head) bh.
+    static __device__ __forceinline__ void run(const ScanArgs &a, const Work &wk, int bh, int seg, unsigned char *lds, Scalars &sc)
+    {
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, hh = lane >> 5;
+        const int b = bh / a.H, h = bh - b * a.H;
+        const int n = tokens_of(a, b);
+        const int nblk = (n + kBlock - 1) / kBlock;
+        const int blk0 = seg * wk.seg, blk1 = min(blk0 + wk.seg, nblk);
+        const int nact = max(1, (nblk + wk.seg - 1) / wk.seg);
+        if (seg >= nact) return;                                  // (without tokens the first segment hands its state on)
+
+        const uint32_t rs = (uint32_t)a.H * D * 2;                // bytes from token to token
+        const size_t stream = (size_t)b * a.L * rs;
+        const uint32_t range = (uint32_t)n * rs;
+        const void *px = MODE == kOut ? a.q : MODE == kDq ? a.dout : MODE == kDk ? a.v : a.k;
+        const void *py = MODE == kOut || MODE == kSum ? a.k : MODE == kDq ? a.v : MODE == kDk ? a.dout : a.q;
+        const void *pz = MODE == kOut || MODE == kSum ? a.v : MODE == kDq ? a.k : MODE == kDk ? a.q : a.dout;
+        const auto rx = make_rsrc((const char *)px + stream, range), ry = make_rsrc((const char *)py + stream, range),
+                   rz = make_rsrc((const char *)pz + stream, range);
+        const auto rla = make_rsrc(a.la + (a.la ? (size_t)b * a.L * a.H : 0), a.la ? (uint32_t)n * a.H * 4 : 0);
+
+        unsigned char *const lx = lds, *const ly = lds + (ROWS ? C::MAT : 0), *const lz = ly + C::MAT, *const lp = lz + C::MAT;
+
+        // ---- the state: 32 columns of each wavefront, register j of tile t is row 32 t + 16 (j / 8) + 8 hh + j % 8
+        f32x16 st[D / 32];
+        const int e0 = 32 * wave;
+        {
+            const float *from = nullptr;
+            if (ROWS) {
+                if (MODE == kOut) from = wk.nseg == 1 ? (a.S0 ? a.S0 + (size_t)bh * D * D : nullptr) : wk.forth + ((size_t)bh * (wk.nseg + 1) + seg) * D * D;
+                else if (MODE == kDq) from = wk.forth + ((size_t)bh * (wk.nseg + 1) + seg) * D * D;
+                else from = wk.back + ((size_t)bh * (wk.nseg + 1) + seg + 1) * D * D;
+            }
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    if (from == nullptr) { st[t][j] = 0.f; continue; }
+                    const int row = 32 * t + 16 * (j / 8) + 8 * hh + j % 8;
+                    if (TRANSPOSED) {
+                        if (j % 4 == 0) {
+                            const f32x4 x = *reinterpret_cast<const f32x4 *>(from + (size_t)(e0 + l32) * D + row);
+                            st[t][j] = x[0]; st[t][j + 1] = x[1]; st[t][j + 2] = x[2]; st[t][j + 3] = x[3];
+                        }
+                    } else st[t][j] = from[(size_t)row * D + e0 + l32];
+                }
+        }
+
+        // ---- a block's rows on their way through registers: 16-byte pieces, four of each array
+        const uint32_t piece0 = (uint32_t)(tid / C::LPR) * rs + (uint32_t)h * D * 2 + (tid % C::LPR) * 16;
+        u32x4 gx[4], gy[4], gz[4];
+        float gla;
+        auto fetch = [&](int blk) {
+            const uint32_t o = piece0 + (uint32_t)blk * kBlock * rs;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (ROWS) gx[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, o + 16u * i * rs, 0, 0));
+                gy[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ry, o + 16u * i * rs, 0, 0));
+                gz[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rz, o + 16u * i * rs, 0, 0));
+            }
+        };
+        auto fetch_gate = [&](int blk) {
+            gla = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rla, ((uint32_t)(blk * kBlock + lane) * a.H + h) * 4u, 0, 0));
+        };
+        double seg_total = 0.0;                                   // (wavefront 0)
+        auto gates = [&](int buf) {
+            const double c = wave_prefix(log2_gate(gla));
+            const double tot = __builtin_bit_cast(double, ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(__builtin_bit_cast(unsigned long long, c) >> 32), 63) << 32) |
+                                                           (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)__builtin_bit_cast(unsigned long long, c), 63));
+            const double w = __builtin_floor(c);
+            sc.whole[buf][lane] = (float)w;
+            sc.frac[buf][lane] = (float)(c - w);
+            const float up = __builtin_amdgcn_exp2f((float)c), down = __builtin_amdgcn_exp2f((float)(tot - c));
+            sc.first[buf][lane] = REV ? down : up;
+            sc.last[buf][lane] = REV ? up : down;
+            if (lane == 63) sc.total[buf] = up;
+            seg_total += tot;
+        };
+        auto stage = [&](const u32x4 *g, unsigned char *to, float *inverse) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = 16 * i + tid / C::LPR;
+                *reinterpret_cast<u32x4 *>(to + row * C::ROW + (tid % C::LPR) * 16) = g[i];
+                if (inverse != nullptr) {
+                    float s = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float x = __uint_as_float(g[i][j] << 16), y = __uint_as_float(g[i][j] & 0xffff0000u);
+                        s += x * x + y * y;
+                    }
+                    s = lane_group_sum<C::LPR>(s);
+                    if (tid % C::LPR == 0) inverse[row] = a.normalise ? fast_rsqrt(s + a.eps) : 1.f;
+                }
+            }
+        };
+
+        const int count = blk1 - blk0;
+        auto block_at = [&](int i) { return REV ? blk1 - 1 - i : blk0 + i; };
+        if (count > 0) {
+            fetch(block_at(0));
+            fetch_gate(block_at(0));
+            if (wave == 0) gates(0);
+            if (count > 1) fetch_gate(block_at(1));
+        }
+        for (int i = 0; i < count; ++i) {
+            const int blk = block_at(i), buf = i & 1;
+            if (ROWS) stage(gx, lx, MODE == kOut || MODE == kDv ? sc.sx : nullptr);
+            stage(gy, ly, MODE == kDq || MODE == kDk ? nullptr : sc.sy);
+            stage(gz, lz, MODE == kDq || MODE == kDk ? sc.sy : nullptr);
+            if (i + 1 < count) fetch(block_at(i + 1));
+            lds_barrier();
+
+            // ---- X.Y of 32 x 32 rows, times their decays, as rows of X in LDS
+            if constexpr (ROWS) {
+                for (int t = wave; t < 3; t += C::NW) {
+                    const int sb = REV ? (t > 0) : (t == 2), tb = REV ? (t == 2) : (t > 0);
+                    f32x16 p = {};
+                    const unsigned char *const y = ly + (32 * sb + l32) * C::ROW + 16 * hh, *const x = lx + (32 * tb + l32) * C::ROW + 16 * hh;
+#pragma unroll
+                    for (int m = 0; m < D / 16; ++m)
+                        p = mfma(*reinterpret_cast<const bf16x8 *>(y + 32 * m), *reinterpret_cast<const bf16x8 *>(x + 32 * m), p);
+                    const float wt = sc.whole[buf][32 * tb + l32], ft = sc.frac[buf][32 * tb + l32];
+                    unsigned char *const to = lp + (32 * tb + l32) * C::PROW + 64 * sb;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        const int s0 = 8 * g + 4 * hh;            // in the 32
+                        const f32x4 ws = *reinterpret_cast<const f32x4 *>(&sc.whole[buf][32 * sb + s0]), fs = *reinterpret_cast<const f32x4 *>(&sc.frac[buf][32 * sb + s0]),
+                                    ys = *reinterpret_cast<const f32x4 *>(&sc.sy[32 * sb + s0]);
+                        float v[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float d = REV ? (ws[j] - wt) + (fs[j] - ft) : (wt - ws[j]) + (ft - fs[j]);
+                            const bool seen = sb != tb || (REV ? s0 + j >= l32 : s0 + j <= l32);
+                            v[j] = seen ? p[4 * g + j] * ys[j] * __builtin_amdgcn_exp2f(d) : 0.f;
+                        }
+                        u32x2 hi, lo;
+                        if constexpr (SPLIT) {
+                            uint32_t h0, l0, h1, l1;
+                            split_pair(v[0], v[1], h0, l0);
+                            split_pair(v[2], v[3], h1, l1);
+                            hi = u32x2{h0, h1};
+                            lo = u32x2{l0, l1};
+                            *reinterpret_cast<u32x2 *>(to + C::PMAT + 2 * s0) = lo;
+                        } else {
+                            const bf16x4 r = {to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]), to_bf16(v[3])};
+                            hi = __builtin_bit_cast(u32x2, r);
+                        }
+                        *reinterpret_cast<u32x2 *>(to + 2 * s0) = hi;
+                    }
+                }
+            }
+            if (wave == C::NW - 1) sc.ww[lane] = sc.last[buf][lane] * sc.sy[lane];
+            if (i + 1 < count && wave == 0) gates(buf ^ 1);
+            if (i + 2 < count) fetch_gate(block_at(i + 2));
+            lds_barrier();
+
+            // Z^T of the wavefront's columns, 16 tokens each: operand of both products below
+            bf16x8 zf[4];
+            {
+                const int r = lane & 15;
+                const unsigned char *const z = lz + (8 * hh + (r >> 2)) * C::ROW + 2 * (e0 + 16 * ((lane >> 4) & 1) + 4 * (r & 3));
+#pragma unroll
+                for (int m = 0; m < 4; ++m) zf[m] = lds_read_tr_pair(z + 16 * m * C::ROW, 4 * C::ROW);
+            }
+            f32x16 acc[2];
+            u32x2 own[2][4];                                      // the rows whose normalisation has a gradient
+            __amdgpu_buffer_rsrc_t rg;
+            if constexpr (ROWS) {
+                acc[0] = acc[1] = f32x16{};
+                if constexpr (GRAD) {
+                    rg = make_rsrc((const char *)(MODE == kDq ? a.q : a.k) + stream, range);
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g)
+                            own[tb][g] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rg, (uint32_t)(blk * kBlock + 32 * tb + l32) * rs + (h * D + e0 + 8 * g + 4 * hh) * 2, 0, 0));
+                }
+                // ---- rows asked of the state, which is taken in two parts
+                const unsigned char *const x = lx + l32 * C::ROW + 16 * hh;
+#pragma unroll
+                for (int m = 0; m < D / 16; ++m) {
+                    u32x4 hi, lo;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t hj, lj;
+                        split_pair(st[m / 2][8 * (m % 2) + 2 * j], st[m / 2][8 * (m % 2) + 2 * j + 1], hj, lj);
+                        hi[j] = hj; lo[j] = lj;
+                    }
+                    const bf16x8 x0 = *reinterpret_cast<const bf16x8 *>(x + 32 * m), x1 = *reinterpret_cast<const bf16x8 *>(x + 32 * C::ROW + 32 * m);
+                    acc[0] = mfma(hi, x0, acc[0]);
+                    acc[1] = mfma(hi, x1, acc[1]);
+                    acc[0] = mfma(lo, x0, acc[0]);
+                    acc[1] = mfma(lo, x1, acc[1]);
+                }
+                const float f0 = sc.first[buf][l32], f1 = sc.first[buf][32 + l32];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) { acc[0][j] *= f0; acc[1][j] *= f1; }
+                // ---- and of the block's own rows
+                const unsigned char *const p = lp + l32 * C::PROW + 16 * hh;
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+                    for (int m = REV ? 2 * tb : 0; m < (REV ? 4 : 2 + 2 * tb); ++m) {
+                        acc[tb] = mfma(zf[m], *reinterpret_cast<const bf16x8 *>(p + 32 * tb * C::PROW + 32 * m), acc[tb]);
+                        if constexpr (SPLIT) acc[tb] = mfma(zf[m], *reinterpret_cast<const bf16x8 *>(p + C::PMAT + 32 * tb * C::PROW + 32 * m), acc[tb]);
+                    }
+            }
+
+            // ---- the state's step: rows of Z times their weights in two parts
+            const float total = sc.total[buf];
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) st[t][j] *= total;
+            {
+                const int r = lane & 15, piece = ((r & 1) << 1) | ((r >> 1) & 1);       // pieces 1 and 2 of four change places: rows of the
+                // accumulator are then features 8 hh + j as the operand of the state's product wants them
+                const unsigned char *const y = ly + (8 * hh + (r >> 2)) * C::ROW + 2 * (16 * ((lane >> 4) & 1) + 4 * piece);
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    const f32x4 w0 = *reinterpret_cast<const f32x4 *>(&sc.ww[16 * m + 8 * hh]), w1 = *reinterpret_cast<const f32x4 *>(&sc.ww[16 * m + 8 * hh + 4]);
+                    const u32x4 zb = __builtin_bit_cast(u32x4, zf[m]);
+                    u32x4 hi, lo;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t hj, lj;
+                        split_pair(__uint_as_float(zb[j] << 16) * (j < 2 ? w0[2 * j] : w1[2 * j - 4]), __uint_as_float(zb[j] & 0xffff0000u) * (j < 2 ? w0[2 * j + 1] : w1[2 * j - 3]), hj, lj);
+                        hi[j] = hj; lo[j] = lj;
+                    }
+#pragma unroll
+                    for (int t = 0; t < D / 32; ++t) {
+                        const bf16x8 yf = lds_read_tr_pair(y + 16 * m * C::ROW + 64 * t, 4 * C::ROW);
+                        st[t] = mfma(yf, __builtin_bit_cast(bf16x8, hi), st[t]);
+                        st[t] = mfma(yf, __builtin_bit_cast(bf16x8, lo), st[t]);
+                    }
+                }
+            }
+
+            // ---- rows out
+            if constexpr (ROWS) {
+                float scale[2], along[2];
+                if constexpr (GRAD) {
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb) {
+                        float dot = 0.f, ss = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const uint32_t w = own[tb][j / 4][(j / 2) % 2];
+                            const float r = __uint_as_float(j % 2 ? w & 0xffff0000u : w << 16);
+                            dot = fmaf(r, acc[tb][j], dot);
+                            ss = fmaf(r, r, ss);
+                        }
+                        dot = xhalf_sum(dot);
+                        ss = xhalf_sum(ss);
+                        if (hh == 0) { sc.red[wave][32 * tb + l32][0] = dot; sc.red[wave][32 * tb + l32][1] = ss; }
+                    }
+                    lds_barrier();
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb) {
+                        float dot = 0.f, ss = 0.f;
+#pragma unroll
+                        for (int w = 0; w < C::NW; ++w) { dot += sc.red[w][32 * tb + l32][0]; ss += sc.red[w][32 * tb + l32][1]; }
+                        const float inv = a.normalise ? fast_rsqrt(ss + a.eps) : 1.f;
+                        dot *= inv;
+                        scale[tb] = inv;
+                        along[tb] = a.normalise ? -dot * inv * inv : 0.f;
+                        const int t = blk * kBlock + 32 * tb + l32;
+                        if (wave == 0 && hh == 0 && t < n && a.dla != nullptr) (MODE == kDq ? wk.qq : wk.kk)[(size_t)bh * a.L + t] = dot;
+                    }
+                } else {
+                    scale[0] = sc.sx[l32];
+                    scale[1] = sc.sx[32 + l32];
+                    lds_barrier();                                // all have read the block's rows
+                }
+                void *const po = MODE == kOut ? a.out : MODE == kDq ? a.dq : MODE == kDk ? a.dk : a.dv;
+                const auto ro = make_rsrc((const char *)po + stream, range);
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb) {
+                    uint32_t w[4][2];
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            float x0 = acc[tb][4 * g + 2 * j] * scale[tb], x1 = acc[tb][4 * g + 2 * j + 1] * scale[tb];
+                            if constexpr (GRAD) {
+                                x0 = fmaf(along[tb], __uint_as_float(own[tb][g][j] << 16), x0);
+                                x1 = fmaf(along[tb], __uint_as_float(own[tb][g][j] & 0xffff0000u), x1);
+                            }
+                            const bf16x2 r = {to_bf16(x0), to_bf16(x1)};
+                            w[g][j] = __builtin_bit_cast(uint32_t, r);
+                        }
+                    // 16 bytes of a row together: the half-waves hold 8 bytes each of four pieces
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        const auto s0 = __builtin_amdgcn_permlane32_swap(w[g][0], w[g + 2][0], false, false);
+                        const auto s1 = __builtin_amdgcn_permlane32_swap(w[g][1], w[g + 2][1], false, false);
+                        const u32x4 v = {s0[0], s1[0], s0[1], s1[1]};
+                        __builtin_amdgcn_raw_buffer_store_b128(v, ro, (uint32_t)(blk * kBlock + 32 * tb + l32) * rs + (h * D + e0 + 16 * hh + 8 * g) * 2, 0, 0);
+                    }
+                }
+            } else lds_barrier();
+        }
+
+        // ---- the state at the end
+        float *to = nullptr;
+        if (MODE == kOut) to = seg == nact - 1 && a.S != nullptr ? a.S + (size_t)bh * D * D : nullptr;
+        if (MODE == kSum) to = wk.forth + ((size_t)bh * (wk.nseg + 1) + seg + 1) * D * D;
+        if (MODE == kSumBack) to = wk.back + ((size_t)bh * (wk.nseg + 1) + seg) * D * D;
+        if (to != nullptr)
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) to[(size_t)(32 * t + 16 * (j / 8) + 8 * hh + j % 8) * D + e0 + l32] = st[t][j];
+        if (!ROWS && tid == 0) (MODE == kSum ? wk.decay_forth : wk.decay_back)[(size_t)bh * wk.nseg + seg] = (float)::exp2(fmax(seg_total, -4096.0));
+    }
+};
+
+template <int D>
+__global__ __launch_bounds__(Cfg<D>::NT, 2) void scan_out_kernel(ScanArgs a, Work wk)
+{
+    using W = Walk<D, kOut>;
+    __shared__ __align__(16) unsigned char lds[W::LDS_ROWS];
+    __shared__ __align__(16) Scalars sc;
+    const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
+    W::run(a, wk, id / wk.nseg, id % wk.nseg, lds, sc);
+}
+
+// Segments' own states.  `back`: the way back too, as every second workgroup; the last segment of the way forth and the first of
+// the way back only where something reads them.
+template <int D>
+__global__ __launch_bounds__(Cfg<D>::NT, 2) void scan_sum_kernel(ScanArgs a, Work wk, int back, int need_last, int need_first)
+{
+    __shared__ __align__(16) unsigned char lds[Walk<D, kSum>::LDS_ROWS];
+    __shared__ __align__(16) Scalars sc;
+    const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
+    const int unit = back ? id >> 1 : id;
+    const int bh = unit / wk.nseg, seg = unit % wk.nseg;
+    const int blocks = (tokens_of(a, bh / a.H) + kBlock - 1) / kBlock, nact = max(1, (blocks + wk.seg - 1) / wk.seg);
+    if (back && (id & 1)) {
+        if (seg > 0 || need_first) Walk<D, kSumBack>::run(a, wk, bh, seg, lds, sc);
+    } else if (seg < nact - 1 || need_last) Walk<D, kSum>::run(a, wk, bh, seg, lds, sc);
+}
+
+// States at the segments' borders from the segments' own: each its decay times the one before, plus its own.
+__global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, Work wk, int need_last, int need_first)
+{
+    const int nn = a.D * a.D, per = nn / 1024, unit = blockIdx.x / per;
+    const int e = ((blockIdx.x - unit * per) * 256 + threadIdx.x) * 4;
+    const bool back = unit >= a.B * a.H;
+    const int bh = back ? unit - a.B * a.H : unit;
+    const int blocks = (tokens_of(a, bh / a.H) + kBlock - 1) / kBlock, nact = max(1, (blocks + wk.seg - 1) / wk.seg);
+    float *const base = (back ? wk.back : wk.forth) + (size_t)bh * (wk.nseg + 1) * nn + e;
+    const float *const decay = (back ? wk.decay_back : wk.decay_forth) + (size_t)bh * wk.nseg;
+    const float *const start = back ? a.dS : a.S0;
+    f32x4 x = {};
+    if (start != nullptr) x = *reinterpret_cast<const f32x4 *>(start + (size_t)bh * nn + e);
+    *reinterpret_cast<f32x4 *>(base + (size_t)(back ? nact : 0) * nn) = x;
+    const int steps = back ? nact - 1 + need_first : nact - 1 + need_last;
+    for (int i = 0; i < steps; ++i) {
+        const int seg = back ? nact - 1 - i : i;
+        float *const at = base + (size_t)(back ? seg : seg + 1) * nn;
+        const f32x4 own = *reinterpret_cast<const f32x4 *>(at);
+        const float d = decay[seg];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = fmaf(d, x[j], own[j]);
+        *reinterpret_cast<f32x4 *>(at) = x;
+    }
+    if (back && a.dS0 != nullptr) *reinterpret_cast<f32x4 *>(a.dS0 + (size_t)bh * nn + e) = x;
+}
+
+// The rows' gradients: three walks of a segment by three workgroups that follow one another.
+template <int D>
+__global__ __launch_bounds__(Cfg<D>::NT, 2) void scan_grad_kernel(ScanArgs a, Work wk)
+{
+    __shared__ __align__(16) unsigned char lds[Walk<D, kDq>::LDS_ROWS];
+    __shared__ __align__(16) Scalars sc;
+    const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
+    const int unit = id / 3, which = id - 3 * unit;
+    const int bh = unit / wk.nseg, seg = unit % wk.nseg;
+    if (which == 0) Walk<D, kDq>::run(a, wk, bh, seg, lds, sc);
+    else if (which == 1) Walk<D, kDk>::run(a, wk, bh, seg, lds, sc);
+    else Walk<D, kDv>::run(a, wk, bh, seg, lds, sc);
+}
+
+// The gates' gradients of a segment: from <state, gradient of the state> at its end backwards, a sum of q'.dq' - k'.dk' that a gate of
+// zero begins anew.
+__global__ __launch_bounds__(256) void scan_gate_kernel(ScanArgs a, Work wk)
+{
+    __shared__ double part[4];
+    const int bh = blockIdx.x / wk.nseg, seg = blockIdx.x % wk.nseg, b = bh / a.H, h = bh - b * a.H;
+    const int tid = threadIdx.x, lane = tid & 63, nn = a.D * a.D;
+    const int n = tokens_of(a, b), blocks = (n + kBlock - 1) / kBlock, nact = max(1, (blocks + wk.seg - 1) / wk.seg);
+    const int t0 = seg * wk.seg * kBlock, t1 = min(n, t0 + wk.seg * kBlock);
+    if (t0 >= t1) return;
+    double dot = 0.0;
+    if (seg < nact - 1 || a.dS != nullptr) {
+        const size_t at = ((size_t)bh * (wk.nseg + 1) + seg + 1) * nn;
+        for (int e = tid * 4; e < nn; e += 1024) {
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(wk.forth + at + e), y = *reinterpret_cast<const f32x4 *>(wk.back + at + e);
+            dot += (double)x[0] * y[0] + (double)x[1] * y[1] + (double)x[2] * y[2] + (double)x[3] * y[3];
+        }
+    }
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) dot += __shfl_xor(dot, m, kWave);
+    if (lane == 0) part[tid >> 6] = dot;
+    __syncthreads();
+    if (tid >= 64) return;
+    double carry = part[0] + part[1] + part[2] + part[3];
+    for (int t = t0 + (t1 - 1 - t0) / 64 * 64; t >= t0; t -= 64) {
+        const int i = t + 63 - lane;                              // later tokens in lower lanes
+        double v = 0.0;
+        int cut = 0;
+        if (i < t1) {
+            v = (double)wk.qq[(size_t)bh * a.L + i] - (double)wk.kk[(size_t)bh * a.L + i];
+            cut = a.la != nullptr && a.la[((size_t)b * a.L + i) * a.H + h] < -2839.2f;
+            if (cut) v = 0.0;
+        }
+        for (int m = 1; m < 64; m <<= 1) {
+            const double u = __shfl_up(v, m, kWave);
+            const int c = __shfl_up(cut, m, kWave);
+            if (lane >= m) {
+                if (!cut) v += u;
+                cut |= c;
+            }
+        }
+        if (!cut) v += carry;
+        if (i < t1) a.dla[((size_t)b * a.L + i) * a.H + h] = (float)v;
+        carry = __shfl(v, 63, kWave);
+    }
+}
+
+// ---- few tokens: the state once in and out, by elements; 32 columns to a workgroup, 8 lanes to a row of them
+template <int D>
+__global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a)
+{
+    constexpr int RPT = D / 32;                                   // rows per thread
+    __shared__ __align__(16) float sq[kStepTokens][D], sk[kStepTokens][D], sv[kStepTokens][32];
+    __shared__ float gate[kStepTokens];
+    __shared__ __align__(16) float part[kStepTokens][4][32];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int e0 = 32 * (blockIdx.x % (D / 32)), bh = blockIdx.x / (D / 32), b = bh / a.H, h = bh - b * a.H;
+    const int n = tokens_of(a, b);
+    const int c4 = 4 * (tid & 7), r0 = tid >> 3;
+    const size_t at = (size_t)bh * D * D + (size_t)r0 * D + e0 + c4;
+    f32x4 st[RPT];
+#pragma unroll
+    for (int i = 0; i < RPT; ++i) st[i] = a.S0 != nullptr ? *reinterpret_cast<const f32x4 *>(a.S0 + at + (size_t)32 * i * D) : f32x4{};
+    // one wavefront to a row of q or k
+    for (int r = wave; r < 2 * n; r += 4) {
+        const int t = r >> 1;
+        const bf16_t *const src = (const bf16_t *)(r & 1 ? a.k : a.q) + (((size_t)b * a.L + t) * a.H + h) * D;
+        const float x0 = lane < D / 2 ? (float)src[2 * lane] : 0.f, x1 = lane < D / 2 ? (float)src[2 * lane + 1] : 0.f;
+        float s = x0 * x0 + x1 * x1;
+#pragma unroll
+        for (int m = 32; m > 0; m >>= 1) s += __shfl_xor(s, m, kWave);
+        const float inv = a.normalise ? fast_rsqrt(s + a.eps) : 1.f;
+        if (lane < D / 2) *reinterpret_cast<f32x2 *>(&(r & 1 ? sk : sq)[t][2 * lane]) = f32x2{x0 * inv, x1 * inv};
+    }
+    if (tid < 32 * n) sv[tid >> 5][tid & 31] = (float)((const bf16_t *)a.v)[(((size_t)b * a.L + (tid >> 5)) * a.H + h) * D + e0 + (tid & 31)];
+    if (tid < n) gate[tid] = a.la == nullptr ? 1.f : (float)::exp2(log2_gate(a.la[((size_t)b * a.L + tid) * a.H + h]));
+    __syncthreads();
+    for (int t = 0; t < n; ++t) {
+        const float g = gate[t];
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(&sv[t][c4]);
+        f32x4 o = {};
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+            const float k = sk[t][r0 + 32 * i], q = sq[t][r0 + 32 * i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                st[i][j] = fmaf(k, v[j], g * st[i][j]);
+                o[j] = fmaf(q, st[i][j], o[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int m = 8; m < 64; m <<= 1) o[j] += __shfl_xor(o[j], m, kWave);
+        if (lane < 8) *reinterpret_cast<f32x4 *>(&part[t][wave][c4]) = o;
+    }
+    if (a.S != nullptr)
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) *reinterpret_cast<f32x4 *>(a.S + at + (size_t)32 * i * D) = st[i];
+    __syncthreads();
+    if (tid < 32 * n) {
+        const int t = tid >> 5, e = tid & 31;
+        const float o = (part[t][0][e] + part[t][1][e]) + (part[t][2][e] + part[t][3][e]);
+        ((bf16_t *)a.out)[(((size_t)b * a.L + t) * a.H + h) * D + e0 + e] = to_bf16(o);
+    }
+}
+
+Work work_of(const ScanArgs &a, const ScanPlan &p)
+{
+    char *const w = (char *)a.workspace;
+    const size_t decays = (size_t)a.B * a.H * p.nseg, rows = (size_t)a.B * a.H * a.L;
+    Work wk;
+    wk.forth = (float *)w;
+    wk.back = (float *)(w + p.back);
+    wk.decay_forth = (float *)(w + p.decay);
+    wk.decay_back = wk.decay_forth + decays;
+    wk.qq = (float *)(w + p.dots);
+    wk.kk = wk.qq + rows;
+    wk.nseg = p.nseg;
+    wk.seg = p.seg;
+    return wk;
+}
+
+template <int D>
+hipError_t launch_fwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
+{
+    const int bh = a.B * a.H;
+    if (p.step) return launch_kernel(scan_step_kernel<D>, dim3(bh * (D / 32)), dim3(256), stream, a);
+    const Work wk = work_of(a, p);
+    if (p.nseg > 1) {
+        hipError_t e = launch_kernel(scan_sum_kernel<D>, dim3(bh * p.nseg), dim3(Cfg<D>::NT), stream, a, wk, 0, 0, 0);
+        if (e != hipSuccess) return e;
+        e = launch_kernel(scan_join_kernel, dim3(bh * (D * D / 1024)), dim3(256), stream, a, wk, 0, 0);
+        if (e != hipSuccess) return e;
+    }
+    return launch_kernel(scan_out_kernel<D>, dim3(bh * p.nseg), dim3(Cfg<D>::NT), stream, a, wk);
+}
+
+template <int D>
+hipError_t launch_bwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
+{
+    const int bh = a.B * a.H, last = a.dS != nullptr, first = a.dS0 != nullptr;
+    const Work wk = work_of(a, p);
+    hipError_t e = launch_kernel(scan_sum_kernel<D>, dim3(2 * bh * p.nseg), dim3(Cfg<D>::NT), stream, a, wk, 1, last, first);
+    if (e != hipSuccess) return e;
+    e = launch_kernel(scan_join_kernel, dim3(2 * bh * (D * D / 1024)), dim3(256), stream, a, wk, last, first);
+    if (e != hipSuccess) return e;
+    e = launch_kernel(scan_grad_kernel<D>, dim3(3 * bh * p.nseg), dim3(Cfg<D>::NT), stream, a, wk);
+    if (e != hipSuccess || a.dla == nullptr) return e;
+    return launch_kernel(scan_gate_kernel, dim3(bh * p.nseg), dim3(256), stream, a, wk);
+}
+
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+}  // namespace
+
+ScanPlan scan_plan(int B, int H, int L, int D, bool backward)
+{
+    ScanPlan p = {};
+    const int bh = B * H, blocks = (L + kBlock - 1) / kBlock;
+    if (!backward && L <= kStepTokens) {
+        p.step = 1;
+        p.nseg = 1;
+        return p;
+    }
+    // two workgroups a CU
+    int nseg = 2 * kNumCu / bh;
+    nseg = nseg < 1 ? 1 : nseg > blocks ? blocks : nseg;
+    p.seg = (blocks + nseg - 1) / nseg;
+    if (backward && p.seg > 16) p.seg = 16;
+    p.nseg = (blocks + p.seg - 1) / p.seg;
+    const size_t states = align256((size_t)bh * (p.nseg + 1) * D * D * sizeof(float));
+    if (backward) {
+        p.back = states;
+        p.decay = 2 * states;
+        p.dots = p.decay + align256((size_t)2 * bh * p.nseg * sizeof(float));
+        p.bytes = p.dots + align256((size_t)2 * bh * L * sizeof(float));
+    } else if (p.nseg > 1) {
+        p.back = p.decay = states;
+        p.bytes = p.dots = p.decay + align256((size_t)2 * bh * p.nseg * sizeof(float));
+    }
+    return p;
+}
+
+hipError_t launch_scan_fwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
+{
+    return a.D == 128 ? launch_fwd<128>(a, p, stream) : launch_fwd<64>(a, p, stream);
+}
+
+hipError_t launch_scan_bwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
+{
+    return a.D == 128 ? launch_bwd<128>(a, p, stream) : launch_bwd<64>(a, p, stream);
+}
+
+}  // namespace arl2
