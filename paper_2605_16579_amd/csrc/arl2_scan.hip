@@ -5,10 +5,13 @@
 //   E_t = a_t <S_{t-1}, G_t> = E_{t+1} + q'_t . dq'_t - k'_t . dk'_t,  the gradient of log a_t;    E_{L+1} = <S_L, dS>
 //
 // All four row results are one walk over blocks of 64 tokens.  With c_t the sum of log2 a over the block's tokens up to t, rows
-// X that ask, rows Y and Z that make the state, T the state that the block begins with (r_t = 2^(c_t), w_s = 2^(c_end - c_s)):
-//   row_t = r_t X_t T + sum_{s <= t} 2^(c_t - c_s) (X_t . Y_s) Z_s,        T <- 2^(c_end) T + sum_s w_s Y_s^T Z_s
+// X that ask, rows Y and Z that make the state, T the state that the block begins with, r_t = 2^(c_t):
+//   row_t = r_t (X_t T + sum_{s <= t} (X_t . Y_s) Z_s / r_s),        T <- 2^(c_end) (T + sum_s Y_s^T Z_s / r_s)
 //   out: X, Y, Z = q', k', v        dq': dout, v, k', the state transposed
-//   and backwards in time (r and w change places, s >= t):    dv: k', q', dout        dk': v, dout, q', the state transposed
+//   and backwards in time (r_t = 2^(c_end - c_t), s >= t):    dv: k', q', dout        dk': v, dout, q', the state transposed
+// The state is held without the factor 2^(base + c_end) that its blocks so far have gathered: c counts on from block to block (as `base`), and
+// only where it has run below -32 is the state multiplied by it, and c begins anew.  Where it runs below -64 in a block (gates of zero among
+// them) 1 / r_s would leave the range: such a block's products take their decays 2^(c_t - c_s) pair by pair.
 #include "arl2_device.h"
 #include "arl2_scan.h"
 
@@ -41,11 +44,17 @@ struct Cfg {
     static constexpr int PMAT = kBlock * PROW;
 };
 
-// The exponents c_t of a block as whole and fractional parts: differences of parts lose nothing, however far c runs, and a gate of
-// zero is 2^-4096 (which a block's other gates cannot bring back).
+// What a block's tokens are multiplied with.  Exponents are taken apart into whole and fractional parts, whose differences lose nothing however
+// far c runs; a gate of zero is 2^-4096 (which a block's other gates cannot bring back).
+constexpr float kFold = -32.f, kPairs = -64.f;
 struct Scalars {
-    float whole[2][kBlock], frac[2][kBlock], first[2][kBlock], last[2][kBlock], total[2];     // of two blocks in turn
-    float sx[kBlock], sy[kBlock], ww[kBlock];             // 1 / |X row|, 1 / |Y or Z row|, weights of the rows in the state
+    // by the gates alone, of two blocks in turn
+    float whole[2][kBlock], frac[2][kBlock];              // c_t
+    float row[2][kBlock], col[2][kBlock], enter[2][kBlock];     // r_t, 1 / r_s, and what rows enter the state with
+    float fold[2];                                        // what the state is multiplied with before they do; 1: it is left
+    int pairs[2];                                         // products take their decays pair by pair
+    // with the norms of the rows
+    float post[kBlock], pcol[kBlock], penter[kBlock], norm[kBlock];
     float red[4][kBlock][2];
 };
 
@@ -79,6 +88,14 @@ __device__ __forceinline__ double log2_gate(float la)
     double x = (double)la * kLog2e;
     x = x > 0.0 ? 0.0 : x;
     return x < -4096.0 ? -4096.0 : x;                     // (a NaN stays one)
+}
+
+// 2^x, with the fraction's exponential scaled by the whole part: fp32's own precision whatever the size of x.
+__device__ __forceinline__ float exp2_of(double x)
+{
+    const double w = __builtin_floor(fmax(x, -4096.0));
+    const float f = __builtin_amdgcn_exp2f((float)(x - w));
+    return x < -4096.0 ? 0.f : __builtin_ldexpf(f, (int)w);
 }
 
 // Two fp32 values as two bf16 each, hi + lo to 2^-17 of them.
@@ -166,99 +183,74 @@ struct Walk {
         auto fetch_gate = [&](int blk) {
             gla = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rla, ((uint32_t)(blk * kBlock + lane) * a.H + h) * 4u, 0, 0));
         };
-        double seg_total = 0.0;                                   // (wavefront 0)
+        double seg_total = 0.0, base = 0.0;                       // (of the wavefront that does this; base is whole)
         auto gates = [&](int buf) {
             const double c = wave_prefix(log2_gate(gla));
-            const double tot = __builtin_bit_cast(double, ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(__builtin_bit_cast(unsigned long long, c) >> 32), 63) << 32) |
-                                                           (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)__builtin_bit_cast(unsigned long long, c), 63));
-            const double w = __builtin_floor(c);
-            sc.whole[buf][lane] = (float)w;
-            sc.frac[buf][lane] = (float)(c - w);
-            const float up = __builtin_amdgcn_exp2f((float)c), down = __builtin_amdgcn_exp2f((float)(tot - c));
-            sc.first[buf][lane] = REV ? down : up;
-            sc.last[buf][lane] = REV ? up : down;
-            if (lane == 63) sc.total[buf] = up;
+            const unsigned long long u = __builtin_bit_cast(unsigned long long, c);
+            const double tot = __builtin_bit_cast(double, ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(u >> 32), 63) << 32) |
+                                                           (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 63));
+            const double r = base + (REV ? tot - c : c), end = base + tot;
+            const bool fold = !(end >= kFold), pairs = !(end >= kPairs);
+            sc.whole[buf][lane] = (float)__builtin_floor(c);
+            sc.frac[buf][lane] = (float)(c - __builtin_floor(c));
+            sc.row[buf][lane] = exp2_of(r);
+            const float col = pairs ? 0.f : exp2_of(-r);
+            sc.col[buf][lane] = col;
+            sc.enter[buf][lane] = fold ? exp2_of(REV ? c : tot - c) : col;
+            if (lane == 0) {
+                sc.fold[buf] = fold ? exp2_of(end) : 1.f;
+                sc.pairs[buf] = pairs;
+            }
+            base = fold ? 0.0 : end;
             seg_total += tot;
         };
-        auto stage = [&](const u32x4 *g, unsigned char *to, float *inverse) {
+        // rows of one array to LDS; `kind` 1: its norms go with the rows that ask, 2: with those that make the state
+        auto stage = [&](const u32x4 *g, unsigned char *to, int kind, int buf) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int row = 16 * i + tid / C::LPR;
                 *reinterpret_cast<u32x4 *>(to + row * C::ROW + (tid % C::LPR) * 16) = g[i];
-                if (inverse != nullptr) {
-                    float s = 0.f;
+                if (kind) {
+                    float x = 0.f;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float x = __uint_as_float(g[i][j] << 16), y = __uint_as_float(g[i][j] & 0xffff0000u);
-                        s += x * x + y * y;
+                        const float x0 = __uint_as_float(g[i][j] << 16), x1 = __uint_as_float(g[i][j] & 0xffff0000u);
+                        x = fmaf(x0, x0, fmaf(x1, x1, x));
                     }
-                    s = lane_group_sum<C::LPR>(s);
-                    if (tid % C::LPR == 0) inverse[row] = a.normalise ? fast_rsqrt(s + a.eps) : 1.f;
+                    x = lane_group_sum<C::LPR>(x);
+                    x = a.normalise ? fast_rsqrt(x + a.eps) : 1.f;
+                    if (tid % C::LPR == 0) {
+                        if (kind == 1) sc.post[row] = sc.pairs[buf] ? x : x * sc.row[buf][row];
+                        else {
+                            sc.pcol[row] = x * sc.col[buf][row];
+                            sc.penter[row] = x * sc.enter[buf][row];
+                            sc.norm[row] = x;
+                        }
+                    }
                 }
             }
         };
 
         const int count = blk1 - blk0;
         auto block_at = [&](int i) { return REV ? blk1 - 1 - i : blk0 + i; };
+        constexpr int GW = C::NW - 1;                             // the wavefront with the gates: it has fewest products
         if (count > 0) {
             fetch(block_at(0));
             fetch_gate(block_at(0));
-            if (wave == 0) gates(0);
+            if (wave == GW) gates(0);
             if (count > 1) fetch_gate(block_at(1));
+            lds_barrier();
         }
         for (int i = 0; i < count; ++i) {
             const int blk = block_at(i), buf = i & 1;
-            if (ROWS) stage(gx, lx, MODE == kOut || MODE == kDv ? sc.sx : nullptr);
-            stage(gy, ly, MODE == kDq || MODE == kDk ? nullptr : sc.sy);
-            stage(gz, lz, MODE == kDq || MODE == kDk ? sc.sy : nullptr);
+            if (ROWS) stage(gx, lx, MODE == kOut || MODE == kDv ? 1 : 0, buf);
+            stage(gy, ly, MODE == kDq || MODE == kDk ? 0 : 2, buf);
+            stage(gz, lz, MODE == kDq || MODE == kDk ? 2 : 0, buf);
             if (i + 1 < count) fetch(block_at(i + 1));
+            const bool pairs = __builtin_amdgcn_readfirstlane(sc.pairs[buf]) != 0;
             lds_barrier();
 
-            // ---- X.Y of 32 x 32 rows, times their decays, as rows of X in LDS
-            if constexpr (ROWS) {
-                for (int t = wave; t < 3; t += C::NW) {
-                    const int sb = REV ? (t > 0) : (t == 2), tb = REV ? (t == 2) : (t > 0);
-                    f32x16 p = {};
-                    const unsigned char *const y = ly + (32 * sb + l32) * C::ROW + 16 * hh, *const x = lx + (32 * tb + l32) * C::ROW + 16 * hh;
-#pragma unroll
-                    for (int m = 0; m < D / 16; ++m)
-                        p = mfma(*reinterpret_cast<const bf16x8 *>(y + 32 * m), *reinterpret_cast<const bf16x8 *>(x + 32 * m), p);
-                    const float wt = sc.whole[buf][32 * tb + l32], ft = sc.frac[buf][32 * tb + l32];
-                    unsigned char *const to = lp + (32 * tb + l32) * C::PROW + 64 * sb;
-#pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const int s0 = 8 * g + 4 * hh;            // in the 32
-                        const f32x4 ws = *reinterpret_cast<const f32x4 *>(&sc.whole[buf][32 * sb + s0]), fs = *reinterpret_cast<const f32x4 *>(&sc.frac[buf][32 * sb + s0]),
-                                    ys = *reinterpret_cast<const f32x4 *>(&sc.sy[32 * sb + s0]);
-                        float v[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float d = REV ? (ws[j] - wt) + (fs[j] - ft) : (wt - ws[j]) + (ft - fs[j]);
-                            const bool seen = sb != tb || (REV ? s0 + j >= l32 : s0 + j <= l32);
-                            v[j] = seen ? p[4 * g + j] * ys[j] * __builtin_amdgcn_exp2f(d) : 0.f;
-                        }
-                        u32x2 hi, lo;
-                        if constexpr (SPLIT) {
-                            uint32_t h0, l0, h1, l1;
-                            split_pair(v[0], v[1], h0, l0);
-                            split_pair(v[2], v[3], h1, l1);
-                            hi = u32x2{h0, h1};
-                            lo = u32x2{l0, l1};
-                            *reinterpret_cast<u32x2 *>(to + C::PMAT + 2 * s0) = lo;
-                        } else {
-                            const bf16x4 r = {to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]), to_bf16(v[3])};
-                            hi = __builtin_bit_cast(u32x2, r);
-                        }
-                        *reinterpret_cast<u32x2 *>(to + 2 * s0) = hi;
-                    }
-                }
-            }
-            if (wave == C::NW - 1) sc.ww[lane] = sc.last[buf][lane] * sc.sy[lane];
-            if (i + 1 < count && wave == 0) gates(buf ^ 1);
-            if (i + 2 < count) fetch_gate(block_at(i + 2));
-            lds_barrier();
-
-            // Z^T of the wavefront's columns, 16 tokens each: operand of both products below
+            // Z^T of the wavefront's columns, 16 tokens each: operand of two products below
             bf16x8 zf[4];
             {
                 const int r = lane & 15;
@@ -268,16 +260,69 @@ struct Walk {
             }
             f32x16 acc[2];
             u32x2 own[2][4];                                      // the rows whose normalisation has a gradient
-            __amdgpu_buffer_rsrc_t rg;
             if constexpr (ROWS) {
                 acc[0] = acc[1] = f32x16{};
                 if constexpr (GRAD) {
-                    rg = make_rsrc((const char *)(MODE == kDq ? a.q : a.k) + stream, range);
+                    const auto rg = make_rsrc((const char *)(MODE == kDq ? a.q : a.k) + stream, range);
 #pragma unroll
                     for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
                         for (int g = 0; g < 4; ++g)
                             own[tb][g] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rg, (uint32_t)(blk * kBlock + 32 * tb + l32) * rs + (h * D + e0 + 8 * g + 4 * hh) * 2, 0, 0));
+                }
+                // ---- X.Y of 32 x 32 rows, times their decays, as rows of X in LDS
+#pragma unroll
+                for (int t0 = 0; t0 < 3; t0 += C::NW) {
+                    const int t = t0 + wave;
+                    if (t >= 3) break;
+                    const int sb = REV ? (t > 0) : (t == 2), tb = REV ? (t == 2) : (t > 0);
+                    f32x16 p = {};
+                    const unsigned char *const y = ly + (32 * sb + l32) * C::ROW + 16 * hh, *const x = lx + (32 * tb + l32) * C::ROW + 16 * hh;
+#pragma unroll
+                    for (int m = 0; m < D / 16; ++m)
+                        p = mfma(*reinterpret_cast<const bf16x8 *>(y + 32 * m), *reinterpret_cast<const bf16x8 *>(x + 32 * m), p);
+                    unsigned char *const to = lp + (32 * tb + l32) * C::PROW + 64 * sb;
+                    if (!pairs) {
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const f32x4 f = *reinterpret_cast<const f32x4 *>(&sc.pcol[32 * sb + 8 * g + 4 * hh]);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) p[4 * g + j] *= f[j];
+                        }
+                    } else {
+                        const float wt = sc.whole[buf][32 * tb + l32], ft = sc.frac[buf][32 * tb + l32];
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const int s0 = 32 * sb + 8 * g + 4 * hh;
+                            const f32x4 ws = *reinterpret_cast<const f32x4 *>(&sc.whole[buf][s0]), fs = *reinterpret_cast<const f32x4 *>(&sc.frac[buf][s0]),
+                                        ys = *reinterpret_cast<const f32x4 *>(&sc.norm[s0]);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) p[4 * g + j] *= ys[j] * __builtin_amdgcn_exp2f(REV ? (ws[j] - wt) + (fs[j] - ft) : (wt - ws[j]) + (ft - fs[j]));
+                        }
+                    }
+                    if (sb == tb) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const int d = 8 * (j / 4) + 4 * hh + j % 4 - l32;
+                            p[j] = (REV ? d >= 0 : d <= 0) ? p[j] : 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        u32x2 hi, lo;
+                        if constexpr (SPLIT) {
+                            uint32_t h0, l0, h1, l1;
+                            split_pair(p[4 * g], p[4 * g + 1], h0, l0);
+                            split_pair(p[4 * g + 2], p[4 * g + 3], h1, l1);
+                            hi = u32x2{h0, h1};
+                            lo = u32x2{l0, l1};
+                            *reinterpret_cast<u32x2 *>(to + C::PMAT + 16 * g + 8 * hh) = lo;
+                        } else {
+                            const bf16x4 r = {to_bf16(p[4 * g]), to_bf16(p[4 * g + 1]), to_bf16(p[4 * g + 2]), to_bf16(p[4 * g + 3])};
+                            hi = __builtin_bit_cast(u32x2, r);
+                        }
+                        *reinterpret_cast<u32x2 *>(to + 16 * g + 8 * hh) = hi;
+                    }
                 }
                 // ---- rows asked of the state, which is taken in two parts
                 const unsigned char *const x = lx + l32 * C::ROW + 16 * hh;
@@ -296,10 +341,18 @@ struct Walk {
                     acc[0] = mfma(lo, x0, acc[0]);
                     acc[1] = mfma(lo, x1, acc[1]);
                 }
-                const float f0 = sc.first[buf][l32], f1 = sc.first[buf][32 + l32];
+                if (pairs) {
+                    const float f0 = sc.row[buf][l32], f1 = sc.row[buf][32 + l32];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) { acc[0][j] *= f0; acc[1][j] *= f1; }
-                // ---- and of the block's own rows
+                    for (int j = 0; j < 16; ++j) { acc[0][j] *= f0; acc[1][j] *= f1; }
+                }
+            }
+            if (i + 1 < count && wave == GW) gates(buf ^ 1);
+            if (i + 2 < count) fetch_gate(block_at(i + 2));
+            if (ROWS) lds_barrier();
+
+            // ---- and of the block's own rows
+            if constexpr (ROWS) {
                 const unsigned char *const p = lp + l32 * C::PROW + 16 * hh;
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb)
@@ -311,18 +364,20 @@ struct Walk {
             }
 
             // ---- the state's step: rows of Z times their weights in two parts
-            const float total = sc.total[buf];
+            const float fold = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(sc.fold[buf])));
+            if (fold != 1.f) {
 #pragma unroll
-            for (int t = 0; t < D / 32; ++t)
+                for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) st[t][j] *= total;
+                    for (int j = 0; j < 16; ++j) st[t][j] *= fold;
+            }
             {
                 const int r = lane & 15, piece = ((r & 1) << 1) | ((r >> 1) & 1);       // pieces 1 and 2 of four change places: rows of the
                 // accumulator are then features 8 hh + j as the operand of the state's product wants them
                 const unsigned char *const y = ly + (8 * hh + (r >> 2)) * C::ROW + 2 * (16 * ((lane >> 4) & 1) + 4 * piece);
 #pragma unroll
                 for (int m = 0; m < 4; ++m) {
-                    const f32x4 w0 = *reinterpret_cast<const f32x4 *>(&sc.ww[16 * m + 8 * hh]), w1 = *reinterpret_cast<const f32x4 *>(&sc.ww[16 * m + 8 * hh + 4]);
+                    const f32x4 w0 = *reinterpret_cast<const f32x4 *>(&sc.penter[16 * m + 8 * hh]), w1 = *reinterpret_cast<const f32x4 *>(&sc.penter[16 * m + 8 * hh + 4]);
                     const u32x4 zb = __builtin_bit_cast(u32x4, zf[m]);
                     u32x4 hi, lo;
 #pragma unroll
@@ -364,16 +419,16 @@ struct Walk {
                         float dot = 0.f, ss = 0.f;
 #pragma unroll
                         for (int w = 0; w < C::NW; ++w) { dot += sc.red[w][32 * tb + l32][0]; ss += sc.red[w][32 * tb + l32][1]; }
-                        const float inv = a.normalise ? fast_rsqrt(ss + a.eps) : 1.f;
-                        dot *= inv;
-                        scale[tb] = inv;
+                        const float inv = a.normalise ? fast_rsqrt(ss + a.eps) : 1.f, row = pairs ? 1.f : sc.row[buf][32 * tb + l32];
+                        dot *= inv * row;
+                        scale[tb] = inv * row;
                         along[tb] = a.normalise ? -dot * inv * inv : 0.f;
                         const int t = blk * kBlock + 32 * tb + l32;
                         if (wave == 0 && hh == 0 && t < n && a.dla != nullptr) (MODE == kDq ? wk.qq : wk.kk)[(size_t)bh * a.L + t] = dot;
                     }
                 } else {
-                    scale[0] = sc.sx[l32];
-                    scale[1] = sc.sx[32 + l32];
+                    scale[0] = sc.post[l32];
+                    scale[1] = sc.post[32 + l32];
                     lds_barrier();                                // all have read the block's rows
                 }
                 void *const po = MODE == kOut ? a.out : MODE == kDq ? a.dq : MODE == kDk ? a.dk : a.dv;
@@ -410,12 +465,19 @@ struct Walk {
         if (MODE == kOut) to = seg == nact - 1 && a.S != nullptr ? a.S + (size_t)bh * D * D : nullptr;
         if (MODE == kSum) to = wk.forth + ((size_t)bh * (wk.nseg + 1) + seg + 1) * D * D;
         if (MODE == kSumBack) to = wk.back + ((size_t)bh * (wk.nseg + 1) + seg) * D * D;
-        if (to != nullptr)
+        if (to != nullptr) {
+            float gathered = 1.f;
+            if (count > 0) {
+                if (tid == 64 * GW) sc.fold[0] = exp2_of(base);   // (all have read it: a barrier ends every block)
+                lds_barrier();
+                gathered = sc.fold[0];
+            }
 #pragma unroll
             for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) to[(size_t)(32 * t + 16 * (j / 8) + 8 * hh + j % 8) * D + e0 + l32] = st[t][j];
-        if (!ROWS && tid == 0) (MODE == kSum ? wk.decay_forth : wk.decay_back)[(size_t)bh * wk.nseg + seg] = (float)::exp2(fmax(seg_total, -4096.0));
+                for (int j = 0; j < 16; ++j) to[(size_t)(32 * t + 16 * (j / 8) + 8 * hh + j % 8) * D + e0 + l32] = st[t][j] * gathered;
+        }
+        if (!ROWS && tid == 64 * GW) (MODE == kSum ? wk.decay_forth : wk.decay_back)[(size_t)bh * wk.nseg + seg] = exp2_of(seg_total);
     }
 };
 
@@ -460,21 +522,32 @@ __global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, Work wk, int
     if (start != nullptr) x = *reinterpret_cast<const f32x4 *>(start + (size_t)bh * nn + e);
     *reinterpret_cast<f32x4 *>(base + (size_t)(back ? nact : 0) * nn) = x;
     const int steps = back ? nact - 1 + need_first : nact - 1 + need_last;
-    for (int i = 0; i < steps; ++i) {
-        const int seg = back ? nact - 1 - i : i;
-        float *const at = base + (size_t)(back ? seg : seg + 1) * nn;
-        const f32x4 own = *reinterpret_cast<const f32x4 *>(at);
-        const float d = decay[seg];
+    constexpr int AHEAD = 8;                                      // states on their way at a time
+    for (int i0 = 0; i0 < steps; i0 += AHEAD) {
+        f32x4 own[AHEAD];
+        float d[AHEAD];
+        float *at[AHEAD];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = fmaf(d, x[j], own[j]);
-        *reinterpret_cast<f32x4 *>(at) = x;
+        for (int i = 0; i < AHEAD; ++i) {
+            const int step = min(i0 + i, steps - 1), seg = back ? nact - 1 - step : step;
+            at[i] = base + (size_t)(back ? seg : seg + 1) * nn;
+            own[i] = *reinterpret_cast<const f32x4 *>(at[i]);
+            d[i] = decay[seg];
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (i0 + i >= steps) break;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = fmaf(d[i], x[j], own[i][j]);
+            *reinterpret_cast<f32x4 *>(at[i]) = x;
+        }
     }
     if (back && a.dS0 != nullptr) *reinterpret_cast<f32x4 *>(a.dS0 + (size_t)bh * nn + e) = x;
 }
 
 // The rows' gradients: three walks of a segment by three workgroups that follow one another.
 template <int D>
-__global__ __launch_bounds__(Cfg<D>::NT, 2) void scan_grad_kernel(ScanArgs a, Work wk)
+__global__ __launch_bounds__(Cfg<D>::NT, D / 64) void scan_grad_kernel(ScanArgs a, Work wk)
 {
     __shared__ __align__(16) unsigned char lds[Walk<D, kDq>::LDS_ROWS];
     __shared__ __align__(16) Scalars sc;
