@@ -25,7 +25,6 @@ struct RopeArgs {
     double turns[64];            // of each pair for one step of its position
 };
 
-int rope_workgroups(int B, int L, int D, int heads);             // of the gradients' kernel
 size_t rope_workspace_bytes(int B, int L, int D, int heads);
 constexpr int kRopeMostUnits = 1536;                             // of 16 features, queries and keys of a token together
 

@@ -5,19 +5,23 @@
 //   z = R(-pos) dy,   dw = sum over tokens of z . x r,   g = w z,   dx = r (g - x r mean(g . x r))
 //
 // The angle in turns is position times the pair's turns in fp64 (exact to 2^-53 of it, so far positions lose nothing), its
-// fraction goes to fp32; a wavefront's lanes compute one pair each and hand cosine and sine on through LDS.  Memory bounds both.
+// fraction goes to fp32; cosines and sines of a token are computed once and pass through LDS to the lanes.  Memory bounds both.
 //
-// A unit is 8 pairs of a head, 16 features: neighbours (2i, 2i + 1), or i and i + D / 2.  A token's units (queries, then keys) are
-// dealt to the lanes of WPT wavefronts, NU to a lane; 64 is a multiple of a head's units, so a lane's units all have the same pairs.
+// A unit is 8 pairs of a head, 16 features: neighbours (2i, 2i + 1), or i and i + D / 2.  A token's units (queries, then keys) are dealt to
+// LPT lanes of a workgroup, the least power of two from 16 on that holds them, 256 at the most and then NU to a lane; a head's units divide LPT, so
+// a lane's units all have the same pairs.  A workgroup takes 256 / LPT tokens side by side and TOK of each in a row: their loads are all
+// requested before the first sum, their sums cross the wavefronts together, and a weight's gradient stays with its lane.
 #include "arl2_device.h"
 #include "arl2_rope.h"
+
+#include <algorithm>
 
 namespace arl2 {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostWorkgroups = 2048;
-constexpr int kGradWorkgroups = 512;
+constexpr int kMostWorkgroups = 4096;
+constexpr int kGradWorkgroups = 768;
 
 template <class T> struct Raw;                    // 8 features as they lie in memory
 template <> struct Raw<bf16_t> { u32x4 v; };
@@ -25,16 +29,8 @@ template <> struct Raw<float> { f32x4 v[2]; };
 
 __device__ __forceinline__ Raw<bf16_t> load8(const bf16_t *p) { return {*reinterpret_cast<const u32x4 *>(p)}; }
 __device__ __forceinline__ Raw<float> load8(const float *p) { return {{*reinterpret_cast<const f32x4 *>(p), *reinterpret_cast<const f32x4 *>(p + 4)}}; }
-__device__ __forceinline__ void widen(const Raw<bf16_t> &r, float *x)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(r.v[i] << 16); x[2 * i + 1] = __uint_as_float(r.v[i] & 0xffff0000u); }
-}
-__device__ __forceinline__ void widen(const Raw<float> &r, float *x)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = r.v[i / 4][i % 4];
-}
+__device__ __forceinline__ float feature(const Raw<bf16_t> &r, int i) { return __uint_as_float(i % 2 ? r.v[i / 2] & 0xffff0000u : r.v[i / 2] << 16); }
+__device__ __forceinline__ float feature(const Raw<float> &r, int i) { return r.v[i / 4][i % 4]; }
 __device__ __forceinline__ void store8(bf16_t *p, const float *x)
 {
     u32x4 v;
@@ -51,63 +47,66 @@ __device__ __forceinline__ void store8(float *p, const float *x)
     *reinterpret_cast<f32x4 *>(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
 }
 
+// 8 pairs: halves of a head apart, or neighbours (then `hi` follows `lo`).
 template <class T> struct Unit { Raw<T> lo, hi; };
-
-// 16 features as floats in memory order (neighbours: 16 in a row; halves: 8 and, D / 2 further, 8)
 template <class T>
-__device__ __forceinline__ void widen(const Unit<T> &u, float *x) { widen(u.lo, x); widen(u.hi, x + 8); }
+__device__ __forceinline__ Unit<T> load_unit(const T *p, int hi) { return {load8(p), load8(p + hi)}; }
 
-struct Turn { float c[8], s[8]; };
+// Place of a pair's two features among the unit's 16.
+template <bool HALVES> __device__ __forceinline__ constexpr int first_of(int pair) { return HALVES ? pair : 2 * pair; }
+template <bool HALVES> __device__ __forceinline__ constexpr int second_of(int pair) { return HALVES ? 8 + pair : 2 * pair + 1; }
+template <class T>
+__device__ __forceinline__ float feature(const Unit<T> &u, int i) { return i < 8 ? feature(u.lo, i) : feature(u.hi, i - 8); }
 
-// The unit's pairs turned, backwards with SIGN -1; pairs from `pairs` on (counted from the unit's first) stay.
-template <int SIGN>
-__device__ __forceinline__ void turn_unit(float *x, const Turn &t, bool halves, bool partial, int pairs)
+// The compiler is to take these registers for new values: else it keeps what it has widened and turned of every token for the second
+// time that they are used (the gradients of a row: 256 registers and 1 KB of scratch a lane).
+__device__ __forceinline__ void forget(Raw<bf16_t> &r) { asm volatile("" : "+v"(r.v)); }
+__device__ __forceinline__ void forget(Raw<float> &r) { asm volatile("" : "+v"(r.v[0]), "+v"(r.v[1])); }
+template <class T>
+__device__ __forceinline__ void forget(Unit<T> &u) { forget(u.lo); forget(u.hi); }
+
+// f(pair, cosine, sine) for the unit's eight pairs, two after the other: what is on its way at a time decides how many registers it takes.
+template <class F>
+__device__ __forceinline__ void each_pair(const f32x2 *turn, F &&f)
 {
-    auto one = [&](float &x0, float &x1, int i) {
-        const float s = SIGN * t.s[i], y0 = x0 * t.c[i] - x1 * s, y1 = x0 * s + x1 * t.c[i];
-        const bool stays = partial && i >= pairs;
-        x0 = stays ? x0 : y0;
-        x1 = stays ? x1 : y1;
-    };
-    if (halves) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) one(x[i], x[8 + i], i);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) one(x[2 * i], x[2 * i + 1], i);
+    for (int i = 0; i < 8; i += 2) {
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(turn + i);
+        f(i, v[0], v[1]);
+        f(i + 1, v[2], v[3]);
+        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
-// What a lane knows of its units: unit u of a token is number u * 64 * WPT + (lane among the token's).
+// What a lane knows of its units: unit u of a token is number li + 256 u.
 struct Lane {
-    int upt, units[2], first, step, in_head, hi;     // units per head, of queries and keys; its first, from one to the next; place in the head
+    int upt, units0, units, lpt, slots, slot, li;     // units per head, of queries, of a token; lanes per token, tokens side by side
+    int in_head, at, hi;                              // which of its head's units; its first features' place there, the others' distance
 };
-
-template <int WPT>
-__device__ __forceinline__ Lane lane_of(const RopeArgs &a)
+__device__ __forceinline__ Lane lane_of(const RopeArgs &a, int lpt, bool halves)
 {
     Lane m;
     m.upt = a.D / 16;
-    m.units[0] = a.heads[0] * m.upt;
-    m.units[1] = a.heads[1] * m.upt;
-    m.first = WPT == 1 ? threadIdx.x & 63 : threadIdx.x;
-    m.step = 64 * WPT;
-    m.in_head = m.first & (m.upt - 1);
-    m.hi = a.halves ? a.D / 2 : 8;
+    m.units0 = a.heads[0] * m.upt;
+    m.units = m.units0 + a.heads[1] * m.upt;
+    m.lpt = lpt;
+    m.slots = kThreads / lpt;
+    m.slot = threadIdx.x / lpt;
+    m.li = threadIdx.x & (lpt - 1);
+    m.in_head = m.li & (m.upt - 1);
+    m.hi = halves ? a.D / 2 : 8;
+    m.at = m.in_head * (halves ? 8 : 16);
     return m;
 }
 // Which array (0, 1; 2: none) the lane's unit u lies in, and the offset of its features in that array's rows.
 __device__ __forceinline__ int place(const RopeArgs &a, const Lane &m, int u, int &offset)
 {
-    int i = m.first + u * m.step;
-    const int which = i < m.units[0] ? 0 : i < m.units[0] + m.units[1] ? 1 : 2;
-    if (which) i -= m.units[0];
-    offset = i / m.upt * a.D + m.in_head * (a.halves ? 8 : 16);
+    int i = m.li + u * kThreads;
+    const int which = i < m.units0 ? 0 : i < m.units ? 1 : 2;
+    if (which) i -= m.units0;
+    offset = i / m.upt * a.D + m.at;
     return which;
 }
-
-template <class T>
-__device__ __forceinline__ Unit<T> load_unit(const T *p, int hi) { return {load8(p), load8(p + hi)}; }
 
 // Sum over the lanes of a head's units (8 at D = 128, 4 at D = 64).
 __device__ __forceinline__ float head_sum(float x, int upt)
@@ -116,232 +115,299 @@ __device__ __forceinline__ float head_sum(float x, int upt)
     x += dpp_peek<0x4E>(x);
     return upt == 8 ? x + dpp_peek<0x141>(x) : x;
 }
-__device__ __forceinline__ float wave_sum(float x)
+// Sum over aligned groups of `n` lanes, 16 to 64.
+__device__ __forceinline__ float group_sum(float x, int n)
 {
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) x += __shfl_xor(x, m, kWave);
+    x = lane_group_sum<16>(x);
+    if (n >= 32) x += __shfl_xor(x, 16, kWave);
+    if (n >= 64) x += __shfl_xor(x, 32, kWave);
     return x;
 }
 
-// Sums over a token's lanes of two values; `red` and two barriers where the token has several wavefronts.
-template <int WPT>
-__device__ __forceinline__ void token_sums(float &x, float &y, float (*red)[2])
+// Sums over a token's lanes of N values of each of TOK tokens; `red` and a barrier where the token has several wavefronts.
+template <int TOK, int N>
+__device__ __forceinline__ void token_sums(float (*x)[N], const Lane &m, float (*red)[TOK * N])
 {
-    x = wave_sum(x);
-    y = wave_sum(y);
-    if constexpr (WPT > 1) {
-        if ((threadIdx.x & 63) == 0) { red[threadIdx.x >> 6][0] = x; red[threadIdx.x >> 6][1] = y; }
-        __syncthreads();
-        x = y = 0.f;
+    const int wave = threadIdx.x >> 6, n = min(m.lpt, 64);
 #pragma unroll
-        for (int w = 0; w < WPT; ++w) { x += red[w][0]; y += red[w][1]; }
-        __syncthreads();
-    }
+    for (int t = 0; t < TOK; ++t)
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[t][i] = group_sum(x[t][i], n);
+    if (m.lpt <= 64) return;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int t = 0; t < TOK; ++t)
+#pragma unroll
+            for (int i = 0; i < N; ++i) red[wave][t * N + i] = x[t][i];
+    __syncthreads();
+    const int w0 = m.lpt == 128 ? wave & 2 : 0;
+#pragma unroll
+    for (int t = 0; t < TOK; ++t)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            x[t][i] = red[w0][t * N + i] + red[w0 + 1][t * N + i];
+            if (m.lpt == 256) x[t][i] += red[2][t * N + i] + red[3][t * N + i];
+        }
 }
 
-// Cosines and sines of the lane's eight pairs at a token (b, l).
-__device__ __forceinline__ Turn turns_of(const RopeArgs &a, const Lane &m, double step, int axis, int b, int l, f32x2 *own)
+// Cosines and sines of all pairs of `tokens` tokens from `first` on, by all threads; a barrier has to follow.
+__device__ __forceinline__ void turns_of(const RopeArgs &a, long long first, long long all, int tokens, f32x2 (*turns)[64])
 {
-    const int lane = threadIdx.x & 63;
-    if (lane < a.D / 2) {
-        const int32_t p = a.pos[((a.pos_per_stream ? (size_t)b * a.L : 0) + l) * a.axes + axis];
-        const double t = (double)p * step;
-        float s, c;
-        sincospif(2.f * (float)(t - ::rint(t)), &s, &c);
-        own[lane] = f32x2{c, s};
+    const int half = a.D / 2;
+    for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
+        const int pair = i & (half - 1), t = i / half;
+        if (first + t >= all) break;
+        float c = 1.f, s = 0.f;
+        if (pair < a.pairs) {
+            const size_t at = a.pos_per_stream ? (size_t)(first + t) : (size_t)((first + t) % a.L);
+            const double turn = (double)a.pos[at * a.axes + a.axis[pair]] * a.turns[pair];
+            sincospif(2.f * (float)(turn - ::rint(turn)), &s, &c);
+        }
+        turns[t][pair] = f32x2{c, s};
     }
-    __builtin_amdgcn_wave_barrier();
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    Turn r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const f32x4 v = *reinterpret_cast<const f32x4 *>(&own[8 * m.in_head + 2 * i]);
-        r.c[2 * i] = v[0]; r.s[2 * i] = v[1]; r.c[2 * i + 1] = v[2]; r.s[2 * i + 1] = v[3];
-    }
-    __builtin_amdgcn_wave_barrier();
-    return r;
+}
+// Is there such a token (of a sequence that goes so far)?
+__device__ __forceinline__ bool token_there(const RopeArgs &a, long long t, long long all)
+{
+    if (t >= all) return false;
+    if (a.len == nullptr) return true;
+    const int b = (int)(t / a.L);
+    return (int)(t - (long long)b * a.L) < a.len[b];
 }
 
-template <class T, int NU, int WPT>
-__global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a)
+// 1 over the root of the mean square.
+__device__ __forceinline__ float inverse_rms(float squares, int n, float eps) { return 1.f / sqrtf(squares / (float)n + eps); }
+
+template <class T, int NORM, bool HALVES, int NU, int TOK>
+__global__ __launch_bounds__(kThreads, NU == 1 ? 4 : NU <= 3 ? 3 : 2) void rope_kernel(RopeArgs a, int lpt)
 {
-    __shared__ __align__(16) f32x2 turns[4][64];
-    __shared__ float red[4][2];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const Lane m = lane_of<WPT>(a);
+    extern __shared__ __align__(16) f32x2 turns[][64];            // of two rounds in turn
+    __shared__ float red[2][4][TOK * 2];
+    const Lane m = lane_of(a, lpt, HALVES);
     const bool partial = a.pairs < a.D / 2;
-    const double step = lane < a.D / 2 ? a.turns[lane] : 0.0;
-    const int axis = lane < a.D / 2 ? a.axis[lane] : 0;
+    const int at_a_time = m.slots * TOK, left = a.pairs - 8 * m.in_head;
     Unit<T> w[NU];
     int which[NU], off[NU];
+    bool weighted[NU];
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
         which[u] = place(a, m, u, off[u]);
-        if (which[u] < 2 && a.w[which[u]] != nullptr)
-            w[u] = load_unit((const T *)a.w[which[u]] + (a.norm == kNormHead ? off[u] % a.D : off[u]), m.hi);
+        weighted[u] = NORM != kNormNone && which[u] < 2 && a.w[which[u]] != nullptr;
+        if (weighted[u]) w[u] = load_unit((const T *)a.w[which[u]] + (NORM == kNormHead ? m.at : off[u]), m.hi);
     }
-    const long long tokens = (long long)a.B * a.L;
-    for (long long t = WPT == 1 ? (long long)blockIdx.x * 4 + wave : blockIdx.x; t < tokens; t += (long long)gridDim.x * (WPT == 1 ? 4 : 1)) {
-        const int b = (int)(t / a.L), l = (int)(t - (long long)b * a.L);
-        if (a.len != nullptr && l >= a.len[b]) continue;
-        Unit<T> x[NU];
+    const long long all = (long long)a.B * a.L;
+    int round = 0;
+    for (long long t0 = (long long)blockIdx.x * at_a_time; t0 < all; t0 += (long long)gridDim.x * at_a_time, round ^= 1) {
+        bool there[TOK];
+        Unit<T> x[TOK][NU];
 #pragma unroll
-        for (int u = 0; u < NU; ++u)
-            if (which[u] < 2) x[u] = load_unit((const T *)a.x[which[u]] + (size_t)t * a.heads[which[u]] * a.D + off[u], m.hi);
-        const Turn turn = turns_of(a, m, step, axis, b, l, turns[wave]);
-        float row[2] = {1.f, 1.f};
-        if (a.norm == kNormRow) {
-            row[0] = row[1] = 0.f;
+        for (int t = 0; t < TOK; ++t) {
+            const long long tok = t0 + m.slot * TOK + t;
+            there[t] = token_there(a, tok, all);
 #pragma unroll
-            for (int u = 0; u < NU; ++u) {
-                float f[16], s = 0.f;
-                widen(x[u], f);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s = fmaf(f[i], f[i], s);
-                row[0] += which[u] == 0 ? s : 0.f;
-                row[1] += which[u] == 1 ? s : 0.f;
-            }
-            token_sums<WPT>(row[0], row[1], red);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) row[i] = 1.f / sqrtf(row[i] / (float)(a.heads[i] * a.D) + a.eps);
+            for (int u = 0; u < NU; ++u)
+                if (there[t] && which[u] < 2) x[t][u] = load_unit((const T *)a.x[which[u]] + (size_t)tok * a.heads[which[u]] * a.D + off[u], m.hi);
         }
+        f32x2 (*const mine)[64] = turns + round * at_a_time;
+        turns_of(a, t0, all, at_a_time, mine);
+        float row[TOK][2];
+        if constexpr (NORM == kNormRow) {
 #pragma unroll
-        for (int u = 0; u < NU; ++u) {
-            float f[16];
-            widen(x[u], f);
-            float r = which[u] == 1 ? row[1] : row[0];
-            if (a.norm == kNormHead) {
-                float s = 0.f;
+            for (int t = 0; t < TOK; ++t) {
+                row[t][0] = row[t][1] = 0.f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s = fmaf(f[i], f[i], s);
-                s = head_sum(s, m.upt);
-                r = 1.f / sqrtf(s / (float)a.D + a.eps);
-            }
-            if (which[u] == 2) continue;
-            if (a.norm != kNormNone) {
+                for (int u = 0; u < NU; ++u) {
+                    float s = 0.f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) f[i] *= r;
-                if (a.w[which[u]] != nullptr) {
-                    float g[16];
-                    widen(w[u], g);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) f[i] *= g[i];
+                    for (int i = 0; i < 16; ++i) { const float f = feature(x[t][u], i); s = fmaf(f, f, s); }
+                    row[t][0] += which[u] == 0 ? s : 0.f;
+                    row[t][1] += which[u] == 1 ? s : 0.f;
                 }
             }
-            turn_unit<1>(f, turn, a.halves, partial, a.pairs - 8 * m.in_head);
-            T *const to = (T *)a.y[which[u]] + (size_t)t * a.heads[which[u]] * a.D + off[u];
-            store8(to, f);
-            store8(to + m.hi, f + 8);
+            token_sums<TOK, 2>(row, m, red[round]);
+        }
+        if (NORM != kNormRow || m.lpt <= 64) __syncthreads();
+#pragma unroll
+        for (int t = 0; t < TOK; ++t) {
+            const f32x2 *const turn = &mine[m.slot * TOK + t][8 * m.in_head];
+            if constexpr (NORM == kNormRow)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) row[t][i] = inverse_rms(row[t][i], a.heads[i] * a.D, a.eps);
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                float r = 1.f, y[16];
+                if constexpr (NORM == kNormHead) {
+                    float s = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) { const float f = feature(x[t][u], i); s = fmaf(f, f, s); }
+                    r = inverse_rms(head_sum(s, m.upt), a.D, a.eps);
+                } else if constexpr (NORM == kNormRow) r = which[u] == 1 ? row[t][1] : row[t][0];
+                forget(x[t][u]);
+                if (NORM != kNormNone) forget(w[u]);
+                each_pair(turn, [&](int i, float c, float s) {
+                    const int j0 = first_of<HALVES>(i), j1 = second_of<HALVES>(i);
+                    float f0 = feature(x[t][u], j0), f1 = feature(x[t][u], j1);
+                    if constexpr (NORM != kNormNone) {
+                        f0 *= r;
+                        f1 *= r;
+                        f0 *= weighted[u] ? feature(w[u], j0) : 1.f;
+                        f1 *= weighted[u] ? feature(w[u], j1) : 1.f;
+                    }
+                    y[j0] = f0 * c - f1 * s;
+                    y[j1] = f0 * s + f1 * c;
+                    if (partial && i >= left) { y[j0] = f0; y[j1] = f1; }
+                });
+                if (!there[t] || which[u] == 2) continue;
+                T *const to = (T *)a.y[which[u]] + (size_t)(t0 + m.slot * TOK + t) * a.heads[which[u]] * a.D + off[u];
+                store8(to, y);
+                store8(to + m.hi, y + 8);
+            }
         }
     }
 }
 
-// Sums of weights' gradients stay with their lane over all of a workgroup's tokens (one axis of the units for weights of a head's
-// features), are joined in LDS and written as this workgroup's part.
-template <class T, int NU, int WPT>
-__global__ __launch_bounds__(kThreads) void rope_bwd_kernel(RopeArgs a)
+// A weight's gradient is summed over all of a workgroup's tokens by the lanes that have its feature, joined among them at the end and written
+// as this workgroup's part.
+template <class T, int NORM, bool HALVES, int NU, int TOK>
+__global__ __launch_bounds__(kThreads, NU == 1 ? 3 : 2) void rope_bwd_kernel(RopeArgs a, int lpt)
 {
-    __shared__ __align__(16) f32x2 turns[4][64];
-    __shared__ float red[4][2];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const Lane m = lane_of<WPT>(a);
+    extern __shared__ __align__(16) f32x2 turns[][64];
+    __shared__ float red[2][4][TOK * 4];
+    const Lane m = lane_of(a, lpt, HALVES);
     const bool partial = a.pairs < a.D / 2;
-    const double step = lane < a.D / 2 ? a.turns[lane] : 0.0;
-    const int axis = lane < a.D / 2 ? a.axis[lane] : 0;
+    const int at_a_time = m.slots * TOK, left = a.pairs - 8 * m.in_head;
     Unit<T> w[NU];
     float dw[NU][16] = {};
     int which[NU], off[NU];
+    bool weighted[NU];
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
         which[u] = place(a, m, u, off[u]);
-        if (which[u] < 2 && a.w[which[u]] != nullptr)
-            w[u] = load_unit((const T *)a.w[which[u]] + (a.norm == kNormHead ? off[u] % a.D : off[u]), m.hi);
+        weighted[u] = NORM != kNormNone && which[u] < 2 && a.w[which[u]] != nullptr;
+        if (weighted[u]) w[u] = load_unit((const T *)a.w[which[u]] + (NORM == kNormHead ? m.at : off[u]), m.hi);
     }
-    const long long tokens = (long long)a.B * a.L;
-    for (long long t = WPT == 1 ? (long long)blockIdx.x * 4 + wave : blockIdx.x; t < tokens; t += (long long)gridDim.x * (WPT == 1 ? 4 : 1)) {
-        const int b = (int)(t / a.L), l = (int)(t - (long long)b * a.L);
-        if (a.len != nullptr && l >= a.len[b]) continue;
-        Unit<T> x[NU], d[NU];
+    const long long all = (long long)a.B * a.L;
+    int round = 0;
+    for (long long t0 = (long long)blockIdx.x * at_a_time; t0 < all; t0 += (long long)gridDim.x * at_a_time, round ^= 1) {
+        bool there[TOK];
+        Unit<T> x[TOK][NU], d[TOK][NU];
 #pragma unroll
-        for (int u = 0; u < NU; ++u)
-            if (which[u] < 2) {
-                const size_t at = (size_t)t * a.heads[which[u]] * a.D + off[u];
-                d[u] = load_unit((const T *)a.dy[which[u]] + at, m.hi);
-                if (a.norm != kNormNone) x[u] = load_unit((const T *)a.x[which[u]] + at, m.hi);
+        for (int t = 0; t < TOK; ++t) {
+            const long long tok = t0 + m.slot * TOK + t;
+            there[t] = token_there(a, tok, all);
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+                if (there[t] && which[u] < 2) {
+                    const size_t at = (size_t)tok * a.heads[which[u]] * a.D + off[u];
+                    d[t][u] = load_unit((const T *)a.dy[which[u]] + at, m.hi);
+                    if (NORM != kNormNone) x[t][u] = load_unit((const T *)a.x[which[u]] + at, m.hi);
+                }
+        }
+        f32x2 (*const mine)[64] = turns + round * at_a_time;
+        turns_of(a, t0, all, at_a_time, mine);
+        __syncthreads();
+        // a pair of dy turned back, times the weights: z into z0, z1 and w z into the others
+        auto back = [&](int t, int u, int i, float c, float s, float &z0, float &z1, float &g0, float &g1) {
+            const int j0 = first_of<HALVES>(i), j1 = second_of<HALVES>(i);
+            const float d0 = feature(d[t][u], j0), d1 = feature(d[t][u], j1);
+            z0 = d0 * c + d1 * s;
+            z1 = d1 * c - d0 * s;
+            if (partial && i >= left) { z0 = d0; z1 = d1; }
+            g0 = z0;
+            g1 = z1;
+            if (NORM != kNormNone) {
+                g0 *= weighted[u] ? feature(w[u], j0) : 1.f;
+                g1 *= weighted[u] ? feature(w[u], j1) : 1.f;
             }
-        const Turn turn = turns_of(a, m, step, axis, b, l, turns[wave]);
-        float row[2] = {0.f, 0.f}, dot[2] = {0.f, 0.f};
-        if (a.norm == kNormRow) {
+        };
+        // squares of the unit's features, and their products with w z
+        auto sums = [&](int t, int u, const f32x2 *turn, float &sq, float &dot) {
+            float q = 0.f, p = 0.f;
+            forget(w[u]);
+            each_pair(turn, [&](int i, float c, float s) {
+                float z0, z1, g0, g1;
+                back(t, u, i, c, s, z0, z1, g0, g1);
+                const float f0 = feature(x[t][u], first_of<HALVES>(i)), f1 = feature(x[t][u], second_of<HALVES>(i));
+                q = fmaf(f0, f0, fmaf(f1, f1, q));
+                p = fmaf(f0, g0, fmaf(f1, g1, p));
+                asm volatile("" : "+v"(q), "+v"(p));
+            });
+            sq = q;
+            dot = p;
+        };
+        float row[TOK][4];                                        // squares of queries and keys, products with their gradients
+        if constexpr (NORM == kNormRow) {
+#pragma unroll
+            for (int t = 0; t < TOK; ++t) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) row[t][i] = 0.f;
+#pragma unroll
+                for (int u = 0; u < NU; ++u) {
+                    float s, p;
+                    sums(t, u, &mine[m.slot * TOK + t][8 * m.in_head], s, p);
+                    row[t][0] += which[u] == 0 ? s : 0.f;
+                    row[t][1] += which[u] == 1 ? s : 0.f;
+                    row[t][2] += which[u] == 0 ? p : 0.f;
+                    row[t][3] += which[u] == 1 ? p : 0.f;
+                }
+            }
+            token_sums<TOK, 4>(row, m, red[round]);
+        }
+#pragma unroll
+        for (int t = 0; t < TOK; ++t) {
+            const f32x2 *const turn = &mine[m.slot * TOK + t][8 * m.in_head];
+            if constexpr (NORM == kNormRow)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    row[t][i] = inverse_rms(row[t][i], a.heads[i] * a.D, a.eps);
+                    row[t][2 + i] *= row[t][i] / (float)(a.heads[i] * a.D);
+                }
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
-                float f[16], g[16], wf[16], s = 0.f, p = 0.f;
-                widen(x[u], f);
-                widen(d[u], g);
-                turn_unit<-1>(g, turn, a.halves, partial, a.pairs - 8 * m.in_head);
-                const bool weighted = which[u] < 2 && a.w[which[u]] != nullptr;
-                if (weighted) widen(w[u], wf);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s = fmaf(f[i], f[i], s);
-                    p = fmaf(f[i], weighted ? g[i] * wf[i] : g[i], p);
+                float r = 1.f, p = 0.f, y[16];
+                if constexpr (NORM == kNormHead) {
+                    float s;
+                    sums(t, u, turn, s, p);
+                    r = inverse_rms(head_sum(s, m.upt), a.D, a.eps);
+                    p = head_sum(p, m.upt) * r / (float)a.D;
+                } else if constexpr (NORM == kNormRow) {
+                    r = which[u] == 1 ? row[t][1] : row[t][0];
+                    p = which[u] == 1 ? row[t][3] : row[t][2];
                 }
-                row[0] += which[u] == 0 ? s : 0.f;
-                row[1] += which[u] == 1 ? s : 0.f;
-                dot[0] += which[u] == 0 ? p : 0.f;
-                dot[1] += which[u] == 1 ? p : 0.f;
-            }
-            token_sums<WPT>(row[0], row[1], red);
-            token_sums<WPT>(dot[0], dot[1], red);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float over = 1.f / (float)(a.heads[i] * a.D);
-                row[i] = 1.f / sqrtf(row[i] * over + a.eps);
-                dot[i] *= row[i] * over;
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < NU; ++u) {
-            float g[16];
-            widen(d[u], g);
-            turn_unit<-1>(g, turn, a.halves, partial, a.pairs - 8 * m.in_head);
-            if (a.norm != kNormNone) {
-                float f[16], wf[16];
-                widen(x[u], f);
-                const bool weighted = which[u] < 2 && a.w[which[u]] != nullptr;
-                if (weighted) widen(w[u], wf);
-                float r = which[u] == 1 ? row[1] : row[0], p = which[u] == 1 ? dot[1] : dot[0];
-                if (a.norm == kNormHead) {
-                    float s = 0.f;
-                    p = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        s = fmaf(f[i], f[i], s);
-                        p = fmaf(f[i], weighted ? g[i] * wf[i] : g[i], p);
+                forget(d[t][u]);
+                if (NORM != kNormNone) {
+                    forget(x[t][u]);
+                    forget(w[u]);
+                }
+                const bool counts = there[t] && which[u] < 2;
+                each_pair(turn, [&](int i, float c, float s) {
+                    const int j0 = first_of<HALVES>(i), j1 = second_of<HALVES>(i);
+                    float z0, z1, g0, g1;
+                    back(t, u, i, c, s, z0, z1, g0, g1);
+                    if constexpr (NORM != kNormNone) {
+                        const float h0 = feature(x[t][u], j0) * r, h1 = feature(x[t][u], j1) * r;
+                        dw[u][j0] = counts ? fmaf(z0, h0, dw[u][j0]) : dw[u][j0];
+                        dw[u][j1] = counts ? fmaf(z1, h1, dw[u][j1]) : dw[u][j1];
+                        asm volatile("" : "+v"(dw[u][j0]), "+v"(dw[u][j1]));      // (now, not where the next token needs them: z and h would be kept)
+                        g0 = r * (g0 - h0 * p);
+                        g1 = r * (g1 - h1 * p);
                     }
-                    s = head_sum(s, m.upt);
-                    p = head_sum(p, m.upt);
-                    r = 1.f / sqrtf(s / (float)a.D + a.eps);
-                    p *= r / (float)a.D;
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float xh = f[i] * r;
-                    if (which[u] < 2) dw[u][i] = fmaf(g[i], xh, dw[u][i]);
-                    g[i] = r * ((weighted ? g[i] * wf[i] : g[i]) - xh * p);
-                }
+                    y[j0] = g0;
+                    y[j1] = g1;
+                    if (i % 2) asm volatile("" : "+v"(y[first_of<HALVES>(i - 1)]), "+v"(y[second_of<HALVES>(i - 1)]), "+v"(y[j0]), "+v"(y[j1]));
+                });
+                if (!counts) continue;
+                T *const to = (T *)a.y[which[u]] + (size_t)(t0 + m.slot * TOK + t) * a.heads[which[u]] * a.D + off[u];
+                store8(to, y);
+                store8(to + m.hi, y + 8);
             }
-            if (which[u] == 2) continue;
-            T *const to = (T *)a.y[which[u]] + (size_t)t * a.heads[which[u]] * a.D + off[u];
-            store8(to, g);
-            store8(to + m.hi, g + 8);
         }
     }
-    if (a.norm == kNormNone || (a.dw[0] == nullptr && a.dw[1] == nullptr)) return;
+    if (NORM == kNormNone || (a.dw[0] == nullptr && a.dw[1] == nullptr)) return;
     // this workgroup's part: [D] and [D], or [heads D] and [heads D]
-    extern __shared__ __align__(16) float part[];
-    const int width0 = a.norm == kNormHead ? a.D : a.heads[0] * a.D, width = width0 + (a.norm == kNormHead ? a.D : a.heads[1] * a.D);
-    if (WPT > 1 && a.norm == kNormRow) {                          // each of its elements is one lane's
-        float *const to = a.part + (size_t)blockIdx.x * width;
+    const int width0 = NORM == kNormHead ? a.D : a.heads[0] * a.D, width = width0 + (NORM == kNormHead ? a.D : a.heads[1] * a.D);
+    float *const to = a.part + (size_t)blockIdx.x * width;
+    if (NORM == kNormRow && m.lpt == kThreads) {                  // each of its elements is one lane's
 #pragma unroll
         for (int u = 0; u < NU; ++u)
             if (which[u] < 2)
@@ -349,43 +415,42 @@ __global__ __launch_bounds__(kThreads) void rope_bwd_kernel(RopeArgs a)
                 for (int i = 0; i < 16; ++i) to[(which[u] ? width0 : 0) + off[u] + (i < 8 ? i : m.hi + i - 8)] = dw[u][i];
         return;
     }
+    float *const part = reinterpret_cast<float *>(&turns[0][0]);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    __syncthreads();                                              // the turns have been read
     for (int i = threadIdx.x; i < width; i += kThreads) part[i] = 0.f;
     __syncthreads();
-    if (a.norm == kNormHead) {
+    if constexpr (NORM == kNormHead) {
         // lanes of the same place in their heads, units of a lane: one sum of each array
-        float sum[2][16] = {};
 #pragma unroll
-        for (int u = 0; u < NU; ++u)
+        for (int k = 0; k < 2; ++k) {
+            float sum[16] = {};
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                sum[0][i] += which[u] == 0 ? dw[u][i] : 0.f;
-                sum[1][i] += which[u] == 1 ? dw[u][i] : 0.f;
-            }
+            for (int u = 0; u < NU; ++u)
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+                for (int i = 0; i < 16; ++i) sum[i] += which[u] == k ? dw[u][i] : 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                for (int s = m.upt; s < 64; s <<= 1) sum[k][i] += __shfl_xor(sum[k][i], s, kWave);
-        for (int v = 0; v < 4; ++v) {
-            if (wave == v && lane < m.upt)
+                for (int s = m.upt; s < 64; s <<= 1) sum[i] += __shfl_xor(sum[i], s, kWave);
+            for (int v = 0; v < 4; ++v) {
+                if (wave == v && lane < m.upt)
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) part[(k ? width0 : 0) + m.in_head * (a.halves ? 8 : 16) + (i < 8 ? i : m.hi + i - 8)] += sum[k][i];
-            __syncthreads();
+                    for (int i = 0; i < 16; ++i) part[(k ? width0 : 0) + m.at + (i < 8 ? i : m.hi + i - 8)] += sum[i];
+                __syncthreads();
+            }
         }
-    } else {
+    } else {                                                      // NU is 1: the tokens side by side, in a wavefront and then among them
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            for (int s = m.lpt; s < 64; s <<= 1) dw[0][i] += __shfl_xor(dw[0][i], s, kWave);
         for (int v = 0; v < 4; ++v) {
-            if (wave == v)
+            if (wave == v && lane < m.lpt && which[0] < 2)
 #pragma unroll
-                for (int u = 0; u < NU; ++u)
-                    if (which[u] < 2)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) part[(which[u] ? width0 : 0) + off[u] + (i < 8 ? i : m.hi + i - 8)] += dw[u][i];
+                for (int i = 0; i < 16; ++i) part[(which[0] ? width0 : 0) + off[0] + (i < 8 ? i : m.hi + i - 8)] += dw[0][i];
             __syncthreads();
         }
     }
-    for (int i = threadIdx.x; i < width; i += kThreads) a.part[(size_t)blockIdx.x * width + i] = part[i];
+    for (int i = threadIdx.x; i < width; i += kThreads) to[i] = part[i];
 }
 
 // Weights' gradients: 16 columns to a workgroup, the workgroups' parts in 16 groups added in order.
@@ -394,7 +459,13 @@ __global__ __launch_bounds__(256) void rope_dw_kernel(RopeArgs a, int parts, int
     __shared__ float sums[16][17];
     const int c = threadIdx.x & 15, g = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
     float s = 0.f;
-    for (int p = g; p < parts; p += 16) s += a.part[(size_t)p * width + col];
+    for (int p0 = g; p0 < parts; p0 += 128) {                     // eight on their way at a time
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = p0 + 16 * i < parts ? a.part[(size_t)(p0 + 16 * i) * width + col] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s += v[i];
+    }
     sums[g][c] = s;
     __syncthreads();
     if (g > 0) return;
@@ -405,54 +476,71 @@ __global__ __launch_bounds__(256) void rope_dw_kernel(RopeArgs a, int parts, int
     if (to != nullptr) to[col < width0 ? col : col - width0] = s;
 }
 
-// Wavefronts to a token and units to a lane: one wavefront while five units do.
-struct Shape { int wpt, nu; };
-Shape shape_of(int units)
+// How tokens are dealt: lanes to a token, units to a lane, tokens of a lane at a time.
+struct Shape { int lpt, nu, tok; };
+Shape shape_of(int units, bool f32)
 {
-    if (units <= 320) return {1, units <= 64 ? 1 : units <= 128 ? 2 : units <= 192 ? 3 : 5};
-    return {4, units <= 512 ? 2 : units <= 768 ? 3 : 6};
+    int lpt = 16;                                                 // (fewer would want more LDS for the turns of more tokens)
+    while (lpt < units && lpt < kThreads) lpt <<= 1;
+    const int nu = units <= kThreads ? 1 : units <= 2 * kThreads ? 2 : units <= 3 * kThreads ? 3 : 6;
+    return {lpt, nu, nu == 1 ? (f32 || lpt == 16 ? 2 : 4) : nu == 2 ? (f32 ? 1 : 2) : 1};
 }
 
-template <class T, bool BWD>
-hipError_t launch_shape(const RopeArgs &a, dim3 grid, unsigned lds, hipStream_t stream)
+template <class T, int NORM, bool HALVES, bool BWD>
+hipError_t launch_shape(const RopeArgs &a, const Shape &s, dim3 grid, unsigned lds, hipStream_t stream)
 {
-    const Shape s = shape_of((a.heads[0] + a.heads[1]) * (a.D / 16));
-#define ARL2_ROPE(NU, WPT) launch_kernel_lds(BWD ? rope_bwd_kernel<T, NU, WPT> : rope_kernel<T, NU, WPT>, grid, dim3(kThreads), lds, stream, a)
-    if (s.wpt == 1) return s.nu == 1 ? ARL2_ROPE(1, 1) : s.nu == 2 ? ARL2_ROPE(2, 1) : s.nu == 3 ? ARL2_ROPE(3, 1) : ARL2_ROPE(5, 1);
-    return s.nu == 2 ? ARL2_ROPE(2, 4) : s.nu == 3 ? ARL2_ROPE(3, 4) : ARL2_ROPE(6, 4);
+    constexpr bool f32 = std::is_same<T, float>::value;
+#define ARL2_ROPE(NU, TOK) launch_kernel_lds(BWD ? rope_bwd_kernel<T, NORM, HALVES, NU, TOK> : rope_kernel<T, NORM, HALVES, NU, TOK>, grid, dim3(kThreads), lds, stream, a, s.lpt)
+    return s.tok == 4 ? ARL2_ROPE(1, f32 ? 2 : 4) : s.nu == 1 ? ARL2_ROPE(1, 2) : s.nu == 2 ? ARL2_ROPE(2, f32 ? 1 : 2) : s.nu == 3 ? ARL2_ROPE(3, 1) : ARL2_ROPE(6, 1);
 #undef ARL2_ROPE
 }
-
-int workgroups(int B, int L, int units, int most)
+template <class T, bool BWD>
+hipError_t launch_norm(const RopeArgs &a, const Shape &s, dim3 grid, unsigned lds, hipStream_t stream)
 {
-    const long long tokens = (long long)B * L, n = shape_of(units).wpt == 1 ? (tokens + 3) / 4 : tokens;
-    return (int)(n < most ? n : most);
+    if (a.halves)
+        return a.norm == kNormNone ? launch_shape<T, kNormNone, true, BWD>(a, s, grid, lds, stream)
+             : a.norm == kNormHead ? launch_shape<T, kNormHead, true, BWD>(a, s, grid, lds, stream) : launch_shape<T, kNormRow, true, BWD>(a, s, grid, lds, stream);
+    return a.norm == kNormNone ? launch_shape<T, kNormNone, false, BWD>(a, s, grid, lds, stream)
+         : a.norm == kNormHead ? launch_shape<T, kNormHead, false, BWD>(a, s, grid, lds, stream) : launch_shape<T, kNormRow, false, BWD>(a, s, grid, lds, stream);
+}
+template <bool BWD>
+hipError_t launch_any(const RopeArgs &a, const Shape &s, int grid, hipStream_t stream)
+{
+    // the turns of two rounds; at the end the weights' gradients of a workgroup: 2 D of them, or (several tokens side by side) at most 2048
+    const int width = a.norm == kNormHead ? 2 * a.D : s.lpt < kThreads ? (a.heads[0] + a.heads[1]) * a.D : 0;
+    const unsigned lds = (unsigned)std::max<size_t>(2 * (kThreads / s.lpt) * s.tok * 64 * sizeof(f32x2), BWD ? width * sizeof(float) : 0);
+    return a.f32 ? launch_norm<float, BWD>(a, s, dim3(grid), lds, stream) : launch_norm<bf16_t, BWD>(a, s, dim3(grid), lds, stream);
+}
+
+int workgroups(int B, int L, const Shape &s, int most)
+{
+    const long long at_a_time = (long long)(kThreads / s.lpt) * s.tok, n = ((long long)B * L + at_a_time - 1) / at_a_time;
+    const long long rounds = (n + most - 1) / most;
+    return (int)((n + rounds - 1) / rounds);                      // (as many tokens for each as can be)
 }
 
 }  // namespace
 
-int rope_workgroups(int B, int L, int D, int heads) { return workgroups(B, L, heads * (D / 16), kGradWorkgroups); }
-
 size_t rope_workspace_bytes(int B, int L, int D, int heads)
 {
-    return (((size_t)rope_workgroups(B, L, D, heads) * heads * D * sizeof(float)) + 255) & ~(size_t)255;
+    // (fp32 rows have the more workgroups: fewer tokens at a time)
+    const size_t n = (size_t)workgroups(B, L, shape_of(heads * (D / 16), true), kGradWorkgroups);
+    return (n * heads * D * sizeof(float) + 255) & ~(size_t)255;
 }
 
 hipError_t launch_rope(const RopeArgs &a, hipStream_t stream)
 {
-    const dim3 grid(workgroups(a.B, a.L, (a.heads[0] + a.heads[1]) * (a.D / 16), kMostWorkgroups));
-    return a.f32 ? launch_shape<float, false>(a, grid, 0, stream) : launch_shape<bf16_t, false>(a, grid, 0, stream);
+    const Shape s = shape_of((a.heads[0] + a.heads[1]) * (a.D / 16), a.f32);
+    return launch_any<false>(a, s, workgroups(a.B, a.L, s, kMostWorkgroups), stream);
 }
 
 hipError_t launch_rope_bwd(const RopeArgs &a, hipStream_t stream)
 {
-    const int n = rope_workgroups(a.B, a.L, a.D, a.heads[0] + a.heads[1]);
-    const bool weights = a.norm != kNormNone && (a.dw[0] != nullptr || a.dw[1] != nullptr);
+    const Shape s = shape_of((a.heads[0] + a.heads[1]) * (a.D / 16), a.f32);
+    const int n = workgroups(a.B, a.L, s, kGradWorkgroups);
+    const hipError_t e = launch_any<true>(a, s, n, stream);
+    if (e != hipSuccess || a.norm == kNormNone || (a.dw[0] == nullptr && a.dw[1] == nullptr)) return e;
     const int width0 = a.norm == kNormHead ? a.D : a.heads[0] * a.D, width = a.norm == kNormHead ? 2 * a.D : (a.heads[0] + a.heads[1]) * a.D;
-    const bool direct = a.norm == kNormRow && shape_of((a.heads[0] + a.heads[1]) * (a.D / 16)).wpt > 1;
-    const unsigned lds = weights && !direct ? (unsigned)(width * sizeof(float)) : 0;        // 20 KB at the most
-    const hipError_t e = a.f32 ? launch_shape<float, true>(a, dim3(n), lds, stream) : launch_shape<bf16_t, true>(a, dim3(n), lds, stream);
-    if (e != hipSuccess || !weights) return e;
     return launch_kernel(rope_dw_kernel, dim3(width / 16), dim3(256), stream, a, n, width0, width);
 }
 
