@@ -20,7 +20,6 @@ namespace arl2 {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMostWorkgroups = 4096;
 constexpr int kGradWorkgroups = 768;
 
 template <class T> struct Raw;                    // 8 features as they lie in memory
@@ -151,7 +150,7 @@ __device__ __forceinline__ void token_sums(float (*x)[N], const Lane &m, float (
 }
 
 // Cosines and sines of all pairs of `tokens` tokens from `first` on, by all threads; a barrier has to follow.
-__device__ __forceinline__ void turns_of(const RopeArgs &a, long long first, long long all, int tokens, f32x2 (*turns)[64])
+__device__ __forceinline__ void turns_of(const RopeArgs &a, uint32_t first, uint32_t all, int tokens, f32x2 (*turns)[64])
 {
     const int half = a.D / 2;
     for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
@@ -159,7 +158,7 @@ __device__ __forceinline__ void turns_of(const RopeArgs &a, long long first, lon
         if (first + t >= all) break;
         float c = 1.f, s = 0.f;
         if (pair < a.pairs) {
-            const size_t at = a.pos_per_stream ? (size_t)(first + t) : (size_t)((first + t) % a.L);
+            const size_t at = a.pos_per_stream ? first + t : (first + t) % (uint32_t)a.L;
             const double turn = (double)a.pos[at * a.axes + a.axis[pair]] * a.turns[pair];
             sincospif(2.f * (float)(turn - ::rint(turn)), &s, &c);
         }
@@ -167,16 +166,16 @@ __device__ __forceinline__ void turns_of(const RopeArgs &a, long long first, lon
     }
 }
 // Is there such a token (of a sequence that goes so far)?
-__device__ __forceinline__ bool token_there(const RopeArgs &a, long long t, long long all)
+__device__ __forceinline__ bool token_there(const RopeArgs &a, uint32_t t, uint32_t all)
 {
     if (t >= all) return false;
     if (a.len == nullptr) return true;
-    const int b = (int)(t / a.L);
-    return (int)(t - (long long)b * a.L) < a.len[b];
+    const uint32_t b = t / (uint32_t)a.L;
+    return (int)(t - b * a.L) < a.len[b];
 }
 
-// 1 over the root of the mean square.
-__device__ __forceinline__ float inverse_rms(float squares, int n, float eps) { return 1.f / sqrtf(squares / (float)n + eps); }
+// 1 over the root of the mean square; `over`: 1 over the number of features.
+__device__ __forceinline__ float inverse_rms(float squares, float over, float eps) { return fast_rsqrt(fmaf(squares, over, eps)); }
 
 template <class T, int NORM, bool HALVES, int NU, int TOK>
 __global__ __launch_bounds__(kThreads, NU == 1 ? 4 : NU <= 3 ? 3 : 2) void rope_kernel(RopeArgs a, int lpt)
@@ -195,14 +194,15 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 4 : NU <= 3 ? 3 : 2) void rope_
         weighted[u] = NORM != kNormNone && which[u] < 2 && a.w[which[u]] != nullptr;
         if (weighted[u]) w[u] = load_unit((const T *)a.w[which[u]] + (NORM == kNormHead ? m.at : off[u]), m.hi);
     }
-    const long long all = (long long)a.B * a.L;
+    const uint32_t all = (uint32_t)a.B * a.L;                     // (2e9 at the most: no step past it wraps around)
+    const float over_head = 1.f / (float)a.D, over_row[2] = {1.f / (float)(a.heads[0] * a.D), 1.f / (float)(max(a.heads[1], 1) * a.D)};
     int round = 0;
-    for (long long t0 = (long long)blockIdx.x * at_a_time; t0 < all; t0 += (long long)gridDim.x * at_a_time, round ^= 1) {
+    for (uint32_t t0 = blockIdx.x * at_a_time; t0 < all; t0 += gridDim.x * at_a_time, round ^= 1) {
         bool there[TOK];
         Unit<T> x[TOK][NU];
 #pragma unroll
         for (int t = 0; t < TOK; ++t) {
-            const long long tok = t0 + m.slot * TOK + t;
+            const uint32_t tok = t0 + m.slot * TOK + t;
             there[t] = token_there(a, tok, all);
 #pragma unroll
             for (int u = 0; u < NU; ++u)
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 4 : NU <= 3 ? 3 : 2) void rope_
             const f32x2 *const turn = &mine[m.slot * TOK + t][8 * m.in_head];
             if constexpr (NORM == kNormRow)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) row[t][i] = inverse_rms(row[t][i], a.heads[i] * a.D, a.eps);
+                for (int i = 0; i < 2; ++i) row[t][i] = inverse_rms(row[t][i], over_row[i], a.eps);
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
                 float r = 1.f, y[16];
@@ -240,7 +240,7 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 4 : NU <= 3 ? 3 : 2) void rope_
                     float s = 0.f;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) { const float f = feature(x[t][u], i); s = fmaf(f, f, s); }
-                    r = inverse_rms(head_sum(s, m.upt), a.D, a.eps);
+                    r = inverse_rms(head_sum(s, m.upt), over_head, a.eps);
                 } else if constexpr (NORM == kNormRow) r = which[u] == 1 ? row[t][1] : row[t][0];
                 forget(x[t][u]);
                 if (NORM != kNormNone) forget(w[u]);
@@ -286,14 +286,15 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 3 : 2) void rope_bwd_kernel(Rop
         weighted[u] = NORM != kNormNone && which[u] < 2 && a.w[which[u]] != nullptr;
         if (weighted[u]) w[u] = load_unit((const T *)a.w[which[u]] + (NORM == kNormHead ? m.at : off[u]), m.hi);
     }
-    const long long all = (long long)a.B * a.L;
+    const uint32_t all = (uint32_t)a.B * a.L;                     // (2e9 at the most: no step past it wraps around)
+    const float over_head = 1.f / (float)a.D, over_row[2] = {1.f / (float)(a.heads[0] * a.D), 1.f / (float)(max(a.heads[1], 1) * a.D)};
     int round = 0;
-    for (long long t0 = (long long)blockIdx.x * at_a_time; t0 < all; t0 += (long long)gridDim.x * at_a_time, round ^= 1) {
+    for (uint32_t t0 = blockIdx.x * at_a_time; t0 < all; t0 += gridDim.x * at_a_time, round ^= 1) {
         bool there[TOK];
         Unit<T> x[TOK][NU], d[TOK][NU];
 #pragma unroll
         for (int t = 0; t < TOK; ++t) {
-            const long long tok = t0 + m.slot * TOK + t;
+            const uint32_t tok = t0 + m.slot * TOK + t;
             there[t] = token_there(a, tok, all);
 #pragma unroll
             for (int u = 0; u < NU; ++u)
@@ -359,8 +360,8 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 3 : 2) void rope_bwd_kernel(Rop
             if constexpr (NORM == kNormRow)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    row[t][i] = inverse_rms(row[t][i], a.heads[i] * a.D, a.eps);
-                    row[t][2 + i] *= row[t][i] / (float)(a.heads[i] * a.D);
+                    row[t][i] = inverse_rms(row[t][i], over_row[i], a.eps);
+                    row[t][2 + i] *= row[t][i] * over_row[i];
                 }
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
@@ -368,8 +369,8 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 3 : 2) void rope_bwd_kernel(Rop
                 if constexpr (NORM == kNormHead) {
                     float s;
                     sums(t, u, turn, s, p);
-                    r = inverse_rms(head_sum(s, m.upt), a.D, a.eps);
-                    p = head_sum(p, m.upt) * r / (float)a.D;
+                    r = inverse_rms(head_sum(s, m.upt), over_head, a.eps);
+                    p = head_sum(p, m.upt) * r * over_head;
                 } else if constexpr (NORM == kNormRow) {
                     r = which[u] == 1 ? row[t][1] : row[t][0];
                     p = which[u] == 1 ? row[t][3] : row[t][2];
@@ -478,12 +479,12 @@ __global__ __launch_bounds__(256) void rope_dw_kernel(RopeArgs a, int parts, int
 
 // How tokens are dealt: lanes to a token, units to a lane, tokens of a lane at a time.
 struct Shape { int lpt, nu, tok; };
-Shape shape_of(int units, bool f32)
+Shape shape_of(int units, bool f32, bool bwd)
 {
     int lpt = 16;                                                 // (fewer would want more LDS for the turns of more tokens)
     while (lpt < units && lpt < kThreads) lpt <<= 1;
     const int nu = units <= kThreads ? 1 : units <= 2 * kThreads ? 2 : units <= 3 * kThreads ? 3 : 6;
-    return {lpt, nu, nu == 1 ? (f32 || lpt == 16 ? 2 : 4) : nu == 2 ? (f32 ? 1 : 2) : 1};
+    return {lpt, nu, nu == 1 ? (bwd && !f32 && lpt > 16 ? 4 : 2) : nu == 2 ? (f32 ? 1 : 2) : 1};
 }
 
 template <class T, int NORM, bool HALVES, bool BWD>
@@ -491,7 +492,7 @@ hipError_t launch_shape(const RopeArgs &a, const Shape &s, dim3 grid, unsigned l
 {
     constexpr bool f32 = std::is_same<T, float>::value;
 #define ARL2_ROPE(NU, TOK) launch_kernel_lds(BWD ? rope_bwd_kernel<T, NORM, HALVES, NU, TOK> : rope_kernel<T, NORM, HALVES, NU, TOK>, grid, dim3(kThreads), lds, stream, a, s.lpt)
-    return s.tok == 4 ? ARL2_ROPE(1, f32 ? 2 : 4) : s.nu == 1 ? ARL2_ROPE(1, 2) : s.nu == 2 ? ARL2_ROPE(2, f32 ? 1 : 2) : s.nu == 3 ? ARL2_ROPE(3, 1) : ARL2_ROPE(6, 1);
+    return s.tok == 4 ? ARL2_ROPE(1, f32 || !BWD ? 2 : 4) : s.nu == 1 ? ARL2_ROPE(1, 2) : s.nu == 2 ? ARL2_ROPE(2, f32 ? 1 : 2) : s.nu == 3 ? ARL2_ROPE(3, 1) : ARL2_ROPE(6, 1);
 #undef ARL2_ROPE
 }
 template <class T, bool BWD>
@@ -524,19 +525,22 @@ int workgroups(int B, int L, const Shape &s, int most)
 size_t rope_workspace_bytes(int B, int L, int D, int heads)
 {
     // (fp32 rows have the more workgroups: fewer tokens at a time)
-    const size_t n = (size_t)workgroups(B, L, shape_of(heads * (D / 16), true), kGradWorkgroups);
+    const size_t n = (size_t)workgroups(B, L, shape_of(heads * (D / 16), true, true), kGradWorkgroups);
     return (n * heads * D * sizeof(float) + 255) & ~(size_t)255;
 }
 
 hipError_t launch_rope(const RopeArgs &a, hipStream_t stream)
 {
-    const Shape s = shape_of((a.heads[0] + a.heads[1]) * (a.D / 16), a.f32);
-    return launch_any<false>(a, s, workgroups(a.B, a.L, s, kMostWorkgroups), stream);
+    const Shape s = shape_of((a.heads[0] + a.heads[1]) * (a.D / 16), a.f32, false);
+    // Without weights to load a workgroup takes one round of tokens; else 4 x 10920 tokens of 32 + 8 heads x 128 (two units a lane) took 196, 209, 221 us
+    // with at most 1024, 4096 and any number of workgroups, 7 x 4680 tokens of 12 + 12 heads (one unit) 101, 90, 97 us.
+    const int most = a.norm == kNormNone ? 1 << 30 : s.nu == 1 ? 4096 : 1024;
+    return launch_any<false>(a, s, workgroups(a.B, a.L, s, most), stream);
 }
 
 hipError_t launch_rope_bwd(const RopeArgs &a, hipStream_t stream)
 {
-    const Shape s = shape_of((a.heads[0] + a.heads[1]) * (a.D / 16), a.f32);
+    const Shape s = shape_of((a.heads[0] + a.heads[1]) * (a.D / 16), a.f32, true);
     const int n = workgroups(a.B, a.L, s, kGradWorkgroups);
     const hipError_t e = launch_any<true>(a, s, n, stream);
     if (e != hipSuccess || a.norm == kNormNone || (a.dw[0] == nullptr && a.dw[1] == nullptr)) return e;
