@@ -9,6 +9,11 @@
 //   row_t = r_t (X_t T + sum_{s <= t} (X_t . Y_s) Z_s / r_s),        T <- 2^(c_end) (T + sum_s Y_s^T Z_s / r_s)
 //   out: X, Y, Z = q', k', v        dq': dout, v, k', the state transposed
 //   and backwards in time (r_t = 2^(c_end - c_t), s >= t):    dv: k', q', dout        dk': v, dout, q', the state transposed
+// E by the same blocks: with G_ts = 2^(c_t - c_s) (q'_t . k'_s)(dout_t . v_s) for s < t in a block, a_t the part of q'_t . dq'_t that comes from the state, b_t
+// that of k'_t . dk'_t,
+//   E_t = E_{t+1} + a_t - b_t + sum_s G_ts - sum_u G_ut:
+// a pair's product goes in and out again as one fp32 value.  (q'.dq' - k'.dk' of the rows would do it too, but each holds that product rounded in its own way,
+// and E is small against it where the memory is short: one head with gates of 0.8, 1024 tokens: E was off by 2.1e-5 in the 2-norm.)
 // The state is held without the factor 2^(base + c_end) that its blocks so far have gathered: c counts on from block to block (as `base`), and
 // only where it has run below -32 is the state multiplied by it, and c begins anew.  Where it runs below -64 in a block (gates of zero among
 // them) 1 / r_s would leave the range: such a block's products take their decays 2^(c_t - c_s) pair by pair.
@@ -22,12 +27,12 @@ constexpr int kBlock = 64;                    // tokens
 constexpr int kStepTokens = 8;
 constexpr double kLog2e = 1.4426950408889634;
 
-enum Mode { kOut, kDq, kDk, kDv, kSum, kSumBack };       // the last two make states and no rows
+enum Mode { kOut, kDq, kBack, kSum, kSumBack };          // kBack: dk and dv; the last two make states and no rows
 
 // One call's arrays in the workspace: states [B*H][nseg + 1][D][D], the way forth (state i: what segment i begins with) and back
-// (state i: the gradient of what segment i - 1 ends with), the segments' decays, and q'.dq', k'.dk' [B*H][L].
+// (state i: the gradient of what segment i - 1 ends with), the segments' decays, and a_t, b_t and G's part of E [B*H][L].
 struct Work {
-    float *forth, *back, *decay_forth, *decay_back, *qq, *kk;
+    float *forth, *back, *decay_forth, *decay_back, *a, *b;
     int nseg, seg;
 };
 
@@ -54,8 +59,9 @@ struct Scalars {
     float fold[2];                                        // what the state is multiplied with before they do; 1: it is left
     int pairs[2];                                         // products take their decays pair by pair
     // with the norms of the rows
-    float post[kBlock], pcol[kBlock], penter[kBlock], norm[kBlock];
-    float red[4][kBlock][2];
+    float post[kBlock], unit[kBlock], pcol[kBlock], penter[kBlock], norm[kBlock];
+    float red[4][kBlock][3];
+    float later[3][32], earlier[3][32];                   // of the 32 x 32 pairs of a block: sums of G over s, over u
 };
 
 __device__ __forceinline__ int tokens_of(const ScanArgs &a, int b)
@@ -109,20 +115,43 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t &hi, uint3
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mfma(u32x4 a, bf16x8 b, f32x16 c) { return mfma(__builtin_bit_cast(bf16x8, a), b, c); }
 
+// Sums over the 32 lanes of a half-wave of each of 16 registers: lane l receives that of register l % 16.
+__device__ __forceinline__ float lanes_sums(float (&v)[16], int lane)
+{
+    auto halve = [&](auto ctrl, int n, bool upper) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float keep = upper ? v[i + n] : v[i], send = upper ? v[i] : v[i + n];
+            v[i] = keep + dpp_peek<decltype(ctrl)::value>(send);
+        }
+    };
+    halve(std::integral_constant<int, 0x140>{}, 8, lane & 8);          // row_mirror: lane 15 - l
+    halve(std::integral_constant<int, 0x141>{}, 4, lane & 4);          // row_half_mirror: 7 - l of the 8
+    halve(std::integral_constant<int, 0x1B>{}, 2, lane & 2);           // quad_perm [3,2,1,0]
+    halve(std::integral_constant<int, 0xB1>{}, 1, lane & 1);           // quad_perm [1,0,3,2]
+    return v[0] + __shfl_xor(v[0], 16, kWave);
+}
+
 template <int D, int MODE>
 struct Walk {
     using C = Cfg<D>;
-    static constexpr bool REV = MODE == kDk || MODE == kDv || MODE == kSumBack;
+    static constexpr bool REV = MODE == kBack || MODE == kSumBack;
     static constexpr bool ROWS = MODE != kSum && MODE != kSumBack;
-    static constexpr bool TRANSPOSED = MODE == kDq || MODE == kDk;
-    static constexpr bool GRAD = MODE == kDq || MODE == kDk;      // the normalisation's gradient at the end
-    static constexpr bool SPLIT = MODE != kOut;                   // products of rows in two parts: their sums with q and k meet in E
-    static constexpr int LDS_ROWS = (ROWS ? 3 : 2) * C::MAT + (ROWS ? (SPLIT ? 2 : 1) * C::PMAT : 0);
+    static constexpr bool BOTH = MODE == kBack;                   // two groups of wavefronts: dv, and dk
+    static constexpr int NT = (BOTH ? 2 : 1) * C::NT;
+    static constexpr int ROUND = NT / C::LPR, ROUNDS = kBlock / ROUND;       // rows that the threads stage at a time
+    static constexpr int MATS = BOTH ? 4 : ROWS ? 3 : 2;
+    // products: as rows of X in bf16, one or two such arrays; with two, those of dout and v as they are
+    static constexpr int PAIR = 64 * 16 * 4;                      // bytes of 32 x 32 of them in fp32
+    static constexpr int LDS_ROWS = MATS * C::MAT + (BOTH ? 2 * C::PMAT + 3 * PAIR : ROWS ? C::PMAT : 0);
 
     // `lds`: LDS_ROWS bytes.  Segment `seg` of (stream, head) bh.
     static __device__ __forceinline__ void run(const ScanArgs &a, const Work &wk, int bh, int seg, unsigned char *lds, Scalars &sc)
     {
-        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, hh = lane >> 5;
+        const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
+        const int all_wave = __builtin_amdgcn_readfirstlane(tid >> 6), wave = BOTH ? all_wave % C::NW : all_wave;
+        const bool dk = BOTH && all_wave >= C::NW;                // the second group
+        const bool grad = MODE == kDq || dk;                      // rows through the normalisation
         const int b = bh / a.H, h = bh - b * a.H;
         const int n = tokens_of(a, b);
         const int nblk = (n + kBlock - 1) / kBlock;
@@ -133,57 +162,64 @@ struct Walk {
         const uint32_t rs = (uint32_t)a.H * D * 2;                // bytes from token to token
         const size_t stream = (size_t)b * a.L * rs;
         const uint32_t range = (uint32_t)n * rs;
-        const void *px = MODE == kOut ? a.q : MODE == kDq ? a.dout : MODE == kDk ? a.v : a.k;
-        const void *py = MODE == kOut || MODE == kSum ? a.k : MODE == kDq ? a.v : MODE == kDk ? a.dout : a.q;
-        const void *pz = MODE == kOut || MODE == kSum ? a.v : MODE == kDq ? a.k : MODE == kDk ? a.q : a.dout;
-        const auto rx = make_rsrc((const char *)px + stream, range), ry = make_rsrc((const char *)py + stream, range),
-                   rz = make_rsrc((const char *)pz + stream, range);
+        auto rows_of = [&](const void *p) { return make_rsrc((const char *)p + stream, range); };
+        // the arrays as they lie in LDS; kBack: k, q, v, dout
+        const void *const in[4] = {MODE == kOut ? a.q : MODE == kDq ? a.dout : a.k, MODE == kDq ? a.v : REV ? a.q : a.k, MODE == kDq ? a.k : MODE == kSumBack ? a.dout : a.v, a.dout};
+        constexpr int IN0 = ROWS ? 0 : 1;                         // states alone need the second and third
+        const auto r0 = rows_of(in[0]), r1 = rows_of(in[1]), r2 = rows_of(in[2]), r3 = rows_of(in[3]);
         const auto rla = make_rsrc(a.la + (a.la ? (size_t)b * a.L * a.H : 0), a.la ? (uint32_t)n * a.H * 4 : 0);
 
-        unsigned char *const lx = lds, *const ly = lds + (ROWS ? C::MAT : 0), *const lz = ly + C::MAT, *const lp = lz + C::MAT;
+        unsigned char *const m1 = lds + (ROWS ? C::MAT : 0), *const m2 = m1 + C::MAT, *const m3 = m2 + C::MAT, *const products = lds + MATS * C::MAT;
+        const unsigned char *const lx = dk ? m2 : lds, *const ly = dk ? m3 : m1, *const lz = BOTH ? (dk ? m1 : m3) : m2;
+        unsigned char *const lp = products + (dk ? C::PMAT : 0), *const raw = products + 2 * C::PMAT;
 
         // ---- the state: 32 columns of each wavefront, register j of tile t is row 32 t + 16 (j / 8) + 8 hh + j % 8
         f32x16 st[D / 32];
         const int e0 = 32 * wave;
         {
             const float *from = nullptr;
-            if (ROWS) {
-                if (MODE == kOut) from = wk.nseg == 1 ? (a.S0 ? a.S0 + (size_t)bh * D * D : nullptr) : wk.forth + ((size_t)bh * (wk.nseg + 1) + seg) * D * D;
-                else if (MODE == kDq) from = wk.forth + ((size_t)bh * (wk.nseg + 1) + seg) * D * D;
-                else from = wk.back + ((size_t)bh * (wk.nseg + 1) + seg + 1) * D * D;
+            if (MODE == kOut) from = wk.nseg == 1 ? (a.S0 ? a.S0 + (size_t)bh * D * D : nullptr) : wk.forth + ((size_t)bh * (wk.nseg + 1) + seg) * D * D;
+            if (MODE == kDq) from = wk.forth + ((size_t)bh * (wk.nseg + 1) + seg) * D * D;
+            if (MODE == kBack) from = wk.back + ((size_t)bh * (wk.nseg + 1) + seg + 1) * D * D;
+            if (from == nullptr) {
+#pragma unroll
+                for (int t = 0; t < D / 32; ++t) st[t] = f32x16{};
+            } else if (grad) {                                    // transposed
+#pragma unroll
+                for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                    for (int j = 0; j < 16; j += 4) {
+                        const f32x4 x = *reinterpret_cast<const f32x4 *>(from + (size_t)(e0 + l32) * D + 32 * t + 16 * (j / 8) + 8 * hh + j % 8);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) st[t][j + i] = x[i];
+                    }
+            } else {
+#pragma unroll
+                for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) st[t][j] = from[(size_t)(32 * t + 16 * (j / 8) + 8 * hh + j % 8) * D + e0 + l32];
             }
-#pragma unroll
-            for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    if (from == nullptr) { st[t][j] = 0.f; continue; }
-                    const int row = 32 * t + 16 * (j / 8) + 8 * hh + j % 8;
-                    if (TRANSPOSED) {
-                        if (j % 4 == 0) {
-                            const f32x4 x = *reinterpret_cast<const f32x4 *>(from + (size_t)(e0 + l32) * D + row);
-                            st[t][j] = x[0]; st[t][j + 1] = x[1]; st[t][j + 2] = x[2]; st[t][j + 3] = x[3];
-                        }
-                    } else st[t][j] = from[(size_t)row * D + e0 + l32];
-                }
         }
 
-        // ---- a block's rows on their way through registers: 16-byte pieces, four of each array
+        // ---- a block's rows on their way through registers, in 16-byte pieces
         const uint32_t piece0 = (uint32_t)(tid / C::LPR) * rs + (uint32_t)h * D * 2 + (tid % C::LPR) * 16;
-        u32x4 gx[4], gy[4], gz[4];
+        u32x4 g0[ROUNDS], g1[ROUNDS], g2[ROUNDS], g3[ROUNDS];
         float gla;
         auto fetch = [&](int blk) {
             const uint32_t o = piece0 + (uint32_t)blk * kBlock * rs;
+            auto piece = [&](__amdgpu_buffer_rsrc_t r, int i) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, o + (uint32_t)(ROUND * i) * rs, 0, 0)); };
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (ROWS) gx[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, o + 16u * i * rs, 0, 0));
-                gy[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ry, o + 16u * i * rs, 0, 0));
-                gz[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rz, o + 16u * i * rs, 0, 0));
+            for (int i = 0; i < ROUNDS; ++i) {
+                if (IN0 == 0) g0[i] = piece(r0, i);
+                g1[i] = piece(r1, i);
+                g2[i] = piece(r2, i);
+                if (BOTH) g3[i] = piece(r3, i);
             }
         };
         auto fetch_gate = [&](int blk) {
             gla = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rla, ((uint32_t)(blk * kBlock + lane) * a.H + h) * 4u, 0, 0));
         };
-        double seg_total = 0.0, base = 0.0;                       // (of the wavefront that does this; base is whole)
+        double seg_total = 0.0, base = 0.0;                       // (of the wavefront that does this)
         auto gates = [&](int buf) {
             const double c = wave_prefix(log2_gate(gla));
             const unsigned long long u = __builtin_bit_cast(unsigned long long, c);
@@ -207,8 +243,8 @@ struct Walk {
         // rows of one array to LDS; `kind` 1: its norms go with the rows that ask, 2: with those that make the state
         auto stage = [&](const u32x4 *g, unsigned char *to, int kind, int buf) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int row = 16 * i + tid / C::LPR;
+            for (int i = 0; i < ROUNDS; ++i) {
+                const int row = ROUND * i + tid / C::LPR;
                 *reinterpret_cast<u32x4 *>(to + row * C::ROW + (tid % C::LPR) * 16) = g[i];
                 if (kind) {
                     float x = 0.f;
@@ -220,8 +256,10 @@ struct Walk {
                     x = lane_group_sum<C::LPR>(x);
                     x = a.normalise ? fast_rsqrt(x + a.eps) : 1.f;
                     if (tid % C::LPR == 0) {
-                        if (kind == 1) sc.post[row] = sc.pairs[buf] ? x : x * sc.row[buf][row];
-                        else {
+                        if (kind == 1) {
+                            sc.post[row] = sc.pairs[buf] ? x : x * sc.row[buf][row];
+                            sc.unit[row] = x;
+                        } else {
                             sc.pcol[row] = x * sc.col[buf][row];
                             sc.penter[row] = x * sc.enter[buf][row];
                             sc.norm[row] = x;
@@ -233,19 +271,20 @@ struct Walk {
 
         const int count = blk1 - blk0;
         auto block_at = [&](int i) { return REV ? blk1 - 1 - i : blk0 + i; };
-        constexpr int GW = C::NW - 1;                             // the wavefront with the gates: it has fewest products
+        constexpr int GW = NT / 64 - 1;                           // the wavefront with the gates: it has fewest products
         if (count > 0) {
             fetch(block_at(0));
             fetch_gate(block_at(0));
-            if (wave == GW) gates(0);
+            if (all_wave == GW) gates(0);
             if (count > 1) fetch_gate(block_at(1));
             lds_barrier();
         }
         for (int i = 0; i < count; ++i) {
             const int blk = block_at(i), buf = i & 1;
-            if (ROWS) stage(gx, lx, MODE == kOut || MODE == kDv ? 1 : 0, buf);
-            stage(gy, ly, MODE == kDq || MODE == kDk ? 0 : 2, buf);
-            stage(gz, lz, MODE == kDq || MODE == kDk ? 2 : 0, buf);
+            if (IN0 == 0) stage(g0, lds, MODE == kDq ? 0 : 1, buf);
+            stage(g1, m1, MODE == kDq ? 0 : 2, buf);
+            stage(g2, m2, MODE == kDq ? 2 : 0, buf);
+            if (BOTH) stage(g3, m3, 0, buf);
             if (i + 1 < count) fetch(block_at(i + 1));
             const bool pairs = __builtin_amdgcn_readfirstlane(sc.pairs[buf]) != 0;
             lds_barrier();
@@ -258,12 +297,16 @@ struct Walk {
 #pragma unroll
                 for (int m = 0; m < 4; ++m) zf[m] = lds_read_tr_pair(z + 16 * m * C::ROW, 4 * C::ROW);
             }
-            f32x16 acc[2];
+            f32x16 acc[2], p;
             u32x2 own[2][4];                                      // the rows whose normalisation has a gradient
+            float asked[2] = {0.f, 0.f};                          // their products with what the state gives
+            // pairs of 32 x 32 rows: which of Y, which of X
+            auto y_of = [](int t) { return REV ? (int)(t > 0) : (int)(t == 2); };
+            auto x_of = [](int t) { return REV ? (int)(t == 2) : (int)(t > 0); };
             if constexpr (ROWS) {
                 acc[0] = acc[1] = f32x16{};
-                if constexpr (GRAD) {
-                    const auto rg = make_rsrc((const char *)(MODE == kDq ? a.q : a.k) + stream, range);
+                if (MODE == kDq) {
+                    const auto rg = rows_of(a.q);
 #pragma unroll
                     for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
@@ -275,12 +318,16 @@ struct Walk {
                 for (int t0 = 0; t0 < 3; t0 += C::NW) {
                     const int t = t0 + wave;
                     if (t >= 3) break;
-                    const int sb = REV ? (t > 0) : (t == 2), tb = REV ? (t == 2) : (t > 0);
-                    f32x16 p = {};
+                    const int sb = y_of(t), tb = x_of(t);
+                    p = f32x16{};
                     const unsigned char *const y = ly + (32 * sb + l32) * C::ROW + 16 * hh, *const x = lx + (32 * tb + l32) * C::ROW + 16 * hh;
 #pragma unroll
                     for (int m = 0; m < D / 16; ++m)
                         p = mfma(*reinterpret_cast<const bf16x8 *>(y + 32 * m), *reinterpret_cast<const bf16x8 *>(x + 32 * m), p);
+                    if (dk) {
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4 *>(raw + t * PAIR + g * 1024 + lane * 16) = f32x4{p[4 * g], p[4 * g + 1], p[4 * g + 2], p[4 * g + 3]};
+                    }
                     unsigned char *const to = lp + (32 * tb + l32) * C::PROW + 64 * sb;
                     if (!pairs) {
 #pragma unroll
@@ -309,19 +356,8 @@ struct Walk {
                     }
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
-                        u32x2 hi, lo;
-                        if constexpr (SPLIT) {
-                            uint32_t h0, l0, h1, l1;
-                            split_pair(p[4 * g], p[4 * g + 1], h0, l0);
-                            split_pair(p[4 * g + 2], p[4 * g + 3], h1, l1);
-                            hi = u32x2{h0, h1};
-                            lo = u32x2{l0, l1};
-                            *reinterpret_cast<u32x2 *>(to + C::PMAT + 16 * g + 8 * hh) = lo;
-                        } else {
-                            const bf16x4 r = {to_bf16(p[4 * g]), to_bf16(p[4 * g + 1]), to_bf16(p[4 * g + 2]), to_bf16(p[4 * g + 3])};
-                            hi = __builtin_bit_cast(u32x2, r);
-                        }
-                        *reinterpret_cast<u32x2 *>(to + 16 * g + 8 * hh) = hi;
+                        const bf16x4 r = {to_bf16(p[4 * g]), to_bf16(p[4 * g + 1]), to_bf16(p[4 * g + 2]), to_bf16(p[4 * g + 3])};
+                        *reinterpret_cast<bf16x4 *>(to + 16 * g + 8 * hh) = r;
                     }
                 }
                 // ---- rows asked of the state, which is taken in two parts
@@ -346,21 +382,71 @@ struct Walk {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) { acc[0][j] *= f0; acc[1][j] *= f1; }
                 }
+                if (grad) {
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb) {
+                        if (dk)
+#pragma unroll
+                            for (int g = 0; g < 4; ++g) own[tb][g] = *reinterpret_cast<const u32x2 *>(lds + (32 * tb + l32) * C::ROW + 2 * (e0 + 8 * g + 4 * hh));
+                        asked[tb] = dot_of(own[tb], acc[tb]);
+                    }
+                }
             }
-            if (i + 1 < count && wave == GW) gates(buf ^ 1);
+            if (i + 1 < count && all_wave == GW) gates(buf ^ 1);
             if (i + 2 < count) fetch_gate(block_at(i + 2));
             if (ROWS) lds_barrier();
 
             // ---- and of the block's own rows
             if constexpr (ROWS) {
-                const unsigned char *const p = lp + l32 * C::PROW + 16 * hh;
+                const unsigned char *const from = lp + l32 * C::PROW + 16 * hh;
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
-                    for (int m = REV ? 2 * tb : 0; m < (REV ? 4 : 2 + 2 * tb); ++m) {
-                        acc[tb] = mfma(zf[m], *reinterpret_cast<const bf16x8 *>(p + 32 * tb * C::PROW + 32 * m), acc[tb]);
-                        if constexpr (SPLIT) acc[tb] = mfma(zf[m], *reinterpret_cast<const bf16x8 *>(p + C::PMAT + 32 * tb * C::PROW + 32 * m), acc[tb]);
+                    for (int m = REV ? 2 * tb : 0; m < (REV ? 4 : 2 + 2 * tb); ++m)
+                        acc[tb] = mfma(zf[m], *reinterpret_cast<const bf16x8 *>(from + 32 * tb * C::PROW + 32 * m), acc[tb]);
+            }
+            if constexpr (BOTH) {
+                // ---- G: the products of k and q, which are here, times those of dout and v
+                if (!dk && a.dla != nullptr) {
+#pragma unroll
+                    for (int t0 = 0; t0 < 3; t0 += C::NW) {
+                        const int t = t0 + wave;
+                        if (t >= 3) break;
+                        const int sb = y_of(t), tb = x_of(t);
+                        if (C::NW < 3) {                          // (two of them: the other's products are no longer here)
+                            const unsigned char *const y = ly + (32 * sb + l32) * C::ROW + 16 * hh, *const x = lx + (32 * tb + l32) * C::ROW + 16 * hh;
+                            p = f32x16{};
+#pragma unroll
+                            for (int m = 0; m < D / 16; ++m)
+                                p = mfma(*reinterpret_cast<const bf16x8 *>(y + 32 * m), *reinterpret_cast<const bf16x8 *>(x + 32 * m), p);
+                            const float wt = sc.whole[buf][32 * tb + l32], ft = sc.frac[buf][32 * tb + l32];
+#pragma unroll
+                            for (int g = 0; g < 4; ++g) {
+                                const int s0 = 32 * sb + 8 * g + 4 * hh;
+                                const f32x4 f = *reinterpret_cast<const f32x4 *>(&sc.pcol[s0]), ws = *reinterpret_cast<const f32x4 *>(&sc.whole[buf][s0]),
+                                            fs = *reinterpret_cast<const f32x4 *>(&sc.frac[buf][s0]), ys = *reinterpret_cast<const f32x4 *>(&sc.norm[s0]);
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) p[4 * g + j] *= pairs ? ys[j] * __builtin_amdgcn_exp2f((ws[j] - wt) + (fs[j] - ft)) : f[j];
+                            }
+                        }
+                        const float post = sc.post[32 * tb + l32];
+                        float v[16], sum = 0.f;
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const f32x4 w = *reinterpret_cast<const f32x4 *>(raw + t * PAIR + g * 1024 + lane * 16);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const bool strictly = sb != tb || 8 * g + 4 * hh + j > l32;
+                                v[4 * g + j] = strictly ? p[4 * g + j] * w[j] * post : 0.f;
+                                sum += v[4 * g + j];
+                            }
+                        }
+                        sum = xhalf_sum(sum);
+                        if (hh == 0) sc.earlier[t][l32] = sum;
+                        const float of = lanes_sums(v, lane);
+                        if ((lane & 16) == 0) sc.later[t][8 * ((lane & 15) / 4) + 4 * hh + lane % 4] = of;
                     }
+                }
             }
 
             // ---- the state's step: rows of Z times their weights in two parts
@@ -397,42 +483,58 @@ struct Walk {
 
             // ---- rows out
             if constexpr (ROWS) {
-                float scale[2], along[2];
-                if constexpr (GRAD) {
+                float scale[2], along[2] = {0.f, 0.f}, unit[2];
 #pragma unroll
-                    for (int tb = 0; tb < 2; ++tb) {
-                        float dot = 0.f, ss = 0.f;
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const uint32_t w = own[tb][j / 4][(j / 2) % 2];
-                            const float r = __uint_as_float(j % 2 ? w & 0xffff0000u : w << 16);
-                            dot = fmaf(r, acc[tb][j], dot);
-                            ss = fmaf(r, r, ss);
-                        }
-                        dot = xhalf_sum(dot);
-                        ss = xhalf_sum(ss);
-                        if (hh == 0) { sc.red[wave][32 * tb + l32][0] = dot; sc.red[wave][32 * tb + l32][1] = ss; }
-                    }
-                    lds_barrier();
-#pragma unroll
-                    for (int tb = 0; tb < 2; ++tb) {
-                        float dot = 0.f, ss = 0.f;
-#pragma unroll
-                        for (int w = 0; w < C::NW; ++w) { dot += sc.red[w][32 * tb + l32][0]; ss += sc.red[w][32 * tb + l32][1]; }
-                        const float inv = a.normalise ? fast_rsqrt(ss + a.eps) : 1.f, row = pairs ? 1.f : sc.row[buf][32 * tb + l32];
-                        dot *= inv * row;
-                        scale[tb] = inv * row;
-                        along[tb] = a.normalise ? -dot * inv * inv : 0.f;
-                        const int t = blk * kBlock + 32 * tb + l32;
-                        if (wave == 0 && hh == 0 && t < n && a.dla != nullptr) (MODE == kDq ? wk.qq : wk.kk)[(size_t)bh * a.L + t] = dot;
-                    }
-                } else {
-                    scale[0] = sc.post[l32];
-                    scale[1] = sc.post[32 + l32];
-                    lds_barrier();                                // all have read the block's rows
+                for (int tb = 0; tb < 2; ++tb) {
+                    scale[tb] = MODE == kDq ? (pairs ? 1.f : sc.row[buf][32 * tb + l32]) : sc.post[32 * tb + l32];
+                    unit[tb] = MODE == kDq ? 1.f : sc.unit[32 * tb + l32];
                 }
-                void *const po = MODE == kOut ? a.out : MODE == kDq ? a.dq : MODE == kDk ? a.dk : a.dv;
-                const auto ro = make_rsrc((const char *)po + stream, range);
+                if (grad) {
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb) {
+                        const float dot = xhalf_sum(dot_of(own[tb], acc[tb])), from_state = xhalf_sum(asked[tb]);
+                        if (hh == 0) { sc.red[wave][32 * tb + l32][0] = dot; sc.red[wave][32 * tb + l32][1] = from_state; }
+                        if (MODE == kDq) {
+                            float ss = 0.f;
+#pragma unroll
+                            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {
+                                    const float x0 = __uint_as_float(own[tb][g][j] << 16), x1 = __uint_as_float(own[tb][g][j] & 0xffff0000u);
+                                    ss = fmaf(x0, x0, fmaf(x1, x1, ss));
+                                }
+                            ss = xhalf_sum(ss);
+                            if (hh == 0) sc.red[wave][32 * tb + l32][2] = ss;
+                        }
+                    }
+                }
+                lds_barrier();                                    // all have read the block's rows
+                if (grad) {
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb) {
+                        float dot = 0.f, from_state = 0.f, ss = 0.f;
+#pragma unroll
+                        for (int w = 0; w < C::NW; ++w) {
+                            dot += sc.red[w][32 * tb + l32][0];
+                            from_state += sc.red[w][32 * tb + l32][1];
+                            if (MODE == kDq) ss += sc.red[w][32 * tb + l32][2];
+                        }
+                        if (MODE == kDq) {
+                            unit[tb] = a.normalise ? fast_rsqrt(ss + a.eps) : 1.f;
+                            scale[tb] *= unit[tb];
+                        }
+                        along[tb] = a.normalise ? -(dot * scale[tb]) * unit[tb] * unit[tb] : 0.f;
+                        const int t = blk * kBlock + 32 * tb + l32;
+                        if (wave == 0 && hh == 0 && t < n && a.dla != nullptr) {
+                            float e = from_state * scale[tb];
+                            if (BOTH) {
+                                e = tb == 0 ? sc.later[0][l32] - sc.earlier[0][l32] - sc.earlier[1][l32] - e : sc.later[1][l32] + sc.later[2][l32] - sc.earlier[2][l32] - e;
+                            }
+                            (MODE == kDq ? wk.a : wk.b)[(size_t)bh * a.L + t] = e;
+                        }
+                    }
+                }
+                const auto ro = rows_of(MODE == kOut ? a.out : MODE == kDq ? a.dq : dk ? a.dk : a.dv);
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb) {
                     uint32_t w[4][2];
@@ -441,7 +543,7 @@ struct Walk {
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
                             float x0 = acc[tb][4 * g + 2 * j] * scale[tb], x1 = acc[tb][4 * g + 2 * j + 1] * scale[tb];
-                            if constexpr (GRAD) {
+                            if (grad) {
                                 x0 = fmaf(along[tb], __uint_as_float(own[tb][g][j] << 16), x0);
                                 x1 = fmaf(along[tb], __uint_as_float(own[tb][g][j] & 0xffff0000u), x1);
                             }
@@ -478,6 +580,18 @@ struct Walk {
                 for (int j = 0; j < 16; ++j) to[(size_t)(32 * t + 16 * (j / 8) + 8 * hh + j % 8) * D + e0 + l32] = st[t][j] * gathered;
         }
         if (!ROWS && tid == 64 * GW) (MODE == kSum ? wk.decay_forth : wk.decay_back)[(size_t)bh * wk.nseg + seg] = exp2_of(seg_total);
+    }
+
+    // Product of 16 features of a row with the accumulator that lies over them.
+    static __device__ __forceinline__ float dot_of(const u32x2 (&row)[4], const f32x16 &acc)
+    {
+        float dot = 0.f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const uint32_t w = row[j / 4][(j / 2) % 2];
+            dot = fmaf(__uint_as_float(j % 2 ? w & 0xffff0000u : w << 16), acc[j], dot);
+        }
+        return dot;
     }
 };
 
@@ -545,22 +659,26 @@ __global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, Work wk, int
     if (back && a.dS0 != nullptr) *reinterpret_cast<f32x4 *>(a.dS0 + (size_t)bh * nn + e) = x;
 }
 
-// The rows' gradients: three walks of a segment by three workgroups that follow one another.
 template <int D>
-__global__ __launch_bounds__(Cfg<D>::NT, D / 64) void scan_grad_kernel(ScanArgs a, Work wk)
+__global__ __launch_bounds__(Cfg<D>::NT, 2) void scan_dq_kernel(ScanArgs a, Work wk)
 {
-    __shared__ __align__(16) unsigned char lds[Walk<D, kDq>::LDS_ROWS];
+    using W = Walk<D, kDq>;
+    __shared__ __align__(16) unsigned char lds[W::LDS_ROWS];
     __shared__ __align__(16) Scalars sc;
     const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
-    const int unit = id / 3, which = id - 3 * unit;
-    const int bh = unit / wk.nseg, seg = unit % wk.nseg;
-    if (which == 0) Walk<D, kDq>::run(a, wk, bh, seg, lds, sc);
-    else if (which == 1) Walk<D, kDk>::run(a, wk, bh, seg, lds, sc);
-    else Walk<D, kDv>::run(a, wk, bh, seg, lds, sc);
+    W::run(a, wk, id / wk.nseg, id % wk.nseg, lds, sc);
+}
+template <int D>
+__global__ __launch_bounds__(2 * Cfg<D>::NT, 2) void scan_back_kernel(ScanArgs a, Work wk)
+{
+    using W = Walk<D, kBack>;
+    __shared__ __align__(16) unsigned char lds[W::LDS_ROWS];
+    __shared__ __align__(16) Scalars sc;
+    const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
+    W::run(a, wk, id / wk.nseg, id % wk.nseg, lds, sc);
 }
 
-// The gates' gradients of a segment: from <state, gradient of the state> at its end backwards, a sum of q'.dq' - k'.dk' that a gate of
-// zero begins anew.
+// The gates' gradients of a segment: from <state, gradient of the state> at its end backwards, a sum that a gate of zero begins anew.
 __global__ __launch_bounds__(256) void scan_gate_kernel(ScanArgs a, Work wk)
 {
     __shared__ double part[4];
@@ -588,7 +706,7 @@ __global__ __launch_bounds__(256) void scan_gate_kernel(ScanArgs a, Work wk)
         double v = 0.0;
         int cut = 0;
         if (i < t1) {
-            v = (double)wk.qq[(size_t)bh * a.L + i] - (double)wk.kk[(size_t)bh * a.L + i];
+            v = (double)wk.a[(size_t)bh * a.L + i] + (double)wk.b[(size_t)bh * a.L + i];
             cut = a.la != nullptr && a.la[((size_t)b * a.L + i) * a.H + h] < -2839.2f;
             if (cut) v = 0.0;
         }
@@ -675,8 +793,8 @@ Work work_of(const ScanArgs &a, const ScanPlan &p)
     wk.back = (float *)(w + p.back);
     wk.decay_forth = (float *)(w + p.decay);
     wk.decay_back = wk.decay_forth + decays;
-    wk.qq = (float *)(w + p.dots);
-    wk.kk = wk.qq + rows;
+    wk.a = (float *)(w + p.dots);
+    wk.b = wk.a + rows;
     wk.nseg = p.nseg;
     wk.seg = p.seg;
     return wk;
@@ -706,7 +824,9 @@ hipError_t launch_bwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
     if (e != hipSuccess) return e;
     e = launch_kernel(scan_join_kernel, dim3(2 * bh * (D * D / 1024)), dim3(256), stream, a, wk, last, first);
     if (e != hipSuccess) return e;
-    e = launch_kernel(scan_grad_kernel<D>, dim3(3 * bh * p.nseg), dim3(Cfg<D>::NT), stream, a, wk);
+    e = launch_kernel(scan_dq_kernel<D>, dim3(bh * p.nseg), dim3(Cfg<D>::NT), stream, a, wk);
+    if (e != hipSuccess) return e;
+    e = launch_kernel(scan_back_kernel<D>, dim3(bh * p.nseg), dim3(2 * Cfg<D>::NT), stream, a, wk);
     if (e != hipSuccess || a.dla == nullptr) return e;
     return launch_kernel(scan_gate_kernel, dim3(bh * p.nseg), dim3(256), stream, a, wk);
 }

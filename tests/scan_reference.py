@@ -7,7 +7,9 @@ EPS = 1e-6
 BLOCK, LONGEST = 64, 1024        # tokens of a block; of a segment of the gradients' walk at the most
 
 # One rounding to bf16 is off by at most U16 of the value.  A value in two bf16 parts is off by U16 of U16, fp32 arithmetic on the way (norms,
-# decays, products, sums of up to some hundred terms) by less than another 2^-17 of the terms' magnitudes.
+# decays, products, sums of up to some hundred terms) by less than another 2^-17 of the terms' magnitudes.  A block's own products
+# (q'.k' for out and dv, dout.v for dq and dk, from 9 tokens on for out) are rounded to bf16 before they multiply rows of the block: U16
+# of each term's magnitude more, `near` below.
 U16 = 2.0 ** -8
 TWO = U16 * U16 + 2.0 ** -17
 
@@ -78,19 +80,29 @@ class Case:
         q, k = q0 * iq, k0 * ik
         B, L = self.B, self.L
         dq, dk, dv = np.zeros_like(q), np.zeros_like(q), np.zeros_like(q)
-        mq, mk, mv = np.zeros_like(q), np.zeros_like(q), np.zeros_like(q)
+        mq, mk, mv, nq, nk, nv = (np.zeros_like(q) for _ in range(6))
         E, ME, MS = np.zeros(q.shape[:3]), np.zeros(q.shape[:3]), [None] * L
-        states, M = [None] * L, np.abs(S)
+        states, M, near = [None] * L, np.abs(S), np.zeros_like(S)
         for t in range(L):
             on = np.array([t < n for n in self.lens])
+            if t % BLOCK == 0:
+                near[:] = 0.0
+            near[on] = a[on, t, :, None, None] * near[on] + np.abs(k[on, t])[..., :, None] * np.abs(v[on, t])[..., None, :]
+            nq[on, t] = np.einsum("bhe,bhde->bhd", np.abs(do[on, t]), near[on])
             states[t], MS[t] = S.copy(), M.copy()         # before the token
             S[on] = a[on, t, :, None, None] * S[on] + k[on, t][..., :, None] * v[on, t][..., None, :]
             M[on] = a[on, t, :, None, None] * M[on] + np.abs(k[on, t])[..., :, None] * np.abs(v[on, t])[..., None, :]
             dq[on, t] = np.einsum("bhe,bhde->bhd", do[on, t], S[on])
             mq[on, t] = np.einsum("bhe,bhde->bhd", np.abs(do[on, t]), M[on])
         N = np.abs(G)
+        near[:] = 0.0
         for t in reversed(range(L)):
             on = np.array([t < n for n in self.lens])
+            if t % BLOCK == BLOCK - 1:
+                near[:] = 0.0
+            near[on] += np.abs(q[on, t])[..., :, None] * np.abs(do[on, t])[..., None, :]
+            nk[on, t], nv[on, t] = np.einsum("bhe,bhde->bhd", np.abs(v[on, t]), near[on]), np.einsum("bhd,bhde->bhe", np.abs(k[on, t]), near[on])
+            near[on] *= a[on, t, :, None, None]
             G[on] += q[on, t][..., :, None] * do[on, t][..., None, :]
             N[on] += np.abs(q[on, t])[..., :, None] * np.abs(do[on, t])[..., None, :]
             dk[on, t], mk[on, t] = np.einsum("bhe,bhde->bhd", v[on, t], G[on]), np.einsum("bhe,bhde->bhd", np.abs(v[on, t]), N[on])
@@ -106,12 +118,13 @@ class Case:
             along[:, t] = each[:, t:t + LONGEST].sum(1)
         ends = ME.max(1, keepdims=True) + (np.abs(self.dS.numpy().astype(np.float64)) * M).sum((-1, -2))[:, None] if self.dS is not None else ME.max(1, keepdims=True)
         limits = []
-        for d, m, x, i in ((dq, mq, q, iq), (dk, mk, k, ik)):
+        for d, m, c, x, i in ((dq, mq, nq, q, iq), (dk, mk, nk, k, ik)):
             if self.normalise:
                 d[:] = i * (d - x * (x * d).sum(-1, keepdims=True))
-                m[:] = i * (m + np.abs(x) * (np.abs(x) * m).sum(-1, keepdims=True))
-            limits.append(U16 * np.abs(d) + 2.0 * TWO * m)
-        limits += [U16 * np.abs(dv) + TWO * mv, 2.0 * TWO * (along + ends) + 1e-30, TWO * N + 1e-30]
+                for y in (m, c):
+                    y[:] = i * (y + np.abs(x) * (np.abs(x) * y).sum(-1, keepdims=True))
+            limits.append(U16 * (np.abs(d) + c) + 2.0 * TWO * m)
+        limits += [U16 * (np.abs(dv) + nv) + TWO * mv, 2.0 * TWO * (along + ends) + 1e-30, TWO * N + 1e-30]
         return (dq, dk, dv, E, G), limits
 
 
