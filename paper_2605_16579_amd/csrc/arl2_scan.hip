@@ -27,12 +27,13 @@ constexpr int kBlock = 64;                    // tokens
 constexpr int kStepTokens = 8;
 constexpr double kLog2e = 1.4426950408889634;
 
-enum Mode { kOut, kDq, kBack, kSum, kSumBack };          // kBack: dk and dv; the last two make states and no rows
+enum Mode { kOut, kDq, kDk, kDv, kSum, kSumBack };       // the last two make states and no rows
 
 // One call's arrays in the workspace: states [B*H][nseg + 1][D][D], the way forth (state i: what segment i begins with) and back
-// (state i: the gradient of what segment i - 1 ends with), the segments' decays, and a_t, b_t and G's part of E [B*H][L].
+// (state i: the gradient of what segment i - 1 ends with), the segments' decays, the parts
+// of E by tokens [3][B*H][L] (a_t; -b_t; G's), and <S_L, dS> [B*H] where a sequence is one segment.
 struct Work {
-    float *forth, *back, *decay_forth, *decay_back, *a, *b;
+    float *forth, *back, *decay_forth, *decay_back, *parts, *anchor;
     int nseg, seg;
 };
 
@@ -59,7 +60,7 @@ struct Scalars {
     float fold[2];                                        // what the state is multiplied with before they do; 1: it is left
     int pairs[2];                                         // products take their decays pair by pair
     // with the norms of the rows
-    float post[kBlock], unit[kBlock], pcol[kBlock], penter[kBlock], norm[kBlock];
+    float post[kBlock], pcol[kBlock], penter[kBlock], norm[kBlock];
     float red[4][kBlock][3];
     float later[3][32], earlier[3][32];                   // of the 32 x 32 pairs of a block: sums of G over s, over u
 };
@@ -135,23 +136,17 @@ __device__ __forceinline__ float lanes_sums(float (&v)[16], int lane)
 template <int D, int MODE>
 struct Walk {
     using C = Cfg<D>;
-    static constexpr bool REV = MODE == kBack || MODE == kSumBack;
+    static constexpr bool REV = MODE == kDk || MODE == kDv || MODE == kSumBack;
     static constexpr bool ROWS = MODE != kSum && MODE != kSumBack;
-    static constexpr bool BOTH = MODE == kBack;                   // two groups of wavefronts: dv, and dk
-    static constexpr int NT = (BOTH ? 2 : 1) * C::NT;
-    static constexpr int ROUND = NT / C::LPR, ROUNDS = kBlock / ROUND;       // rows that the threads stage at a time
-    static constexpr int MATS = BOTH ? 4 : ROWS ? 3 : 2;
-    // products: as rows of X in bf16, one or two such arrays; with two, those of dout and v as they are
-    static constexpr int PAIR = 64 * 16 * 4;                      // bytes of 32 x 32 of them in fp32
-    static constexpr int LDS_ROWS = MATS * C::MAT + (BOTH ? 2 * C::PMAT + 3 * PAIR : ROWS ? C::PMAT : 0);
+    static constexpr bool GRAD = MODE == kDq || MODE == kDk;      // rows through the normalisation
+    static constexpr int ROUND = C::NT / C::LPR, ROUNDS = kBlock / ROUND;    // rows that the threads stage at a time
+    static constexpr int LDS_ROWS = (ROWS ? 3 : 2) * C::MAT + (ROWS ? C::PMAT : 0);
 
     // `lds`: LDS_ROWS bytes.  Segment `seg` of (stream, head) bh.
     static __device__ __forceinline__ void run(const ScanArgs &a, const Work &wk, int bh, int seg, unsigned char *lds, Scalars &sc)
     {
         const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
-        const int all_wave = __builtin_amdgcn_readfirstlane(tid >> 6), wave = BOTH ? all_wave % C::NW : all_wave;
-        const bool dk = BOTH && all_wave >= C::NW;                // the second group
-        const bool grad = MODE == kDq || dk;                      // rows through the normalisation
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
         const int b = bh / a.H, h = bh - b * a.H;
         const int n = tokens_of(a, b);
         const int nblk = (n + kBlock - 1) / kBlock;
@@ -163,28 +158,27 @@ struct Walk {
         const size_t stream = (size_t)b * a.L * rs;
         const uint32_t range = (uint32_t)n * rs;
         auto rows_of = [&](const void *p) { return make_rsrc((const char *)p + stream, range); };
-        // the arrays as they lie in LDS; kBack: k, q, v, dout
-        const void *const in[4] = {MODE == kOut ? a.q : MODE == kDq ? a.dout : a.k, MODE == kDq ? a.v : REV ? a.q : a.k, MODE == kDq ? a.k : MODE == kSumBack ? a.dout : a.v, a.dout};
-        constexpr int IN0 = ROWS ? 0 : 1;                         // states alone need the second and third
-        const auto r0 = rows_of(in[0]), r1 = rows_of(in[1]), r2 = rows_of(in[2]), r3 = rows_of(in[3]);
+        const auto rv = rows_of(MODE == kDv ? a.v : a.k);         // (for G)
+        const auto rx = rows_of(MODE == kOut ? a.q : MODE == kDq ? a.dout : MODE == kDk ? a.v : a.k);
+        const auto ry = rows_of(MODE == kOut || MODE == kSum ? a.k : MODE == kDq ? a.v : MODE == kDk ? a.dout : a.q);
+        const auto rz = rows_of(MODE == kOut || MODE == kSum ? a.v : MODE == kDq ? a.k : MODE == kDk ? a.q : a.dout);
         const auto rla = make_rsrc(a.la + (a.la ? (size_t)b * a.L * a.H : 0), a.la ? (uint32_t)n * a.H * 4 : 0);
 
-        unsigned char *const m1 = lds + (ROWS ? C::MAT : 0), *const m2 = m1 + C::MAT, *const m3 = m2 + C::MAT, *const products = lds + MATS * C::MAT;
-        const unsigned char *const lx = dk ? m2 : lds, *const ly = dk ? m3 : m1, *const lz = BOTH ? (dk ? m1 : m3) : m2;
-        unsigned char *const lp = products + (dk ? C::PMAT : 0), *const raw = products + 2 * C::PMAT;
+        unsigned char *const lx = lds, *const ly = lds + (ROWS ? C::MAT : 0), *const lz = ly + C::MAT, *const lp = lz + C::MAT;
 
         // ---- the state: 32 columns of each wavefront, register j of tile t is row 32 t + 16 (j / 8) + 8 hh + j % 8
         f32x16 st[D / 32];
         const int e0 = 32 * wave;
         {
             const float *from = nullptr;
-            if (MODE == kOut) from = wk.nseg == 1 ? (a.S0 ? a.S0 + (size_t)bh * D * D : nullptr) : wk.forth + ((size_t)bh * (wk.nseg + 1) + seg) * D * D;
-            if (MODE == kDq) from = wk.forth + ((size_t)bh * (wk.nseg + 1) + seg) * D * D;
-            if (MODE == kBack) from = wk.back + ((size_t)bh * (wk.nseg + 1) + seg + 1) * D * D;
+            if (ROWS && wk.nseg == 1) {                           // one segment: what the call begins with
+                from = REV ? a.dS : a.S0;
+                if (from != nullptr) from += (size_t)bh * D * D;
+            } else if (ROWS) from = (REV ? wk.back : wk.forth) + ((size_t)bh * (wk.nseg + 1) + seg + (REV ? 1 : 0)) * D * D;
             if (from == nullptr) {
 #pragma unroll
                 for (int t = 0; t < D / 32; ++t) st[t] = f32x16{};
-            } else if (grad) {                                    // transposed
+            } else if (GRAD) {                                    // transposed
 #pragma unroll
                 for (int t = 0; t < D / 32; ++t)
 #pragma unroll
@@ -203,17 +197,16 @@ struct Walk {
 
         // ---- a block's rows on their way through registers, in 16-byte pieces
         const uint32_t piece0 = (uint32_t)(tid / C::LPR) * rs + (uint32_t)h * D * 2 + (tid % C::LPR) * 16;
-        u32x4 g0[ROUNDS], g1[ROUNDS], g2[ROUNDS], g3[ROUNDS];
+        u32x4 gx[ROUNDS], gy[ROUNDS], gz[ROUNDS];
         float gla;
         auto fetch = [&](int blk) {
             const uint32_t o = piece0 + (uint32_t)blk * kBlock * rs;
             auto piece = [&](__amdgpu_buffer_rsrc_t r, int i) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, o + (uint32_t)(ROUND * i) * rs, 0, 0)); };
 #pragma unroll
             for (int i = 0; i < ROUNDS; ++i) {
-                if (IN0 == 0) g0[i] = piece(r0, i);
-                g1[i] = piece(r1, i);
-                g2[i] = piece(r2, i);
-                if (BOTH) g3[i] = piece(r3, i);
+                if (ROWS) gx[i] = piece(rx, i);
+                gy[i] = piece(ry, i);
+                gz[i] = piece(rz, i);
             }
         };
         auto fetch_gate = [&](int blk) {
@@ -256,10 +249,8 @@ struct Walk {
                     x = lane_group_sum<C::LPR>(x);
                     x = a.normalise ? fast_rsqrt(x + a.eps) : 1.f;
                     if (tid % C::LPR == 0) {
-                        if (kind == 1) {
-                            sc.post[row] = sc.pairs[buf] ? x : x * sc.row[buf][row];
-                            sc.unit[row] = x;
-                        } else {
+                        if (kind == 1) sc.post[row] = sc.pairs[buf] ? x : x * sc.row[buf][row];
+                        else {
                             sc.pcol[row] = x * sc.col[buf][row];
                             sc.penter[row] = x * sc.enter[buf][row];
                             sc.norm[row] = x;
@@ -271,20 +262,19 @@ struct Walk {
 
         const int count = blk1 - blk0;
         auto block_at = [&](int i) { return REV ? blk1 - 1 - i : blk0 + i; };
-        constexpr int GW = NT / 64 - 1;                           // the wavefront with the gates: it has fewest products
+        constexpr int GW = C::NW - 1;                             // the wavefront with the gates: it has fewest products
         if (count > 0) {
             fetch(block_at(0));
             fetch_gate(block_at(0));
-            if (all_wave == GW) gates(0);
+            if (wave == GW) gates(0);
             if (count > 1) fetch_gate(block_at(1));
             lds_barrier();
         }
         for (int i = 0; i < count; ++i) {
             const int blk = block_at(i), buf = i & 1;
-            if (IN0 == 0) stage(g0, lds, MODE == kDq ? 0 : 1, buf);
-            stage(g1, m1, MODE == kDq ? 0 : 2, buf);
-            stage(g2, m2, MODE == kDq ? 2 : 0, buf);
-            if (BOTH) stage(g3, m3, 0, buf);
+            if (ROWS) stage(gx, lx, GRAD ? 0 : 1, buf);
+            stage(gy, ly, GRAD ? 0 : 2, buf);
+            stage(gz, lz, GRAD ? 2 : 0, buf);
             if (i + 1 < count) fetch(block_at(i + 1));
             const bool pairs = __builtin_amdgcn_readfirstlane(sc.pairs[buf]) != 0;
             lds_barrier();
@@ -297,7 +287,7 @@ struct Walk {
 #pragma unroll
                 for (int m = 0; m < 4; ++m) zf[m] = lds_read_tr_pair(z + 16 * m * C::ROW, 4 * C::ROW);
             }
-            f32x16 acc[2], p;
+            f32x16 acc[2];
             u32x2 own[2][4];                                      // the rows whose normalisation has a gradient
             float asked[2] = {0.f, 0.f};                          // their products with what the state gives
             // pairs of 32 x 32 rows: which of Y, which of X
@@ -305,8 +295,8 @@ struct Walk {
             auto x_of = [](int t) { return REV ? (int)(t == 2) : (int)(t > 0); };
             if constexpr (ROWS) {
                 acc[0] = acc[1] = f32x16{};
-                if (MODE == kDq) {
-                    const auto rg = rows_of(a.q);
+                if (GRAD) {
+                    const auto rg = rows_of(MODE == kDq ? a.q : a.k);
 #pragma unroll
                     for (int tb = 0; tb < 2; ++tb)
 #pragma unroll
@@ -319,15 +309,11 @@ struct Walk {
                     const int t = t0 + wave;
                     if (t >= 3) break;
                     const int sb = y_of(t), tb = x_of(t);
-                    p = f32x16{};
+                    f32x16 p = {};
                     const unsigned char *const y = ly + (32 * sb + l32) * C::ROW + 16 * hh, *const x = lx + (32 * tb + l32) * C::ROW + 16 * hh;
 #pragma unroll
                     for (int m = 0; m < D / 16; ++m)
                         p = mfma(*reinterpret_cast<const bf16x8 *>(y + 32 * m), *reinterpret_cast<const bf16x8 *>(x + 32 * m), p);
-                    if (dk) {
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4 *>(raw + t * PAIR + g * 1024 + lane * 16) = f32x4{p[4 * g], p[4 * g + 1], p[4 * g + 2], p[4 * g + 3]};
-                    }
                     unsigned char *const to = lp + (32 * tb + l32) * C::PROW + 64 * sb;
                     if (!pairs) {
 #pragma unroll
@@ -359,6 +345,27 @@ struct Walk {
                         const bf16x4 r = {to_bf16(p[4 * g]), to_bf16(p[4 * g + 1]), to_bf16(p[4 * g + 2]), to_bf16(p[4 * g + 3])};
                         *reinterpret_cast<bf16x4 *>(to + 16 * g + 8 * hh) = r;
                     }
+                    // ---- G: these products of k and q times those of dout, which lies in Z's place, and v
+                    if (MODE == kDv && a.dla != nullptr) {
+                        f32x16 w = {};
+                        const unsigned char *const z = lz + (32 * sb + l32) * C::ROW + 16 * hh;
+                        const uint32_t row = (uint32_t)(blk * kBlock + 32 * tb + l32) * rs + (h * D + 8 * hh) * 2;
+#pragma unroll
+                        for (int m = 0; m < D / 16; ++m)
+                            w = mfma(*reinterpret_cast<const bf16x8 *>(z + 32 * m), __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rv, row + 32 * m, 0, 0)), w);
+                        const float post = sc.post[32 * tb + l32];
+                        float v[16], sum = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const bool strictly = sb != tb || 8 * (j / 4) + 4 * hh + j % 4 > l32;
+                            v[j] = strictly ? p[j] * w[j] * post : 0.f;
+                            sum += v[j];
+                        }
+                        sum = xhalf_sum(sum);
+                        if (hh == 0) sc.earlier[t][l32] = sum;
+                        const float of = lanes_sums(v, lane);
+                        if ((lane & 16) == 0) sc.later[t][8 * ((lane & 15) / 4) + 4 * hh + lane % 4] = of;
+                    }
                 }
                 // ---- rows asked of the state, which is taken in two parts
                 const unsigned char *const x = lx + l32 * C::ROW + 16 * hh;
@@ -382,17 +389,12 @@ struct Walk {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) { acc[0][j] *= f0; acc[1][j] *= f1; }
                 }
-                if (grad) {
+                if (GRAD) {
 #pragma unroll
-                    for (int tb = 0; tb < 2; ++tb) {
-                        if (dk)
-#pragma unroll
-                            for (int g = 0; g < 4; ++g) own[tb][g] = *reinterpret_cast<const u32x2 *>(lds + (32 * tb + l32) * C::ROW + 2 * (e0 + 8 * g + 4 * hh));
-                        asked[tb] = dot_of(own[tb], acc[tb]);
-                    }
+                    for (int tb = 0; tb < 2; ++tb) asked[tb] = dot_of(own[tb], acc[tb]);
                 }
             }
-            if (i + 1 < count && all_wave == GW) gates(buf ^ 1);
+            if (i + 1 < count && wave == GW) gates(buf ^ 1);
             if (i + 2 < count) fetch_gate(block_at(i + 2));
             if (ROWS) lds_barrier();
 
@@ -405,50 +407,6 @@ struct Walk {
                     for (int m = REV ? 2 * tb : 0; m < (REV ? 4 : 2 + 2 * tb); ++m)
                         acc[tb] = mfma(zf[m], *reinterpret_cast<const bf16x8 *>(from + 32 * tb * C::PROW + 32 * m), acc[tb]);
             }
-            if constexpr (BOTH) {
-                // ---- G: the products of k and q, which are here, times those of dout and v
-                if (!dk && a.dla != nullptr) {
-#pragma unroll
-                    for (int t0 = 0; t0 < 3; t0 += C::NW) {
-                        const int t = t0 + wave;
-                        if (t >= 3) break;
-                        const int sb = y_of(t), tb = x_of(t);
-                        if (C::NW < 3) {                          // (two of them: the other's products are no longer here)
-                            const unsigned char *const y = ly + (32 * sb + l32) * C::ROW + 16 * hh, *const x = lx + (32 * tb + l32) * C::ROW + 16 * hh;
-                            p = f32x16{};
-#pragma unroll
-                            for (int m = 0; m < D / 16; ++m)
-                                p = mfma(*reinterpret_cast<const bf16x8 *>(y + 32 * m), *reinterpret_cast<const bf16x8 *>(x + 32 * m), p);
-                            const float wt = sc.whole[buf][32 * tb + l32], ft = sc.frac[buf][32 * tb + l32];
-#pragma unroll
-                            for (int g = 0; g < 4; ++g) {
-                                const int s0 = 32 * sb + 8 * g + 4 * hh;
-                                const f32x4 f = *reinterpret_cast<const f32x4 *>(&sc.pcol[s0]), ws = *reinterpret_cast<const f32x4 *>(&sc.whole[buf][s0]),
-                                            fs = *reinterpret_cast<const f32x4 *>(&sc.frac[buf][s0]), ys = *reinterpret_cast<const f32x4 *>(&sc.norm[s0]);
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) p[4 * g + j] *= pairs ? ys[j] * __builtin_amdgcn_exp2f((ws[j] - wt) + (fs[j] - ft)) : f[j];
-                            }
-                        }
-                        const float post = sc.post[32 * tb + l32];
-                        float v[16], sum = 0.f;
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            const f32x4 w = *reinterpret_cast<const f32x4 *>(raw + t * PAIR + g * 1024 + lane * 16);
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const bool strictly = sb != tb || 8 * g + 4 * hh + j > l32;
-                                v[4 * g + j] = strictly ? p[4 * g + j] * w[j] * post : 0.f;
-                                sum += v[4 * g + j];
-                            }
-                        }
-                        sum = xhalf_sum(sum);
-                        if (hh == 0) sc.earlier[t][l32] = sum;
-                        const float of = lanes_sums(v, lane);
-                        if ((lane & 16) == 0) sc.later[t][8 * ((lane & 15) / 4) + 4 * hh + lane % 4] = of;
-                    }
-                }
-            }
-
             // ---- the state's step: rows of Z times their weights in two parts
             const float fold = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(sc.fold[buf])));
             if (fold != 1.f) {
@@ -483,33 +441,32 @@ struct Walk {
 
             // ---- rows out
             if constexpr (ROWS) {
-                float scale[2], along[2] = {0.f, 0.f}, unit[2];
+                float scale[2], along[2] = {0.f, 0.f};
 #pragma unroll
-                for (int tb = 0; tb < 2; ++tb) {
-                    scale[tb] = MODE == kDq ? (pairs ? 1.f : sc.row[buf][32 * tb + l32]) : sc.post[32 * tb + l32];
-                    unit[tb] = MODE == kDq ? 1.f : sc.unit[32 * tb + l32];
-                }
-                if (grad) {
+                for (int tb = 0; tb < 2; ++tb) scale[tb] = GRAD ? (pairs ? 1.f : sc.row[buf][32 * tb + l32]) : sc.post[32 * tb + l32];
+                if (GRAD) {
 #pragma unroll
                     for (int tb = 0; tb < 2; ++tb) {
+                        float ss = 0.f;
+#pragma unroll
+                        for (int g = 0; g < 4; ++g)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                const float x0 = __uint_as_float(own[tb][g][j] << 16), x1 = __uint_as_float(own[tb][g][j] & 0xffff0000u);
+                                ss = fmaf(x0, x0, fmaf(x1, x1, ss));
+                            }
+                        ss = xhalf_sum(ss);
                         const float dot = xhalf_sum(dot_of(own[tb], acc[tb])), from_state = xhalf_sum(asked[tb]);
-                        if (hh == 0) { sc.red[wave][32 * tb + l32][0] = dot; sc.red[wave][32 * tb + l32][1] = from_state; }
-                        if (MODE == kDq) {
-                            float ss = 0.f;
-#pragma unroll
-                            for (int g = 0; g < 4; ++g)
-#pragma unroll
-                                for (int j = 0; j < 2; ++j) {
-                                    const float x0 = __uint_as_float(own[tb][g][j] << 16), x1 = __uint_as_float(own[tb][g][j] & 0xffff0000u);
-                                    ss = fmaf(x0, x0, fmaf(x1, x1, ss));
-                                }
-                            ss = xhalf_sum(ss);
-                            if (hh == 0) sc.red[wave][32 * tb + l32][2] = ss;
+                        if (hh == 0) {
+                            sc.red[wave][32 * tb + l32][0] = dot;
+                            sc.red[wave][32 * tb + l32][1] = from_state;
+                            sc.red[wave][32 * tb + l32][2] = ss;
                         }
                     }
                 }
                 lds_barrier();                                    // all have read the block's rows
-                if (grad) {
+                float *const parts = wk.parts + ((MODE == kDq ? 0 : MODE == kDk ? (size_t)a.B * a.H : 2 * (size_t)a.B * a.H) + bh) * a.L + blk * kBlock;
+                if (GRAD) {
 #pragma unroll
                     for (int tb = 0; tb < 2; ++tb) {
                         float dot = 0.f, from_state = 0.f, ss = 0.f;
@@ -517,24 +474,18 @@ struct Walk {
                         for (int w = 0; w < C::NW; ++w) {
                             dot += sc.red[w][32 * tb + l32][0];
                             from_state += sc.red[w][32 * tb + l32][1];
-                            if (MODE == kDq) ss += sc.red[w][32 * tb + l32][2];
+                            ss += sc.red[w][32 * tb + l32][2];
                         }
-                        if (MODE == kDq) {
-                            unit[tb] = a.normalise ? fast_rsqrt(ss + a.eps) : 1.f;
-                            scale[tb] *= unit[tb];
-                        }
-                        along[tb] = a.normalise ? -(dot * scale[tb]) * unit[tb] * unit[tb] : 0.f;
-                        const int t = blk * kBlock + 32 * tb + l32;
-                        if (wave == 0 && hh == 0 && t < n && a.dla != nullptr) {
-                            float e = from_state * scale[tb];
-                            if (BOTH) {
-                                e = tb == 0 ? sc.later[0][l32] - sc.earlier[0][l32] - sc.earlier[1][l32] - e : sc.later[1][l32] + sc.later[2][l32] - sc.earlier[2][l32] - e;
-                            }
-                            (MODE == kDq ? wk.a : wk.b)[(size_t)bh * a.L + t] = e;
-                        }
+                        const float unit = a.normalise ? fast_rsqrt(ss + a.eps) : 1.f;
+                        scale[tb] *= unit;
+                        along[tb] = a.normalise ? -(dot * scale[tb]) * unit * unit : 0.f;
+                        if (wave == 0 && hh == 0 && blk * kBlock + 32 * tb + l32 < n && a.dla != nullptr)
+                            parts[32 * tb + l32] = MODE == kDq ? from_state * scale[tb] : -(from_state * scale[tb]);
                     }
                 }
-                const auto ro = rows_of(MODE == kOut ? a.out : MODE == kDq ? a.dq : dk ? a.dk : a.dv);
+                if (MODE == kDv && wave == 0 && blk * kBlock + lane < n && a.dla != nullptr)
+                    parts[lane] = hh == 0 ? sc.later[0][l32] - sc.earlier[0][l32] - sc.earlier[1][l32] : sc.later[1][l32] + sc.later[2][l32] - sc.earlier[2][l32];
+                const auto ro = rows_of(MODE == kOut ? a.out : MODE == kDq ? a.dq : MODE == kDk ? a.dk : a.dv);
 #pragma unroll
                 for (int tb = 0; tb < 2; ++tb) {
                     uint32_t w[4][2];
@@ -543,7 +494,7 @@ struct Walk {
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
                             float x0 = acc[tb][4 * g + 2 * j] * scale[tb], x1 = acc[tb][4 * g + 2 * j + 1] * scale[tb];
-                            if (grad) {
+                            if (GRAD) {
                                 x0 = fmaf(along[tb], __uint_as_float(own[tb][g][j] << 16), x0);
                                 x1 = fmaf(along[tb], __uint_as_float(own[tb][g][j] & 0xffff0000u), x1);
                             }
@@ -565,6 +516,7 @@ struct Walk {
         // ---- the state at the end
         float *to = nullptr;
         if (MODE == kOut) to = seg == nact - 1 && a.S != nullptr ? a.S + (size_t)bh * D * D : nullptr;
+        if (MODE == kDv) to = wk.nseg == 1 && a.dS0 != nullptr ? a.dS0 + (size_t)bh * D * D : nullptr;
         if (MODE == kSum) to = wk.forth + ((size_t)bh * (wk.nseg + 1) + seg + 1) * D * D;
         if (MODE == kSumBack) to = wk.back + ((size_t)bh * (wk.nseg + 1) + seg) * D * D;
         if (to != nullptr) {
@@ -578,6 +530,29 @@ struct Walk {
             for (int t = 0; t < D / 32; ++t)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) to[(size_t)(32 * t + 16 * (j / 8) + 8 * hh + j % 8) * D + e0 + l32] = st[t][j] * gathered;
+        }
+        if (MODE == kDq && wk.nseg == 1 && a.dS != nullptr && a.dla != nullptr) {        // <S_L, dS>: the state is transposed here
+            lds_barrier();                                        // all have read the last block's sums
+            if (tid == 64 * GW) sc.fold[0] = count > 0 ? exp2_of(base) : 1.f;
+            const float *const from = a.dS + (size_t)bh * D * D + (size_t)(e0 + l32) * D;
+            float dot = 0.f;
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+                for (int j = 0; j < 16; j += 4) {
+                    const f32x4 x = *reinterpret_cast<const f32x4 *>(from + 32 * t + 16 * (j / 8) + 8 * hh + j % 8);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) dot = fmaf(x[i], st[t][j + i], dot);
+                }
+#pragma unroll
+            for (int m = 32; m > 0; m >>= 1) dot += __shfl_xor(dot, m, kWave);
+            if (lane == 0) sc.red[wave][0][0] = dot;
+            lds_barrier();
+            if (tid == 0) {
+                dot = 0.f;
+                for (int w = 0; w < C::NW; ++w) dot += sc.red[w][0][0];
+                wk.anchor[bh] = dot * sc.fold[0];
+            }
         }
         if (!ROWS && tid == 64 * GW) (MODE == kSum ? wk.decay_forth : wk.decay_back)[(size_t)bh * wk.nseg + seg] = exp2_of(seg_total);
     }
@@ -636,91 +611,111 @@ __global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, Work wk, int
     if (start != nullptr) x = *reinterpret_cast<const f32x4 *>(start + (size_t)bh * nn + e);
     *reinterpret_cast<f32x4 *>(base + (size_t)(back ? nact : 0) * nn) = x;
     const int steps = back ? nact - 1 + need_first : nact - 1 + need_last;
-    constexpr int AHEAD = 8;                                      // states on their way at a time
+    constexpr int AHEAD = 16;                                     // states on their way at a time
     for (int i0 = 0; i0 < steps; i0 += AHEAD) {
         f32x4 own[AHEAD];
         float d[AHEAD];
-        float *at[AHEAD];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             const int step = min(i0 + i, steps - 1), seg = back ? nact - 1 - step : step;
-            at[i] = base + (size_t)(back ? seg : seg + 1) * nn;
-            own[i] = *reinterpret_cast<const f32x4 *>(at[i]);
+            own[i] = *reinterpret_cast<const f32x4 *>(base + (size_t)(back ? seg : seg + 1) * nn);
             d[i] = decay[seg];
         }
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             if (i0 + i >= steps) break;
+            const int seg = back ? nact - 1 - (i0 + i) : i0 + i;
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[j] = fmaf(d[i], x[j], own[i][j]);
-            *reinterpret_cast<f32x4 *>(at[i]) = x;
+            *reinterpret_cast<f32x4 *>(base + (size_t)(back ? seg : seg + 1) * nn) = x;
         }
     }
     if (back && a.dS0 != nullptr) *reinterpret_cast<f32x4 *>(a.dS0 + (size_t)bh * nn + e) = x;
 }
 
+// The rows' gradients: three walks of a segment by three workgroups that follow one another.
 template <int D>
-__global__ __launch_bounds__(Cfg<D>::NT, 2) void scan_dq_kernel(ScanArgs a, Work wk)
+__global__ __launch_bounds__(Cfg<D>::NT, D / 64) void scan_grad_kernel(ScanArgs a, Work wk)
 {
-    using W = Walk<D, kDq>;
-    __shared__ __align__(16) unsigned char lds[W::LDS_ROWS];
+    __shared__ __align__(16) unsigned char lds[Walk<D, kDq>::LDS_ROWS];
     __shared__ __align__(16) Scalars sc;
     const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
-    W::run(a, wk, id / wk.nseg, id % wk.nseg, lds, sc);
-}
-template <int D>
-__global__ __launch_bounds__(2 * Cfg<D>::NT, 2) void scan_back_kernel(ScanArgs a, Work wk)
-{
-    using W = Walk<D, kBack>;
-    __shared__ __align__(16) unsigned char lds[W::LDS_ROWS];
-    __shared__ __align__(16) Scalars sc;
-    const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
-    W::run(a, wk, id / wk.nseg, id % wk.nseg, lds, sc);
+    const int unit = id / 3, which = id - 3 * unit;
+    const int bh = unit / wk.nseg, seg = unit % wk.nseg;
+    if (which == 0) Walk<D, kDv>::run(a, wk, bh, seg, lds, sc);
+    else if (which == 1) Walk<D, kDk>::run(a, wk, bh, seg, lds, sc);
+    else Walk<D, kDq>::run(a, wk, bh, seg, lds, sc);
 }
 
 // The gates' gradients of a segment: from <state, gradient of the state> at its end backwards, a sum that a gate of zero begins anew.
 __global__ __launch_bounds__(256) void scan_gate_kernel(ScanArgs a, Work wk)
 {
-    __shared__ double part[4];
+    constexpr int PER = 4;                                        // tokens of a thread: 1024 of a workgroup, which a segment has at the most
+    __shared__ double sums[4], ends[4];
+    __shared__ int cuts[4];
     const int bh = blockIdx.x / wk.nseg, seg = blockIdx.x % wk.nseg, b = bh / a.H, h = bh - b * a.H;
-    const int tid = threadIdx.x, lane = tid & 63, nn = a.D * a.D;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nn = a.D * a.D;
     const int n = tokens_of(a, b), blocks = (n + kBlock - 1) / kBlock, nact = max(1, (blocks + wk.seg - 1) / wk.seg);
     const int t0 = seg * wk.seg * kBlock, t1 = min(n, t0 + wk.seg * kBlock);
     if (t0 >= t1) return;
-    double dot = 0.0;
-    if (seg < nact - 1 || a.dS != nullptr) {
-        const size_t at = ((size_t)bh * (wk.nseg + 1) + seg + 1) * nn;
-        for (int e = tid * 4; e < nn; e += 1024) {
-            const f32x4 x = *reinterpret_cast<const f32x4 *>(wk.forth + at + e), y = *reinterpret_cast<const f32x4 *>(wk.back + at + e);
-            dot += (double)x[0] * y[0] + (double)x[1] * y[1] + (double)x[2] * y[2] + (double)x[3] * y[3];
-        }
+    // this thread's tokens from late to early, later tokens in lower lanes
+    double v[PER];
+    int cut = 0;                                                  // bit i: a gate of zero; what lies behind it does not reach what lies before
+    const int last = t0 + PER * 256 - 1 - PER * tid;
+    const size_t rows = (size_t)a.B * a.H * a.L;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int t = last - i;
+        const float *const p = wk.parts + (size_t)bh * a.L + t;
+        v[i] = t < t1 ? (double)p[0] + p[rows] + p[2 * rows] : 0.0;
+        if (t < t1 && a.la[((size_t)b * a.L + t) * a.H + h] < -2839.2f) cut |= 1 << i;
     }
+    double dot = 0.0;
+    if (wk.nseg > 1 && (seg < nact - 1 || a.dS != nullptr)) {
+        const float *const x = wk.forth + ((size_t)bh * (wk.nseg + 1) + seg + 1) * nn, *const y = wk.back + ((size_t)bh * (wk.nseg + 1) + seg + 1) * nn;
+        for (int e = tid * 4; e < nn; e += 4096) {
+            f32x4 p[4], q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p[i] = *reinterpret_cast<const f32x4 *>(x + e + 1024 * i);
+                q[i] = *reinterpret_cast<const f32x4 *>(y + e + 1024 * i);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dot += ((double)p[i][0] * q[i][0] + (double)p[i][1] * q[i][1]) + ((double)p[i][2] * q[i][2] + (double)p[i][3] * q[i][3]);
+        }
+    } else if (wk.nseg == 1 && a.dS != nullptr && tid == 0) dot = wk.anchor[bh];
 #pragma unroll
     for (int m = 32; m > 0; m >>= 1) dot += __shfl_xor(dot, m, kWave);
-    if (lane == 0) part[tid >> 6] = dot;
+    // sums within the thread, over the lanes before it, over the wavefronts before that
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (cut & 1 << i) v[i] = 0.0;
+        else if (i > 0) v[i] += v[i - 1];
+    }
+    double run = v[PER - 1];
+    int any = cut != 0;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const double u = __shfl_up(run, m, kWave);
+        const int c = __shfl_up(any, m, kWave);
+        if (lane >= m) {
+            if (!any) run += u;
+            any |= c;
+        }
+    }
+    if (lane == 63) { ends[wave] = run; cuts[wave] = any; }
+    if (lane == 0) sums[wave] = dot;
     __syncthreads();
-    if (tid >= 64) return;
-    double carry = part[0] + part[1] + part[2] + part[3];
-    for (int t = t0 + (t1 - 1 - t0) / 64 * 64; t >= t0; t -= 64) {
-        const int i = t + 63 - lane;                              // later tokens in lower lanes
-        double v = 0.0;
-        int cut = 0;
-        if (i < t1) {
-            v = (double)wk.a[(size_t)bh * a.L + i] + (double)wk.b[(size_t)bh * a.L + i];
-            cut = a.la != nullptr && a.la[((size_t)b * a.L + i) * a.H + h] < -2839.2f;
-            if (cut) v = 0.0;
-        }
-        for (int m = 1; m < 64; m <<= 1) {
-            const double u = __shfl_up(v, m, kWave);
-            const int c = __shfl_up(cut, m, kWave);
-            if (lane >= m) {
-                if (!cut) v += u;
-                cut |= c;
-            }
-        }
-        if (!cut) v += carry;
-        if (i < t1) a.dla[((size_t)b * a.L + i) * a.H + h] = (float)v;
-        carry = __shfl(v, 63, kWave);
+    double before = sums[0] + sums[1] + sums[2] + sums[3];
+    for (int w = 0; w < wave; ++w) before = cuts[w] ? ends[w] : before + ends[w];
+    const double lanes = __shfl_up(run, 1, kWave);
+    const int lane_cut = __shfl_up(any, 1, kWave);
+    if (lane > 0) before = lane_cut ? lanes : before + lanes;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int t = last - i;
+        if ((cut & ((2 << i) - 1)) == 0) v[i] += before;          // (no gate of zero among this thread's tokens from the last to this one)
+        if (t < t1) a.dla[((size_t)b * a.L + t) * a.H + h] = (float)v[i];
     }
 }
 
@@ -793,8 +788,8 @@ Work work_of(const ScanArgs &a, const ScanPlan &p)
     wk.back = (float *)(w + p.back);
     wk.decay_forth = (float *)(w + p.decay);
     wk.decay_back = wk.decay_forth + decays;
-    wk.a = (float *)(w + p.dots);
-    wk.b = wk.a + rows;
+    wk.parts = (float *)(w + p.dots);
+    wk.anchor = wk.parts + 3 * rows;
     wk.nseg = p.nseg;
     wk.seg = p.seg;
     return wk;
@@ -820,13 +815,14 @@ hipError_t launch_bwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
 {
     const int bh = a.B * a.H, last = a.dS != nullptr, first = a.dS0 != nullptr;
     const Work wk = work_of(a, p);
-    hipError_t e = launch_kernel(scan_sum_kernel<D>, dim3(2 * bh * p.nseg), dim3(Cfg<D>::NT), stream, a, wk, 1, last, first);
-    if (e != hipSuccess) return e;
-    e = launch_kernel(scan_join_kernel, dim3(2 * bh * (D * D / 1024)), dim3(256), stream, a, wk, last, first);
-    if (e != hipSuccess) return e;
-    e = launch_kernel(scan_dq_kernel<D>, dim3(bh * p.nseg), dim3(Cfg<D>::NT), stream, a, wk);
-    if (e != hipSuccess) return e;
-    e = launch_kernel(scan_back_kernel<D>, dim3(bh * p.nseg), dim3(2 * Cfg<D>::NT), stream, a, wk);
+    hipError_t e = hipSuccess;
+    if (p.nseg > 1) {
+        e = launch_kernel(scan_sum_kernel<D>, dim3(2 * bh * p.nseg), dim3(Cfg<D>::NT), stream, a, wk, 1, last, first);
+        if (e != hipSuccess) return e;
+        e = launch_kernel(scan_join_kernel, dim3(2 * bh * (D * D / 1024)), dim3(256), stream, a, wk, last, first);
+        if (e != hipSuccess) return e;
+    }
+    e = launch_kernel(scan_grad_kernel<D>, dim3(3 * bh * p.nseg), dim3(Cfg<D>::NT), stream, a, wk);
     if (e != hipSuccess || a.dla == nullptr) return e;
     return launch_kernel(scan_gate_kernel, dim3(bh * p.nseg), dim3(256), stream, a, wk);
 }
@@ -852,10 +848,10 @@ ScanPlan scan_plan(int B, int H, int L, int D, bool backward)
     p.nseg = (blocks + p.seg - 1) / p.seg;
     const size_t states = align256((size_t)bh * (p.nseg + 1) * D * D * sizeof(float));
     if (backward) {
-        p.back = states;
-        p.decay = 2 * states;
+        p.back = p.nseg > 1 ? states : 0;
+        p.decay = 2 * p.back;
         p.dots = p.decay + align256((size_t)2 * bh * p.nseg * sizeof(float));
-        p.bytes = p.dots + align256((size_t)2 * bh * L * sizeof(float));
+        p.bytes = p.dots + align256((size_t)bh * (3 * (size_t)L + 1) * sizeof(float));
     } else if (p.nseg > 1) {
         p.back = p.decay = states;
         p.bytes = p.dots = p.decay + align256((size_t)2 * bh * p.nseg * sizeof(float));
