@@ -26,7 +26,7 @@ struct ScanArgs {
 struct ScanPlan {
     int step;                 // by the kernel of few tokens
     int nseg, seg;
-    size_t back, decay, dots, bytes;     // of the workspace: the states of the way back, the segments' decays, the rows' products; all
+    size_t back, decay, dots, bytes;     // of the workspace: the states of the way back, the segments' decays, the parts of E; all
 };
 ScanPlan scan_plan(int B, int H, int L, int D, bool backward);
 

@@ -20,6 +20,8 @@
 #include "arl2_device.h"
 #include "arl2_scan.h"
 
+#include <algorithm>
+
 namespace arl2 {
 namespace {
 
@@ -37,22 +39,29 @@ struct Work {
     int nseg, seg;
 };
 
-template <int D>
+// A wavefront has 32 columns of the state, and all of its rows or (HALVES = 2) half of them: then twice as many wavefronts ask the state for
+// half of the sums each and hand them on to the one of two that finishes a token's row.
+template <int D, int HALVES>
 struct Cfg {
-    static constexpr int NW = D / 32;                     // wavefronts, each with 32 columns of the state
+    static constexpr int NC = D / 32, NW = HALVES * NC;
     static constexpr int NT = 64 * NW;
+    static constexpr int TPW = NC / HALVES;               // 32 x 32 tiles of the state
+    static constexpr int OWN = 2 / HALVES;                // of a block's two times 32 tokens: rows that a wavefront finishes
     static constexpr int LPR = D / 8;                     // lanes to a row of 16-byte pieces
-    // Rows 32 bytes further than their length: four rows' 32-byte pieces of a transposing read lie in different banks, and so do
-    // eight rows' 16-byte pieces.
-    static constexpr int ROW = 2 * D + 32;
+    static constexpr int ROW = 2 * D;
     static constexpr int MAT = kBlock * ROW;
-    static constexpr int PROW = 2 * kBlock + 16;
+    static constexpr int PROW = 2 * kBlock;               // products: pieces lie as those of rows of 64 features
     static constexpr int PMAT = kBlock * PROW;
+    // The 16-byte piece c of row r lies at place c ^ swizzle(r): 16 rows' pieces c are in different banks, and so are 64 bytes of each of four
+    // rows 4 i .. 4 i + 3, which a transposing read of half a wavefront takes.
+    static __device__ __forceinline__ int swizzle64(int r) { return (r >> 1 & 1) << 2 | (r >> 2 & 3); }
+    static __device__ __forceinline__ int swizzle(int r) { return D == 128 ? (r & 3) << 2 | (r >> 2 & 3) : swizzle64(r); }
 };
 
 // What a block's tokens are multiplied with.  Exponents are taken apart into whole and fractional parts, whose differences lose nothing however
 // far c runs; a gate of zero is 2^-4096 (which a block's other gates cannot bring back).
 constexpr float kFold = -32.f, kPairs = -64.f;
+template <int D>
 struct Scalars {
     // by the gates alone, of two blocks in turn
     float whole[2][kBlock], frac[2][kBlock];              // c_t
@@ -61,8 +70,10 @@ struct Scalars {
     int pairs[2];                                         // products take their decays pair by pair
     // with the norms of the rows
     float post[kBlock], pcol[kBlock], penter[kBlock], norm[kBlock];
-    float red[4][kBlock][3];
-    float later[3][32], earlier[3][32];                   // of the 32 x 32 pairs of a block: sums of G over s, over u
+    union {
+        float red[D / 32][kBlock][3];
+        struct { float later[3][32], earlier[3][32]; } pair;      // of the 32 x 32 pairs of a block: sums of G over s, over u
+    };
 };
 
 __device__ __forceinline__ int tokens_of(const ScanArgs &a, int b)
@@ -133,20 +144,25 @@ __device__ __forceinline__ float lanes_sums(float (&v)[16], int lane)
     return v[0] + __shfl_xor(v[0], 16, kWave);
 }
 
-template <int D, int MODE>
+template <int D, int MODE, int HALVES>
 struct Walk {
-    using C = Cfg<D>;
+    using C = Cfg<D, HALVES>;
     static constexpr bool REV = MODE == kDk || MODE == kDv || MODE == kSumBack;
     static constexpr bool ROWS = MODE != kSum && MODE != kSumBack;
     static constexpr bool GRAD = MODE == kDq || MODE == kDk;      // rows through the normalisation
+    // The state that rows are asked of as two bf16 parts: where their sums with q and k are parts of E.  Else once rounded, as the products of
+    // rows are and the result: each is off by 2^-9 of itself on the average of the whole.
+    static constexpr bool TWO = GRAD;
     static constexpr int ROUND = C::NT / C::LPR, ROUNDS = kBlock / ROUND;    // rows that the threads stage at a time
-    static constexpr int LDS_ROWS = (ROWS ? 3 : 2) * C::MAT + (ROWS ? C::PMAT : 0);
+    // Sums for the other half lie where X and Z were at D = 64, whose workgroups have to leave room for others.
+    static constexpr bool HANDS_ON = ROWS && HALVES == 2, IN_PLACE = D == 64;
+    static constexpr int LDS_ROWS = (ROWS ? 3 : 2) * C::MAT + (ROWS ? C::PMAT : 0) + (HANDS_ON && !IN_PLACE ? C::NW * 4096 : 0);
 
     // `lds`: LDS_ROWS bytes.  Segment `seg` of (stream, head) bh.
-    static __device__ __forceinline__ void run(const ScanArgs &a, const Work &wk, int bh, int seg, unsigned char *lds, Scalars &sc)
+    static __device__ __forceinline__ void run(const ScanArgs &a, const Work &wk, int bh, int seg, unsigned char *lds, Scalars<D> &sc)
     {
         const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
-        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), column = HALVES == 1 ? wave : wave % C::NC, half = HALVES == 1 ? 0 : wave / C::NC;
         const int b = bh / a.H, h = bh - b * a.H;
         const int n = tokens_of(a, b);
         const int nblk = (n + kBlock - 1) / kBlock;
@@ -166,9 +182,9 @@ struct Walk {
 
         unsigned char *const lx = lds, *const ly = lds + (ROWS ? C::MAT : 0), *const lz = ly + C::MAT, *const lp = lz + C::MAT;
 
-        // ---- the state: 32 columns of each wavefront, register j of tile t is row 32 t + 16 (j / 8) + 8 hh + j % 8
-        f32x16 st[D / 32];
-        const int e0 = 32 * wave;
+        // ---- the state: register j of the wavefront's tile t is row r0 + 32 t + 16 (j / 8) + 8 hh + j % 8, column e0 + l32
+        f32x16 st[C::TPW];
+        const int e0 = 32 * column, r0 = 32 * C::TPW * half;
         {
             const float *from = nullptr;
             if (ROWS && wk.nseg == 1) {                           // one segment: what the call begins with
@@ -177,21 +193,21 @@ struct Walk {
             } else if (ROWS) from = (REV ? wk.back : wk.forth) + ((size_t)bh * (wk.nseg + 1) + seg + (REV ? 1 : 0)) * D * D;
             if (from == nullptr) {
 #pragma unroll
-                for (int t = 0; t < D / 32; ++t) st[t] = f32x16{};
+                for (int t = 0; t < C::TPW; ++t) st[t] = f32x16{};
             } else if (GRAD) {                                    // transposed
 #pragma unroll
-                for (int t = 0; t < D / 32; ++t)
+                for (int t = 0; t < C::TPW; ++t)
 #pragma unroll
                     for (int j = 0; j < 16; j += 4) {
-                        const f32x4 x = *reinterpret_cast<const f32x4 *>(from + (size_t)(e0 + l32) * D + 32 * t + 16 * (j / 8) + 8 * hh + j % 8);
+                        const f32x4 x = *reinterpret_cast<const f32x4 *>(from + (size_t)(e0 + l32) * D + r0 + 32 * t + 16 * (j / 8) + 8 * hh + j % 8);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) st[t][j + i] = x[i];
                     }
             } else {
 #pragma unroll
-                for (int t = 0; t < D / 32; ++t)
+                for (int t = 0; t < C::TPW; ++t)
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) st[t][j] = from[(size_t)(32 * t + 16 * (j / 8) + 8 * hh + j % 8) * D + e0 + l32];
+                    for (int j = 0; j < 16; ++j) st[t][j] = from[(size_t)(r0 + 32 * t + 16 * (j / 8) + 8 * hh + j % 8) * D + e0 + l32];
             }
         }
 
@@ -238,7 +254,7 @@ struct Walk {
 #pragma unroll
             for (int i = 0; i < ROUNDS; ++i) {
                 const int row = ROUND * i + tid / C::LPR;
-                *reinterpret_cast<u32x4 *>(to + row * C::ROW + (tid % C::LPR) * 16) = g[i];
+                *reinterpret_cast<u32x4 *>(to + row * C::ROW + (tid % C::LPR ^ C::swizzle(row)) * 16) = g[i];
                 if (kind) {
                     float x = 0.f;
 #pragma unroll
@@ -262,7 +278,7 @@ struct Walk {
 
         const int count = blk1 - blk0;
         auto block_at = [&](int i) { return REV ? blk1 - 1 - i : blk0 + i; };
-        constexpr int GW = C::NW - 1;                             // the wavefront with the gates: it has fewest products
+        constexpr int GW = 3;                                     // the wavefront with the gates: it has fewest products
         if (count > 0) {
             fetch(block_at(0));
             fetch_gate(block_at(0));
@@ -270,8 +286,25 @@ struct Walk {
             if (count > 1) fetch_gate(block_at(1));
             lds_barrier();
         }
+        // rows as operands: the lane's piece 2 m + hh of row l32 of a block's 32 lies at (row_at ^ 32 m); by columns, the lane's 8 bytes of
+        // four of 16 tokens at tr_at[0], of the next four at tr_at[1], each ^ 64 per 32 columns.  For the state's step pieces 1 and 2 of four change
+        // places: rows of its accumulator are then features 8 hh + j, as the operand of the rows' product with the state wants them.
+        int row_at = l32 * C::ROW + 16 * (hh ^ C::swizzle(l32));
+        int z_at[2], y_at[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int r = lane & 15, row = 8 * hh + 4 * k + (r >> 2), group = 2 * ((lane >> 4) & 1), swapped = (r & 1) << 1 | (r >> 1 & 1);
+            z_at[k] = row * C::ROW + 16 * ((group + (r & 3) / 2) ^ C::swizzle(row)) + 8 * (r & 1);
+            y_at[k] = row * C::ROW + 16 * ((group + swapped / 2) ^ C::swizzle(row)) + 8 * (swapped & 1);
+        }
+        auto by_columns = [&](const unsigned char *mat, const int (&at)[2], int tile, int m) {
+            return __builtin_shufflevector(lds_read_tr(mat + (at[0] ^ 64 * tile) + 16 * m * C::ROW), lds_read_tr(mat + (at[1] ^ 64 * tile) + 16 * m * C::ROW), 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        auto by_rows = [&](const unsigned char *mat, int block, int m) { return *reinterpret_cast<const bf16x8 *>(mat + 32 * block * C::ROW + (row_at ^ 32 * m)); };
         for (int i = 0; i < count; ++i) {
             const int blk = block_at(i), buf = i & 1;
+            // (the compiler is to compute what it makes of these anew: kept from block to block they would take the registers of the state)
+            asm volatile("" : "+v"(row_at), "+v"(y_at[0]), "+v"(y_at[1]), "+v"(z_at[0]), "+v"(z_at[1]));
             if (ROWS) stage(gx, lx, GRAD ? 0 : 1, buf);
             stage(gy, ly, GRAD ? 0 : 2, buf);
             stage(gz, lz, GRAD ? 2 : 0, buf);
@@ -279,42 +312,28 @@ struct Walk {
             const bool pairs = __builtin_amdgcn_readfirstlane(sc.pairs[buf]) != 0;
             lds_barrier();
 
-            // Z^T of the wavefront's columns, 16 tokens each: operand of two products below
-            bf16x8 zf[4];
-            {
-                const int r = lane & 15;
-                const unsigned char *const z = lz + (8 * hh + (r >> 2)) * C::ROW + 2 * (e0 + 16 * ((lane >> 4) & 1) + 4 * (r & 3));
-#pragma unroll
-                for (int m = 0; m < 4; ++m) zf[m] = lds_read_tr_pair(z + 16 * m * C::ROW, 4 * C::ROW);
-            }
-            f32x16 acc[2];
-            u32x2 own[2][4];                                      // the rows whose normalisation has a gradient
-            float asked[2] = {0.f, 0.f};                          // their products with what the state gives
+            bf16x8 zf[4];                                         // Z^T of the wavefront's columns, 16 tokens each
+            f32x16 acc[2] = {};                                   // rows of 32 tokens each, with two halves the wavefront's own ones first
+            u32x2 own[C::OWN][4];                                 // the rows whose normalisation has a gradient
+            float asked[C::OWN];                                  // their products with what the state gives
             // pairs of 32 x 32 rows: which of Y, which of X
             auto y_of = [](int t) { return REV ? (int)(t > 0) : (int)(t == 2); };
             auto x_of = [](int t) { return REV ? (int)(t == 2) : (int)(t > 0); };
             if constexpr (ROWS) {
-                acc[0] = acc[1] = f32x16{};
                 if (GRAD) {
                     const auto rg = rows_of(MODE == kDq ? a.q : a.k);
 #pragma unroll
-                    for (int tb = 0; tb < 2; ++tb)
+                    for (int o = 0; o < C::OWN; ++o)
 #pragma unroll
                         for (int g = 0; g < 4; ++g)
-                            own[tb][g] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rg, (uint32_t)(blk * kBlock + 32 * tb + l32) * rs + (h * D + e0 + 8 * g + 4 * hh) * 2, 0, 0));
+                            own[o][g] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rg, (uint32_t)(blk * kBlock + 32 * (o ^ half) + l32) * rs + (h * D + e0 + 8 * g + 4 * hh) * 2, 0, 0));
                 }
-                // ---- X.Y of 32 x 32 rows, times their decays, as rows of X in LDS
-#pragma unroll
-                for (int t0 = 0; t0 < 3; t0 += C::NW) {
-                    const int t = t0 + wave;
-                    if (t >= 3) break;
+                // the products of pair t, times their decays
+                auto products = [&](int t) {
                     const int sb = y_of(t), tb = x_of(t);
                     f32x16 p = {};
-                    const unsigned char *const y = ly + (32 * sb + l32) * C::ROW + 16 * hh, *const x = lx + (32 * tb + l32) * C::ROW + 16 * hh;
 #pragma unroll
-                    for (int m = 0; m < D / 16; ++m)
-                        p = mfma(*reinterpret_cast<const bf16x8 *>(y + 32 * m), *reinterpret_cast<const bf16x8 *>(x + 32 * m), p);
-                    unsigned char *const to = lp + (32 * tb + l32) * C::PROW + 64 * sb;
+                    for (int m = 0; m < D / 16; ++m) p = mfma(by_rows(ly, sb, m), by_rows(lx, tb, m), p);
                     if (!pairs) {
 #pragma unroll
                         for (int g = 0; g < 4; ++g) {
@@ -333,6 +352,12 @@ struct Walk {
                             for (int j = 0; j < 4; ++j) p[4 * g + j] *= ys[j] * __builtin_amdgcn_exp2f(REV ? (ws[j] - wt) + (fs[j] - ft) : (wt - ws[j]) + (ft - fs[j]));
                         }
                     }
+                    return p;
+                };
+                // ---- X.Y as rows of X in LDS
+                if (wave < 3) {
+                    const int t = wave, sb = y_of(t), tb = x_of(t);
+                    f32x16 p = products(t);
                     if (sb == tb) {
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
@@ -340,85 +365,107 @@ struct Walk {
                             p[j] = (REV ? d >= 0 : d <= 0) ? p[j] : 0.f;
                         }
                     }
+                    unsigned char *const to = lp + (32 * tb + l32) * C::PROW + 8 * hh;
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         const bf16x4 r = {to_bf16(p[4 * g]), to_bf16(p[4 * g + 1]), to_bf16(p[4 * g + 2]), to_bf16(p[4 * g + 3])};
-                        *reinterpret_cast<bf16x4 *>(to + 16 * g + 8 * hh) = r;
-                    }
-                    // ---- G: these products of k and q times those of dout, which lies in Z's place, and v
-                    if (MODE == kDv && a.dla != nullptr) {
-                        f32x16 w = {};
-                        const unsigned char *const z = lz + (32 * sb + l32) * C::ROW + 16 * hh;
-                        const uint32_t row = (uint32_t)(blk * kBlock + 32 * tb + l32) * rs + (h * D + 8 * hh) * 2;
-#pragma unroll
-                        for (int m = 0; m < D / 16; ++m)
-                            w = mfma(*reinterpret_cast<const bf16x8 *>(z + 32 * m), __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rv, row + 32 * m, 0, 0)), w);
-                        const float post = sc.post[32 * tb + l32];
-                        float v[16], sum = 0.f;
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const bool strictly = sb != tb || 8 * (j / 4) + 4 * hh + j % 4 > l32;
-                            v[j] = strictly ? p[j] * w[j] * post : 0.f;
-                            sum += v[j];
-                        }
-                        sum = xhalf_sum(sum);
-                        if (hh == 0) sc.earlier[t][l32] = sum;
-                        const float of = lanes_sums(v, lane);
-                        if ((lane & 16) == 0) sc.later[t][8 * ((lane & 15) / 4) + 4 * hh + lane % 4] = of;
+                        *reinterpret_cast<bf16x4 *>(to + 16 * ((4 * sb + g) ^ C::swizzle64(l32))) = r;
                     }
                 }
-                // ---- rows asked of the state, which is taken in two parts
-                const unsigned char *const x = lx + l32 * C::ROW + 16 * hh;
+                // ---- G: products of k and q times those of dout, which lies in Z's place, and v; by the last wavefronts
+                if (MODE == kDv && a.dla != nullptr && wave >= C::NW - 3) {
+                    const int t = C::NW - 1 - wave, sb = y_of(t), tb = x_of(t);
+                    const uint32_t row = (uint32_t)(blk * kBlock + 32 * tb + l32) * rs + (h * D + 8 * hh) * 2;
+                    bf16x8 vf[4];                                 // (four pieces at a time: the registers are taken)
+                    f32x16 w = {}, p;
 #pragma unroll
-                for (int m = 0; m < D / 16; ++m) {
+                    for (int m0 = 0; m0 < D / 16; m0 += 4) {
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) vf[m] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rv, row + 32 * (m0 + m), 0, 0));
+                        if (m0 == 0) p = products(t);
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) w = mfma(by_rows(lz, sb, m0 + m), vf[m], w);
+                    }
+                    const float post = sc.post[32 * tb + l32];
+                    float v[16], sum = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const bool strictly = sb != tb || 8 * (j / 4) + 4 * hh + j % 4 > l32;
+                        v[j] = strictly ? p[j] * w[j] * post : 0.f;
+                        sum += v[j];
+                    }
+                    sum = xhalf_sum(sum);
+                    if (hh == 0) sc.pair.earlier[t][l32] = sum;
+                    const float of = lanes_sums(v, lane);
+                    if ((lane & 16) == 0) sc.pair.later[t][8 * ((lane & 15) / 4) + 4 * hh + lane % 4] = of;
+                }
+                // ---- rows asked of the wavefront's part of the state, which is taken in two parts
+#pragma unroll
+                for (int m = 0; m < 2 * C::TPW; ++m) {
                     u32x4 hi, lo;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         uint32_t hj, lj;
                         split_pair(st[m / 2][8 * (m % 2) + 2 * j], st[m / 2][8 * (m % 2) + 2 * j + 1], hj, lj);
-                        hi[j] = hj; lo[j] = lj;
+                        hi[j] = hj; lo[j] = lj;                   // (unused where one part is enough)
                     }
-                    const bf16x8 x0 = *reinterpret_cast<const bf16x8 *>(x + 32 * m), x1 = *reinterpret_cast<const bf16x8 *>(x + 32 * C::ROW + 32 * m);
+                    const bf16x8 x0 = by_rows(lx, half, m + 2 * C::TPW * half), x1 = by_rows(lx, 1 - half, m + 2 * C::TPW * half);
                     acc[0] = mfma(hi, x0, acc[0]);
                     acc[1] = mfma(hi, x1, acc[1]);
-                    acc[0] = mfma(lo, x0, acc[0]);
-                    acc[1] = mfma(lo, x1, acc[1]);
+                    if (TWO) {
+                        acc[0] = mfma(lo, x0, acc[0]);
+                        acc[1] = mfma(lo, x1, acc[1]);
+                    }
                 }
                 if (pairs) {
-                    const float f0 = sc.row[buf][l32], f1 = sc.row[buf][32 + l32];
+                    const float f0 = sc.row[buf][32 * half + l32], f1 = sc.row[buf][32 * (1 - half) + l32];
 #pragma unroll
                     for (int j = 0; j < 16; ++j) { acc[0][j] *= f0; acc[1][j] *= f1; }
                 }
-                if (GRAD) {
+                if (GRAD)
 #pragma unroll
-                    for (int tb = 0; tb < 2; ++tb) asked[tb] = dot_of(own[tb], acc[tb]);
-                }
+                    for (int o = 0; o < C::OWN; ++o) asked[o] = dot_of(own[o], acc[o]);
             }
+#pragma unroll
+            for (int m = 0; m < 4; ++m) zf[m] = by_columns(lz, z_at, column, m);
             if (i + 1 < count && wave == GW) gates(buf ^ 1);
             if (i + 2 < count) fetch_gate(block_at(i + 2));
+            unsigned char *const exchange = !IN_PLACE ? lp + C::PMAT : column < C::NC / 2 ? lx : lz;
+            const int place = IN_PLACE ? column % (C::NC / 2) * 2 : column * 2;
+            auto hand_on = [&] {
+                unsigned char *const to = exchange + (place + 1 - half) * 4096 + lane * 16;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4 *>(to + 1024 * g) = f32x4{acc[1][4 * g], acc[1][4 * g + 1], acc[1][4 * g + 2], acc[1][4 * g + 3]};
+            };
+            if (HANDS_ON && !IN_PLACE) hand_on();
             if (ROWS) lds_barrier();
+            if (HANDS_ON && IN_PLACE) hand_on();                  // (nobody reads X and Z any more)
 
             // ---- and of the block's own rows
-            if constexpr (ROWS) {
-                const unsigned char *const from = lp + l32 * C::PROW + 16 * hh;
+            if constexpr (ROWS)
 #pragma unroll
-                for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                    for (int m = REV ? 2 * tb : 0; m < (REV ? 4 : 2 + 2 * tb); ++m)
-                        acc[tb] = mfma(zf[m], *reinterpret_cast<const bf16x8 *>(from + 32 * tb * C::PROW + 32 * m), acc[tb]);
-            }
+                for (int o = 0; o < C::OWN; ++o) {
+                    const int tb = o ^ half;
+                    const unsigned char *const from = lp + (32 * tb + l32) * C::PROW;
+                    auto tokens = [&](int m) { acc[o] = mfma(zf[m], *reinterpret_cast<const bf16x8 *>(from + 16 * ((2 * m + hh) ^ C::swizzle64(l32))), acc[o]); };
+                    constexpr int same = REV ? 2 : 0;             // 32 tokens that all see, and those that the earlier or the later ones see
+                    tokens(same);
+                    tokens(same + 1);
+                    if (tb == (REV ? 0 : 1)) {
+                        tokens(2 - same);
+                        tokens(3 - same);
+                    }
+                }
+
             // ---- the state's step: rows of Z times their weights in two parts
             const float fold = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(sc.fold[buf])));
             if (fold != 1.f) {
 #pragma unroll
-                for (int t = 0; t < D / 32; ++t)
+                for (int t = 0; t < C::TPW; ++t)
 #pragma unroll
                     for (int j = 0; j < 16; ++j) st[t][j] *= fold;
             }
             {
-                const int r = lane & 15, piece = ((r & 1) << 1) | ((r >> 1) & 1);       // pieces 1 and 2 of four change places: rows of the
-                // accumulator are then features 8 hh + j as the operand of the state's product wants them
-                const unsigned char *const y = ly + (8 * hh + (r >> 2)) * C::ROW + 2 * (16 * ((lane >> 4) & 1) + 4 * piece);
 #pragma unroll
                 for (int m = 0; m < 4; ++m) {
                     const f32x4 w0 = *reinterpret_cast<const f32x4 *>(&sc.penter[16 * m + 8 * hh]), w1 = *reinterpret_cast<const f32x4 *>(&sc.penter[16 * m + 8 * hh + 4]);
@@ -431,8 +478,8 @@ struct Walk {
                         hi[j] = hj; lo[j] = lj;
                     }
 #pragma unroll
-                    for (int t = 0; t < D / 32; ++t) {
-                        const bf16x8 yf = lds_read_tr_pair(y + 16 * m * C::ROW + 64 * t, 4 * C::ROW);
+                    for (int t = 0; t < C::TPW; ++t) {
+                        const bf16x8 yf = by_columns(ly, y_at, C::TPW * half + t, m);
                         st[t] = mfma(yf, __builtin_bit_cast(bf16x8, hi), st[t]);
                         st[t] = mfma(yf, __builtin_bit_cast(bf16x8, lo), st[t]);
                     }
@@ -441,62 +488,74 @@ struct Walk {
 
             // ---- rows out
             if constexpr (ROWS) {
-                float scale[2], along[2] = {0.f, 0.f};
+                if constexpr (HANDS_ON) {
+                    if (IN_PLACE) lds_barrier();
+                    const unsigned char *const from = exchange + (place + half) * 4096 + lane * 16;
+                    f32x16 more;
 #pragma unroll
-                for (int tb = 0; tb < 2; ++tb) scale[tb] = GRAD ? (pairs ? 1.f : sc.row[buf][32 * tb + l32]) : sc.post[32 * tb + l32];
-                if (GRAD) {
+                    for (int g = 0; g < 4; ++g) {
+                        const f32x4 x = *reinterpret_cast<const f32x4 *>(from + 1024 * g);
 #pragma unroll
-                    for (int tb = 0; tb < 2; ++tb) {
+                        for (int j = 0; j < 4; ++j) more[4 * g + j] = x[j];
+                    }
+                    if (GRAD) asked[0] += dot_of(own[0], more);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) acc[0][j] += more[j];
+                }
+                float scale[C::OWN], along[C::OWN];
+#pragma unroll
+                for (int o = 0; o < C::OWN; ++o) {
+                    const int tok = 32 * (o ^ half) + l32;        // in the block
+                    scale[o] = GRAD ? (pairs ? 1.f : sc.row[buf][tok]) : sc.post[tok];
+                    if (GRAD) {
                         float ss = 0.f;
 #pragma unroll
                         for (int g = 0; g < 4; ++g)
 #pragma unroll
                             for (int j = 0; j < 2; ++j) {
-                                const float x0 = __uint_as_float(own[tb][g][j] << 16), x1 = __uint_as_float(own[tb][g][j] & 0xffff0000u);
+                                const float x0 = __uint_as_float(own[o][g][j] << 16), x1 = __uint_as_float(own[o][g][j] & 0xffff0000u);
                                 ss = fmaf(x0, x0, fmaf(x1, x1, ss));
                             }
                         ss = xhalf_sum(ss);
-                        const float dot = xhalf_sum(dot_of(own[tb], acc[tb])), from_state = xhalf_sum(asked[tb]);
+                        const float dot = xhalf_sum(dot_of(own[o], acc[o])), from_state = xhalf_sum(asked[o]);
                         if (hh == 0) {
-                            sc.red[wave][32 * tb + l32][0] = dot;
-                            sc.red[wave][32 * tb + l32][1] = from_state;
-                            sc.red[wave][32 * tb + l32][2] = ss;
+                            sc.red[column][tok][0] = dot;
+                            sc.red[column][tok][1] = from_state;
+                            sc.red[column][tok][2] = ss;
                         }
                     }
                 }
-                lds_barrier();                                    // all have read the block's rows
                 float *const parts = wk.parts + ((MODE == kDq ? 0 : MODE == kDk ? (size_t)a.B * a.H : 2 * (size_t)a.B * a.H) + bh) * a.L + blk * kBlock;
-                if (GRAD) {
-#pragma unroll
-                    for (int tb = 0; tb < 2; ++tb) {
-                        float dot = 0.f, from_state = 0.f, ss = 0.f;
-#pragma unroll
-                        for (int w = 0; w < C::NW; ++w) {
-                            dot += sc.red[w][32 * tb + l32][0];
-                            from_state += sc.red[w][32 * tb + l32][1];
-                            ss += sc.red[w][32 * tb + l32][2];
-                        }
-                        const float unit = a.normalise ? fast_rsqrt(ss + a.eps) : 1.f;
-                        scale[tb] *= unit;
-                        along[tb] = a.normalise ? -(dot * scale[tb]) * unit * unit : 0.f;
-                        if (wave == 0 && hh == 0 && blk * kBlock + 32 * tb + l32 < n && a.dla != nullptr)
-                            parts[32 * tb + l32] = MODE == kDq ? from_state * scale[tb] : -(from_state * scale[tb]);
-                    }
-                }
                 if (MODE == kDv && wave == 0 && blk * kBlock + lane < n && a.dla != nullptr)
-                    parts[lane] = hh == 0 ? sc.later[0][l32] - sc.earlier[0][l32] - sc.earlier[1][l32] : sc.later[1][l32] + sc.later[2][l32] - sc.earlier[2][l32];
+                    parts[lane] = hh == 0 ? sc.pair.later[0][l32] - sc.pair.earlier[0][l32] - sc.pair.earlier[1][l32]
+                                          : sc.pair.later[1][l32] + sc.pair.later[2][l32] - sc.pair.earlier[2][l32];
+                lds_barrier();                                    // all have read the block's rows
                 const auto ro = rows_of(MODE == kOut ? a.out : MODE == kDq ? a.dq : MODE == kDk ? a.dk : a.dv);
 #pragma unroll
-                for (int tb = 0; tb < 2; ++tb) {
+                for (int o = 0; o < C::OWN; ++o) {
+                    const int tok = 32 * (o ^ half) + l32;
+                    if (GRAD) {
+                        float dot = 0.f, from_state = 0.f, ss = 0.f;
+#pragma unroll
+                        for (int w = 0; w < C::NC; ++w) {
+                            dot += sc.red[w][tok][0];
+                            from_state += sc.red[w][tok][1];
+                            ss += sc.red[w][tok][2];
+                        }
+                        const float unit = a.normalise ? fast_rsqrt(ss + a.eps) : 1.f;
+                        scale[o] *= unit;
+                        along[o] = a.normalise ? -(dot * scale[o]) * unit * unit : 0.f;
+                        if (column == 0 && hh == 0 && blk * kBlock + tok < n && a.dla != nullptr) parts[tok] = MODE == kDq ? from_state * scale[o] : -(from_state * scale[o]);
+                    }
                     uint32_t w[4][2];
 #pragma unroll
                     for (int g = 0; g < 4; ++g)
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
-                            float x0 = acc[tb][4 * g + 2 * j] * scale[tb], x1 = acc[tb][4 * g + 2 * j + 1] * scale[tb];
+                            float x0 = acc[o][4 * g + 2 * j] * scale[o], x1 = acc[o][4 * g + 2 * j + 1] * scale[o];
                             if (GRAD) {
-                                x0 = fmaf(along[tb], __uint_as_float(own[tb][g][j] << 16), x0);
-                                x1 = fmaf(along[tb], __uint_as_float(own[tb][g][j] & 0xffff0000u), x1);
+                                x0 = fmaf(along[o], __uint_as_float(own[o][g][j] << 16), x0);
+                                x1 = fmaf(along[o], __uint_as_float(own[o][g][j] & 0xffff0000u), x1);
                             }
                             const bf16x2 r = {to_bf16(x0), to_bf16(x1)};
                             w[g][j] = __builtin_bit_cast(uint32_t, r);
@@ -507,7 +566,7 @@ struct Walk {
                         const auto s0 = __builtin_amdgcn_permlane32_swap(w[g][0], w[g + 2][0], false, false);
                         const auto s1 = __builtin_amdgcn_permlane32_swap(w[g][1], w[g + 2][1], false, false);
                         const u32x4 v = {s0[0], s1[0], s0[1], s1[1]};
-                        __builtin_amdgcn_raw_buffer_store_b128(v, ro, (uint32_t)(blk * kBlock + 32 * tb + l32) * rs + (h * D + e0 + 16 * hh + 8 * g) * 2, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b128(v, ro, (uint32_t)(blk * kBlock + tok) * rs + (h * D + e0 + 16 * hh + 8 * g) * 2, 0, 0);
                     }
                 }
             } else lds_barrier();
@@ -527,9 +586,9 @@ struct Walk {
                 gathered = sc.fold[0];
             }
 #pragma unroll
-            for (int t = 0; t < D / 32; ++t)
+            for (int t = 0; t < C::TPW; ++t)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) to[(size_t)(32 * t + 16 * (j / 8) + 8 * hh + j % 8) * D + e0 + l32] = st[t][j] * gathered;
+                for (int j = 0; j < 16; ++j) to[(size_t)(r0 + 32 * t + 16 * (j / 8) + 8 * hh + j % 8) * D + e0 + l32] = st[t][j] * gathered;
         }
         if (MODE == kDq && wk.nseg == 1 && a.dS != nullptr && a.dla != nullptr) {        // <S_L, dS>: the state is transposed here
             lds_barrier();                                        // all have read the last block's sums
@@ -537,20 +596,20 @@ struct Walk {
             const float *const from = a.dS + (size_t)bh * D * D + (size_t)(e0 + l32) * D;
             float dot = 0.f;
 #pragma unroll
-            for (int t = 0; t < D / 32; ++t)
+            for (int t = 0; t < C::TPW; ++t)
 #pragma unroll
                 for (int j = 0; j < 16; j += 4) {
-                    const f32x4 x = *reinterpret_cast<const f32x4 *>(from + 32 * t + 16 * (j / 8) + 8 * hh + j % 8);
+                    const f32x4 x = *reinterpret_cast<const f32x4 *>(from + r0 + 32 * t + 16 * (j / 8) + 8 * hh + j % 8);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) dot = fmaf(x[i], st[t][j + i], dot);
                 }
 #pragma unroll
             for (int m = 32; m > 0; m >>= 1) dot += __shfl_xor(dot, m, kWave);
-            if (lane == 0) sc.red[wave][0][0] = dot;
+            if (lane == 0) sc.red[column][half][0] = dot;
             lds_barrier();
             if (tid == 0) {
                 dot = 0.f;
-                for (int w = 0; w < C::NW; ++w) dot += sc.red[w][0][0];
+                for (int w = 0; w < C::NW; ++w) dot += sc.red[w % C::NC][w / C::NC][0];
                 wk.anchor[bh] = dot * sc.fold[0];
             }
         }
@@ -570,30 +629,30 @@ struct Walk {
     }
 };
 
-template <int D>
-__global__ __launch_bounds__(Cfg<D>::NT, 2) void scan_out_kernel(ScanArgs a, Work wk)
+template <int D, int HALVES>
+__global__ __launch_bounds__((Cfg<D, HALVES>::NT), D == 64 ? 3 : 2) void scan_out_kernel(ScanArgs a, Work wk)
 {
-    using W = Walk<D, kOut>;
+    using W = Walk<D, kOut, HALVES>;
     __shared__ __align__(16) unsigned char lds[W::LDS_ROWS];
-    __shared__ __align__(16) Scalars sc;
+    __shared__ __align__(16) Scalars<D> sc;
     const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
     W::run(a, wk, id / wk.nseg, id % wk.nseg, lds, sc);
 }
 
 // Segments' own states.  `back`: the way back too, as every second workgroup; the last segment of the way forth and the first of
 // the way back only where something reads them.
-template <int D>
-__global__ __launch_bounds__(Cfg<D>::NT, 2) void scan_sum_kernel(ScanArgs a, Work wk, int back, int need_last, int need_first)
+template <int D, int HALVES>
+__global__ __launch_bounds__((Cfg<D, HALVES>::NT), 3) void scan_sum_kernel(ScanArgs a, Work wk, int back, int need_last, int need_first)
 {
-    __shared__ __align__(16) unsigned char lds[Walk<D, kSum>::LDS_ROWS];
-    __shared__ __align__(16) Scalars sc;
+    __shared__ __align__(16) unsigned char lds[Walk<D, kSum, HALVES>::LDS_ROWS];
+    __shared__ __align__(16) Scalars<D> sc;
     const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
     const int unit = back ? id >> 1 : id;
     const int bh = unit / wk.nseg, seg = unit % wk.nseg;
     const int blocks = (tokens_of(a, bh / a.H) + kBlock - 1) / kBlock, nact = max(1, (blocks + wk.seg - 1) / wk.seg);
     if (back && (id & 1)) {
-        if (seg > 0 || need_first) Walk<D, kSumBack>::run(a, wk, bh, seg, lds, sc);
-    } else if (seg < nact - 1 || need_last) Walk<D, kSum>::run(a, wk, bh, seg, lds, sc);
+        if (seg > 0 || need_first) Walk<D, kSumBack, HALVES>::run(a, wk, bh, seg, lds, sc);
+    } else if (seg < nact - 1 || need_last) Walk<D, kSum, HALVES>::run(a, wk, bh, seg, lds, sc);
 }
 
 // States at the segments' borders from the segments' own: each its decay times the one before, plus its own.
@@ -634,17 +693,17 @@ __global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, Work wk, int
 }
 
 // The rows' gradients: three walks of a segment by three workgroups that follow one another.
-template <int D>
-__global__ __launch_bounds__(Cfg<D>::NT, D / 64) void scan_grad_kernel(ScanArgs a, Work wk)
+template <int D, int HALVES>
+__global__ __launch_bounds__((Cfg<D, HALVES>::NT), D == 64 ? 3 : 2) void scan_grad_kernel(ScanArgs a, Work wk)
 {
-    __shared__ __align__(16) unsigned char lds[Walk<D, kDq>::LDS_ROWS];
-    __shared__ __align__(16) Scalars sc;
+    __shared__ __align__(16) unsigned char lds[Walk<D, kDq, HALVES>::LDS_ROWS];
+    __shared__ __align__(16) Scalars<D> sc;
     const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
     const int unit = id / 3, which = id - 3 * unit;
     const int bh = unit / wk.nseg, seg = unit % wk.nseg;
-    if (which == 0) Walk<D, kDv>::run(a, wk, bh, seg, lds, sc);
-    else if (which == 1) Walk<D, kDk>::run(a, wk, bh, seg, lds, sc);
-    else Walk<D, kDq>::run(a, wk, bh, seg, lds, sc);
+    if (which == 0) Walk<D, kDv, HALVES>::run(a, wk, bh, seg, lds, sc);
+    else if (which == 1) Walk<D, kDk, HALVES>::run(a, wk, bh, seg, lds, sc);
+    else Walk<D, kDq, HALVES>::run(a, wk, bh, seg, lds, sc);
 }
 
 // The gates' gradients of a segment: from <state, gradient of the state> at its end backwards, a sum that a gate of zero begins anew.
@@ -672,7 +731,8 @@ __global__ __launch_bounds__(256) void scan_gate_kernel(ScanArgs a, Work wk)
     }
     double dot = 0.0;
     if (wk.nseg > 1 && (seg < nact - 1 || a.dS != nullptr)) {
-        const float *const x = wk.forth + ((size_t)bh * (wk.nseg + 1) + seg + 1) * nn, *const y = wk.back + ((size_t)bh * (wk.nseg + 1) + seg + 1) * nn;
+        const size_t at = ((size_t)bh * (wk.nseg + 1) + seg + 1) * nn;
+        const float *const x = wk.forth + at, *const y = wk.back + at;
         for (int e = tid * 4; e < nn; e += 4096) {
             f32x4 p[4], q[4];
 #pragma unroll
@@ -795,34 +855,36 @@ Work work_of(const ScanArgs &a, const ScanPlan &p)
     return wk;
 }
 
-template <int D>
+// Halves of the state's rows by wavefront: see scan_plan.
+template <int D, int HALVES>
+hipError_t launch_sums(const ScanArgs &a, const ScanPlan &p, const Work &wk, bool back, int last, int first, hipStream_t stream)
+{
+    if (p.nseg == 1) return hipSuccess;
+    const int bh = a.B * a.H, ways = back ? 2 : 1;
+    const hipError_t e = launch_kernel(scan_sum_kernel<D, HALVES>, dim3(ways * bh * p.nseg), dim3(Cfg<D, HALVES>::NT), stream, a, wk, (int)back, last, first);
+    if (e != hipSuccess) return e;
+    return launch_kernel(scan_join_kernel, dim3(ways * bh * (D * D / 1024)), dim3(256), stream, a, wk, last, first);
+}
+
+template <int D, int SUM_HALVES>
 hipError_t launch_fwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
 {
     const int bh = a.B * a.H;
     if (p.step) return launch_kernel(scan_step_kernel<D>, dim3(bh * (D / 32)), dim3(256), stream, a);
     const Work wk = work_of(a, p);
-    if (p.nseg > 1) {
-        hipError_t e = launch_kernel(scan_sum_kernel<D>, dim3(bh * p.nseg), dim3(Cfg<D>::NT), stream, a, wk, 0, 0, 0);
-        if (e != hipSuccess) return e;
-        e = launch_kernel(scan_join_kernel, dim3(bh * (D * D / 1024)), dim3(256), stream, a, wk, 0, 0);
-        if (e != hipSuccess) return e;
-    }
-    return launch_kernel(scan_out_kernel<D>, dim3(bh * p.nseg), dim3(Cfg<D>::NT), stream, a, wk);
+    const hipError_t e = launch_sums<D, SUM_HALVES>(a, p, wk, false, 0, 0, stream);
+    if (e != hipSuccess) return e;
+    return launch_kernel(scan_out_kernel<D, 2>, dim3(bh * p.nseg), dim3(Cfg<D, 2>::NT), stream, a, wk);
 }
 
-template <int D>
+template <int D, int SUM_HALVES, int HALVES>
 hipError_t launch_bwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
 {
-    const int bh = a.B * a.H, last = a.dS != nullptr, first = a.dS0 != nullptr;
+    const int bh = a.B * a.H;
     const Work wk = work_of(a, p);
-    hipError_t e = hipSuccess;
-    if (p.nseg > 1) {
-        e = launch_kernel(scan_sum_kernel<D>, dim3(2 * bh * p.nseg), dim3(Cfg<D>::NT), stream, a, wk, 1, last, first);
-        if (e != hipSuccess) return e;
-        e = launch_kernel(scan_join_kernel, dim3(2 * bh * (D * D / 1024)), dim3(256), stream, a, wk, last, first);
-        if (e != hipSuccess) return e;
-    }
-    e = launch_kernel(scan_grad_kernel<D>, dim3(3 * bh * p.nseg), dim3(Cfg<D>::NT), stream, a, wk);
+    hipError_t e = launch_sums<D, SUM_HALVES>(a, p, wk, true, a.dS != nullptr, a.dS0 != nullptr, stream);
+    if (e != hipSuccess) return e;
+    e = launch_kernel(scan_grad_kernel<D, HALVES>, dim3(3 * bh * p.nseg), dim3(Cfg<D, HALVES>::NT), stream, a, wk);
     if (e != hipSuccess || a.dla == nullptr) return e;
     return launch_kernel(scan_gate_kernel, dim3(bh * p.nseg), dim3(256), stream, a, wk);
 }
@@ -831,42 +893,51 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 }  // namespace
 
+// Segments: enough workgroups for the chip, no more states than that takes.  Time is counted in hundredths of a block of a full chip, which has `per_cu` workgroups
+// on a CU (one alone takes 70 and 60 hundredths of two's and three's); a second part of the sequence costs the sums of the segments (a block half of one), what joins them,
+// by segment, and two launches.  12 heads x 128 (block: 4.5 us; gradients 9.9 us): 1560 tokens in 7, 13 (taken), 25 segments 32.8, 25.9, 27.3 us; 32760 in 15, 21 (taken), 32, 42: 219,
+// 176, 199, 183 us; gradients of 1560 in 3, 7, 13 (taken), 25: 86, 54, 51, 66 us; of 8 x 4680 in 5 (taken), 6, 8, 10: 532, 571, 581, 594 us.
 ScanPlan scan_plan(int B, int H, int L, int D, bool backward)
 {
     ScanPlan p = {};
-    const int bh = B * H, blocks = (L + kBlock - 1) / kBlock;
+    const int blocks = (L + kBlock - 1) / kBlock, per_cu = D == 64 ? 3 : backward ? 2 : 1;
+    const long long bh = (long long)B * H, walks = (backward ? 3 : 1) * bh;
+    p.nseg = 1;
     if (!backward && L <= kStepTokens) {
         p.step = 1;
-        p.nseg = 1;
         return p;
     }
-    // two workgroups a CU
-    int nseg = 2 * kNumCu / bh;
-    nseg = nseg < 1 ? 1 : nseg > blocks ? blocks : nseg;
-    p.seg = (blocks + nseg - 1) / nseg;
-    if (backward && p.seg > 16) p.seg = 16;
-    p.nseg = (blocks + p.seg - 1) / p.seg;
-    const size_t states = align256((size_t)bh * (p.nseg + 1) * D * D * sizeof(float));
-    if (backward) {
-        p.back = p.nseg > 1 ? states : 0;
-        p.decay = 2 * p.back;
-        p.dots = p.decay + align256((size_t)2 * bh * p.nseg * sizeof(float));
-        p.bytes = p.dots + align256((size_t)bh * (3 * (size_t)L + 1) * sizeof(float));
-    } else if (p.nseg > 1) {
-        p.back = p.decay = states;
-        p.bytes = p.dots = p.decay + align256((size_t)2 * bh * p.nseg * sizeof(float));
+    double best = 0.0;
+    for (int r = 0; r <= 2 * per_cu + 2; ++r) {                   // segments for r workgroups on each CU
+        const long long want = r == 0 ? 1 : std::min<long long>(r * kNumCu / walks, blocks);
+        if (want < 1) continue;
+        const int seg = std::min((int)((blocks + want - 1) / want), backward ? 16 : blocks), nseg = (blocks + seg - 1) / seg;
+        const long long all = walks * nseg, full = all / (per_cu * kNumCu), rest = (all % (per_cu * kNumCu) + kNumCu - 1) / kNumCu;
+        double cost = seg * (100.0 * full + (rest ? 40.0 + 60.0 * rest / per_cu : 0.0));
+        if (nseg > 1) cost += 50.0 * seg * ((bh * nseg + kNumCu - 1) / kNumCu) + 8.0 * nseg + 150.0;
+        if (best == 0.0 || cost < best) {
+            best = cost;
+            p.seg = seg;
+            p.nseg = nseg;
+        }
     }
+    const size_t states = p.nseg > 1 ? align256((size_t)bh * (p.nseg + 1) * D * D * sizeof(float)) : 0;
+    const size_t decays = p.nseg > 1 ? align256((size_t)2 * bh * p.nseg * sizeof(float)) : 0;
+    p.back = states;
+    p.decay = backward ? 2 * states : states;
+    p.dots = p.decay + decays;
+    p.bytes = p.dots + (backward ? align256((size_t)bh * (3 * (size_t)L + 1) * sizeof(float)) : 0);
     return p;
 }
 
 hipError_t launch_scan_fwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
 {
-    return a.D == 128 ? launch_fwd<128>(a, p, stream) : launch_fwd<64>(a, p, stream);
+    return a.D == 128 ? launch_fwd<128, 2>(a, p, stream) : launch_fwd<64, 2>(a, p, stream);
 }
 
 hipError_t launch_scan_bwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
 {
-    return a.D == 128 ? launch_bwd<128>(a, p, stream) : launch_bwd<64>(a, p, stream);
+    return a.D == 128 ? launch_bwd<128, 2, 1>(a, p, stream) : launch_bwd<64, 2, 2>(a, p, stream);
 }
 
 }  // namespace arl2

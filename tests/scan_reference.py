@@ -8,8 +8,9 @@ BLOCK, LONGEST = 64, 1024        # tokens of a block; of a segment of the gradie
 
 # One rounding to bf16 is off by at most U16 of the value.  A value in two bf16 parts is off by U16 of U16, fp32 arithmetic on the way (norms,
 # decays, products, sums of up to some hundred terms) by less than another 2^-17 of the terms' magnitudes.  A block's own products
-# (q'.k' for out and dv, dout.v for dq and dk, from 9 tokens on for out) are rounded to bf16 before they multiply rows of the block: U16
-# of each term's magnitude more, `near` below.
+# (dout.v for dq and dk) are rounded to bf16 before they multiply rows of the block: U16 of each term's magnitude more, `near` below.
+# For out (from 9 tokens on) and dv these products and the state's features that the block's rows are multiplied with both are: a term is one of
+# the two, so that U16 of all magnitudes comes in.
 U16 = 2.0 ** -8
 TWO = U16 * U16 + 2.0 ** -17
 
@@ -60,19 +61,16 @@ class Case:
         """out, S, and their limits."""
         q, k, v, do, iq, ik, a, S, _ = self._inputs()
         q, k = q * iq, k * ik
-        out, most, near = np.zeros_like(q), np.zeros_like(q), np.zeros_like(q)
-        M, N = np.abs(S), np.zeros_like(S)                # magnitudes of all, and of the block's own
+        out, most = np.zeros_like(q), np.zeros_like(q)
+        M = np.abs(S)                                     # magnitudes
         for t in range(self.L):
             on = np.array([t < n for n in self.lens])
-            if t % BLOCK == 0:
-                N[:] = 0.0
-            for X, f in ((S, lambda x: x), (M, np.abs), (N, np.abs)):
+            for X, f in ((S, lambda x: x), (M, np.abs)):
                 X[on] = a[on, t, :, None, None] * X[on] + f(k[on, t])[..., :, None] * f(v[on, t])[..., None, :]
             out[on, t] = np.einsum("bhd,bhde->bhe", q[on, t], S[on])
             most[on, t] = np.einsum("bhd,bhde->bhe", np.abs(q[on, t]), M[on])
-            near[on, t] = np.einsum("bhd,bhde->bhe", np.abs(q[on, t]), N[on])
         few = self.L <= 8
-        return out, S, U16 * np.abs(out) + (0.0 if few else U16) * near + TWO * most, TWO * M + 1e-30
+        return out, S, U16 * np.abs(out) + (0.0 if few else U16) * most + TWO * most, TWO * M + 1e-30
 
     def backward(self):
         """dq, dk, dv, dla, dS0, and their limits."""
@@ -80,7 +78,7 @@ class Case:
         q, k = q0 * iq, k0 * ik
         B, L = self.B, self.L
         dq, dk, dv = np.zeros_like(q), np.zeros_like(q), np.zeros_like(q)
-        mq, mk, mv, nq, nk, nv = (np.zeros_like(q) for _ in range(6))
+        mq, mk, mv, nq, nk = (np.zeros_like(q) for _ in range(5))
         E, ME, MS = np.zeros(q.shape[:3]), np.zeros(q.shape[:3]), [None] * L
         states, M, near = [None] * L, np.abs(S), np.zeros_like(S)
         for t in range(L):
@@ -101,7 +99,7 @@ class Case:
             if t % BLOCK == BLOCK - 1:
                 near[:] = 0.0
             near[on] += np.abs(q[on, t])[..., :, None] * np.abs(do[on, t])[..., None, :]
-            nk[on, t], nv[on, t] = np.einsum("bhe,bhde->bhd", np.abs(v[on, t]), near[on]), np.einsum("bhd,bhde->bhe", np.abs(k[on, t]), near[on])
+            nk[on, t] = np.einsum("bhe,bhde->bhd", np.abs(v[on, t]), near[on])
             near[on] *= a[on, t, :, None, None]
             G[on] += q[on, t][..., :, None] * do[on, t][..., None, :]
             N[on] += np.abs(q[on, t])[..., :, None] * np.abs(do[on, t])[..., None, :]
@@ -124,7 +122,7 @@ class Case:
                 for y in (m, c):
                     y[:] = i * (y + np.abs(x) * (np.abs(x) * y).sum(-1, keepdims=True))
             limits.append(U16 * (np.abs(d) + c) + 2.0 * TWO * m)
-        limits += [U16 * (np.abs(dv) + nv) + TWO * mv, 2.0 * TWO * (along + ends) + 1e-30, TWO * N + 1e-30]
+        limits += [U16 * (np.abs(dv) + mv) + TWO * mv, 2.0 * TWO * (along + ends) + 1e-30, TWO * N + 1e-30]
         return (dq, dk, dv, E, G), limits
 
 
