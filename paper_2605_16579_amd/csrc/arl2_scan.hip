@@ -116,13 +116,17 @@ __device__ __forceinline__ float exp2_of(double x)
     return x < -4096.0 ? 0.f : __builtin_ldexpf(f, (int)w);
 }
 
-// Two fp32 values as two bf16 each, hi + lo to 2^-17 of them.
-__device__ __forceinline__ void split_pair(float x, float y, uint32_t &hi, uint32_t &lo)
+// Two fp32 values as N bf16 each, whose sum is off by 2^(-8 N) of them at the most.
+template <int N>
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t (&part)[N])
 {
-    const bf16x2 h = {to_bf16(x), to_bf16(y)};
-    hi = __builtin_bit_cast(uint32_t, h);
-    const bf16x2 l = {to_bf16(x - __uint_as_float(hi << 16)), to_bf16(y - __uint_as_float(hi & 0xffff0000u))};
-    lo = __builtin_bit_cast(uint32_t, l);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const bf16x2 p = {to_bf16(x), to_bf16(y)};
+        part[i] = __builtin_bit_cast(uint32_t, p);
+        x -= __uint_as_float(part[i] << 16);
+        y -= __uint_as_float(part[i] & 0xffff0000u);
+    }
 }
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mfma(u32x4 a, bf16x8 b, f32x16 c) { return mfma(__builtin_bit_cast(bf16x8, a), b, c); }
@@ -150,9 +154,10 @@ struct Walk {
     static constexpr bool REV = MODE == kDk || MODE == kDv || MODE == kSumBack;
     static constexpr bool ROWS = MODE != kSum && MODE != kSumBack;
     static constexpr bool GRAD = MODE == kDq || MODE == kDk;      // rows through the normalisation
-    // The state that rows are asked of as two bf16 parts: where their sums with q and k are parts of E.  Else once rounded, as the products of
-    // rows are and the result: each is off by 2^-9 of itself on the average of the whole.
-    static constexpr bool TWO = GRAD;
+    // bf16 parts of the state that rows are asked of, and of the weighted rows that enter it.  Of the state: one, as the products of rows are rounded once and the
+    // result; of what enters: two, the state is off by 2.4e-6 in the 2-norm.  Three of either where sums with q and k are parts of E, whose errors add up over a segment:
+    // with two, heads with gates of 0.8 had E off by 9.1e-6, with three by 1.0e-6 (with three of one and two of the other 6e-6).
+    static constexpr int ASKED = GRAD ? 3 : 1, ENTER = GRAD ? 3 : 2;
     static constexpr int ROUND = C::NT / C::LPR, ROUNDS = kBlock / ROUND;    // rows that the threads stage at a time
     // Sums for the other half lie where X and Z were at D = 64, whose workgroups have to leave room for others.
     static constexpr bool HANDS_ON = ROWS && HALVES == 2, IN_PLACE = D == 64;
@@ -236,14 +241,24 @@ struct Walk {
                                                            (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, 63));
             const double r = base + (REV ? tot - c : c), end = base + tot;
             const bool fold = !(end >= kFold), pairs = !(end >= kPairs);
-            sc.whole[buf][lane] = (float)__builtin_floor(c);
-            sc.frac[buf][lane] = (float)(c - __builtin_floor(c));
-            sc.row[buf][lane] = exp2_of(r);
-            const float col = pairs ? 0.f : exp2_of(-r);
+            const double w = __builtin_floor(fmax(r, -4096.0));
+            const float f = (float)(r - w);                       // (a NaN stays one)
+            sc.row[buf][lane] = r < -4096.0 ? 0.f : __builtin_ldexpf(__builtin_amdgcn_exp2f(f), (int)w);
+            float col = __builtin_ldexpf(__builtin_amdgcn_exp2f(-f), -(int)w);
+            if (pairs) {
+                sc.whole[buf][lane] = (float)__builtin_floor(c);
+                sc.frac[buf][lane] = (float)(c - __builtin_floor(c));
+                col = 0.f;
+            }
             sc.col[buf][lane] = col;
-            sc.enter[buf][lane] = fold ? exp2_of(REV ? c : tot - c) : col;
+            sc.enter[buf][lane] = col;
+            float all = 1.f;
+            if (fold) {
+                sc.enter[buf][lane] = exp2_of(end - r);
+                all = exp2_of(end);
+            }
             if (lane == 0) {
-                sc.fold[buf] = fold ? exp2_of(end) : 1.f;
+                sc.fold[buf] = all;
                 sc.pairs[buf] = pairs;
             }
             base = fold ? 0.0 : end;
@@ -402,19 +417,19 @@ struct Walk {
                 // ---- rows asked of the wavefront's part of the state, which is taken in two parts
 #pragma unroll
                 for (int m = 0; m < 2 * C::TPW; ++m) {
-                    u32x4 hi, lo;
+                    u32x4 part[ASKED];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        uint32_t hj, lj;
-                        split_pair(st[m / 2][8 * (m % 2) + 2 * j], st[m / 2][8 * (m % 2) + 2 * j + 1], hj, lj);
-                        hi[j] = hj; lo[j] = lj;                   // (unused where one part is enough)
+                        uint32_t w[ASKED];
+                        split_pair(st[m / 2][8 * (m % 2) + 2 * j], st[m / 2][8 * (m % 2) + 2 * j + 1], w);
+#pragma unroll
+                        for (int k = 0; k < ASKED; ++k) part[k][j] = w[k];
                     }
                     const bf16x8 x0 = by_rows(lx, half, m + 2 * C::TPW * half), x1 = by_rows(lx, 1 - half, m + 2 * C::TPW * half);
-                    acc[0] = mfma(hi, x0, acc[0]);
-                    acc[1] = mfma(hi, x1, acc[1]);
-                    if (TWO) {
-                        acc[0] = mfma(lo, x0, acc[0]);
-                        acc[1] = mfma(lo, x1, acc[1]);
+#pragma unroll
+                    for (int k = 0; k < ASKED; ++k) {
+                        acc[0] = mfma(part[k], x0, acc[0]);
+                        acc[1] = mfma(part[k], x1, acc[1]);
                     }
                 }
                 if (pairs) {
@@ -470,18 +485,19 @@ struct Walk {
                 for (int m = 0; m < 4; ++m) {
                     const f32x4 w0 = *reinterpret_cast<const f32x4 *>(&sc.penter[16 * m + 8 * hh]), w1 = *reinterpret_cast<const f32x4 *>(&sc.penter[16 * m + 8 * hh + 4]);
                     const u32x4 zb = __builtin_bit_cast(u32x4, zf[m]);
-                    u32x4 hi, lo;
+                    u32x4 part[ENTER];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        uint32_t hj, lj;
-                        split_pair(__uint_as_float(zb[j] << 16) * (j < 2 ? w0[2 * j] : w1[2 * j - 4]), __uint_as_float(zb[j] & 0xffff0000u) * (j < 2 ? w0[2 * j + 1] : w1[2 * j - 3]), hj, lj);
-                        hi[j] = hj; lo[j] = lj;
+                        uint32_t w[ENTER];
+                        split_pair(__uint_as_float(zb[j] << 16) * (j < 2 ? w0[2 * j] : w1[2 * j - 4]), __uint_as_float(zb[j] & 0xffff0000u) * (j < 2 ? w0[2 * j + 1] : w1[2 * j - 3]), w);
+#pragma unroll
+                        for (int k = 0; k < ENTER; ++k) part[k][j] = w[k];
                     }
 #pragma unroll
                     for (int t = 0; t < C::TPW; ++t) {
                         const bf16x8 yf = by_columns(ly, y_at, C::TPW * half + t, m);
-                        st[t] = mfma(yf, __builtin_bit_cast(bf16x8, hi), st[t]);
-                        st[t] = mfma(yf, __builtin_bit_cast(bf16x8, lo), st[t]);
+#pragma unroll
+                        for (int k = 0; k < ENTER; ++k) st[t] = mfma(yf, __builtin_bit_cast(bf16x8, part[k]), st[t]);
                     }
                 }
             }
