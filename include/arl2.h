@@ -402,8 +402,8 @@ arl2_status arl2_scan_fwd(const arl2_scan_desc *desc, const void *q, const void 
  *   dS        device fp32 [B][H][D][D], gradient of the last state; NULL: zeros.
  *   dq, dk, dv  device bf16 [B][L][H][D], written (through the normalisation where there is one).
  *   dlog_alpha  device fp32 [B][L][H], written: the gradient of log_alpha as if it had no upper limit; zero at a gate of zero.  NULL: it is not wanted.
- *   dS0       device fp32 [B][H][D][D], written; NULL: it is not wanted.  May be dS itself.
- * What is written must overlap neither an input (dS0 and dS apart) nor what else is written.  Deterministic.
+ *   dS0       device fp32 [B][H][D][D], written; NULL: it is not wanted.
+ * What is written must overlap neither an input nor what else is written.  Deterministic.
  */
 arl2_status arl2_scan_bwd(const arl2_scan_desc *desc, const void *q, const void *k, const void *v, const float *log_alpha,
                           const int32_t *seq_len, const float *S0, const void *dout, const float *dS,

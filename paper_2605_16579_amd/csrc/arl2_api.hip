@@ -759,8 +759,7 @@ arl2_status arl2_scan_bwd(const arl2_scan_desc *desc, const void *q, const void 
     const Range made[] = {{dq, rows}, {dk, rows}, {dv, rows}, {dlog_alpha, gates}, {dS0, state}, {desc->workspace, plan.bytes}};
     for (const Range &m : made) {
         for (const Range &i : in)
-            if (overlaps(m.p, m.n, i.p, i.n) && !(m.p == dS0 && i.p == dS && dS0 == dS))
-                return fail(ARL2_ERR_INVALID_ARG, "gradients and the workspace must not overlap an input (dS0 may be dS)");
+            if (overlaps(m.p, m.n, i.p, i.n)) return fail(ARL2_ERR_INVALID_ARG, "gradients and the workspace must not overlap an input");
         for (const Range &o : made)
             if (&o != &m && overlaps(m.p, m.n, o.p, o.n)) return fail(ARL2_ERR_INVALID_ARG, "gradients and the workspace must not overlap each other");
     }

@@ -80,9 +80,8 @@ def test_scan_arguments(A):
     assert st == 1 and "dlog_alpha" in why
     for i in (8, 9, 10, 11, 12):
         for j in (0, 1, 2, 3, 5, 6, 7):
-            if (i, j) != (12, 7):
-                st, why = scan(A, True, at={i: PTR[j]})
-                assert st == 1 and "overlap" in why, (i, j)
+            st, why = scan(A, True, at={i: PTR[j]})           # (dS0 is not dS either: other workgroups still read it)
+            assert st == 1 and "overlap" in why, (i, j)
         for j in (8, 9, 10, 11, 12):
             if i != j:
                 st, why = scan(A, True, at={i: PTR[j]})
