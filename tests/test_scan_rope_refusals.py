@@ -33,7 +33,7 @@ def test_descriptors_match_the_header(A, name):
 
 
 def scan(A, bwd=False, at=(), **kw):
-    d = A.arl2_scan_desc(**{**dict(B=2, H=3, L=100, D=64, workspace=WS, workspace_bytes=1 << 40), **kw})
+    d = A.arl2_scan_desc(**{**dict(B=2, H=3, L=1000, D=64, workspace=WS, workspace_bytes=1 << 40), **kw})
     p = PTR[:13 if bwd else 8]
     for i, x in dict(at).items():
         p[i] = x
@@ -47,10 +47,10 @@ def test_scan_sizes(A, bwd):
     lib = A.load_library()
     for bad in (dict(B=0), dict(H=0), dict(L=0), dict(raw_rows=2), dict(raw_rows=-1), dict(l2_eps=-1.0), dict(l2_eps=float("nan"))):
         assert scan(A, bwd, **bad)[0] == 1, bad
-        assert lib.arl2_scan_workspace_bytes(ctypes.byref(A.arl2_scan_desc(**{**dict(B=2, H=3, L=100, D=64), **bad}))) == 0
+        assert lib.arl2_scan_workspace_bytes(ctypes.byref(A.arl2_scan_desc(**{**dict(B=2, H=3, L=1000, D=64), **bad}))) == 0
     for bad in (dict(D=96), dict(D=256), dict(L=1 << 23), dict(H=1 << 18, L=1), dict(B=1 << 20)):
         assert scan(A, bwd, **bad)[0] == 2, bad
-    need = (lib.arl2_scan_bwd_workspace_bytes if bwd else lib.arl2_scan_workspace_bytes)(ctypes.byref(A.arl2_scan_desc(B=2, H=3, L=100, D=64)))
+    need = (lib.arl2_scan_bwd_workspace_bytes if bwd else lib.arl2_scan_workspace_bytes)(ctypes.byref(A.arl2_scan_desc(B=2, H=3, L=1000, D=64)))
     assert need > 0
     for bad in (dict(workspace=None), dict(workspace_bytes=need - 1)):
         assert scan(A, bwd, **bad)[0] == 3, bad
@@ -64,8 +64,8 @@ def test_scan_arguments(A):
         assert scan(A, at={i: PTR[i] + 8})[0] == 1
     for i in (3, 4):
         assert scan(A, at={i: PTR[i] + 2})[0] == 1
-    rows, state = 2 * 100 * 3 * 64 * 2, 2 * 3 * 64 * 64 * 4
-    for i, n in ((0, rows), (1, rows), (2, rows), (3, 2 * 100 * 3 * 4), (4, 8), (5, state), (7, state)):
+    rows, state = 2 * 1000 * 3 * 64 * 2, 2 * 3 * 64 * 64 * 4
+    for i, n in ((0, rows), (1, rows), (2, rows), (3, 2 * 1000 * 3 * 4), (4, 8), (5, state), (7, state)):
         st, why = scan(A, at={6: (PTR[i] + n - 1) // 16 * 16})
         assert st == 1 and "overlap" in why, i                # out's first bytes are the argument's last
     st, why = scan(A, at={7: PTR[5] + 16})                    # S may be S0, not a part of it
