@@ -9,8 +9,10 @@
 //
 // A unit is 8 pairs of a head, 16 features: neighbours (2i, 2i + 1), or i and i + D / 2.  A token's units (queries, then keys) are dealt to
 // LPT lanes of a workgroup, the least power of two from 16 on that holds them, 256 at the most and then NU to a lane; a head's units divide LPT, so
-// a lane's units all have the same pairs.  A workgroup takes 256 / LPT tokens side by side and TOK of each in a row: their loads are all
-// requested before the first sum, their sums cross the wavefronts together, and a weight's gradient stays with its lane.
+// a lane's units all have the same pairs.  A workgroup takes 256 / LPT tokens side by side and, forward, TOK of each in a row: their loads are all
+// requested before the first sum, and their sums cross the wavefronts together.  The gradients hold twice the rows and the weights' sums: one token,
+// turned back once, and the more wavefronts on a SIMD (four tokens with their turns back made twice and three wavefronts: 39.4 us, this one: 34.9; 4680 tokens
+// of 12 + 12 heads x 128 by rows, 2.2 and 2.5 TB/s; 32 + 8 heads, two units a lane: 93 and 61 us).  A weight's gradient stays with its lane.
 #include "arl2_device.h"
 #include "arl2_rope.h"
 
@@ -20,7 +22,9 @@ namespace arl2 {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kGradWorkgroups = 768;
+// Wavefronts on a SIMD that the gradients' registers leave room for, and workgroups on a CU: with more, weights' gradients come in more parts, and with fewer (768 of
+// one unit, 4680 tokens as above) 38.6 us for 36.0.
+constexpr int bwd_waves(int nu, bool f32) { return nu == 1 ? 4 : nu == 2 && !f32 ? 3 : 2; }
 
 template <class T> struct Raw;                    // 8 features as they lie in memory
 template <> struct Raw<bf16_t> { u32x4 v; };
@@ -268,14 +272,14 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 4 : NU <= 3 ? 3 : 2) void rope_
 
 // A weight's gradient is summed over all of a workgroup's tokens by the lanes that have its feature, joined among them at the end and written
 // as this workgroup's part.
-template <class T, int NORM, bool HALVES, int NU, int TOK>
-__global__ __launch_bounds__(kThreads, NU == 1 ? 3 : 2) void rope_bwd_kernel(RopeArgs a, int lpt)
+template <class T, int NORM, bool HALVES, int NU>
+__global__ __launch_bounds__(kThreads, bwd_waves(NU, std::is_same<T, float>::value)) void rope_bwd_kernel(RopeArgs a, int lpt)
 {
     extern __shared__ __align__(16) f32x2 turns[][64];
-    __shared__ float red[2][4][TOK * 4];
+    __shared__ float red[2][4][4];
     const Lane m = lane_of(a, lpt, HALVES);
     const bool partial = a.pairs < a.D / 2;
-    const int at_a_time = m.slots * TOK, left = a.pairs - 8 * m.in_head;
+    const int left = a.pairs - 8 * m.in_head;
     Unit<T> w[NU];
     float dw[NU][16] = {};
     int which[NU], off[NU];
@@ -289,28 +293,25 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 3 : 2) void rope_bwd_kernel(Rop
     const uint32_t all = (uint32_t)a.B * a.L;                     // (2e9 at the most: no step past it wraps around)
     const float over_head = 1.f / (float)a.D, over_row[2] = {1.f / (float)(a.heads[0] * a.D), 1.f / (float)(max(a.heads[1], 1) * a.D)};
     int round = 0;
-    for (uint32_t t0 = blockIdx.x * at_a_time; t0 < all; t0 += gridDim.x * at_a_time, round ^= 1) {
-        bool there[TOK];
-        Unit<T> x[TOK][NU], d[TOK][NU];
+    for (uint32_t t0 = blockIdx.x * m.slots; t0 < all; t0 += gridDim.x * m.slots, round ^= 1) {
+        const uint32_t tok = t0 + m.slot;
+        const bool there = token_there(a, tok, all);
+        Unit<T> x[NU], d[NU];
 #pragma unroll
-        for (int t = 0; t < TOK; ++t) {
-            const uint32_t tok = t0 + m.slot * TOK + t;
-            there[t] = token_there(a, tok, all);
-#pragma unroll
-            for (int u = 0; u < NU; ++u)
-                if (there[t] && which[u] < 2) {
-                    const size_t at = (size_t)tok * a.heads[which[u]] * a.D + off[u];
-                    d[t][u] = load_unit((const T *)a.dy[which[u]] + at, m.hi);
-                    if (NORM != kNormNone) x[t][u] = load_unit((const T *)a.x[which[u]] + at, m.hi);
-                }
-        }
-        f32x2 (*const mine)[64] = turns + round * at_a_time;
-        turns_of(a, t0, all, at_a_time, mine);
-        __syncthreads();
+        for (int u = 0; u < NU; ++u)
+            if (there && which[u] < 2) {
+                const size_t at = (size_t)tok * a.heads[which[u]] * a.D + off[u];
+                d[u] = load_unit((const T *)a.dy[which[u]] + at, m.hi);
+                if (NORM != kNormNone) x[u] = load_unit((const T *)a.x[which[u]] + at, m.hi);
+            }
+        f32x2 (*const mine)[64] = turns + round * m.slots;
+        turns_of(a, t0, all, m.slots, mine);
+        lds_barrier();
+        const f32x2 *const turn = &mine[m.slot][8 * m.in_head];
         // a pair of dy turned back, times the weights: z into z0, z1 and w z into the others
-        auto back = [&](int t, int u, int i, float c, float s, float &z0, float &z1, float &g0, float &g1) {
+        auto back = [&](int u, int i, float c, float s, float &z0, float &z1, float &g0, float &g1) {
             const int j0 = first_of<HALVES>(i), j1 = second_of<HALVES>(i);
-            const float d0 = feature(d[t][u], j0), d1 = feature(d[t][u], j1);
+            const float d0 = feature(d[u], j0), d1 = feature(d[u], j1);
             z0 = d0 * c + d1 * s;
             z1 = d1 * c - d0 * s;
             if (partial && i >= left) { z0 = d0; z1 = d1; }
@@ -322,13 +323,13 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 3 : 2) void rope_bwd_kernel(Rop
             }
         };
         // squares of the unit's features, and their products with w z
-        auto sums = [&](int t, int u, const f32x2 *turn, float &sq, float &dot) {
+        auto sums = [&](int u, float &sq, float &dot) {
             float q = 0.f, p = 0.f;
-            forget(w[u]);
+            if (NU > 1) forget(w[u]);
             each_pair(turn, [&](int i, float c, float s) {
                 float z0, z1, g0, g1;
-                back(t, u, i, c, s, z0, z1, g0, g1);
-                const float f0 = feature(x[t][u], first_of<HALVES>(i)), f1 = feature(x[t][u], second_of<HALVES>(i));
+                back(u, i, c, s, z0, z1, g0, g1);
+                const float f0 = feature(x[u], first_of<HALVES>(i)), f1 = feature(x[u], second_of<HALVES>(i));
                 q = fmaf(f0, f0, fmaf(f1, f1, q));
                 p = fmaf(f0, g0, fmaf(f1, g1, p));
                 asm volatile("" : "+v"(q), "+v"(p));
@@ -336,72 +337,64 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 3 : 2) void rope_bwd_kernel(Rop
             sq = q;
             dot = p;
         };
-        float row[TOK][4];                                        // squares of queries and keys, products with their gradients
+        float row[1][4] = {};                                     // squares of queries and keys, products with their gradients
         if constexpr (NORM == kNormRow) {
 #pragma unroll
-            for (int t = 0; t < TOK; ++t) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) row[t][i] = 0.f;
-#pragma unroll
-                for (int u = 0; u < NU; ++u) {
-                    float s, p;
-                    sums(t, u, &mine[m.slot * TOK + t][8 * m.in_head], s, p);
-                    row[t][0] += which[u] == 0 ? s : 0.f;
-                    row[t][1] += which[u] == 1 ? s : 0.f;
-                    row[t][2] += which[u] == 0 ? p : 0.f;
-                    row[t][3] += which[u] == 1 ? p : 0.f;
-                }
+            for (int u = 0; u < NU; ++u) {
+                float s, p;
+                sums(u, s, p);
+                row[0][0] += which[u] == 0 ? s : 0.f;
+                row[0][1] += which[u] == 1 ? s : 0.f;
+                row[0][2] += which[u] == 0 ? p : 0.f;
+                row[0][3] += which[u] == 1 ? p : 0.f;
             }
-            token_sums<TOK, 4>(row, m, red[round]);
+            token_sums<1, 4>(row, m, red[round]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                row[0][i] = inverse_rms(row[0][i], over_row[i], a.eps);
+                row[0][2 + i] *= row[0][i] * over_row[i];
+            }
         }
 #pragma unroll
-        for (int t = 0; t < TOK; ++t) {
-            const f32x2 *const turn = &mine[m.slot * TOK + t][8 * m.in_head];
-            if constexpr (NORM == kNormRow)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    row[t][i] = inverse_rms(row[t][i], over_row[i], a.eps);
-                    row[t][2 + i] *= row[t][i] * over_row[i];
-                }
-#pragma unroll
-            for (int u = 0; u < NU; ++u) {
-                float r = 1.f, p = 0.f, y[16];
-                if constexpr (NORM == kNormHead) {
-                    float s;
-                    sums(t, u, turn, s, p);
-                    r = inverse_rms(head_sum(s, m.upt), over_head, a.eps);
-                    p = head_sum(p, m.upt) * r * over_head;
-                } else if constexpr (NORM == kNormRow) {
-                    r = which[u] == 1 ? row[t][1] : row[t][0];
-                    p = which[u] == 1 ? row[t][3] : row[t][2];
-                }
-                forget(d[t][u]);
+        for (int u = 0; u < NU; ++u) {
+            float r = 1.f, p = 0.f, y[16];
+            if constexpr (NORM == kNormHead) {
+                float s;
+                sums(u, s, p);
+                r = inverse_rms(head_sum(s, m.upt), over_head, a.eps);
+                p = head_sum(p, m.upt) * r * over_head;
+            } else if constexpr (NORM == kNormRow) {
+                r = which[u] == 1 ? row[0][1] : row[0][0];
+                p = which[u] == 1 ? row[0][3] : row[0][2];
+            }
+            if (NU > 1) {
+                forget(d[u]);
                 if (NORM != kNormNone) {
-                    forget(x[t][u]);
+                    forget(x[u]);
                     forget(w[u]);
                 }
-                const bool counts = there[t] && which[u] < 2;
-                each_pair(turn, [&](int i, float c, float s) {
-                    const int j0 = first_of<HALVES>(i), j1 = second_of<HALVES>(i);
-                    float z0, z1, g0, g1;
-                    back(t, u, i, c, s, z0, z1, g0, g1);
-                    if constexpr (NORM != kNormNone) {
-                        const float h0 = feature(x[t][u], j0) * r, h1 = feature(x[t][u], j1) * r;
-                        dw[u][j0] = counts ? fmaf(z0, h0, dw[u][j0]) : dw[u][j0];
-                        dw[u][j1] = counts ? fmaf(z1, h1, dw[u][j1]) : dw[u][j1];
-                        asm volatile("" : "+v"(dw[u][j0]), "+v"(dw[u][j1]));      // (now, not where the next token needs them: z and h would be kept)
-                        g0 = r * (g0 - h0 * p);
-                        g1 = r * (g1 - h1 * p);
-                    }
-                    y[j0] = g0;
-                    y[j1] = g1;
-                    if (i % 2) asm volatile("" : "+v"(y[first_of<HALVES>(i - 1)]), "+v"(y[second_of<HALVES>(i - 1)]), "+v"(y[j0]), "+v"(y[j1]));
-                });
-                if (!counts) continue;
-                T *const to = (T *)a.y[which[u]] + (size_t)(t0 + m.slot * TOK + t) * a.heads[which[u]] * a.D + off[u];
-                store8(to, y);
-                store8(to + m.hi, y + 8);
             }
+            const bool counts = there && which[u] < 2;
+            each_pair(turn, [&](int i, float c, float s) {
+                const int j0 = first_of<HALVES>(i), j1 = second_of<HALVES>(i);
+                float z0, z1, g0, g1;
+                back(u, i, c, s, z0, z1, g0, g1);
+                if constexpr (NORM != kNormNone) {
+                    const float h0 = feature(x[u], j0) * r, h1 = feature(x[u], j1) * r;
+                    dw[u][j0] = counts ? fmaf(z0, h0, dw[u][j0]) : dw[u][j0];
+                    dw[u][j1] = counts ? fmaf(z1, h1, dw[u][j1]) : dw[u][j1];
+                    asm volatile("" : "+v"(dw[u][j0]), "+v"(dw[u][j1]));      // (now, not where the next token needs them: z and h would be kept)
+                    g0 = r * (g0 - h0 * p);
+                    g1 = r * (g1 - h1 * p);
+                }
+                y[j0] = g0;
+                y[j1] = g1;
+                if (i % 2) asm volatile("" : "+v"(y[first_of<HALVES>(i - 1)]), "+v"(y[second_of<HALVES>(i - 1)]), "+v"(y[j0]), "+v"(y[j1]));
+            });
+            if (!counts) continue;
+            T *const to = (T *)a.y[which[u]] + (size_t)tok * a.heads[which[u]] * a.D + off[u];
+            store8(to, y);
+            store8(to + m.hi, y + 8);
         }
     }
     if (NORM == kNormNone || (a.dw[0] == nullptr && a.dw[1] == nullptr)) return;
@@ -454,27 +447,30 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 3 : 2) void rope_bwd_kernel(Rop
     for (int i = threadIdx.x; i < width; i += kThreads) to[i] = part[i];
 }
 
-// Weights' gradients: 16 columns to a workgroup, the workgroups' parts in 16 groups added in order.
-__global__ __launch_bounds__(256) void rope_dw_kernel(RopeArgs a, int parts, int width0, int width)
+// Weights' gradients: 16 columns to a workgroup, the workgroups' parts in 64 groups added in order.
+__global__ __launch_bounds__(1024) void rope_dw_kernel(RopeArgs a, int parts, int width0, int width)
 {
-    __shared__ float sums[16][17];
+    __shared__ float sums[64][17];
     const int c = threadIdx.x & 15, g = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
     float s = 0.f;
-    for (int p0 = g; p0 < parts; p0 += 128) {                     // eight on their way at a time
+    for (int p0 = g; p0 < parts; p0 += 512) {                     // eight on their way at a time
         float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = p0 + 16 * i < parts ? a.part[(size_t)(p0 + 16 * i) * width + col] : 0.f;
+        for (int i = 0; i < 8; ++i) v[i] = p0 + 64 * i < parts ? a.part[(size_t)(p0 + 64 * i) * width + col] : 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) s += v[i];
     }
     sums[g][c] = s;
     __syncthreads();
-    if (g > 0) return;
+    if (g >= 16) return;
     s = 0.f;
+    const int first = 4 * c;                                      // column g: four groups to a lane
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s += sums[i][c];
-    float *const to = col < width0 ? a.dw[0] : a.dw[1];
-    if (to != nullptr) to[col < width0 ? col : col - width0] = s;
+    for (int i = 0; i < 4; ++i) s += sums[first + i][g];
+    s = lane_group_sum<16>(s);
+    const int to_col = blockIdx.x * 16 + g;
+    float *const to = to_col < width0 ? a.dw[0] : a.dw[1];
+    if (to != nullptr && c == 0) to[to_col < width0 ? to_col : to_col - width0] = s;
 }
 
 // How tokens are dealt: lanes to a token, units to a lane, tokens of a lane at a time.
@@ -484,15 +480,15 @@ Shape shape_of(int units, bool f32, bool bwd)
     int lpt = 16;                                                 // (fewer would want more LDS for the turns of more tokens)
     while (lpt < units && lpt < kThreads) lpt <<= 1;
     const int nu = units <= kThreads ? 1 : units <= 2 * kThreads ? 2 : units <= 3 * kThreads ? 3 : 6;
-    return {lpt, nu, nu == 1 ? (bwd && !f32 && lpt > 16 ? 4 : 2) : nu == 2 ? (f32 ? 1 : 2) : 1};
+    return {lpt, nu, bwd || nu > 2 || (nu == 2 && f32) ? 1 : 2};
 }
 
 template <class T, int NORM, bool HALVES, bool BWD>
 hipError_t launch_shape(const RopeArgs &a, const Shape &s, dim3 grid, unsigned lds, hipStream_t stream)
 {
     constexpr bool f32 = std::is_same<T, float>::value;
-#define ARL2_ROPE(NU, TOK) launch_kernel_lds(BWD ? rope_bwd_kernel<T, NORM, HALVES, NU, TOK> : rope_kernel<T, NORM, HALVES, NU, TOK>, grid, dim3(kThreads), lds, stream, a, s.lpt)
-    return s.tok == 4 ? ARL2_ROPE(1, f32 || !BWD ? 2 : 4) : s.nu == 1 ? ARL2_ROPE(1, 2) : s.nu == 2 ? ARL2_ROPE(2, f32 ? 1 : 2) : s.nu == 3 ? ARL2_ROPE(3, 1) : ARL2_ROPE(6, 1);
+#define ARL2_ROPE(NU, TOK) launch_kernel_lds(BWD ? rope_bwd_kernel<T, NORM, HALVES, NU> : rope_kernel<T, NORM, HALVES, NU, TOK>, grid, dim3(kThreads), lds, stream, a, s.lpt)
+    return s.nu == 1 ? ARL2_ROPE(1, 2) : s.nu == 2 ? ARL2_ROPE(2, f32 ? 1 : 2) : s.nu == 3 ? ARL2_ROPE(3, 1) : ARL2_ROPE(6, 1);
 #undef ARL2_ROPE
 }
 template <class T, bool BWD>
@@ -524,8 +520,8 @@ int workgroups(int B, int L, const Shape &s, int most)
 
 size_t rope_workspace_bytes(int B, int L, int D, int heads)
 {
-    // (fp32 rows have the more workgroups: fewer tokens at a time)
-    const size_t n = (size_t)workgroups(B, L, shape_of(heads * (D / 16), true, true), kGradWorkgroups);
+    const Shape s = shape_of(heads * (D / 16), false, true);      // (bf16 rows have the more workgroups)
+    const size_t n = (size_t)workgroups(B, L, s, bwd_waves(s.nu, false) * kNumCu);
     return (n * heads * D * sizeof(float) + 255) & ~(size_t)255;
 }
 
@@ -541,11 +537,11 @@ hipError_t launch_rope(const RopeArgs &a, hipStream_t stream)
 hipError_t launch_rope_bwd(const RopeArgs &a, hipStream_t stream)
 {
     const Shape s = shape_of((a.heads[0] + a.heads[1]) * (a.D / 16), a.f32, true);
-    const int n = workgroups(a.B, a.L, s, kGradWorkgroups);
+    const int n = workgroups(a.B, a.L, s, a.norm == kNormNone ? 1 << 30 : bwd_waves(s.nu, a.f32) * kNumCu);
     const hipError_t e = launch_any<true>(a, s, n, stream);
     if (e != hipSuccess || a.norm == kNormNone || (a.dw[0] == nullptr && a.dw[1] == nullptr)) return e;
     const int width0 = a.norm == kNormHead ? a.D : a.heads[0] * a.D, width = a.norm == kNormHead ? 2 * a.D : (a.heads[0] + a.heads[1]) * a.D;
-    return launch_kernel(rope_dw_kernel, dim3(width / 16), dim3(256), stream, a, n, width0, width);
+    return launch_kernel(rope_dw_kernel, dim3(width / 16), dim3(1024), stream, a, n, width0, width);
 }
 
 }  // namespace arl2
