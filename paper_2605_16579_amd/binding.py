@@ -610,6 +610,7 @@ def arl2_scan_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_alpha: 
 # ---- rotary positions on several axes
 
 _NORMS = {"none": ARL2_NORM_NONE, "head": ARL2_NORM_HEAD, "row": ARL2_NORM_ROW}
+_NORM_LETTERS = {"none": b"n", "head": b"h", "row": b"r"}
 
 
 def _rope_desc(B, H, L, D, Hk, io_dtype=ARL2_BF16, norm="none", halves=False, pos_per_stream=False, axis_pairs=(1,), theta=None, norm_eps=0.0,
@@ -632,6 +633,10 @@ def arl2_rope_workspace_bytes(B: int, H: int, Hk: int, L: int, D: int) -> int:
 def alloc_rope_workspace(B: int, H: int, Hk: int, L: int, D: int, device="cuda") -> torch.Tensor:
     """Convenience: a torch buffer of arl2_rope_workspace_bytes() bytes."""
     return torch.empty(max(arl2_rope_workspace_bytes(B, H, Hk, L, D), 16), dtype=torch.uint8, device=device)
+
+
+def _rope_kinds(norm: str, halves: bool, letters: bytes) -> bytes:
+    return b"O" + _NORM_LETTERS.get(norm, b"") + (b"1" if halves else b"0") + letters
 
 
 def _rope_call(rows, keys, wq, wk, pos, seq_len, norm, axis_pairs, kw):
@@ -657,6 +662,8 @@ def arl2_rope_fwd(q: torch.Tensor, k: Optional[torch.Tensor], wq: Optional[torch
     weights [D]), of a token's row ("row", weights [H * D] and [Hk * D]) or as they are ("none"), times the weights (None: ones), rotated by
     pos [L, axes] or [B, L, axes] int32: ``axis_pairs`` pairs of features by each axis with frequencies theta^(-i / pairs) (None, 0: 10000);
     pairs are neighbours, or (``halves``) features i and i + D / 2.  fp32 or bf16."""
+    if _plain_call("arl2_rope_fwd", _rope_kinds(norm, halves, b"qkwupnqk"), (axis_pairs, theta), norm_eps, stream, None, q, k, wq, wk, pos, seq_len, yq, yk):
+        return
     d, like_q, like_k, _, _, (pwq, pwk, ppos, plen) = _rope_call(q, k, wq, wk, pos, seq_len, norm, axis_pairs,
                                                                  dict(theta=theta, halves=halves, norm_eps=norm_eps, stream=stream))
     ptrs = (_dev(q, "q", *like_q), _dev(k, "k", *like_k), pwq, pwk, ppos, plen, _dev(yq, "yq", *like_q), _dev(yk, "yk", *like_k))
@@ -670,6 +677,9 @@ def arl2_rope_bwd(q: Optional[torch.Tensor], k: Optional[torch.Tensor], wq: Opti
                   seq_len: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> None:
     """Gradients of ``arl2_rope_fwd``: from dyq, dyk into dq, dk (may be dyq, dyk) and, fp32, the weights' dwq, dwk (None: not wanted), which
     take a ``workspace`` of ``alloc_rope_workspace``.  q and k may be None where ``norm`` is "none"."""
+    if _plain_call("arl2_rope_bwd", _rope_kinds(norm, halves, b"xzwupnqkqkWU"), (axis_pairs, theta), norm_eps, stream, workspace,
+                   q, k, wq, wk, pos, seq_len, dyq, dyk, dq, dk, dwq, dwk):
+        return
     d, like_q, like_k, of_q, of_k, (pwq, pwk, ppos, plen) = _rope_call(dyq, dyk, wq, wk, pos, seq_len, norm, axis_pairs,
                                                                        dict(theta=theta, halves=halves, norm_eps=norm_eps, workspace=workspace, stream=stream))
     ptrs = (_dev(q, "q", *like_q), _dev(k, "k", *like_k), pwq, pwk, ppos, plen, _dev(dyq, "dyq", *like_q), _dev(dyk, "dyk", *like_k),

@@ -15,6 +15,11 @@
 // Calls of the recurrence begin with C and take `raw_rows` in the place of sm_scale; their descriptor is arl2_scan_desc, all of their tensors are on
 // the current device, and a letter is
 //   q  [B][L][H][D] bf16 (the first names the sizes)     t  [B][L][H] fp32 or None     S  [B][H][D][D] fp32 or None     n  [B] int32 or None
+// Calls of the rotation begin with O, the norm (n, h or r) and the pairing (0: neighbours, 1: halves), and take (axis_pairs, theta or None) in the place of
+// sm_scale and norm_eps in that of l2_eps; their descriptor is arl2_rope_desc, all of their tensors are on the current device, and a letter is
+//   q  [B][L][H][D] fp32 or bf16 (the first names the sizes and the type)      k  [B][L][Hk][D], likewise, or None (the first says whether there are keys)
+//   x, z  like q and k, or None     w, u  the weights of queries and keys, of their type, or None     W, U  likewise, fp32     p  [L][axes] or [B][L][axes] int32
+//   n  [B] int32 or None
 // Measured: a call of the smallest size took 7 us to issue through ctypes, of them 3.5 in the library and the runtime.
 #include <Python.h>
 #include <c10/core/impl/VirtualGuardImpl.h>
@@ -165,6 +170,78 @@ bool check_scan(arl2_scan_desc &d, const char *kinds, PyObject *const *args, int
     return true;
 }
 
+// The same for calls of the rotation.
+bool check_rope(arl2_rope_desc &d, const char *kinds, PyObject *axes, PyObject *const *args, int n, const void **p)
+{
+    if (!PyTuple_CheckExact(axes) || PyTuple_GET_SIZE(axes) != 2) return false;
+    PyObject *const pairs = PyTuple_GET_ITEM(axes, 0), *const theta = PyTuple_GET_ITEM(axes, 1);
+    auto sequence = [](PyObject *o) { return PyTuple_CheckExact(o) || PyList_CheckExact(o); };
+    if (!sequence(pairs) || (theta != Py_None && !sequence(theta))) return false;
+    const Py_ssize_t n_axes = PySequence_Fast_GET_SIZE(pairs);
+    if (n_axes < 1 || n_axes > 4 || (theta != Py_None && PySequence_Fast_GET_SIZE(theta) != n_axes)) return false;
+    d.n_axes = (int32_t)n_axes;
+    for (Py_ssize_t i = 0; i < n_axes; ++i) {
+        PyObject *const m = PySequence_Fast_GET_ITEM(pairs, i);
+        if (!PyLong_CheckExact(m)) return false;
+        const long value = PyLong_AsLong(m);
+        if (value < 0 || value > INT32_MAX) return false;
+        d.axis_pairs[i] = (int32_t)value;
+        if (theta == Py_None) continue;
+        PyObject *const t = PySequence_Fast_GET_ITEM(theta, i);
+        if (!PyFloat_CheckExact(t) && !PyLong_CheckExact(t)) return false;
+        d.theta[i] = PyFloat_AsDouble(t);
+    }
+    if (PyErr_Occurred()) return false;
+    d.norm = kinds[0] == 'h' ? ARL2_NORM_HEAD : kinds[0] == 'r' ? ARL2_NORM_ROW : ARL2_NORM_NONE;
+    d.halves = kinds[1] == '1';
+    kinds += 2;
+    const at::Tensor *rows = nullptr, *keys = nullptr;
+    bool no_keys = false;
+    const int device = (int)c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice().index();
+    const at::Tensor *t[kMaxTensors] = {};
+    for (int i = 0; i < n; ++i) {
+        if (args[i] == Py_None) {
+            if (kinds[i] == 'q' || kinds[i] == 'p') return false;
+            if (kinds[i] == 'k' && keys == nullptr) no_keys = true;
+            continue;
+        }
+        if ((t[i] = plain(args[i])) == nullptr || t[i]->get_device() != device) return false;
+        if (kinds[i] == 'q' && rows == nullptr) rows = t[i];
+        if (kinds[i] == 'k' && keys == nullptr) keys = t[i];
+        if (kinds[i] == 'p' && t[i]->dim() != 2 && t[i]->dim() != 3) return false;
+    }
+    if (rows == nullptr || rows->dim() != 4 || (keys != nullptr && (no_keys || keys->dim() != 4))) return false;
+    for (const at::Tensor *x : {rows, keys})
+        for (int64_t m : x ? x->sizes() : at::IntArrayRef())
+            if (m > INT32_MAX) return false;
+    const int64_t B = rows->size(0), L = rows->size(1), H = rows->size(2), D = rows->size(3), Hk = keys ? keys->size(2) : 0;
+    const at::ScalarType io = rows->scalar_type();
+    if (type_code(*rows) < 0) return false;
+    d.B = (int32_t)B; d.H = (int32_t)H; d.L = (int32_t)L; d.D = (int32_t)D; d.Hk = (int32_t)Hk; d.io_dtype = type_code(*rows);
+    const bool head = d.norm == ARL2_NORM_HEAD;
+    for (int i = 0; i < n; ++i) {
+        if (t[i] == nullptr) continue;
+        const at::ScalarType type = t[i]->scalar_type();
+        bool ok = false;
+        switch (kinds[i]) {
+        case 'q': case 'x': ok = type == io && is_shape(*t[i], {B, L, H, D}); break;
+        case 'k': case 'z': ok = type == io && is_shape(*t[i], {B, L, Hk, D}); break;
+        case 'w': ok = type == io && is_shape(*t[i], {head ? D : H * D}); break;
+        case 'u': ok = type == io && is_shape(*t[i], {head ? D : Hk * D}); break;
+        case 'W': ok = type == at::kFloat && is_shape(*t[i], {head ? D : H * D}); break;
+        case 'U': ok = type == at::kFloat && is_shape(*t[i], {head ? D : Hk * D}); break;
+        case 'p':
+            d.pos_per_stream = t[i]->dim() == 3;
+            ok = type == at::kInt && (t[i]->dim() == 3 ? is_shape(*t[i], {B, L, n_axes}) : is_shape(*t[i], {L, n_axes}));
+            break;
+        case 'n': ok = type == at::kInt && is_shape(*t[i], {B}); break;
+        }
+        if (!ok) return false;
+        p[i] = t[i]->data_ptr();
+    }
+    return true;
+}
+
 int invoke(void *f, const void *d, const void *const *p, int n)
 {
     typedef const void *P;
@@ -177,6 +254,8 @@ int invoke(void *f, const void *d, const void *const *p, int n)
     case 8: return ((int (*)(P, P, P, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]);
     case 10:
         return ((int (*)(P, P, P, P, P, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9]);
+    case 12:
+        return ((int (*)(P, P, P, P, P, P, P, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11]);
     case 13:
         return ((int (*)(P, P, P, P, P, P, P, P, P, P, P, P, P, P))f)(d, p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], p[10], p[11], p[12]);
     }
@@ -189,10 +268,10 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     if (nargs <= kFixed || !PyBytes_CheckExact(args[1]) || nargs - kFixed > kMaxTensors) Py_RETURN_NONE;
     const int n = (int)(nargs - kFixed);
     const char *kinds = PyBytes_AS_STRING(args[1]);
-    const bool kv = kinds[0] == 'P', scan = kinds[0] == 'C';
-    if (PyBytes_GET_SIZE(args[1]) != n + (kv || scan)) Py_RETURN_NONE;
+    const bool kv = kinds[0] == 'P', scan = kinds[0] == 'C', rope = kinds[0] == 'O';
+    if (PyBytes_GET_SIZE(args[1]) != n + (rope ? 3 : kv || scan)) Py_RETURN_NONE;
     void *f = PyLong_AsVoidPtr(args[0]);
-    const double sm_scale = PyFloat_AsDouble(args[2]), l2_eps = PyFloat_AsDouble(args[3]);
+    const double sm_scale = rope ? 0.0 : PyFloat_AsDouble(args[2]), l2_eps = PyFloat_AsDouble(args[3]);
     void *stream = PyLong_Check(args[4]) ? PyLong_AsVoidPtr(args[4]) : nullptr;
     if (PyErr_Occurred() || f == nullptr || !PyLong_Check(args[4])) {
         PyErr_Clear();
@@ -201,6 +280,7 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     Checked c;
     arl2_kv_desc kd{};
     arl2_scan_desc sd{};
+    arl2_rope_desc rd{};
     void *workspace = nullptr;
     size_t workspace_bytes = 0;
     try {
@@ -208,13 +288,18 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
             if (!check_kv(kd, kinds + 1, args + kFixed, n, c.p)) Py_RETURN_NONE;
         } else if (scan) {
             if (!check_scan(sd, kinds + 1, args + kFixed, n, c.p)) Py_RETURN_NONE;
+        } else if (rope) {
+            if (!check_rope(rd, kinds + 1, args[2], args + kFixed, n, c.p)) {
+                PyErr_Clear();
+                Py_RETURN_NONE;
+            }
         } else {
             for (int i = 0; i < n; ++i)
                 if (!check(c, kinds[i], args[kFixed + i], i)) Py_RETURN_NONE;
         }
         if (args[5] != Py_None) {
             const at::Tensor *w = plain(args[5]);
-            if (w == nullptr || ((kv || scan) && w->get_device() != THPVariable_Unpack(args[kFixed]).get_device())) Py_RETURN_NONE;
+            if (w == nullptr || ((kv || scan || rope) && w->get_device() != (int)c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice().index())) Py_RETURN_NONE;
             workspace = w->data_ptr();
             workspace_bytes = w->nbytes();
         }
@@ -235,6 +320,12 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         sd.workspace_bytes = workspace_bytes;
         sd.stream = stream;
     }
+    if (rope) {
+        rd.norm_eps = (float)l2_eps;
+        rd.workspace = workspace;
+        rd.workspace_bytes = workspace_bytes;
+        rd.stream = stream;
+    }
     c.d.sm_scale = (float)sm_scale;
     c.d.l2_eps = (float)l2_eps;
     c.d.workspace = workspace;
@@ -242,7 +333,7 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
     c.d.stream = stream;
     int st;
     Py_BEGIN_ALLOW_THREADS
-    st = invoke(f, kv ? (const void *)&kd : scan ? (const void *)&sd : &c.d, c.p, n);
+    st = invoke(f, kv ? (const void *)&kd : scan ? (const void *)&sd : rope ? (const void *)&rd : &c.d, c.p, n);
     Py_END_ALLOW_THREADS
     if (st < 0) Py_RETURN_NONE;
     return PyLong_FromLong(st);

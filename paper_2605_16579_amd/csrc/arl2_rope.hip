@@ -270,6 +270,9 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 4 : NU <= 3 ? 3 : 2) void rope_
     }
 }
 
+// Groups of a workgroup's wavefronts that have sums of the same weights' gradients.
+__host__ __device__ constexpr int part_groups(bool by_heads, int lpt) { return !by_heads && lpt == 128 ? 2 : 4; }
+
 // A weight's gradient is summed over all of a workgroup's tokens by the lanes that have its feature, joined among them at the end and written
 // as this workgroup's part.
 template <class T, int NORM, bool HALVES, int NU>
@@ -409,13 +412,20 @@ __global__ __launch_bounds__(kThreads, bwd_waves(NU, std::is_same<T, float>::val
                 for (int i = 0; i < 16; ++i) to[(which[u] ? width0 : 0) + off[u] + (i < 8 ? i : m.hi + i - 8)] = dw[u][i];
         return;
     }
+    // sums of lanes with the same features in a wavefront, and of the wavefronts (or pairs of them that have a token together) in LDS
     float *const part = reinterpret_cast<float *>(&turns[0][0]);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, groups = part_groups(NORM == kNormHead, m.lpt);
+    auto lanes_sum = [&](float (&x)[16], int from) {
+        for (int s = from; s < 64; s <<= 1)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] += __shfl_xor(x[i], s, kWave);
+    };
+    auto hand_over = [&](const float (&x)[16], float *at) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) at[i < 8 ? i : m.hi + i - 8] = x[i];
+    };
     __syncthreads();                                              // the turns have been read
-    for (int i = threadIdx.x; i < width; i += kThreads) part[i] = 0.f;
-    __syncthreads();
     if constexpr (NORM == kNormHead) {
-        // lanes of the same place in their heads, units of a lane: one sum of each array
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             float sum[16] = {};
@@ -423,28 +433,19 @@ __global__ __launch_bounds__(kThreads, bwd_waves(NU, std::is_same<T, float>::val
             for (int u = 0; u < NU; ++u)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sum[i] += which[u] == k ? dw[u][i] : 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                for (int s = m.upt; s < 64; s <<= 1) sum[i] += __shfl_xor(sum[i], s, kWave);
-            for (int v = 0; v < 4; ++v) {
-                if (wave == v && lane < m.upt)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) part[(k ? width0 : 0) + m.at + (i < 8 ? i : m.hi + i - 8)] += sum[i];
-                __syncthreads();
-            }
+            lanes_sum(sum, m.upt);
+            if (lane < m.upt) hand_over(sum, part + wave * width + (k ? width0 : 0) + m.at);
         }
-    } else {                                                      // NU is 1: the tokens side by side, in a wavefront and then among them
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            for (int s = m.lpt; s < 64; s <<= 1) dw[0][i] += __shfl_xor(dw[0][i], s, kWave);
-        for (int v = 0; v < 4; ++v) {
-            if (wave == v && lane < m.lpt && which[0] < 2)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) part[(which[0] ? width0 : 0) + off[0] + (i < 8 ? i : m.hi + i - 8)] += dw[0][i];
-            __syncthreads();
-        }
+    } else {                                                      // (NU is 1)
+        lanes_sum(dw[0], m.lpt);
+        if (lane < m.lpt && which[0] < 2) hand_over(dw[0], part + wave * groups / 4 * width + (which[0] ? width0 : 0) + off[0]);
     }
-    for (int i = threadIdx.x; i < width; i += kThreads) to[i] = part[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < width; i += kThreads) {
+        float s = 0.f;
+        for (int g = 0; g < groups; ++g) s += part[g * width + i];
+        to[i] = s;
+    }
 }
 
 // Weights' gradients: 16 columns to a workgroup, the workgroups' parts in 64 groups added in order.
@@ -503,8 +504,8 @@ hipError_t launch_norm(const RopeArgs &a, const Shape &s, dim3 grid, unsigned ld
 template <bool BWD>
 hipError_t launch_any(const RopeArgs &a, const Shape &s, int grid, hipStream_t stream)
 {
-    // the turns of two rounds; at the end the weights' gradients of a workgroup: 2 D of them, or (several tokens side by side) at most 2048
-    const int width = a.norm == kNormHead ? 2 * a.D : s.lpt < kThreads ? (a.heads[0] + a.heads[1]) * a.D : 0;
+    // the turns of two rounds; at the end the weights' gradients of a workgroup's groups: 2 D each, or (several tokens side by side) 16 KB together at most
+    const int width = part_groups(a.norm == kNormHead, s.lpt) * (a.norm == kNormHead ? 2 * a.D : s.lpt < kThreads ? (a.heads[0] + a.heads[1]) * a.D : 0);
     const unsigned lds = (unsigned)std::max<size_t>(2 * (kThreads / s.lpt) * s.tok * 64 * sizeof(f32x2), BWD ? width * sizeof(float) : 0);
     return a.f32 ? launch_norm<float, BWD>(a, s, dim3(grid), lds, stream) : launch_norm<bf16_t, BWD>(a, s, dim3(grid), lds, stream);
 }
