@@ -272,3 +272,88 @@ def test_captured_with_the_recurrence(A):
     for got, r64 in ((out, ref), (d[0], grads[0]), (d[1], grads[1]), (d[2], grads[4]), (dla, grads[5]), (dw[0], grads[2]), (dw[1], grads[3])):
         e = (got.double().cpu() - r64).norm() / r64.norm()
         assert e <= 3 * 2.0 ** -8, float(e)
+
+
+@pytest.mark.parametrize("norm", ["head", "row"])
+def test_one_weight_and_one_gradient(A, norm):
+    """Weights of one of the arrays, gradients of one of them, keys' or queries': what the others get does not change."""
+    c = Case(2, 5, 3, 40, 64, norm=norm, lens=[33, 40])
+    full, fw = run_backward(A, c)
+    for i in range(2):
+        x, dy = [dev(t) for t in c.x], [dev(t) for t in c.dy]
+        dx, dw = [torch.full_like(t, 7.0) for t in dy], [None, None]
+        dw[i] = torch.full_like(fw[i], 7.0)
+        ws = A.alloc_rope_workspace(c.B, *c.heads, c.L, c.D)
+        A.arl2_rope_bwd(*x, dev(c.w[0]), dev(c.w[1]), dev(c.pos), *dy, *dx, *dw, workspace=ws, **c.kw())
+        assert all(torch.equal(a, b) for a, b in zip((*dx, dw[i]), (*full, fw[i])))
+        one = Case(2, 5, 3, 40, 64, norm=norm, lens=[33, 40])
+        one.w[1 - i] = None
+        both(A, one)
+
+
+def test_without_norm_the_rows_are_not_needed(A):
+    c = Case(2, 3, 2, 30, 128, norm="none", per_stream=True)
+    want, _ = run_backward(A, c)
+    dy = [dev(t) for t in c.dy]
+    got = [torch.full_like(t, 7.0) for t in dy]
+    A.arl2_rope_bwd(None, None, None, None, dev(c.pos), *dy, *got, None, None, **c.kw())
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    only = Case(2, 3, 0, 30, 128, norm="none")
+    both(A, only)
+
+
+def test_lengths_are_cut(A):
+    c = Case(3, 3, 2, 30, 64, norm="row", lens=[0, 30, 30])
+    given = torch.tensor([-7, 31, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    kw = c.kw()
+    c.kw = lambda: {**kw, "seq_len": given}
+    both(A, c)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_what_a_bad_row_reaches(A, bad):
+    """Its own token (its head's rows, or the row's), and the weights' gradients; nothing from behind a sequence."""
+    for norm in ("head", "row"):
+        c = Case(2, 3, 2, 30, 64, norm=norm, lens=[20, 30])
+        y, (dx, dw) = run_forward(A, c), run_backward(A, c)
+        for t in (*c.x, *c.dy):
+            t[0, 25] = bad
+        y2, (dx2, dw2) = run_forward(A, c), run_backward(A, c)
+        assert all(torch.equal(a, b) for a, b in zip((*y, *dx, *dw), (*y2, *dx2, *dw2)))
+        c.x[0][1, 7, 1, 3] = bad
+        y3, (dx3, _) = run_forward(A, c), run_backward(A, c)
+        for a, b in zip((*y, *dx), (*y3, *dx3)):
+            a, b = a.clone(), b.clone()
+            assert not torch.isfinite(b[1, 7].float()).all() or b.shape[2] == 2
+            a[1, 7], b[1, 7] = 0, 0
+            assert torch.equal(a, b)
+
+
+def test_offsets_past_32_bits(A):
+    B, L, D = 2, 8400011, 128
+    x, dy = (torch.empty((B, L, 1, D), dtype=torch.bfloat16, device="cuda").normal_() for _ in range(2))
+    pos = torch.arange(L, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    y, dx, dw = torch.empty_like(x), torch.empty_like(x), torch.empty(D, device="cuda")
+    kw = dict(axis_pairs=[64], norm="head")
+    A.arl2_rope_fwd(x, None, None, None, pos, y, None, **kw)
+    A.arl2_rope_bwd(x, None, None, None, pos, dy, None, dx, None, dw, None, workspace=A.alloc_rope_workspace(B, 1, 0, L, D), **kw)
+    c = Case(1, 1, 0, 50, D, norm="head", axis_pairs=[64], weights=False)
+    c.x[0], c.dy[0], c.pos = x[-1:, -50:].cpu(), dy[-1:, -50:].cpu(), pos[-50:].cpu()
+    (want, limit), _ = c.forward()
+    check("y", y[-1:, -50:], want, limit)
+    want, limit, _, _ = next(c.backward())
+    check("dx", dx[-1:, -50:], want, limit)
+    # the weight's gradient over all tokens: a sum of 2^24 terms of unit size in fp64 by halves of the streams
+    angle = pos.double() * 10000.0 ** (-torch.arange(64, device="cuda").double() / 64)
+    want = torch.zeros(D, dtype=torch.float64, device="cuda")
+    most = torch.zeros_like(want)
+    for b in range(B):
+        for a in range(0, L, 1 << 21):
+            u, d, t = x[b, a:a + (1 << 21), 0].double(), dy[b, a:a + (1 << 21), 0].double(), angle[a:a + (1 << 21)]
+            u = u * (u.square().mean(-1, keepdim=True) + 1e-6) ** -0.5
+            z = torch.empty_like(d)
+            z[:, 0::2], z[:, 1::2] = d[:, 0::2] * t.cos() + d[:, 1::2] * t.sin(), d[:, 1::2] * t.cos() - d[:, 0::2] * t.sin()
+            want += (z * u).sum(0)
+            most += (z * u).abs().sum(0)
+    # a lane adds L B / (1024 workgroups 16) tokens one by one in fp32: 2^-24 of the sum so far each, 1026 terms, beside the terms' own F32
+    check("dw", dw, want.cpu().numpy(), ((1026 * 2.0 ** -24 + F32) * most).cpu().numpy())

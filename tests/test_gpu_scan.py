@@ -256,3 +256,138 @@ def test_gradients_against_differences(A):
         # gradients rounded to bf16 (rows) or off by 2^-14 (others), and the step's third order
         scale = U = np.linalg.norm(grad) * (R.U16 if name in "qkv" else 2.0 ** -14) * 4
         assert abs(got - want) <= scale + 1e-4 * abs(want), (name, got, want, U)
+
+
+@pytest.mark.parametrize("eps", [1e-12, 1e-3, 4.0])
+@pytest.mark.parametrize("L", [5, 140])
+def test_epsilons(A, monkeypatch, eps, L):
+    monkeypatch.setattr(R, "EPS", float(np.float32(eps)))
+    c = R.Case(2, 2, L, 64, seed=18, rows=0.05)
+    check_forward(A, c, l2_eps=eps)
+    check_backward(A, c, l2_eps=eps)
+
+
+@pytest.mark.parametrize("L", [6, 130])
+def test_gates_above_one_are_one_and_lengths_are_cut(A, L):
+    c = R.Case(3, 2, L, 64, seed=19, lens=[0, L, L])
+    c.la[:, ::3] = 0.7
+    given = torch.tensor([-5, L + 9, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    c.lens_device = lambda: given
+    check_forward(A, c)
+    check_backward(A, c)
+
+
+def test_two_calls_at_once(A):
+    """Two streams, a workspace each, against the same calls one after the other."""
+    cases = [R.Case(2, 4, 900, 128, seed=20), R.Case(3, 2, 700, 64, seed=21, lens=[700, 0, 333])]
+    alone = [(*R.run_forward(A, c), *R.run_backward(A, c)) for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    dev = [{n: getattr(c, n).cuda() for n in ("q", "k", "v", "la", "S0", "do", "dS")} for c in cases]
+    lens = [c.lens_device() for c in cases]
+    rows = [[torch.full_like(d["q"], 7.0) for _ in range(4)] for d in dev]
+    states = [[torch.full_like(d["S0"], 7.0) for _ in range(2)] for d in dev]
+    dla = [torch.full_like(d["la"], 7.0) for d in dev]
+    ws = [[A.alloc_scan_workspace(c.B, c.H, c.L, c.D, backward=b) for b in (False, True)] for c in cases]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            d, r = dev[i], rows[i]
+            with torch.cuda.stream(s):
+                A.arl2_scan_fwd(d["q"], d["k"], d["v"], d["la"], d["S0"], r[0], states[i][0], seq_len=lens[i], workspace=ws[i][0])
+                A.arl2_scan_bwd(d["q"], d["k"], d["v"], d["la"], d["S0"], d["do"], d["dS"], *r[1:], dla[i], states[i][1], seq_len=lens[i], workspace=ws[i][1])
+    torch.cuda.synchronize()
+    for i, (out, S, dq, dk, dv, g, dS0) in enumerate(alone):
+        for x, y in zip((out, S, dq, dk, dv, g, dS0), (rows[i][0], states[i][0], *rows[i][1:], dla[i], states[i][1])):
+            assert torch.equal(x, y), i
+
+
+def test_offsets_past_32_bits(A):
+    """Streams of 2 GB of rows each, of which the last one's end is looked at: gates of exp(-0.5) leave nothing of what lies 128 tokens back."""
+    B, L, D, window, seen = 3, 8000037, 128, 384, 256
+    g = torch.Generator(device="cuda").manual_seed(22)
+    q, k, v, do = (torch.empty((B, L, 1, D), dtype=torch.bfloat16, device="cuda").normal_(generator=g) for _ in range(4))
+    la = torch.full((B, L, 1), -0.5, device="cuda")
+    dS = torch.randn((B, 1, D, D), generator=g, device="cuda")
+    out, rows, dla = torch.empty_like(q), [torch.empty_like(q) for _ in range(3)], torch.empty_like(la)
+    S, dS0 = torch.empty_like(dS), torch.empty_like(dS)
+    A.arl2_scan_fwd(q, k, v, la, None, out, S, workspace=A.alloc_scan_workspace(B, 1, L, D))
+    A.arl2_scan_bwd(q, k, v, la, None, do, dS, *rows, dla, dS0, workspace=A.alloc_scan_workspace(B, 1, L, D, backward=True))
+    c = R.Case(1, 1, window, D, start=False)
+    for n, x in (("q", q), ("k", k), ("v", v), ("do", do), ("la", la)):
+        setattr(c, n, x[-1:, -window:].cpu())
+    c.dS = dS[-1:].cpu()
+    want, state, lo, ls = c.forward()
+    R.check("out", out[-1:, -seen:], want[:, -seen:], lo[:, -seen:])
+    R.check("S", S[-1:], state, ls)
+    for name, x, w, l in zip(("dq", "dk", "dv", "dlog_alpha"), (*rows, dla), *c.backward()):
+        R.check(name, x[-1:, -seen:], w[:, -seen:], l[:, -seen:])
+    for n, x in (("q", q), ("k", k), ("v", v), ("do", do), ("la", la)):
+        setattr(c, n, x[-1:, :window].cpu())
+    c.dS = None
+    want, limits = c.backward()
+    R.check("dS0", dS0[-1:], want[4], limits[4])
+
+
+# ---- the binding's two ways
+
+class Checked(torch.Tensor):
+    """A tensor that is no plain torch.Tensor: a call with it is marshalled in Python."""
+
+
+def test_compiled_and_checked_calls_agree(A, monkeypatch):
+    from paper_2605_16579_amd import binding
+    seen, host_call = [], binding._host_call
+
+    def recorded(*args):
+        seen.append(host_call(*args))
+        return seen[-1]
+
+    monkeypatch.setattr(binding, "_host_call", recorded)
+    B, H, L, D = 2, 3, 90, 64
+    q, k, v, do = (torch.randn((B, L, H, D), device="cuda").bfloat16() for _ in range(4))
+    la, S0, dS = -torch.rand((B, L, H), device="cuda"), torch.randn((B, H, D, D), device="cuda"), torch.randn((B, H, D, D), device="cuda")
+    lens = torch.tensor([90, 50], dtype=torch.int32, device="cuda")
+    x, w, dy = torch.randn((B, L, 2, D), device="cuda").bfloat16(), torch.rand(D, device="cuda").bfloat16(), torch.randn((B, L, 2, D), device="cuda").bfloat16()
+    pos = torch.randint(0, 99, (L, 2), dtype=torch.int32, device="cuda")
+    ws, wr = A.alloc_scan_workspace(B, H, L, D, backward=True), A.alloc_rope_workspace(B, H, 2, L, D)
+    how = dict(axis_pairs=[20, 12], theta=[500.0, 0], halves=True, norm="head", norm_eps=1e-3, seq_len=lens)
+
+    def run(wrap, **kw):
+        out, rows, yq, yk, dq, dk = torch.zeros_like(q), [torch.zeros_like(q) for _ in range(3)], torch.zeros_like(q), torch.zeros_like(x), torch.zeros_like(q), torch.zeros_like(x)
+        S, dS0, dla, dw = torch.zeros_like(S0), torch.zeros_like(S0), torch.zeros_like(la), [torch.zeros(D, device="cuda") for _ in range(2)]
+        A.arl2_scan_fwd(wrap(q), k, v, la, S0, out, S, seq_len=lens, normalise=False, l2_eps=1e-3, workspace=ws, **kw)
+        A.arl2_scan_bwd(wrap(q), k, v, la, S0, do, dS, *rows, dla, dS0, seq_len=lens, l2_eps=1e-3, workspace=ws, **kw)
+        A.arl2_rope_fwd(wrap(q), x, w, None, pos, yq, yk, **how, **kw)
+        A.arl2_rope_bwd(wrap(q), x, w, None, pos, do, dy, dq, dk, *dw, workspace=wr, **how, **kw)
+        torch.cuda.synchronize()
+        return out, *rows, S, dS0, dla, yq, yk, dq, dk, *dw
+
+    plain = run(lambda t: t)
+    assert seen == [0] * 4
+    seen.clear()
+    checked = run(lambda t: t.as_subclass(Checked))
+    assert seen == [None] * 4
+    on_stream = run(lambda t: t, stream=torch.cuda.current_stream().cuda_stream)
+    for a, b, c in zip(plain, checked, on_stream):
+        assert torch.equal(a, b) and torch.equal(a, c) and a.any()
+    # what the compiled way does not take is refused by the other
+    out, S = torch.empty_like(q), torch.empty_like(S0)
+    for bad in (dict(k=k[:, :-1].contiguous()), dict(v=v.float()), dict(la=la[..., None]), dict(la=la.double()), dict(S0=S0[:, :1].contiguous()), dict(out=out.transpose(1, 2)),
+                dict(S=S.cpu()), dict(lens=lens.long()), dict(lens=lens[:1]), dict(q=q[0]), dict(workspace=ws.cpu())):
+        a = dict(q=q, k=k, v=v, la=la, S0=S0, out=out, S=S, lens=lens, workspace=ws)
+        a.update(bad)
+        seen.clear()
+        with pytest.raises((ValueError, TypeError)):
+            A.arl2_scan_fwd(a["q"], a["k"], a["v"], a["la"], a["S0"], a["out"], a["S"], seq_len=a["lens"], workspace=a["workspace"])
+        assert seen == [None], bad
+    y, z = torch.empty_like(q), torch.empty_like(x)
+    for bad in (dict(k=None), dict(z=None), dict(k=x[..., :32].contiguous()), dict(w=w.float()), dict(w=w.repeat(3)), dict(pos=pos.long()), dict(pos=pos[:, :1].contiguous()),
+                dict(pos=pos[None].repeat(3, 1, 1)), dict(y=y.float()), dict(lens=lens.cpu()), dict(q=q[0]), dict(norm="layer"), dict(axis_pairs=[]), dict(theta=[1.0])):
+        a = dict(q=q, k=x, w=w, pos=pos, y=y, z=z, lens=lens, norm="head", axis_pairs=[20, 12], theta=None)
+        a.update(bad)
+        seen.clear()
+        with pytest.raises((ValueError, TypeError, A.Arl2Error)):
+            A.arl2_rope_fwd(a["q"], a["k"], a["w"], None, a["pos"], a["y"], a["z"], seq_len=a["lens"], norm=a["norm"], axis_pairs=a["axis_pairs"], theta=a["theta"])
+        assert seen == [None] or bad == dict(z=None), bad
+    with pytest.raises(A.Arl2Error, match="workspace"):
+        A.arl2_rope_bwd(q, x, w, None, pos, do, dy, y, z, torch.zeros(D, device="cuda"), None, workspace=wr[:-256], **how)
