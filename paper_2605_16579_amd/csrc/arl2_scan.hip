@@ -124,6 +124,7 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t (&part)[N]
     for (int i = 0; i < N; ++i) {
         const bf16x2 p = {to_bf16(x), to_bf16(y)};
         part[i] = __builtin_bit_cast(uint32_t, p);
+        if (i + 1 < N) asm("" : "+v"(part[i]));           // (else the compiler rounds x once more for what is left of it)
         x -= __uint_as_float(part[i] << 16);
         y -= __uint_as_float(part[i] & 0xffff0000u);
     }
@@ -166,7 +167,7 @@ struct Walk {
     // `lds`: LDS_ROWS bytes.  Segment `seg` of (stream, head) bh.
     static __device__ __forceinline__ void run(const ScanArgs &a, const Work &wk, int bh, int seg, unsigned char *lds, Scalars<D> &sc)
     {
-        const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
+        int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), column = HALVES == 1 ? wave : wave % C::NC, half = HALVES == 1 ? 0 : wave / C::NC;
         const int b = bh / a.H, h = bh - b * a.H;
         const int n = tokens_of(a, b);
@@ -316,10 +317,13 @@ struct Walk {
             return __builtin_shufflevector(lds_read_tr(mat + (at[0] ^ 64 * tile) + 16 * m * C::ROW), lds_read_tr(mat + (at[1] ^ 64 * tile) + 16 * m * C::ROW), 0, 1, 2, 3, 4, 5, 6, 7);
         };
         auto by_rows = [&](const unsigned char *mat, int block, int m) { return *reinterpret_cast<const bf16x8 *>(mat + 32 * block * C::ROW + (row_at ^ 32 * m)); };
+        int diagonal = 4 * hh - l32;                              // of a pair of 32 x 32 rows: row of Y less row of X, register 0
         for (int i = 0; i < count; ++i) {
             const int blk = block_at(i), buf = i & 1;
-            // (the compiler is to compute what it makes of these anew: kept from block to block they would take the registers of the state)
-            asm volatile("" : "+v"(row_at), "+v"(y_at[0]), "+v"(y_at[1]), "+v"(z_at[0]), "+v"(z_at[1]));
+            // (the compiler is to compute what it makes of these anew: addresses and masks kept from block to block would take the registers of the state;
+            // gradients of 8 x 4680 tokens with 33 registers in scratch and 147 of the scalar ones in lanes: 610 us, with none and 28: 551)
+            asm volatile("" : "+v"(row_at), "+v"(y_at[0]), "+v"(y_at[1]), "+v"(z_at[0]), "+v"(z_at[1]), "+v"(diagonal));
+            if (HALVES == 1) asm volatile("" : "+v"(tid), "+v"(lane), "+v"(l32), "+v"(hh));
             if (ROWS) stage(gx, lx, GRAD ? 0 : 1, buf);
             stage(gy, ly, GRAD ? 0 : 2, buf);
             stage(gz, lz, GRAD ? 2 : 0, buf);
@@ -376,7 +380,7 @@ struct Walk {
                     if (sb == tb) {
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
-                            const int d = 8 * (j / 4) + 4 * hh + j % 4 - l32;
+                            const int d = 8 * (j / 4) + j % 4 + diagonal;
                             p[j] = (REV ? d >= 0 : d <= 0) ? p[j] : 0.f;
                         }
                     }
@@ -405,7 +409,7 @@ struct Walk {
                     float v[16], sum = 0.f;
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
-                        const bool strictly = sb != tb || 8 * (j / 4) + 4 * hh + j % 4 > l32;
+                        const bool strictly = sb != tb || 8 * (j / 4) + j % 4 + diagonal > 0;
                         v[j] = strictly ? p[j] * w[j] * post : 0.f;
                         sum += v[j];
                     }
