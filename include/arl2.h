@@ -388,8 +388,9 @@ size_t arl2_scan_bwd_workspace_bytes(const arl2_scan_desc *desc);
  *   out       device bf16 [B][L][H][D]; must not overlap an input.
  *   S         device fp32 [B][H][D][D], the state after the last token (S0 where there is none); NULL: it is not wanted.  May be S0 itself
  *             (the state is updated in place), else it must not overlap an input.
- * States, decays and sums are fp32 (a block's decays come from sums in fp64).  On the matrix cores the state and the rows that enter it are taken
- * as two bf16 parts (to 2^-17 of each value), and products q'.k' within a block of 64 tokens are rounded to bf16 once.
+ * States, decays and sums are fp32 (a block's decays come from sums in fp64).  On the matrix cores rows enter the state as two bf16 parts (to
+ * 2^-17 of each value: S is off by 2.4e-6 in the 2-norm), and out's rows take the state's features and the products q'.k' within a block of 64 tokens
+ * rounded to bf16 once.
  * Up to 8 tokens are computed in fp32 throughout, with the state read and written once.  A NaN or an infinity in
  * a row reaches outputs of the 64 tokens, counted from the first, that it lies in and of later ones, not of earlier blocks.  Deterministic.
  */
@@ -403,6 +404,8 @@ arl2_status arl2_scan_fwd(const arl2_scan_desc *desc, const void *q, const void 
  *   dq, dk, dv  device bf16 [B][L][H][D], written (through the normalisation where there is one).
  *   dlog_alpha  device fp32 [B][L][H], written: the gradient of log_alpha as if it had no upper limit; zero at a gate of zero.  NULL: it is not wanted.
  *   dS0       device fp32 [B][H][D][D], written; NULL: it is not wanted.
+ * Of what the matrix cores take, dv and dS0 are rounded as out and S are; dq and dk, whose products with q' and k' add up to dlog_alpha over up to 1024
+ * tokens, take the states and what enters them in three bf16 parts (to 2^-25; dlog_alpha is off by 4.3e-6 in the 2-norm at most where it was looked at).
  * What is written must overlap neither an input nor what else is written.  Deterministic.
  */
 arl2_status arl2_scan_bwd(const arl2_scan_desc *desc, const void *q, const void *k, const void *v, const float *log_alpha,

@@ -11,8 +11,9 @@
 // LPT lanes of a workgroup, the least power of two from 16 on that holds them, 256 at the most and then NU to a lane; a head's units divide LPT, so
 // a lane's units all have the same pairs.  A workgroup takes 256 / LPT tokens side by side and, forward, TOK of each in a row: their loads are all
 // requested before the first sum, and their sums cross the wavefronts together.  The gradients hold twice the rows and the weights' sums: one token,
-// turned back once, and the more wavefronts on a SIMD (four tokens with their turns back made twice and three wavefronts: 39.4 us, this one: 34.9; 4680 tokens
-// of 12 + 12 heads x 128 by rows, 2.2 and 2.5 TB/s; 32 + 8 heads, two units a lane: 93 and 61 us).  A weight's gradient stays with its lane.
+// turned back once, and more wavefronts on a SIMD (4680 tokens of 12 + 12 heads x 128 by rows, four tokens with their turns made twice and three wavefronts: 39.4 us,
+// this one 34.9, 33.1 without selects for weights that are not there, missing tokens and pairs without an axis: 2.6 TB/s, 32760 tokens 143 us, 4.2 TB/s).  A weight's gradient
+// stays with its lane.
 #include "arl2_device.h"
 #include "arl2_rope.h"
 
@@ -22,9 +23,9 @@ namespace arl2 {
 namespace {
 
 constexpr int kThreads = 256;
-// Wavefronts on a SIMD that the gradients' registers leave room for, and workgroups on a CU: with more, weights' gradients come in more parts, and with fewer (768 of
-// one unit, 4680 tokens as above) 38.6 us for 36.0.
-constexpr int bwd_waves(int nu, bool f32) { return nu == 1 ? 4 : nu == 2 && !f32 ? 3 : 2; }
+// Wavefronts on a SIMD that the gradients' registers leave room for, and workgroups on a CU: with more, weights' gradients come in more parts.  One unit, 4680 tokens
+// as above: 3, 4, 5 wavefronts 38.6, 36.0, 37.2 us (the last with registers in scratch); two units, 32 + 8 heads: 3, 4 wavefronts 57.8, 54.5 us.
+constexpr int bwd_waves(int nu, bool f32) { return nu == 1 || (nu == 2 && !f32) ? 4 : 2; }
 
 template <class T> struct Raw;                    // 8 features as they lie in memory
 template <> struct Raw<bf16_t> { u32x4 v; };
@@ -60,6 +61,11 @@ template <bool HALVES> __device__ __forceinline__ constexpr int first_of(int pai
 template <bool HALVES> __device__ __forceinline__ constexpr int second_of(int pair) { return HALVES ? 8 + pair : 2 * pair + 1; }
 template <class T>
 __device__ __forceinline__ float feature(const Unit<T> &u, int i) { return i < 8 ? feature(u.lo, i) : feature(u.hi, i - 8); }
+
+__device__ __forceinline__ void fill(Raw<bf16_t> &r, float x) { r.v = u32x4{} + (__float_as_uint(x) >> 16 | __float_as_uint(x)); }      // (x: 0 or 1)
+__device__ __forceinline__ void fill(Raw<float> &r, float x) { r.v[0] = r.v[1] = f32x4{x, x, x, x}; }
+template <class T>
+__device__ __forceinline__ void fill(Unit<T> &u, float x) { fill(u.lo, x); fill(u.hi, x); }
 
 // The compiler is to take these registers for new values: else it keeps what it has widened and turned of every token for the second
 // time that they are used (the gradients of a row: 256 registers and 1 KB of scratch a lane).
@@ -122,8 +128,9 @@ __device__ __forceinline__ float head_sum(float x, int upt)
 __device__ __forceinline__ float group_sum(float x, int n)
 {
     x = lane_group_sum<16>(x);
-    if (n >= 32) x += __shfl_xor(x, 16, kWave);
-    if (n >= 64) x += __shfl_xor(x, 32, kWave);
+    const auto sum = [](auto v) { return __uint_as_float(v[0]) + __uint_as_float(v[1]); };
+    if (n >= 32) x = sum(__builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+    if (n >= 64) x = sum(__builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
     return x;
 }
 
@@ -142,7 +149,7 @@ __device__ __forceinline__ void token_sums(float (*x)[N], const Lane &m, float (
         for (int t = 0; t < TOK; ++t)
 #pragma unroll
             for (int i = 0; i < N; ++i) red[wave][t * N + i] = x[t][i];
-    __syncthreads();
+    lds_barrier();
     const int w0 = m.lpt == 128 ? wave & 2 : 0;
 #pragma unroll
     for (int t = 0; t < TOK; ++t)
@@ -191,12 +198,11 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 4 : NU <= 3 ? 3 : 2) void rope_
     const int at_a_time = m.slots * TOK, left = a.pairs - 8 * m.in_head;
     Unit<T> w[NU];
     int which[NU], off[NU];
-    bool weighted[NU];
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
         which[u] = place(a, m, u, off[u]);
-        weighted[u] = NORM != kNormNone && which[u] < 2 && a.w[which[u]] != nullptr;
-        if (weighted[u]) w[u] = load_unit((const T *)a.w[which[u]] + (NORM == kNormHead ? m.at : off[u]), m.hi);
+        fill(w[u], 1.f);
+        if (NORM != kNormNone && which[u] < 2 && a.w[which[u]] != nullptr) w[u] = load_unit((const T *)a.w[which[u]] + (NORM == kNormHead ? m.at : off[u]), m.hi);
     }
     const uint32_t all = (uint32_t)a.B * a.L;                     // (2e9 at the most: no step past it wraps around)
     const float over_head = 1.f / (float)a.D, over_row[2] = {1.f / (float)(a.heads[0] * a.D), 1.f / (float)(max(a.heads[1], 1) * a.D)};
@@ -230,7 +236,7 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 4 : NU <= 3 ? 3 : 2) void rope_
             }
             token_sums<TOK, 2>(row, m, red[round]);
         }
-        if (NORM != kNormRow || m.lpt <= 64) __syncthreads();
+        if (NORM != kNormRow || m.lpt <= 64) lds_barrier();
 #pragma unroll
         for (int t = 0; t < TOK; ++t) {
             const f32x2 *const turn = &mine[m.slot * TOK + t][8 * m.in_head];
@@ -254,8 +260,8 @@ __global__ __launch_bounds__(kThreads, NU == 1 ? 4 : NU <= 3 ? 3 : 2) void rope_
                     if constexpr (NORM != kNormNone) {
                         f0 *= r;
                         f1 *= r;
-                        f0 *= weighted[u] ? feature(w[u], j0) : 1.f;
-                        f1 *= weighted[u] ? feature(w[u], j1) : 1.f;
+                        f0 *= feature(w[u], j0);
+                        f1 *= feature(w[u], j1);
                     }
                     y[j0] = f0 * c - f1 * s;
                     y[j1] = f0 * s + f1 * c;
@@ -286,12 +292,11 @@ __global__ __launch_bounds__(kThreads, bwd_waves(NU, std::is_same<T, float>::val
     Unit<T> w[NU];
     float dw[NU][16] = {};
     int which[NU], off[NU];
-    bool weighted[NU];
 #pragma unroll
     for (int u = 0; u < NU; ++u) {
         which[u] = place(a, m, u, off[u]);
-        weighted[u] = NORM != kNormNone && which[u] < 2 && a.w[which[u]] != nullptr;
-        if (weighted[u]) w[u] = load_unit((const T *)a.w[which[u]] + (NORM == kNormHead ? m.at : off[u]), m.hi);
+        fill(w[u], 1.f);
+        if (NORM != kNormNone && which[u] < 2 && a.w[which[u]] != nullptr) w[u] = load_unit((const T *)a.w[which[u]] + (NORM == kNormHead ? m.at : off[u]), m.hi);
     }
     const uint32_t all = (uint32_t)a.B * a.L;                     // (2e9 at the most: no step past it wraps around)
     const float over_head = 1.f / (float)a.D, over_row[2] = {1.f / (float)(a.heads[0] * a.D), 1.f / (float)(max(a.heads[1], 1) * a.D)};
@@ -306,6 +311,9 @@ __global__ __launch_bounds__(kThreads, bwd_waves(NU, std::is_same<T, float>::val
                 const size_t at = (size_t)tok * a.heads[which[u]] * a.D + off[u];
                 d[u] = load_unit((const T *)a.dy[which[u]] + at, m.hi);
                 if (NORM != kNormNone) x[u] = load_unit((const T *)a.x[which[u]] + at, m.hi);
+            } else if (NORM != kNormNone) {                       // (adds nothing to a weight's gradient)
+                fill(d[u], 0.f);
+                fill(x[u], 0.f);
             }
         f32x2 (*const mine)[64] = turns + round * m.slots;
         turns_of(a, t0, all, m.slots, mine);
@@ -317,12 +325,15 @@ __global__ __launch_bounds__(kThreads, bwd_waves(NU, std::is_same<T, float>::val
             const float d0 = feature(d[u], j0), d1 = feature(d[u], j1);
             z0 = d0 * c + d1 * s;
             z1 = d1 * c - d0 * s;
-            if (partial && i >= left) { z0 = d0; z1 = d1; }
+            if (partial) {
+                asm volatile("");
+                if (i >= left) { z0 = d0; z1 = d1; }
+            }
             g0 = z0;
             g1 = z1;
             if (NORM != kNormNone) {
-                g0 *= weighted[u] ? feature(w[u], j0) : 1.f;
-                g1 *= weighted[u] ? feature(w[u], j1) : 1.f;
+                g0 *= feature(w[u], j0);
+                g1 *= feature(w[u], j1);
             }
         };
         // squares of the unit's features, and their products with w z
@@ -377,15 +388,14 @@ __global__ __launch_bounds__(kThreads, bwd_waves(NU, std::is_same<T, float>::val
                     forget(w[u]);
                 }
             }
-            const bool counts = there && which[u] < 2;
             each_pair(turn, [&](int i, float c, float s) {
                 const int j0 = first_of<HALVES>(i), j1 = second_of<HALVES>(i);
                 float z0, z1, g0, g1;
                 back(u, i, c, s, z0, z1, g0, g1);
                 if constexpr (NORM != kNormNone) {
                     const float h0 = feature(x[u], j0) * r, h1 = feature(x[u], j1) * r;
-                    dw[u][j0] = counts ? fmaf(z0, h0, dw[u][j0]) : dw[u][j0];
-                    dw[u][j1] = counts ? fmaf(z1, h1, dw[u][j1]) : dw[u][j1];
+                    dw[u][j0] = fmaf(z0, h0, dw[u][j0]);
+                    dw[u][j1] = fmaf(z1, h1, dw[u][j1]);
                     asm volatile("" : "+v"(dw[u][j0]), "+v"(dw[u][j1]));      // (now, not where the next token needs them: z and h would be kept)
                     g0 = r * (g0 - h0 * p);
                     g1 = r * (g1 - h1 * p);
@@ -394,7 +404,7 @@ __global__ __launch_bounds__(kThreads, bwd_waves(NU, std::is_same<T, float>::val
                 y[j1] = g1;
                 if (i % 2) asm volatile("" : "+v"(y[first_of<HALVES>(i - 1)]), "+v"(y[second_of<HALVES>(i - 1)]), "+v"(y[j0]), "+v"(y[j1]));
             });
-            if (!counts) continue;
+            if (!there || which[u] == 2) continue;
             T *const to = (T *)a.y[which[u]] + (size_t)tok * a.heads[which[u]] * a.D + off[u];
             store8(to, y);
             store8(to + m.hi, y + 8);

@@ -418,7 +418,7 @@ struct Walk {
                     const float of = lanes_sums(v, lane);
                     if ((lane & 16) == 0) sc.pair.later[t][8 * ((lane & 15) / 4) + 4 * hh + lane % 4] = of;
                 }
-                // ---- rows asked of the wavefront's part of the state, which is taken in two parts
+                // ---- rows asked of the wavefront's part of the state
 #pragma unroll
                 for (int m = 0; m < 2 * C::TPW; ++m) {
                     u32x4 part[ASKED];
@@ -476,7 +476,7 @@ struct Walk {
                     }
                 }
 
-            // ---- the state's step: rows of Z times their weights in two parts
+            // ---- the state's step: rows of Z times their weights
             const float fold = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(sc.fold[buf])));
             if (fold != 1.f) {
 #pragma unroll
@@ -649,6 +649,10 @@ struct Walk {
     }
 };
 
+// A block of 64 tokens takes 4.4 us (D = 128, one workgroup of eight wavefronts on a CU): the matrix cores are busy for 20 % of that, vector instructions take 39 % of the
+// SIMDs' issue and LDS 25 % of its cycles, half of the wavefronts' time is waiting, for barriers, LDS and rows.  16 x 4096 tokens of 16 heads, one segment:
+// 276 us, 3.9 TB/s, three quarters of a copy's; 32760 tokens of one stream, whose 21 segments are summed first: 112 + 57 + 7 us.  Two workgroups on a CU
+// (128 registers, sums handed on in place): 168 for 172 us of the latter, 288 for 276 of the former.
 template <int D, int HALVES>
 __global__ __launch_bounds__((Cfg<D, HALVES>::NT), D == 64 ? 3 : 2) void scan_out_kernel(ScanArgs a, Work wk)
 {
@@ -712,7 +716,9 @@ __global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, Work wk, int
     if (back && a.dS0 != nullptr) *reinterpret_cast<f32x4 *>(a.dS0 + (size_t)bh * nn + e) = x;
 }
 
-// The rows' gradients: three walks of a segment by three workgroups that follow one another.
+// The rows' gradients: three walks of a segment by three workgroups that follow one another.  At D = 128 a wavefront has all rows of its columns, and two workgroups of four share a
+// CU: 8 x 4680 tokens of 12 heads take 428 us in three times 15 blocks, 9.5 us for two workgroups' blocks; vector instructions take 46 % of the SIMDs' issue (half of them
+// takes states and rows apart into bf16 parts), the matrix cores are busy for 30 % of the time, wavefronts wait for a third of it.
 template <int D, int HALVES>
 __global__ __launch_bounds__((Cfg<D, HALVES>::NT), D == 64 ? 3 : 2) void scan_grad_kernel(ScanArgs a, Work wk)
 {
@@ -799,7 +805,8 @@ __global__ __launch_bounds__(256) void scan_gate_kernel(ScanArgs a, Work wk)
     }
 }
 
-// ---- few tokens: the state once in and out, by elements; 32 columns to a workgroup, 8 lanes to a row of them
+// ---- few tokens: the state once in and out, by elements; 32 columns to a workgroup, 8 lanes to a row of them.  Bound by memory: one token of 16 streams of 12 heads x 128
+// moves 25 MB in 7.2 us.
 template <int D>
 __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a)
 {
@@ -875,7 +882,6 @@ Work work_of(const ScanArgs &a, const ScanPlan &p)
     return wk;
 }
 
-// Halves of the state's rows by wavefront: see scan_plan.
 template <int D, int HALVES>
 hipError_t launch_sums(const ScanArgs &a, const ScanPlan &p, const Work &wk, bool back, int last, int first, hipStream_t stream)
 {
@@ -915,8 +921,8 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Segments: enough workgroups for the chip, no more states than that takes.  Time is counted in hundredths of a block of a full chip, which has `per_cu` workgroups
 // on a CU (one alone takes 70 and 60 hundredths of two's and three's); a second part of the sequence costs the sums of the segments (a block half of one), what joins them,
-// by segment, and two launches.  12 heads x 128 (block: 4.5 us; gradients 9.9 us): 1560 tokens in 7, 13 (taken), 25 segments 32.8, 25.9, 27.3 us; 32760 in 15, 21 (taken), 32, 42: 219,
-// 176, 199, 183 us; gradients of 1560 in 3, 7, 13 (taken), 25: 86, 54, 51, 66 us; of 8 x 4680 in 5 (taken), 6, 8, 10: 532, 571, 581, 594 us.
+// by segment, and two launches.  12 heads x 128: 1560 tokens in 7, 9, 13 (taken), 25 segments 32.1, 28.3, 25.4, 33.4 us; 32760 in 15, 21 (taken), 32, 42: 214,
+// 172, 198, 181 us; gradients of 1560 in 3, 7, 13 (taken), 25: 87, 54.3, 53.0, 65 us; of 8 x 4680 in 5 (taken), 6, 8, 10: 549, 579, 593, 606 us.
 ScanPlan scan_plan(int B, int H, int L, int D, bool backward)
 {
     ScanPlan p = {};
