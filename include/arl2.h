@@ -391,6 +391,7 @@ size_t arl2_scan_bwd_workspace_bytes(const arl2_scan_desc *desc);
  * States, decays and sums are fp32 (a block's decays come from sums in fp64).  On the matrix cores rows enter the state as two bf16 parts (to
  * 2^-17 of each value: S is off by 2.4e-6 in the 2-norm), and out's rows take the state's features and the products q'.k' within a block of 64 tokens
  * rounded to bf16 once.
+ * Features of rows have to be below 2^16, the state below 2^48 (products of three of them have decays taken out, up to 2^64, before fp32 holds them).
  * Up to 8 tokens are computed in fp32 throughout, with the state read and written once.  A NaN or an infinity in
  * a row reaches outputs of the 64 tokens, counted from the first, that it lies in and of later ones, not of earlier blocks.  Deterministic.
  */
@@ -404,6 +405,7 @@ arl2_status arl2_scan_fwd(const arl2_scan_desc *desc, const void *q, const void 
  *   dq, dk, dv  device bf16 [B][L][H][D], written (through the normalisation where there is one).
  *   dlog_alpha  device fp32 [B][L][H], written: the gradient of log_alpha as if it had no upper limit; zero at a gate of zero.  NULL: it is not wanted.
  *   dS0       device fp32 [B][H][D][D], written; NULL: it is not wanted.
+ * The same ranges hold for features of dout and for the state's gradient.
  * Of what the matrix cores take, dv and dS0 are rounded as out and S are; dq and dk, whose products with q' and k' add up to dlog_alpha over up to 1024
  * tokens, take the states and what enters them in three bf16 parts (to 2^-25; dlog_alpha is off by 4.3e-6 in the 2-norm at most where it was looked at).
  * What is written must overlap neither an input nor what else is written.  Deterministic.
@@ -437,6 +439,7 @@ typedef struct {
     void *stream;         /* hipStream_t; NULL is the default stream                                                 */
 } arl2_rope_desc;
 
+/* Scratch of arl2_rope_bwd where it writes weights' gradients (it depends on B, H, Hk, L and D alone; 0: the descriptor is invalid). */
 size_t arl2_rope_workspace_bytes(const arl2_rope_desc *desc);
 
 /*
@@ -445,7 +448,8 @@ size_t arl2_rope_workspace_bytes(const arl2_rope_desc *desc);
  *   pos       device int32, any values: angles are computed in fp64.
  *   seq_len   device int32 [B], or NULL: L for all.  Rows from seq_len[b] on are not read, and left as they were in what is written.
  *   yq, yk    device, like q and k.  yq may be q and yk may be k (in place); else they must overlap neither an input nor each other.
- * fp32 arithmetic, one rounding to io_dtype.
+ * fp32 arithmetic, one rounding to io_dtype.  Where there is a norm, the sums of a row's squares (and of its products with dy and the weights) have to lie in
+ * fp32's range; a NaN or an infinity reaches the rows that share its norm.
  */
 arl2_status arl2_rope_fwd(const arl2_rope_desc *desc, const void *q, const void *k, const void *wq, const void *wk,
                           const int32_t *pos, const int32_t *seq_len, void *yq, void *yk);

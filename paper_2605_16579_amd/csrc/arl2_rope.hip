@@ -23,6 +23,7 @@ namespace arl2 {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kMostWorkgroups = 1 << 20;         // (a launch has room for 2^32 threads)
 // Wavefronts on a SIMD that the gradients' registers leave room for, and workgroups on a CU: with more, weights' gradients come in more parts.  One unit, 4680 tokens
 // as above: 3, 4, 5 wavefronts 38.6, 36.0, 37.2 us (the last with registers in scratch); two units, 32 + 8 heads: 3, 4 wavefronts 57.8, 54.5 us.
 constexpr int bwd_waves(int nu, bool f32) { return nu == 1 || (nu == 2 && !f32) ? 4 : 2; }
@@ -539,16 +540,16 @@ size_t rope_workspace_bytes(int B, int L, int D, int heads)
 hipError_t launch_rope(const RopeArgs &a, hipStream_t stream)
 {
     const Shape s = shape_of((a.heads[0] + a.heads[1]) * (a.D / 16), a.f32, false);
-    // Without weights to load a workgroup takes one round of tokens; else 4 x 10920 tokens of 32 + 8 heads x 128 (two units a lane) took 196, 209, 221 us
+    // Without weights to load a workgroup takes one round of tokens (up to 2^20 of them); else 4 x 10920 tokens of 32 + 8 heads x 128 (two units a lane) took 196, 209, 221 us
     // with at most 1024, 4096 and any number of workgroups, 7 x 4680 tokens of 12 + 12 heads (one unit) 101, 90, 97 us.
-    const int most = a.norm == kNormNone ? 1 << 30 : s.nu == 1 ? 4096 : 1024;
+    const int most = a.norm == kNormNone ? kMostWorkgroups : s.nu == 1 ? 4096 : 1024;
     return launch_any<false>(a, s, workgroups(a.B, a.L, s, most), stream);
 }
 
 hipError_t launch_rope_bwd(const RopeArgs &a, hipStream_t stream)
 {
     const Shape s = shape_of((a.heads[0] + a.heads[1]) * (a.D / 16), a.f32, true);
-    const int n = workgroups(a.B, a.L, s, a.norm == kNormNone ? 1 << 30 : bwd_waves(s.nu, a.f32) * kNumCu);
+    const int n = workgroups(a.B, a.L, s, a.norm == kNormNone ? kMostWorkgroups : bwd_waves(s.nu, a.f32) * kNumCu);
     const hipError_t e = launch_any<true>(a, s, n, stream);
     if (e != hipSuccess || a.norm == kNormNone || (a.dw[0] == nullptr && a.dw[1] == nullptr)) return e;
     const int width0 = a.norm == kNormHead ? a.D : a.heads[0] * a.D, width = a.norm == kNormHead ? 2 * a.D : (a.heads[0] + a.heads[1]) * a.D;

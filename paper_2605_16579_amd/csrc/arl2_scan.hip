@@ -410,7 +410,7 @@ struct Walk {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         const bool strictly = sb != tb || 8 * (j / 4) + j % 4 + diagonal > 0;
-                        v[j] = strictly ? p[j] * w[j] * post : 0.f;
+                        v[j] = strictly ? p[j] * post * w[j] : 0.f;       // (in this order: p has a decay taken out)
                         sum += v[j];
                     }
                     sum = xhalf_sum(sum);

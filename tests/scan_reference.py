@@ -11,7 +11,9 @@ BLOCK, LONGEST = 64, 1024        # tokens of a block; of a segment of the gradie
 # (dout.v for dq and dk) are rounded to bf16 before they multiply rows of the block: U16 of each term's magnitude more, `near` below.
 # For out (from 9 tokens on) and dv these products and the state's features that the block's rows are multiplied with both are: a term is one of
 # the two, so that U16 of all magnitudes comes in.
+# A value below the normal numbers of both types, 2^-126, may come as zero: off by less than TINY (half of bf16's smallest step would be 2^-134).
 U16 = 2.0 ** -8
+TINY = 2.0 ** -126
 TWO = U16 * U16 + 2.0 ** -17
 
 
@@ -70,7 +72,7 @@ class Case:
             out[on, t] = np.einsum("bhd,bhde->bhe", q[on, t], S[on])
             most[on, t] = np.einsum("bhd,bhde->bhe", np.abs(q[on, t]), M[on])
         few = self.L <= 8
-        return out, S, U16 * np.abs(out) + (0.0 if few else U16) * most + TWO * most, TWO * M + 1e-30
+        return out, S, U16 * np.abs(out) + (0.0 if few else U16) * most + TWO * most + TINY, TWO * M + 1e-30
 
     def backward(self):
         """dq, dk, dv, dla, dS0, and their limits."""
@@ -121,8 +123,8 @@ class Case:
                 d[:] = i * (d - x * (x * d).sum(-1, keepdims=True))
                 for y in (m, c):
                     y[:] = i * (y + np.abs(x) * (np.abs(x) * y).sum(-1, keepdims=True))
-            limits.append(U16 * (np.abs(d) + c) + 2.0 * TWO * m)
-        limits += [U16 * (np.abs(dv) + mv) + TWO * mv, 2.0 * TWO * (along + ends) + 1e-30, TWO * N + 1e-30]
+            limits.append(U16 * (np.abs(d) + c) + 2.0 * TWO * m + TINY)
+        limits += [U16 * (np.abs(dv) + mv) + TWO * mv + TINY, 2.0 * TWO * (along + ends) + 1e-30, TWO * N + 1e-30]
         return (dq, dk, dv, E, G), limits
 
 

@@ -23,7 +23,7 @@ def check_forward(A, c, **kw):
     # in the 2-norm the roundings of out and of a block's products are independent: U16 / sqrt(3) each at the most
     there = np.arange(c.L)[None] < np.array(c.lens)[:, None]
     if there.any() and np.linalg.norm(out[there]) > 0:
-        assert np.linalg.norm(R.wide(got)[there] - out[there]) <= R.U16 * np.linalg.norm(out[there])
+        assert np.linalg.norm(R.wide(got)[there] - out[there]) <= R.U16 * np.linalg.norm(out[there]) + R.TINY * out[there].size ** 0.5
         assert np.linalg.norm(R.wide(state) - S) <= R.TWO * np.linalg.norm(S) + 1e-30
     return got, state
 
@@ -71,6 +71,18 @@ def test_rows_as_they_are(A, D, L):
     c = R.Case(2, 3, L, D, seed=5, normalise=False, rows=0.3)
     check_forward(A, c)
     check_backward(A, c)
+
+
+@pytest.mark.parametrize("gate", [None, -0.4, -0.65, -3.0])
+@pytest.mark.parametrize("normalise,rows", [(True, 2.0 ** 13), (True, 2.0 ** -50), (False, 2.0 ** 13), (False, 2.0 ** -25)])
+def test_large_and_small_rows(A, normalise, rows, gate):
+    """Decays are taken out of rows and states, up to 2^60 of a block here: what they are multiplied with in between has room."""
+    for L in (5, 200):
+        c = R.Case(1, 3, L, 64, seed=23, normalise=normalise, rows=rows, start=False)
+        if gate is not None:
+            c.la[:] = gate
+        check_forward(A, c)
+        check_backward(A, c)
 
 
 def test_rows_of_zeros(A):
