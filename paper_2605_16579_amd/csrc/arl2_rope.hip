@@ -459,30 +459,26 @@ __global__ __launch_bounds__(kThreads, bwd_waves(NU, std::is_same<T, float>::val
     }
 }
 
-// Weights' gradients: 16 columns to a workgroup, the workgroups' parts in 64 groups added in order.
+// Weights' gradients: 32 columns (128 bytes: with 16, halves of a line were read by two XCDs, 5.0 for 3.9 us and 936 parts of 12 KB) to a workgroup, the
+// workgroups' parts in 32 groups added in order.
 __global__ __launch_bounds__(1024) void rope_dw_kernel(RopeArgs a, int parts, int width0, int width)
 {
-    __shared__ float sums[64][17];
-    const int c = threadIdx.x & 15, g = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
+    __shared__ float sums[32][33];
+    const int c = threadIdx.x & 31, g = threadIdx.x >> 5, first = blockIdx.x * 32;
     float s = 0.f;
-    for (int p0 = g; p0 < parts; p0 += 512) {                     // eight on their way at a time
-        float v[8];
+    for (int p0 = g; p0 < parts; p0 += 512) {                     // sixteen on their way at a time
+        float v[16];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = p0 + 64 * i < parts ? a.part[(size_t)(p0 + 64 * i) * width + col] : 0.f;
+        for (int i = 0; i < 16; ++i) v[i] = p0 + 32 * i < parts ? a.part[(size_t)(p0 + 32 * i) * width + first + c] : 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s += v[i];
+        for (int i = 0; i < 16; ++i) s += v[i];
     }
     sums[g][c] = s;
     __syncthreads();
-    if (g >= 16) return;
-    s = 0.f;
-    const int first = 4 * c;                                      // column g: four groups to a lane
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s += sums[first + i][g];
-    s = lane_group_sum<16>(s);
-    const int to_col = blockIdx.x * 16 + g;
-    float *const to = to_col < width0 ? a.dw[0] : a.dw[1];
-    if (to != nullptr && c == 0) to[to_col < width0 ? to_col : to_col - width0] = s;
+    s = group_sum(sums[c][g], 32);                                // column g of the 32
+    const int col = first + g;
+    float *const to = col < width0 ? a.dw[0] : a.dw[1];
+    if (to != nullptr && c == 0) to[col < width0 ? col : col - width0] = s;
 }
 
 // How tokens are dealt: lanes to a token, units to a lane, tokens of a lane at a time.
@@ -553,7 +549,7 @@ hipError_t launch_rope_bwd(const RopeArgs &a, hipStream_t stream)
     const hipError_t e = launch_any<true>(a, s, n, stream);
     if (e != hipSuccess || a.norm == kNormNone || (a.dw[0] == nullptr && a.dw[1] == nullptr)) return e;
     const int width0 = a.norm == kNormHead ? a.D : a.heads[0] * a.D, width = a.norm == kNormHead ? 2 * a.D : (a.heads[0] + a.heads[1]) * a.D;
-    return launch_kernel(rope_dw_kernel, dim3(width / 16), dim3(1024), stream, a, n, width0, width);
+    return launch_kernel(rope_dw_kernel, dim3(width / 32), dim3(1024), stream, a, n, width0, width);
 }
 
 }  // namespace arl2
