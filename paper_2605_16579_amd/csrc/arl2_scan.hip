@@ -324,6 +324,9 @@ struct Walk {
             // gradients of 8 x 4680 tokens with 33 registers in scratch and 147 of the scalar ones in lanes: 610 us, with none and 28: 551)
             asm volatile("" : "+v"(row_at), "+v"(y_at[0]), "+v"(y_at[1]), "+v"(z_at[0]), "+v"(z_at[1]), "+v"(diagonal));
             if (HALVES == 1) asm volatile("" : "+v"(tid), "+v"(lane), "+v"(l32), "+v"(hh));
+            // Of the workgroups on a CU the one that is furthest in its block goes first: they are then not all at the same step.  With one priority gradients of 5 x 999
+            // tokens of 24 heads x 64 took 76.5 us, so 71.4, of 8 x 4680 tokens of 12 heads x 128 547 and 535.
+            __builtin_amdgcn_s_setprio(1);
             if (ROWS) stage(gx, lx, GRAD ? 0 : 1, buf);
             stage(gy, ly, GRAD ? 0 : 2, buf);
             stage(gz, lz, GRAD ? 2 : 0, buf);
@@ -331,6 +334,7 @@ struct Walk {
             const bool pairs = __builtin_amdgcn_readfirstlane(sc.pairs[buf]) != 0;
             lds_barrier();
 
+            __builtin_amdgcn_s_setprio(2);
             bf16x8 zf[4];                                         // Z^T of the wavefront's columns, 16 tokens each
             f32x16 acc[2] = {};                                   // rows of 32 tokens each, with two halves the wavefront's own ones first
             u32x2 own[C::OWN][4];                                 // the rows whose normalisation has a gradient
@@ -457,6 +461,7 @@ struct Walk {
                 for (int g = 0; g < 4; ++g) *reinterpret_cast<f32x4 *>(to + 1024 * g) = f32x4{acc[1][4 * g], acc[1][4 * g + 1], acc[1][4 * g + 2], acc[1][4 * g + 3]};
             };
             if (HANDS_ON && !IN_PLACE) hand_on();
+            __builtin_amdgcn_s_setprio(3);
             if (ROWS) lds_barrier();
             if (HANDS_ON && IN_PLACE) hand_on();                  // (nobody reads X and Z any more)
 
@@ -506,6 +511,7 @@ struct Walk {
                 }
             }
 
+            __builtin_amdgcn_s_setprio(0);
             // ---- rows out
             if constexpr (ROWS) {
                 if constexpr (HANDS_ON) {
