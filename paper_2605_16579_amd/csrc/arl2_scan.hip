@@ -33,7 +33,7 @@ enum Mode { kOut, kDq, kDk, kDv, kSum, kSumBack };       // the last two make st
 
 // One call's arrays in the workspace: states [B*H][nseg + 1][D][D], the way forth (state i: what segment i begins with) and back
 // (state i: the gradient of what segment i - 1 ends with), the segments' decays, the parts
-// of E by tokens [3][B*H][L] (a_t; -b_t; G's), and <S_L, dS> [B*H] where a sequence is one segment.
+// of E by tokens [3][B*H][L] (a_t; -b_t; G's), and <state, its gradient> at the segments' borders [B*H][nseg + 1].
 struct Work {
     float *forth, *back, *decay_forth, *decay_back, *parts, *anchor;
     int nseg, seg;
@@ -191,6 +191,28 @@ struct Walk {
         // ---- the state: register j of the wavefront's tile t is row r0 + 32 t + 16 (j / 8) + 8 hh + j % 8, column e0 + l32
         f32x16 st[C::TPW];
         const int e0 = 32 * column, r0 = 32 * C::TPW * half;
+        // its product with its gradient, which lies there and is not transposed: the wavefronts' sums
+        auto with_gradient = [&](const float *there) {
+            there += (size_t)(e0 + l32) * D + r0 + 8 * hh;
+            float dot = 0.f;
+#pragma unroll
+            for (int t = 0; t < C::TPW; ++t)
+#pragma unroll
+                for (int j = 0; j < 16; j += 4) {
+                    const f32x4 x = *reinterpret_cast<const f32x4 *>(there + 32 * t + 16 * (j / 8) + j % 8);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) dot = fmaf(x[i], st[t][j + i], dot);
+                }
+#pragma unroll
+            for (int m = 32; m > 0; m >>= 1) dot += __shfl_xor(dot, m, kWave);
+            if (lane == 0) sc.red[column][half][0] = dot;
+        };
+        auto anchor = [&](int border, float factor) {             // by one lane, behind a barrier
+            float dot = 0.f;
+#pragma unroll
+            for (int w = 0; w < C::NW; ++w) dot += sc.red[w % C::NC][w / C::NC][0];
+            wk.anchor[(size_t)bh * (wk.nseg + 1) + border] = dot * factor;
+        };
         {
             const float *from = nullptr;
             if (ROWS && wk.nseg == 1) {                           // one segment: what the call begins with
@@ -209,6 +231,7 @@ struct Walk {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) st[t][j + i] = x[i];
                     }
+                if (MODE == kDq && seg > 0 && a.dla != nullptr) with_gradient(wk.back + ((size_t)bh * (wk.nseg + 1) + seg) * D * D);
             } else {
 #pragma unroll
                 for (int t = 0; t < C::TPW; ++t)
@@ -301,6 +324,7 @@ struct Walk {
             if (wave == GW) gates(0);
             if (count > 1) fetch_gate(block_at(1));
             lds_barrier();
+            if (MODE == kDq && tid == 0 && seg > 0 && a.dla != nullptr) anchor(seg, 1.f);
         }
         // rows as operands: the lane's piece 2 m + hh of row l32 of a block's 32 lies at (row_at ^ 32 m); by columns, the lane's 8 bytes of
         // four of 16 tokens at tr_at[0], of the next four at tr_at[1], each ^ 64 per 32 columns.  For the state's step pieces 1 and 2 of four change
@@ -616,28 +640,12 @@ struct Walk {
 #pragma unroll
                 for (int j = 0; j < 16; ++j) to[(size_t)(r0 + 32 * t + 16 * (j / 8) + 8 * hh + j % 8) * D + e0 + l32] = st[t][j] * gathered;
         }
-        if (MODE == kDq && wk.nseg == 1 && a.dS != nullptr && a.dla != nullptr) {        // <S_L, dS>: the state is transposed here
+        if (MODE == kDq && seg == nact - 1 && a.dS != nullptr && a.dla != nullptr) {        // <S_L, dS>
             lds_barrier();                                        // all have read the last block's sums
             if (tid == 64 * GW) sc.fold[0] = count > 0 ? exp2_of(base) : 1.f;
-            const float *const from = a.dS + (size_t)bh * D * D + (size_t)(e0 + l32) * D;
-            float dot = 0.f;
-#pragma unroll
-            for (int t = 0; t < C::TPW; ++t)
-#pragma unroll
-                for (int j = 0; j < 16; j += 4) {
-                    const f32x4 x = *reinterpret_cast<const f32x4 *>(from + r0 + 32 * t + 16 * (j / 8) + 8 * hh + j % 8);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) dot = fmaf(x[i], st[t][j + i], dot);
-                }
-#pragma unroll
-            for (int m = 32; m > 0; m >>= 1) dot += __shfl_xor(dot, m, kWave);
-            if (lane == 0) sc.red[column][half][0] = dot;
+            with_gradient(a.dS + (size_t)bh * D * D);
             lds_barrier();
-            if (tid == 0) {
-                dot = 0.f;
-                for (int w = 0; w < C::NW; ++w) dot += sc.red[w % C::NC][w / C::NC][0];
-                wk.anchor[bh] = dot * sc.fold[0];
-            }
+            if (tid == 0) anchor(nact, sc.fold[0]);
         }
         if (!ROWS && tid == 64 * GW) (MODE == kSum ? wk.decay_forth : wk.decay_back)[(size_t)bh * wk.nseg + seg] = exp2_of(seg_total);
     }
@@ -669,10 +677,10 @@ __global__ __launch_bounds__((Cfg<D, HALVES>::NT), D == 64 ? 3 : 2) void scan_ou
     W::run(a, wk, id / wk.nseg, id % wk.nseg, lds, sc);
 }
 
-// Segments' own states.  `back`: the way back too, as every second workgroup; the last segment of the way forth and the first of
-// the way back only where something reads them.
+// Segments' own states, but for the last of the way forth.  `back`: the way back too, as every second workgroup; the first of the way back only where
+// something reads it.
 template <int D, int HALVES>
-__global__ __launch_bounds__((Cfg<D, HALVES>::NT), 3) void scan_sum_kernel(ScanArgs a, Work wk, int back, int need_last, int need_first)
+__global__ __launch_bounds__((Cfg<D, HALVES>::NT), 3) void scan_sum_kernel(ScanArgs a, Work wk, int back, int need_first)
 {
     __shared__ __align__(16) unsigned char lds[Walk<D, kSum, HALVES>::LDS_ROWS];
     __shared__ __align__(16) Scalars<D> sc;
@@ -682,11 +690,11 @@ __global__ __launch_bounds__((Cfg<D, HALVES>::NT), 3) void scan_sum_kernel(ScanA
     const int blocks = (tokens_of(a, bh / a.H) + kBlock - 1) / kBlock, nact = max(1, (blocks + wk.seg - 1) / wk.seg);
     if (back && (id & 1)) {
         if (seg > 0 || need_first) Walk<D, kSumBack, HALVES>::run(a, wk, bh, seg, lds, sc);
-    } else if (seg < nact - 1 || need_last) Walk<D, kSum, HALVES>::run(a, wk, bh, seg, lds, sc);
+    } else if (seg < nact - 1) Walk<D, kSum, HALVES>::run(a, wk, bh, seg, lds, sc);
 }
 
 // States at the segments' borders from the segments' own: each its decay times the one before, plus its own.
-__global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, Work wk, int need_last, int need_first)
+__global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, Work wk, int need_first)
 {
     const int nn = a.D * a.D, per = nn / 1024, unit = blockIdx.x / per;
     const int e = ((blockIdx.x - unit * per) * 256 + threadIdx.x) * 4;
@@ -699,7 +707,7 @@ __global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, Work wk, int
     f32x4 x = {};
     if (start != nullptr) x = *reinterpret_cast<const f32x4 *>(start + (size_t)bh * nn + e);
     *reinterpret_cast<f32x4 *>(base + (size_t)(back ? nact : 0) * nn) = x;
-    const int steps = back ? nact - 1 + need_first : nact - 1 + need_last;
+    const int steps = nact - 1 + (back ? need_first : 0);
     constexpr int AHEAD = 16;                                     // states on their way at a time
     for (int i0 = 0; i0 < steps; i0 += AHEAD) {
         f32x4 own[AHEAD];
@@ -742,10 +750,10 @@ __global__ __launch_bounds__((Cfg<D, HALVES>::NT), D == 64 ? 3 : 2) void scan_gr
 __global__ __launch_bounds__(256) void scan_gate_kernel(ScanArgs a, Work wk)
 {
     constexpr int PER = 4;                                        // tokens of a thread: 1024 of a workgroup, which a segment has at the most
-    __shared__ double sums[4], ends[4];
+    __shared__ double ends[4];
     __shared__ int cuts[4];
     const int bh = blockIdx.x / wk.nseg, seg = blockIdx.x % wk.nseg, b = bh / a.H, h = bh - b * a.H;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nn = a.D * a.D;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n = tokens_of(a, b), blocks = (n + kBlock - 1) / kBlock, nact = max(1, (blocks + wk.seg - 1) / wk.seg);
     const int t0 = seg * wk.seg * kBlock, t1 = min(n, t0 + wk.seg * kBlock);
     if (t0 >= t1) return;
@@ -761,23 +769,7 @@ __global__ __launch_bounds__(256) void scan_gate_kernel(ScanArgs a, Work wk)
         v[i] = t < t1 ? (double)p[0] + p[rows] + p[2 * rows] : 0.0;
         if (t < t1 && a.la[((size_t)b * a.L + t) * a.H + h] < -2839.2f) cut |= 1 << i;
     }
-    double dot = 0.0;
-    if (wk.nseg > 1 && (seg < nact - 1 || a.dS != nullptr)) {
-        const size_t at = ((size_t)bh * (wk.nseg + 1) + seg + 1) * nn;
-        const float *const x = wk.forth + at, *const y = wk.back + at;
-        for (int e = tid * 4; e < nn; e += 4096) {
-            f32x4 p[4], q[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                p[i] = *reinterpret_cast<const f32x4 *>(x + e + 1024 * i);
-                q[i] = *reinterpret_cast<const f32x4 *>(y + e + 1024 * i);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) dot += ((double)p[i][0] * q[i][0] + (double)p[i][1] * q[i][1]) + ((double)p[i][2] * q[i][2] + (double)p[i][3] * q[i][3]);
-        }
-    } else if (wk.nseg == 1 && a.dS != nullptr && tid == 0) dot = wk.anchor[bh];
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) dot += __shfl_xor(dot, m, kWave);
+    const double end = seg < nact - 1 || a.dS != nullptr ? wk.anchor[(size_t)bh * (wk.nseg + 1) + seg + 1] : 0.f;
     // sums within the thread, over the lanes before it, over the wavefronts before that
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -796,9 +788,8 @@ __global__ __launch_bounds__(256) void scan_gate_kernel(ScanArgs a, Work wk)
         }
     }
     if (lane == 63) { ends[wave] = run; cuts[wave] = any; }
-    if (lane == 0) sums[wave] = dot;
     __syncthreads();
-    double before = sums[0] + sums[1] + sums[2] + sums[3];
+    double before = end;
     for (int w = 0; w < wave; ++w) before = cuts[w] ? ends[w] : before + ends[w];
     const double lanes = __shfl_up(run, 1, kWave);
     const int lane_cut = __shfl_up(any, 1, kWave);
@@ -889,13 +880,13 @@ Work work_of(const ScanArgs &a, const ScanPlan &p)
 }
 
 template <int D, int HALVES>
-hipError_t launch_sums(const ScanArgs &a, const ScanPlan &p, const Work &wk, bool back, int last, int first, hipStream_t stream)
+hipError_t launch_sums(const ScanArgs &a, const ScanPlan &p, const Work &wk, bool back, int first, hipStream_t stream)
 {
     if (p.nseg == 1) return hipSuccess;
     const int bh = a.B * a.H, ways = back ? 2 : 1;
-    const hipError_t e = launch_kernel(scan_sum_kernel<D, HALVES>, dim3(ways * bh * p.nseg), dim3(Cfg<D, HALVES>::NT), stream, a, wk, (int)back, last, first);
+    const hipError_t e = launch_kernel(scan_sum_kernel<D, HALVES>, dim3(ways * bh * p.nseg), dim3(Cfg<D, HALVES>::NT), stream, a, wk, (int)back, first);
     if (e != hipSuccess) return e;
-    return launch_kernel(scan_join_kernel, dim3(ways * bh * (D * D / 1024)), dim3(256), stream, a, wk, last, first);
+    return launch_kernel(scan_join_kernel, dim3(ways * bh * (D * D / 1024)), dim3(256), stream, a, wk, first);
 }
 
 template <int D, int SUM_HALVES>
@@ -904,7 +895,7 @@ hipError_t launch_fwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
     const int bh = a.B * a.H;
     if (p.step) return launch_kernel(scan_step_kernel<D>, dim3(bh * (D / 32)), dim3(256), stream, a);
     const Work wk = work_of(a, p);
-    const hipError_t e = launch_sums<D, SUM_HALVES>(a, p, wk, false, 0, 0, stream);
+    const hipError_t e = launch_sums<D, SUM_HALVES>(a, p, wk, false, 0, stream);
     if (e != hipSuccess) return e;
     return launch_kernel(scan_out_kernel<D, 2>, dim3(bh * p.nseg), dim3(Cfg<D, 2>::NT), stream, a, wk);
 }
@@ -914,7 +905,7 @@ hipError_t launch_bwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
 {
     const int bh = a.B * a.H;
     const Work wk = work_of(a, p);
-    hipError_t e = launch_sums<D, SUM_HALVES>(a, p, wk, true, a.dS != nullptr, a.dS0 != nullptr, stream);
+    hipError_t e = launch_sums<D, SUM_HALVES>(a, p, wk, true, a.dS0 != nullptr, stream);
     if (e != hipSuccess) return e;
     e = launch_kernel(scan_grad_kernel<D, HALVES>, dim3(3 * bh * p.nseg), dim3(Cfg<D, HALVES>::NT), stream, a, wk);
     if (e != hipSuccess || a.dla == nullptr) return e;
@@ -958,7 +949,7 @@ ScanPlan scan_plan(int B, int H, int L, int D, bool backward)
     p.back = states;
     p.decay = backward ? 2 * states : states;
     p.dots = p.decay + decays;
-    p.bytes = p.dots + (backward ? align256((size_t)bh * (3 * (size_t)L + 1) * sizeof(float)) : 0);
+    p.bytes = p.dots + (backward ? align256((size_t)bh * (3 * (size_t)L + p.nseg + 1) * sizeof(float)) : 0);
     return p;
 }
 
