@@ -132,6 +132,12 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t (&part)[N]
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mfma(u32x4 a, bf16x8 b, f32x16 c) { return mfma(__builtin_bit_cast(bf16x8, a), b, c); }
 
+// Sum with the lane in the other half-wave, without LDS.
+__device__ __forceinline__ float halves_sum(float x)
+{
+    const auto v = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(v[0]) + __uint_as_float(v[1]);
+}
 // Sums over the 32 lanes of a half-wave of each of 16 registers: lane l receives that of register l % 16.
 __device__ __forceinline__ float lanes_sums(float (&v)[16], int lane)
 {
@@ -146,7 +152,8 @@ __device__ __forceinline__ float lanes_sums(float (&v)[16], int lane)
     halve(std::integral_constant<int, 0x141>{}, 4, lane & 4);          // row_half_mirror: 7 - l of the 8
     halve(std::integral_constant<int, 0x1B>{}, 2, lane & 2);           // quad_perm [3,2,1,0]
     halve(std::integral_constant<int, 0xB1>{}, 1, lane & 1);           // quad_perm [1,0,3,2]
-    return v[0] + __shfl_xor(v[0], 16, kWave);
+    const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[0]), __float_as_uint(v[0]), false, false);
+    return __uint_as_float(rows[0]) + __uint_as_float(rows[1]);
 }
 
 template <int D, int MODE, int HALVES>
@@ -441,7 +448,7 @@ struct Walk {
                         v[j] = strictly ? p[j] * post * w[j] : 0.f;       // (in this order: p has a decay taken out)
                         sum += v[j];
                     }
-                    sum = xhalf_sum(sum);
+                    sum = halves_sum(sum);
                     if (hh == 0) sc.pair.earlier[t][l32] = sum;
                     const float of = lanes_sums(v, lane);
                     if ((lane & 16) == 0) sc.pair.later[t][8 * ((lane & 15) / 4) + 4 * hh + lane % 4] = of;
@@ -566,8 +573,8 @@ struct Walk {
                                 const float x0 = __uint_as_float(own[o][g][j] << 16), x1 = __uint_as_float(own[o][g][j] & 0xffff0000u);
                                 ss = fmaf(x0, x0, fmaf(x1, x1, ss));
                             }
-                        ss = xhalf_sum(ss);
-                        const float dot = xhalf_sum(dot_of(own[o], acc[o])), from_state = xhalf_sum(asked[o]);
+                        ss = halves_sum(ss);
+                        const float dot = halves_sum(dot_of(own[o], acc[o])), from_state = halves_sum(asked[o]);
                         if (hh == 0) {
                             sc.red[column][tok][0] = dot;
                             sc.red[column][tok][1] = from_state;
