@@ -166,6 +166,7 @@ struct Walk {
     // result; of what enters: two, the state is off by 2.4e-6 in the 2-norm.  Three of either where sums with q and k are parts of E, whose errors add up over a segment:
     // with two, heads with gates of 0.8 had E off by 9.1e-6, with three by 1.0e-6 (with three of one and two of the other 6e-6).
     static constexpr int ASKED = GRAD ? 3 : 1, ENTER = GRAD ? 3 : 2;
+    static constexpr int GROUP = HALVES == 1 ? 2 : 4;             // of D / 16 products of rows: operands requested together
     static constexpr int ROUND = C::NT / C::LPR, ROUNDS = kBlock / ROUND;    // rows that the threads stage at a time
     // Sums for the other half lie where X and Z were at D = 64, whose workgroups have to leave room for others.
     static constexpr bool HANDS_ON = ROWS && HALVES == 2, IN_PLACE = D == 64;
@@ -387,7 +388,17 @@ struct Walk {
                     const int sb = y_of(t), tb = x_of(t);
                     f32x16 p = {};
 #pragma unroll
-                    for (int m = 0; m < D / 16; ++m) p = mfma(by_rows(ly, sb, m), by_rows(lx, tb, m), p);
+                    for (int m0 = 0; m0 < D / 16; m0 += GROUP) {
+                        bf16x8 yf[GROUP], xf[GROUP];
+#pragma unroll
+                        for (int m = 0; m < GROUP; ++m) {
+                            yf[m] = by_rows(ly, sb, m0 + m);
+                            xf[m] = by_rows(lx, tb, m0 + m);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int m = 0; m < GROUP; ++m) p = mfma(yf[m], xf[m], p);
+                    }
                     if (!pairs) {
 #pragma unroll
                         for (int g = 0; g < 4; ++g) {
@@ -738,7 +749,7 @@ __global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, Work wk, int
 }
 
 // The rows' gradients: three walks of a segment by three workgroups that follow one another.  At D = 128 a wavefront has all rows of its columns, and two workgroups of four share a
-// CU: 8 x 4680 tokens of 12 heads take 428 us in three times 15 blocks, 9.5 us for two workgroups' blocks; vector instructions take 46 % of the SIMDs' issue (half of them
+// CU: 8 x 4680 tokens of 12 heads take 420 us in three times 15 blocks, 9.3 us for two workgroups' blocks; vector instructions take 46 % of the SIMDs' issue (half of them
 // takes states and rows apart into bf16 parts), the matrix cores are busy for 30 % of the time, wavefronts wait for a third of it.
 template <int D, int HALVES>
 __global__ __launch_bounds__((Cfg<D, HALVES>::NT), D == 64 ? 3 : 2) void scan_grad_kernel(ScanArgs a, Work wk)
