@@ -749,8 +749,8 @@ __global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, Work wk, int
 }
 
 // The rows' gradients: three walks of a segment by three workgroups that follow one another.  At D = 128 a wavefront has all rows of its columns, and two workgroups of four share a
-// CU: 8 x 4680 tokens of 12 heads take 420 us in three times 15 blocks, 9.3 us for two workgroups' blocks; vector instructions take 46 % of the SIMDs' issue (half of them
-// takes states and rows apart into bf16 parts), the matrix cores are busy for 30 % of the time, wavefronts wait for a third of it.
+// CU: 8 x 4680 tokens of 12 heads take 409 us in three times 15 blocks, 9.1 us for two workgroups' blocks; vector instructions take 51 % of the SIMDs' issue (half of them
+// takes states and rows apart into bf16 parts), the matrix cores are busy for 33 % of the time, wavefronts wait for a third of it.
 template <int D, int HALVES>
 __global__ __launch_bounds__((Cfg<D, HALVES>::NT), D == 64 ? 3 : 2) void scan_grad_kernel(ScanArgs a, Work wk)
 {
@@ -936,8 +936,9 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Segments: enough workgroups for the chip, no more states than that takes.  Time is counted in hundredths of a block of a full chip, which has `per_cu` workgroups
 // on a CU (one alone takes 70 and 60 hundredths of two's and three's); a second part of the sequence costs the sums of the segments (a block half of one), what joins them,
-// by segment, and two launches.  12 heads x 128: 1560 tokens in 7, 9, 13 (taken), 25 segments 32.1, 28.3, 25.4, 33.4 us; 32760 in 15, 21 (taken), 32, 42: 214,
-// 172, 198, 181 us; gradients of 1560 in 3, 7, 13 (taken), 25: 87, 54.3, 53.0, 65 us; of 8 x 4680 in 5 (taken), 6, 8, 10: 549, 579, 593, 606 us.
+// by segment, and two launches.  12 heads x 128: 1560 tokens in 7, 9, 13 (taken), 25 segments 32.0, 28.1, 25.3, 32.8 us; 32760 in 15, 21 (taken), 32, 42: 216,
+// 174, 201, 182 us; gradients of 1560 in 3, 7, 13 (taken), 25: 86, 53, 48.4, 65 us; of 8 x 4680 in 5 (taken), 6, 8, 10: 537, 580, 590, 604 us; 24 heads x 64: 5 x 2999 in
+// 4, 6 (taken), 8: 74, 63, 70 us; gradients of 5 x 999 in 1 (taken), 2, 4: 68.7, 70.3, 74.0 us.
 ScanPlan scan_plan(int B, int H, int L, int D, bool backward)
 {
     ScanPlan p = {};
