@@ -296,31 +296,46 @@ struct Walk {
             base = fold ? 0.0 : end;
             seg_total += tot;
         };
-        // rows of one array to LDS; `kind` 1: its norms go with the rows that ask, 2: with those that make the state
-        auto stage = [&](const u32x4 *g, unsigned char *to, int kind, int buf) {
+        // rows of one array to LDS
+        auto stage = [&](const u32x4 *g, unsigned char *to) {
 #pragma unroll
             for (int i = 0; i < ROUNDS; ++i) {
                 const int row = ROUND * i + tid / C::LPR;
                 *reinterpret_cast<u32x4 *>(to + row * C::ROW + (tid % C::LPR ^ C::swizzle(row)) * 16) = g[i];
-                if (kind) {
-                    float x = 0.f;
+            }
+        };
+        // norms of the rows that make the state and of those that ask, times their decays: lane r of a row's lanes finishes round r's
+        auto norms = [&](const u32x4 *make, const u32x4 *ask, int buf) {
+            const int r = tid % C::LPR;
+            float mine = 0.f;
+            auto squares = [&](const u32x4 *g, int first) {
+                float x[ROUNDS];
+#pragma unroll
+                for (int i = 0; i < ROUNDS; ++i) {
+                    x[i] = 0.f;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float x0 = __uint_as_float(g[i][j] << 16), x1 = __uint_as_float(g[i][j] & 0xffff0000u);
-                        x = fmaf(x0, x0, fmaf(x1, x1, x));
-                    }
-                    x = lane_group_sum<C::LPR>(x);
-                    x = a.normalise ? fast_rsqrt(x + a.eps) : 1.f;
-                    if (tid % C::LPR == 0) {
-                        if (kind == 1) sc.post[row] = sc.pairs[buf] ? x : x * sc.row[buf][row];
-                        else {
-                            sc.pcol[row] = x * sc.col[buf][row];
-                            sc.penter[row] = x * sc.enter[buf][row];
-                            sc.norm[row] = x;
-                        }
+                        x[i] = fmaf(x0, x0, fmaf(x1, x1, x[i]));
                     }
                 }
+#pragma unroll
+                for (int i = 0; i < ROUNDS; ++i) {
+                    x[i] = lane_group_sum<C::LPR>(x[i]);
+                    mine = r == first + i ? x[i] : mine;
+                }
+            };
+            if (a.normalise) {
+                squares(make, 0);
+                if (!GRAD && ROWS) squares(ask, ROUNDS);
             }
+            const float x = a.normalise ? fast_rsqrt(mine + a.eps) : 1.f;
+            const int row = ROUND * (r & (ROUNDS - 1)) + tid / C::LPR;
+            if (r < ROUNDS) {
+                sc.pcol[row] = x * sc.col[buf][row];
+                sc.penter[row] = x * sc.enter[buf][row];
+                sc.norm[row] = x;
+            } else if (!GRAD && ROWS && r < 2 * ROUNDS) sc.post[row] = sc.pairs[buf] ? x : x * sc.row[buf][row];
         };
 
         const int count = blk1 - blk0;
@@ -359,9 +374,10 @@ struct Walk {
             // Of the workgroups on a CU the one that is furthest in its block goes first: they are then not all at the same step.  With one priority gradients of 5 x 999
             // tokens of 24 heads x 64 took 76.5 us, so 71.4, of 8 x 4680 tokens of 12 heads x 128 547 and 535.
             __builtin_amdgcn_s_setprio(1);
-            if (ROWS) stage(gx, lx, GRAD ? 0 : 1, buf);
-            stage(gy, ly, GRAD ? 0 : 2, buf);
-            stage(gz, lz, GRAD ? 2 : 0, buf);
+            norms(GRAD ? gz : gy, gx, buf);
+            if (ROWS) stage(gx, lx);
+            stage(gy, ly);
+            stage(gz, lz);
             if (i + 1 < count) fetch(block_at(i + 1));
             const bool pairs = __builtin_amdgcn_readfirstlane(sc.pairs[buf]) != 0;
             lds_barrier();
