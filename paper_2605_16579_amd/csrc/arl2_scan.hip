@@ -306,7 +306,8 @@ struct Walk {
         };
         // norms of the rows that make the state and of those that ask, times their decays: lane r of a row's lanes finishes round r's
         auto norms = [&](const u32x4 *make, const u32x4 *ask, int buf) {
-            const int r = tid % C::LPR;
+            int r = tid % C::LPR;
+            if (ROWS && MODE != kOut) asm volatile("" : "+v"(r));  // (masks anew: the gradients' walks have no scalar registers left to keep them in)
             float mine = 0.f;
             auto squares = [&](const u32x4 *g, int first) {
                 float x[ROUNDS];
