@@ -436,9 +436,17 @@ struct Walk {
                     }
                     return p;
                 };
-                // ---- X.Y as rows of X in LDS
+                // ---- X.Y as rows of X in LDS, and from them G: products of k and q times those of dout, which lies in Z's place, and v
                 if (wave < 3) {
                     const int t = wave, sb = y_of(t), tb = x_of(t);
+                    constexpr int PIECES = MODE == kDv ? D / 16 : 1;
+                    const bool pairs_too = MODE == kDv && a.dla != nullptr;
+                    bf16x8 vf[PIECES];
+                    if (pairs_too) {
+                        const uint32_t row = (uint32_t)(blk * kBlock + 32 * tb + l32) * rs + (h * D + 8 * hh) * 2;
+#pragma unroll
+                        for (int m = 0; m < PIECES; ++m) vf[m] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rv, row + 32 * m, 0, 0));
+                    }
                     f32x16 p = products(t);
                     if (sb == tb) {
 #pragma unroll
@@ -453,33 +461,23 @@ struct Walk {
                         const bf16x4 r = {to_bf16(p[4 * g]), to_bf16(p[4 * g + 1]), to_bf16(p[4 * g + 2]), to_bf16(p[4 * g + 3])};
                         *reinterpret_cast<bf16x4 *>(to + 16 * ((4 * sb + g) ^ C::swizzle64(l32))) = r;
                     }
-                }
-                // ---- G: products of k and q times those of dout, which lies in Z's place, and v; by the last wavefronts
-                if (MODE == kDv && a.dla != nullptr && wave >= C::NW - 3) {
-                    const int t = C::NW - 1 - wave, sb = y_of(t), tb = x_of(t);
-                    const uint32_t row = (uint32_t)(blk * kBlock + 32 * tb + l32) * rs + (h * D + 8 * hh) * 2;
-                    bf16x8 vf[4];                                 // (four pieces at a time: the registers are taken)
-                    f32x16 w = {}, p;
+                    if (pairs_too) {
+                        f32x16 w = {};
 #pragma unroll
-                    for (int m0 = 0; m0 < D / 16; m0 += 4) {
+                        for (int m = 0; m < PIECES; ++m) w = mfma(by_rows(lz, sb, m), vf[m], w);
+                        const float post = sc.post[32 * tb + l32];
+                        float v[16], sum = 0.f;
 #pragma unroll
-                        for (int m = 0; m < 4; ++m) vf[m] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rv, row + 32 * (m0 + m), 0, 0));
-                        if (m0 == 0) p = products(t);
-#pragma unroll
-                        for (int m = 0; m < 4; ++m) w = mfma(by_rows(lz, sb, m0 + m), vf[m], w);
+                        for (int j = 0; j < 16; ++j) {
+                            const bool strictly = sb != tb || 8 * (j / 4) + j % 4 + diagonal > 0;
+                            v[j] = strictly ? p[j] * post * w[j] : 0.f;   // (in this order: p has a decay taken out)
+                            sum += v[j];
+                        }
+                        sum = halves_sum(sum);
+                        if (hh == 0) sc.pair.earlier[t][l32] = sum;
+                        const float of = lanes_sums(v, lane);
+                        if ((lane & 16) == 0) sc.pair.later[t][8 * ((lane & 15) / 4) + 4 * hh + lane % 4] = of;
                     }
-                    const float post = sc.post[32 * tb + l32];
-                    float v[16], sum = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        const bool strictly = sb != tb || 8 * (j / 4) + j % 4 + diagonal > 0;
-                        v[j] = strictly ? p[j] * post * w[j] : 0.f;       // (in this order: p has a decay taken out)
-                        sum += v[j];
-                    }
-                    sum = halves_sum(sum);
-                    if (hh == 0) sc.pair.earlier[t][l32] = sum;
-                    const float of = lanes_sums(v, lane);
-                    if ((lane & 16) == 0) sc.pair.later[t][8 * ((lane & 15) / 4) + 4 * hh + lane % 4] = of;
                 }
                 // ---- rows asked of the wavefront's part of the state
 #pragma unroll
