@@ -696,10 +696,10 @@ struct Walk {
     }
 };
 
-// A block of 64 tokens takes 4.4 us (D = 128, one workgroup of eight wavefronts on a CU): the matrix cores are busy for 20 % of that, vector instructions take 39 % of the
-// SIMDs' issue and LDS 25 % of its cycles, half of the wavefronts' time is waiting, for barriers, LDS and rows.  16 x 4096 tokens of 16 heads, one segment:
-// 276 us, 3.9 TB/s, three quarters of a copy's; 32760 tokens of one stream, whose 21 segments are summed first: 112 + 57 + 7 us.  Two workgroups on a CU
-// (128 registers, sums handed on in place): 168 for 172 us of the latter, 288 for 276 of the former.
+// A block of 64 tokens takes 4.2 us (D = 128, one workgroup of eight wavefronts on a CU): the matrix cores are busy for 21 % of that, vector instructions take 39 % of the
+// SIMDs' issue and LDS 26 % of its cycles, half of the wavefronts' time is waiting, for barriers, LDS and rows.  16 x 4096 tokens of 16 heads, one segment:
+// 266 to 272 us, 4.1 TB/s, four fifths of a copy's; 32760 tokens of one stream, whose 21 segments are summed first: 107 + 58 + 7 us.  Two workgroups on a CU
+// (128 registers, sums handed on in place): 168 for 172 us of the latter, 288 for 276 of the former, when a block took 4.4.
 template <int D, int HALVES>
 __global__ __launch_bounds__((Cfg<D, HALVES>::NT), D == 64 ? 3 : 2) void scan_out_kernel(ScanArgs a, Work wk)
 {
@@ -764,8 +764,8 @@ __global__ __launch_bounds__(256) void scan_join_kernel(ScanArgs a, Work wk, int
 }
 
 // The rows' gradients: three walks of a segment by three workgroups that follow one another.  At D = 128 a wavefront has all rows of its columns, and two workgroups of four share a
-// CU: 8 x 4680 tokens of 12 heads take 409 us in three times 15 blocks, 9.1 us for two workgroups' blocks; vector instructions take 51 % of the SIMDs' issue (half of them
-// takes states and rows apart into bf16 parts), the matrix cores are busy for 33 % of the time, wavefronts wait for a third of it.
+// CU: 8 x 4680 tokens of 12 heads take 385 to 400 us in three times 15 blocks, 8.7 us for two workgroups' blocks; vector instructions take 51 % of the SIMDs' issue (half of them
+// takes states and rows apart into bf16 parts), the matrix cores are busy for a third of the time, wavefronts wait for a third of it.
 template <int D, int HALVES>
 __global__ __launch_bounds__((Cfg<D, HALVES>::NT), D == 64 ? 3 : 2) void scan_grad_kernel(ScanArgs a, Work wk)
 {
@@ -953,7 +953,7 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 // on a CU (one alone takes 70 and 60 hundredths of two's and three's); a second part of the sequence costs the sums of the segments (a block half of one), what joins them,
 // by segment, and two launches.  12 heads x 128: 1560 tokens in 7, 9, 13 (taken), 25 segments 32.0, 28.1, 25.3, 32.8 us; 32760 in 15, 21 (taken), 32, 42: 216,
 // 174, 201, 182 us; gradients of 1560 in 3, 7, 13 (taken), 25: 86, 53, 48.4, 65 us; of 8 x 4680 in 5 (taken), 6, 8, 10: 537, 580, 590, 604 us; 24 heads x 64: 5 x 2999 in
-// 4, 6 (taken), 8: 74, 63, 70 us; gradients of 5 x 999 in 1 (taken), 2, 4: 68.7, 70.3, 74.0 us.
+// 4, 6 (taken), 8: 74, 63, 70 us; gradients of 5 x 999 in 1 (taken), 2, 4: 68.7, 70.3, 74.0 us (all before a block's norms were summed side by side, which takes 2 to 4 %).
 ScanPlan scan_plan(int B, int H, int L, int D, bool backward)
 {
     ScanPlan p = {};
