@@ -167,9 +167,8 @@ __device__ __forceinline__ void turns_of(const RopeArgs &a, uint32_t first, uint
     const int half = a.D / 2;
     for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
         const int pair = i & (half - 1), t = i / half;
-        if (first + t >= all) break;
-        float c = 1.f, s = 0.f;
-        if (pair < a.pairs) {
+        float c = 1.f, s = 0.f;                                   // (also behind the last token: a weight's gradient takes zeros times these)
+        if (pair < a.pairs && first + t < all) {
             const size_t at = a.pos_per_stream ? first + t : (first + t) % (uint32_t)a.L;
             const double turn = (double)a.pos[at * a.axes + a.axis[pair]] * a.turns[pair];
             sincospif(2.f * (float)(turn - ::rint(turn)), &s, &c);

@@ -302,6 +302,19 @@ def test_without_norm_the_rows_are_not_needed(A):
     both(A, only)
 
 
+@pytest.mark.parametrize("norm", ["head", "row"])
+def test_missing_rows_add_nothing_to_a_weights_gradient(A, norm):
+    """The last workgroup has room for tokens that there are not, in memory that a call before left NaNs in."""
+    bad = torch.full((64, 200, 12, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    out, ws = torch.empty_like(bad), A.alloc_scan_workspace(64, 12, 200, 128)
+    for B, H, Hk, L in ((1, 2, 1, 1), (1, 2, 1, 17), (3, 4, 2, 5), (1, 8, 8, 77)):
+        c = Case(B, H, Hk, L, 64, norm=norm)
+        A.arl2_scan_fwd(bad, bad, bad, None, None, out, None, workspace=ws)
+        _, dw = run_backward(A, c)
+        for name, gw, (_, _, ww, lw) in zip("qk", dw, c.backward()):
+            check("dw" + name, gw, ww, lw)
+
+
 def test_lengths_are_cut(A):
     c = Case(3, 3, 2, 30, 64, norm="row", lens=[0, 30, 30])
     given = torch.tensor([-7, 31, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
