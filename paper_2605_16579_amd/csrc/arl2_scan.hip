@@ -166,7 +166,7 @@ struct Walk {
     // result; of what enters: two, the state is off by 2.4e-6 in the 2-norm.  Three of either where sums with q and k are parts of E, whose errors add up over a segment:
     // with two, heads with gates of 0.8 had E off by 9.1e-6, with three by 1.0e-6 (with three of one and two of the other 6e-6).
     static constexpr int ASKED = GRAD ? 3 : 1, ENTER = GRAD ? 3 : 2;
-    static constexpr int GROUP = HALVES == 1 ? 2 : 4;             // of D / 16 products of rows: operands requested together
+    static constexpr int GROUP = 4;                               // of D / 16 products of rows: operands requested together
     static constexpr int ROUND = C::NT / C::LPR, ROUNDS = kBlock / ROUND;    // rows that the threads stage at a time
     // Sums for the other half lie where X and Z were at D = 64, whose workgroups have to leave room for others.
     static constexpr bool HANDS_ON = ROWS && HALVES == 2, IN_PLACE = D == 64;
@@ -549,6 +549,9 @@ struct Walk {
             {
 #pragma unroll
                 for (int m = 0; m < 4; ++m) {
+                    constexpr bool FIRST = GRAD && HALVES == 2;   // requested before the split, where registers are left and it is long
+                    bf16x8 y0;
+                    if (FIRST) y0 = by_columns(ly, y_at, C::TPW * half, m);
                     const f32x4 w0 = *reinterpret_cast<const f32x4 *>(&sc.penter[16 * m + 8 * hh]), w1 = *reinterpret_cast<const f32x4 *>(&sc.penter[16 * m + 8 * hh + 4]);
                     const u32x4 zb = __builtin_bit_cast(u32x4, zf[m]);
                     u32x4 part[ENTER];
@@ -561,7 +564,7 @@ struct Walk {
                     }
 #pragma unroll
                     for (int t = 0; t < C::TPW; ++t) {
-                        const bf16x8 yf = by_columns(ly, y_at, C::TPW * half + t, m);
+                        const bf16x8 yf = FIRST && t == 0 ? y0 : by_columns(ly, y_at, C::TPW * half + t, m);
 #pragma unroll
                         for (int k = 0; k < ENTER; ++k) st[t] = mfma(yf, __builtin_bit_cast(bf16x8, part[k]), st[t]);
                     }
