@@ -200,6 +200,21 @@ def test_repeats_bit_for_bit_and_streams(A):
     assert all(torch.equal(x, y) for x, y in zip(first, third))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,H,L,lens", [(1, 2, 9, None), (2, 3, 65, [65, 1]), (3, 2, 130, [0, 130, 70]), (2, 12, 1560, [1560, 33])])
+def test_what_a_call_before_left_in_fast_memory(A, D, B, H, L, lens):
+    """Results behind calls on rows of NaNs are the same bits."""
+    bad = torch.full((64, 200, 12, 128), float("nan"), dtype=torch.bfloat16, device="cuda")
+    out, ws = torch.empty_like(bad), A.alloc_scan_workspace(64, 12, 200, 128)
+    c = R.Case(B, H, L, D, seed=L, lens=lens)
+    first = (*R.run_forward(A, c), *R.run_backward(A, c))
+    A.arl2_scan_fwd(bad, bad, bad, None, None, out, None, workspace=ws)
+    second = R.run_forward(A, c)
+    A.arl2_scan_fwd(bad, bad, bad, None, None, out, None, workspace=ws)
+    for x, y in zip(first, (*second, *R.run_backward(A, c))):
+        assert torch.equal(x, y)
+
+
 def test_captured_and_replayed(A):
     """A step of training and single tokens in one graph, replayed on new inputs beside eager work."""
     c = R.Case(2, 2, 300, 64, seed=15)
