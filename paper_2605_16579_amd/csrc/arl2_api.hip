@@ -774,7 +774,7 @@ arl2_status arl2_scan_bwd(const arl2_scan_desc *desc, const void *q, const void 
 // ---- rotary positions ---------------------------------------------------------------------------------
 size_t arl2_rope_workspace_bytes(const arl2_rope_desc *desc)
 {
-    return check_rope_desc(desc) == ARL2_OK ? arl2::rope_workspace_bytes(desc->B, desc->L, desc->D, desc->H + desc->Hk) : 0;
+    return check_rope_desc(desc) == ARL2_OK ? arl2::rope_parts_bytes(desc->B, desc->L, desc->D, desc->H, desc->Hk) : 0;
 }
 
 arl2_status arl2_rope_fwd(const arl2_rope_desc *desc, const void *q, const void *k, const void *wq, const void *wk,

@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "arl2_rope_plan.h"
+
 namespace arl2 {
 
 enum { kNormNone = 0, kNormHead = 1, kNormRow = 2 };
@@ -24,9 +26,6 @@ struct RopeArgs {
     uint8_t axis[64];            // of each pair
     double turns[64];            // of each pair for one step of its position
 };
-
-size_t rope_workspace_bytes(int B, int L, int D, int heads);
-constexpr int kRopeMostUnits = 1536;                             // of 16 features, queries and keys of a token together
 
 hipError_t launch_rope(const RopeArgs &a, hipStream_t stream);
 hipError_t launch_rope_bwd(const RopeArgs &a, hipStream_t stream);

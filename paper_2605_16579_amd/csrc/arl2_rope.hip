@@ -22,11 +22,9 @@
 namespace arl2 {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kRopeThreads;
 constexpr int kMostWorkgroups = 1 << 20;         // (a launch has room for 2^32 threads)
-// Wavefronts on a SIMD that the gradients' registers leave room for, and workgroups on a CU: with more, weights' gradients come in more parts.  One unit, 4680 tokens
-// as above: 3, 4, 5 wavefronts 38.6, 36.0, 37.2 us (the last with registers in scratch); two units, 32 + 8 heads: 3, 4 wavefronts 57.8, 54.5 us.
-constexpr int bwd_waves(int nu, bool f32) { return nu == 1 || (nu == 2 && !f32) ? 4 : 2; }
+static_assert(kRopeChip == kNumCu, "the plan counts this chip's CUs");
 
 template <class T> struct Raw;                    // 8 features as they lie in memory
 template <> struct Raw<bf16_t> { u32x4 v; };
@@ -282,7 +280,7 @@ __host__ __device__ constexpr int part_groups(bool by_heads, int lpt) { return !
 // A weight's gradient is summed over all of a workgroup's tokens by the lanes that have its feature, joined among them at the end and written
 // as this workgroup's part.
 template <class T, int NORM, bool HALVES, int NU>
-__global__ __launch_bounds__(kThreads, bwd_waves(NU, std::is_same<T, float>::value)) void rope_bwd_kernel(RopeArgs a, int lpt)
+__global__ __launch_bounds__(kThreads, rope_bwd_waves(NU, std::is_same<T, float>::value)) void rope_bwd_kernel(RopeArgs a, int lpt)
 {
     extern __shared__ __align__(16) f32x2 turns[][64];
     __shared__ float red[2][4][4];
@@ -411,8 +409,8 @@ __global__ __launch_bounds__(kThreads, bwd_waves(NU, std::is_same<T, float>::val
         }
     }
     if (NORM == kNormNone || (a.dw[0] == nullptr && a.dw[1] == nullptr)) return;
-    // this workgroup's part: [D] and [D], or [heads D] and [heads D]
-    const int width0 = NORM == kNormHead ? a.D : a.heads[0] * a.D, width = width0 + (NORM == kNormHead ? a.D : a.heads[1] * a.D);
+    // this workgroup's part: [D] and, where there are keys, [D], or [heads D] and [heads D]
+    const int width0 = rope_part_queries(NORM == kNormHead, a.D, a.heads[0]), width = rope_part(NORM == kNormHead, a.D, a.heads[0], a.heads[1]);
     float *const to = a.part + (size_t)blockIdx.x * width;
     if (NORM == kNormRow && m.lpt == kThreads) {                  // each of its elements is one lane's
 #pragma unroll
@@ -438,6 +436,7 @@ __global__ __launch_bounds__(kThreads, bwd_waves(NU, std::is_same<T, float>::val
     if constexpr (NORM == kNormHead) {
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
+            if (k == 1 && width == width0) break;                 // there are no keys, and no room for them
             float sum[16] = {};
 #pragma unroll
             for (int u = 0; u < NU; ++u)
@@ -480,18 +479,8 @@ __global__ __launch_bounds__(1024) void rope_dw_kernel(RopeArgs a, int parts, in
     if (to != nullptr && c == 0) to[col < width0 ? col : col - width0] = s;
 }
 
-// How tokens are dealt: lanes to a token, units to a lane, tokens of a lane at a time.
-struct Shape { int lpt, nu, tok; };
-Shape shape_of(int units, bool f32, bool bwd)
-{
-    int lpt = 16;                                                 // (fewer would want more LDS for the turns of more tokens)
-    while (lpt < units && lpt < kThreads) lpt <<= 1;
-    const int nu = units <= kThreads ? 1 : units <= 2 * kThreads ? 2 : units <= 3 * kThreads ? 3 : 6;
-    return {lpt, nu, bwd || nu > 2 || (nu == 2 && f32) ? 1 : 2};
-}
-
 template <class T, int NORM, bool HALVES, bool BWD>
-hipError_t launch_shape(const RopeArgs &a, const Shape &s, dim3 grid, unsigned lds, hipStream_t stream)
+hipError_t launch_shape(const RopeArgs &a, const RopeShape &s, dim3 grid, unsigned lds, hipStream_t stream)
 {
     constexpr bool f32 = std::is_same<T, float>::value;
 #define ARL2_ROPE(NU, TOK) launch_kernel_lds(BWD ? rope_bwd_kernel<T, NORM, HALVES, NU> : rope_kernel<T, NORM, HALVES, NU, TOK>, grid, dim3(kThreads), lds, stream, a, s.lpt)
@@ -499,7 +488,7 @@ hipError_t launch_shape(const RopeArgs &a, const Shape &s, dim3 grid, unsigned l
 #undef ARL2_ROPE
 }
 template <class T, bool BWD>
-hipError_t launch_norm(const RopeArgs &a, const Shape &s, dim3 grid, unsigned lds, hipStream_t stream)
+hipError_t launch_norm(const RopeArgs &a, const RopeShape &s, dim3 grid, unsigned lds, hipStream_t stream)
 {
     if (a.halves)
         return a.norm == kNormNone ? launch_shape<T, kNormNone, true, BWD>(a, s, grid, lds, stream)
@@ -508,46 +497,34 @@ hipError_t launch_norm(const RopeArgs &a, const Shape &s, dim3 grid, unsigned ld
          : a.norm == kNormHead ? launch_shape<T, kNormHead, false, BWD>(a, s, grid, lds, stream) : launch_shape<T, kNormRow, false, BWD>(a, s, grid, lds, stream);
 }
 template <bool BWD>
-hipError_t launch_any(const RopeArgs &a, const Shape &s, int grid, hipStream_t stream)
+hipError_t launch_any(const RopeArgs &a, const RopeShape &s, int grid, hipStream_t stream)
 {
-    // the turns of two rounds; at the end the weights' gradients of a workgroup's groups: 2 D each, or (several tokens side by side) 16 KB together at most
-    const int width = part_groups(a.norm == kNormHead, s.lpt) * (a.norm == kNormHead ? 2 * a.D : s.lpt < kThreads ? (a.heads[0] + a.heads[1]) * a.D : 0);
+    // the turns of two rounds; at the end the weights' gradients of a workgroup's groups: a part each, or (several tokens side by side) 16 KB together at most
+    const bool by_heads = a.norm == kNormHead;
+    const int width = by_heads || s.lpt < kThreads ? part_groups(by_heads, s.lpt) * rope_part(by_heads, a.D, a.heads[0], a.heads[1]) : 0;
     const unsigned lds = (unsigned)std::max<size_t>(2 * (kThreads / s.lpt) * s.tok * 64 * sizeof(f32x2), BWD ? width * sizeof(float) : 0);
     return a.f32 ? launch_norm<float, BWD>(a, s, dim3(grid), lds, stream) : launch_norm<bf16_t, BWD>(a, s, dim3(grid), lds, stream);
 }
 
-int workgroups(int B, int L, const Shape &s, int most)
-{
-    const long long at_a_time = (long long)(kThreads / s.lpt) * s.tok, n = ((long long)B * L + at_a_time - 1) / at_a_time;
-    const long long rounds = (n + most - 1) / most;
-    return (int)((n + rounds - 1) / rounds);                      // (as many tokens for each as can be)
-}
-
 }  // namespace
-
-size_t rope_workspace_bytes(int B, int L, int D, int heads)
-{
-    const Shape s = shape_of(heads * (D / 16), false, true);      // (bf16 rows have the more workgroups)
-    const size_t n = (size_t)workgroups(B, L, s, bwd_waves(s.nu, false) * kNumCu);
-    return (n * heads * D * sizeof(float) + 255) & ~(size_t)255;
-}
 
 hipError_t launch_rope(const RopeArgs &a, hipStream_t stream)
 {
-    const Shape s = shape_of((a.heads[0] + a.heads[1]) * (a.D / 16), a.f32, false);
+    const RopeShape s = rope_shape((a.heads[0] + a.heads[1]) * (a.D / 16), a.f32, false);
     // Without weights to load a workgroup takes one round of tokens (up to 2^20 of them); else 4 x 10920 tokens of 32 + 8 heads x 128 (two units a lane) took 196, 209, 221 us
     // with at most 1024, 4096 and any number of workgroups, 7 x 4680 tokens of 12 + 12 heads (one unit) 101, 90, 97 us.
     const int most = a.norm == kNormNone ? kMostWorkgroups : s.nu == 1 ? 4096 : 1024;
-    return launch_any<false>(a, s, workgroups(a.B, a.L, s, most), stream);
+    return launch_any<false>(a, s, rope_workgroups(a.B, a.L, s, most), stream);
 }
 
 hipError_t launch_rope_bwd(const RopeArgs &a, hipStream_t stream)
 {
-    const Shape s = shape_of((a.heads[0] + a.heads[1]) * (a.D / 16), a.f32, true);
-    const int n = workgroups(a.B, a.L, s, a.norm == kNormNone ? kMostWorkgroups : bwd_waves(s.nu, a.f32) * kNumCu);
+    const RopeShape s = rope_shape((a.heads[0] + a.heads[1]) * (a.D / 16), a.f32, true);
+    const int n = a.norm == kNormNone ? rope_workgroups(a.B, a.L, s, kMostWorkgroups) : rope_bwd_workgroups(a.B, a.L, s, a.f32);
     const hipError_t e = launch_any<true>(a, s, n, stream);
     if (e != hipSuccess || a.norm == kNormNone || (a.dw[0] == nullptr && a.dw[1] == nullptr)) return e;
-    const int width0 = a.norm == kNormHead ? a.D : a.heads[0] * a.D, width = a.norm == kNormHead ? 2 * a.D : (a.heads[0] + a.heads[1]) * a.D;
+    const bool by_heads = a.norm == kNormHead;
+    const int width0 = rope_part_queries(by_heads, a.D, a.heads[0]), width = rope_part(by_heads, a.D, a.heads[0], a.heads[1]);
     return launch_kernel(rope_dw_kernel, dim3(width / 32), dim3(1024), stream, a, n, width0, width);
 }
 
