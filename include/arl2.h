@@ -368,7 +368,7 @@ arl2_status arl2_kv_attn_fwd(const arl2_kv_desc *desc, const void *q, const void
 typedef struct {
     int32_t B, H, L, D;   /* streams, heads, tokens: >= 1; D: 64 or 128.  L*H*D must stay below 2^30                    */
     int32_t raw_rows;     /* 0: rows of q and k are divided by sqrt(|row|^2 + l2_eps); 1: they are taken as they are   */
-    float l2_eps;         /* 0 selects 1e-6                                                                            */
+    float l2_eps;         /* >= 1e-30; 0 selects 1e-6                                                                  */
     void *workspace;      /* device scratch, >= arl2_scan_workspace_bytes or arl2_scan_bwd_workspace_bytes, 16-byte     */
     size_t workspace_bytes;  /* aligned; one for each call in flight                                                   */
     void *stream;         /* hipStream_t; NULL is the default stream                                                   */
@@ -405,7 +405,8 @@ arl2_status arl2_scan_fwd(const arl2_scan_desc *desc, const void *q, const void 
  *   dq, dk, dv  device bf16 [B][L][H][D], written (through the normalisation where there is one).
  *   dlog_alpha  device fp32 [B][L][H], written: the gradient of log_alpha as if it had no upper limit; zero at a gate of zero.  NULL: it is not wanted.
  *   dS0       device fp32 [B][H][D][D], written; NULL: it is not wanted.
- * The same ranges hold for features of dout and for the state's gradient.
+ * The same ranges hold for features of dout and for the state's gradient.  Where l2_eps is below 1e-14, products dout.v have to be below 2^63 sqrt(l2_eps) too, and the
+ * gradients of normalised rows, before the normalisation, below 2^127 l2_eps.
  * Of what the matrix cores take, dv and dS0 are rounded as out and S are; dq and dk, whose products with q' and k' add up to dlog_alpha over up to 1024
  * tokens, take the states and what enters them in three bf16 parts (to 2^-25; dlog_alpha is off by 4.3e-6 in the 2-norm at most where it was looked at).
  * What is written must overlap neither an input nor what else is written.  Deterministic.
@@ -432,8 +433,8 @@ typedef struct {
     int32_t pos_per_stream;  /* pos is 0: [L][n_axes], 1: [B][L][n_axes]                                              */
     int32_t n_axes;       /* 1 to 4                                                                                  */
     int32_t axis_pairs[4];   /* each >= 1, together <= D / 2                                                          */
-    double theta[4];      /* > 0; 0 selects 10000                                                                    */
-    float norm_eps;       /* 0 selects 1e-6                                                                          */
+    double theta[4];      /* 1e-3 to 1e30; 0 selects 10000                                                           */
+    float norm_eps;       /* >= 1e-30; 0 selects 1e-6                                                                */
     void *workspace;      /* arl2_rope_bwd with weights' gradients: >= arl2_rope_workspace_bytes, 16-byte aligned     */
     size_t workspace_bytes;
     void *stream;         /* hipStream_t; NULL is the default stream                                                 */

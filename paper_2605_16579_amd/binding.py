@@ -545,8 +545,14 @@ def arl2_kv_attn_fwd(q: torch.Tensor, cache: torch.Tensor, block_table: torch.Te
 
 # ---- the linear branch as a causal recurrence
 
+def _epsilon(eps: float) -> float:
+    if eps != 0 and ctypes.c_float(eps).value == 0:       # (it would select the default)
+        raise ValueError(f"epsilon {eps} is zero in single precision")
+    return eps
+
+
 def _scan_desc(B, H, L, D, normalise=True, l2_eps=0.0, workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> arl2_scan_desc:
-    return arl2_scan_desc(B, H, L, D, 0 if normalise else 1, l2_eps, _dev(workspace, "workspace"), 0 if workspace is None else workspace.nbytes,
+    return arl2_scan_desc(B, H, L, D, 0 if normalise else 1, _epsilon(l2_eps), _dev(workspace, "workspace"), 0 if workspace is None else workspace.nbytes,
                           _current_stream() if stream is None else stream)
 
 
@@ -621,7 +627,7 @@ def _rope_desc(B, H, L, D, Hk, io_dtype=ARL2_BF16, norm="none", halves=False, po
     if not 1 <= len(axis_pairs) <= 4 or len(theta) != len(axis_pairs):
         raise ValueError("axis_pairs must name 1 to 4 axes, and theta as many")
     return arl2_rope_desc(B, H, L, D, Hk, io_dtype, _NORMS[norm], 1 if halves else 0, 1 if pos_per_stream else 0, len(axis_pairs),
-                          (ctypes.c_int32 * 4)(*axis_pairs), (ctypes.c_double * 4)(*theta), norm_eps, _dev(workspace, "workspace"),
+                          (ctypes.c_int32 * 4)(*axis_pairs), (ctypes.c_double * 4)(*theta), _epsilon(norm_eps), _dev(workspace, "workspace"),
                           0 if workspace is None else workspace.nbytes, _current_stream() if stream is None else stream)
 
 

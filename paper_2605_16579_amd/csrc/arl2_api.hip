@@ -155,6 +155,11 @@ arl2::KvRowsArgs kv_rows_args(const arl2_kv_desc *d, const int32_t *table, const
     return a;
 }
 
+// Rows of zeros, those behind a sequence's end among them, are multiplied by 1 / sqrt(eps) and by decays of up to 2^64 that are taken out: with
+// smaller epsilons by an infinity.
+constexpr float kLeastEps = 1e-30f;
+bool epsilon_ok(float eps) { return eps == 0.f || eps >= kLeastEps; }
+
 // ---- the causal recurrence
 
 arl2_status check_scan_desc(const arl2_scan_desc *d)
@@ -163,7 +168,7 @@ arl2_status check_scan_desc(const arl2_scan_desc *d)
     if (d->B < 1 || d->H < 1 || d->L < 1) return fail(ARL2_ERR_INVALID_ARG, "B, H and L must all be >= 1");
     if (d->D != 64 && d->D != 128) return fail(ARL2_ERR_UNSUPPORTED, "D must be 64 or 128");
     if (d->raw_rows != 0 && d->raw_rows != 1) return fail(ARL2_ERR_INVALID_ARG, "raw_rows must be 0 or 1");
-    if (!(d->l2_eps >= 0.f)) return fail(ARL2_ERR_INVALID_ARG, "l2_eps must be >= 0 (0 selects the default)");
+    if (!epsilon_ok(d->l2_eps)) return fail(ARL2_ERR_INVALID_ARG, "l2_eps must be 0 (it selects the default) or >= 1e-30");
     // A stream's rows are addressed with 32-bit byte offsets, which may point 64 rows past the last.
     if ((double)d->L * d->H * d->D >= 1073741824.0 || 64.0 * d->H * d->D >= 1073741824.0)
         return fail(ARL2_ERR_UNSUPPORTED, "problem too large (L*H*D and 64*H*D must stay below 2^30)");
@@ -205,7 +210,7 @@ arl2_status check_rope_desc(const arl2_rope_desc *d)
         pairs += d->axis_pairs[a];
     }
     if (pairs > d->D / 2) return fail(ARL2_ERR_INVALID_ARG, "axis_pairs must be D / 2 at most together");
-    if (!(d->norm_eps >= 0.f)) return fail(ARL2_ERR_INVALID_ARG, "norm_eps must be >= 0 (0 selects the default)");
+    if (!epsilon_ok(d->norm_eps)) return fail(ARL2_ERR_INVALID_ARG, "norm_eps must be 0 (it selects the default) or >= 1e-30");
     if (((double)d->H + d->Hk) * (d->D / 16) > arl2::kRopeMostUnits) return fail(ARL2_ERR_UNSUPPORTED, "(H + Hk) * D must be 24576 at most");
     if ((double)d->B * d->L > 2.0e9) return fail(ARL2_ERR_UNSUPPORTED, "problem too large (B*L must stay below 2e9)");
     return ARL2_OK;

@@ -277,6 +277,7 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t nargs)
         PyErr_Clear();
         Py_RETURN_NONE;
     }
+    if ((scan || rope) && l2_eps != 0.0 && (float)l2_eps == 0.f) Py_RETURN_NONE;      // (it would select the default)
     Checked c;
     arl2_kv_desc kd{};
     arl2_scan_desc sd{};
