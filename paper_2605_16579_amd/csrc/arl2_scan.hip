@@ -28,6 +28,7 @@ namespace {
 constexpr int kBlock = 64;                    // tokens
 constexpr int kStepTokens = 8;
 constexpr double kLog2e = 1.4426950408889634;
+constexpr float kZeroGate = -2839.f;           // below: a gate of zero (2^-4095.8, of which fp32 has nothing left), from which the gates' gradients begin anew
 
 enum Mode { kOut, kDq, kDk, kDv, kSum, kSumBack };       // the last two make states and no rows
 
@@ -803,7 +804,7 @@ __global__ __launch_bounds__(256) void scan_gate_kernel(ScanArgs a, Work wk)
         const int t = last - i;
         const float *const p = wk.parts + (size_t)bh * a.L + t;
         v[i] = t < t1 ? (double)p[0] + p[rows] + p[2 * rows] : 0.0;
-        if (t < t1 && a.la[((size_t)b * a.L + t) * a.H + h] < -2839.2f) cut |= 1 << i;
+        if (t < t1 && a.la[((size_t)b * a.L + t) * a.H + h] < kZeroGate) cut |= 1 << i;
     }
     const double end = seg < nact - 1 || a.dS != nullptr ? wk.anchor[(size_t)bh * (wk.nseg + 1) + seg + 1] : 0.f;
     // sums within the thread, over the lanes before it, over the wavefronts before that
