@@ -293,7 +293,7 @@ hipError_t launch_gate_proj_bf16(const GateArgs &a, hipStream_t stream)
         // One workgroup per CU: 128 x 128 with deep stages (256 tiles of dm 2048: 25.1 us, with two stages 28.8).  Beyond,
         // the shape with the shorter sum of rounds, one of large tiles taking as long as about 1.5 of small ones
         // (measured 1.47 to 1.6): 564 small or 144 large tiles of dm 1536 47.9 and 46.5 us, 1764 or 444 128 and 106 us,
-        // 444 or 114 31.5 and 47.7 us; 1512 or 384 of rows twice as wide, where the rule is indifferent, 171 and 169 us.
+        // 444 or 114 31.5 and 47.7 us; 1512 or 384 of dm 2 * 1536, where the rule is indifferent, 171 and 169 us.
         const long long small = ((ntok + 127) / 128) * ((a.n_out + 127) / 128), big = ((ntok + 255) / 256) * ((a.n_out + 255) / 256);
         if (small <= kNumCu) return launch_gate_dense<128, 128, 256, 4>(a, ntok, stream);
         const long long small_rounds = (small + 2 * kNumCu - 1) / (2 * kNumCu), big_rounds = (big + kNumCu - 1) / kNumCu;
