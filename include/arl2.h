@@ -389,11 +389,12 @@ size_t arl2_scan_bwd_workspace_bytes(const arl2_scan_desc *desc);
  *   S         device fp32 [B][H][D][D], the state after the last token (S0 where there is none); NULL: it is not wanted.  May be S0 itself
  *             (the state is updated in place), else it must not overlap an input.
  * States, decays and sums are fp32 (a block's decays come from sums in fp64).  On the matrix cores rows enter the state as two bf16 parts (to
- * 2^-17 of each value: S is off by 2.4e-6 in the 2-norm), and out's rows take the state's features and the products q'.k' within a block of 64 tokens
+ * 2^-17 of each value: S is off by 2.5e-6 in the 2-norm), and out's rows take the state's features and the products q'.k' within a block of 64 tokens
  * rounded to bf16 once.
  * Features of rows have to be below 2^16, the state below 2^48 (products of three of them have decays taken out, up to 2^64, before fp32 holds them).
  * Up to 8 tokens are computed in fp32 throughout, with the state read and written once.  A NaN or an infinity in
- * a row reaches outputs of the 64 tokens, counted from the first, that it lies in and of later ones, not of earlier blocks.  Deterministic.
+ * a row reaches outputs of the 64 tokens, counted from the first, that it lies in and of later ones, not of earlier blocks; the state keeps it also behind a gate of
+ * zero, which multiplies by zero.  Deterministic.
  */
 arl2_status arl2_scan_fwd(const arl2_scan_desc *desc, const void *q, const void *k, const void *v, const float *log_alpha,
                           const int32_t *seq_len, const float *S0, void *out, float *S);
@@ -408,7 +409,9 @@ arl2_status arl2_scan_fwd(const arl2_scan_desc *desc, const void *q, const void 
  * The same ranges hold for features of dout and for the state's gradient.  Where l2_eps is below 1e-14, products dout.v have to be below 2^63 sqrt(l2_eps) too, and the
  * gradients of normalised rows, before the normalisation, below 2^127 l2_eps.
  * Of what the matrix cores take, dv and dS0 are rounded as out and S are; dq and dk, whose products with q' and k' add up to dlog_alpha over up to 1024
- * tokens, take the states and what enters them in three bf16 parts (to 2^-25; dlog_alpha is off by 4.3e-6 in the 2-norm at most where it was looked at).
+ * tokens, take the states and what enters them in three bf16 parts (to 2^-25; dlog_alpha is off by 5.5e-6 in the 2-norm at
+ * most where it was looked at, by 8.1e-6 in one head, and by 2.1e-5 in one whose gates leave next to nothing of the state).  A NaN or an infinity in a row
+ * reaches gradients of its own stream and head alone, of tokens on either side of it.
  * What is written must overlap neither an input nor what else is written.  Deterministic.
  */
 arl2_status arl2_scan_bwd(const arl2_scan_desc *desc, const void *q, const void *k, const void *v, const float *log_alpha,

@@ -577,7 +577,8 @@ def arl2_scan_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_alpha: 
                   l2_eps: float = 0.0, workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> None:
     """S_t = exp(log_alpha_t) S_{t-1} + k'_t^T v_t, out_t = q'_t S_t for the first seq_len[b] (None: all) tokens of q, k, v [B, L, H, D] bf16;
     k', q': L2-normalised, or (``normalise`` false) as they are.  log_alpha [B, L, H] fp32 (None: zeros); S0 (None: zeros) and S (None: not
-    wanted) [B, H, D, D] fp32, may be the same.  ``workspace``: of ``alloc_scan_workspace``, one for each call in flight."""
+    wanted) [B, H, D, D] fp32, may be the same.  ``workspace``: of ``alloc_scan_workspace``, one for each call in flight.  Autograd records nothing:
+    the gradients are ``arl2_scan_bwd``'s."""
     if _plain_call("arl2_scan_fwd", b"CqqqtnSqS", 0.0 if normalise else 1.0, l2_eps, stream, workspace, q, k, v, log_alpha, seq_len, S0, out, S):
         return
     if q.dim() != 4:
@@ -667,7 +668,7 @@ def arl2_rope_fwd(q: torch.Tensor, k: Optional[torch.Tensor], wq: Optional[torch
     """yq, yk (may be q, k) = the rows of q [B, L, H, D] and k [B, L, Hk, D] (or None) over their root mean square of a head's features ("head",
     weights [D]), of a token's row ("row", weights [H * D] and [Hk * D]) or as they are ("none"), times the weights (None: ones), rotated by
     pos [L, axes] or [B, L, axes] int32: ``axis_pairs`` pairs of features by each axis with frequencies theta^(-i / pairs) (None, 0: 10000);
-    pairs are neighbours, or (``halves``) features i and i + D / 2.  fp32 or bf16."""
+    pairs are neighbours, or (``halves``) features i and i + D / 2.  fp32 or bf16.  Autograd records nothing: the gradients are ``arl2_rope_bwd``'s."""
     if _plain_call("arl2_rope_fwd", _rope_kinds(norm, halves, b"qkwupnqk"), (axis_pairs, theta), norm_eps, stream, None, q, k, wq, wk, pos, seq_len, yq, yk):
         return
     d, like_q, like_k, _, _, (pwq, pwk, ppos, plen) = _rope_call(q, k, wq, wk, pos, seq_len, norm, axis_pairs,

@@ -164,7 +164,7 @@ struct Walk {
     static constexpr bool ROWS = MODE != kSum && MODE != kSumBack;
     static constexpr bool GRAD = MODE == kDq || MODE == kDk;      // rows through the normalisation
     // bf16 parts of the state that rows are asked of, and of the weighted rows that enter it.  Of the state: one, as the products of rows are rounded once and the
-    // result; of what enters: two, the state is off by 2.4e-6 in the 2-norm.  Three of either where sums with q and k are parts of E, whose errors add up over a segment:
+    // result; of what enters: two, the state is off by 2.5e-6 in the 2-norm.  Three of either where sums with q and k are parts of E, whose errors add up over a segment:
     // with two, heads with gates of 0.8 had E off by 9.1e-6, with three by 1.0e-6 (with three of one and two of the other 6e-6).
     static constexpr int ASKED = GRAD ? 3 : 1, ENTER = GRAD ? 3 : 2;
     static constexpr int GROUP = 4;                               // of D / 16 products of rows: operands requested together
@@ -916,33 +916,33 @@ Work work_of(const ScanArgs &a, const ScanPlan &p)
     return wk;
 }
 
-template <int D, int HALVES>
+template <int D>
 hipError_t launch_sums(const ScanArgs &a, const ScanPlan &p, const Work &wk, bool back, int first, hipStream_t stream)
 {
     if (p.nseg == 1) return hipSuccess;
     const int bh = a.B * a.H, ways = back ? 2 : 1;
-    const hipError_t e = launch_kernel(scan_sum_kernel<D, HALVES>, dim3(ways * bh * p.nseg), dim3(Cfg<D, HALVES>::NT), stream, a, wk, (int)back, first);
+    const hipError_t e = launch_kernel(scan_sum_kernel<D, 2>, dim3(ways * bh * p.nseg), dim3(Cfg<D, 2>::NT), stream, a, wk, (int)back, first);
     if (e != hipSuccess) return e;
     return launch_kernel(scan_join_kernel, dim3(ways * bh * (D * D / 1024)), dim3(256), stream, a, wk, first);
 }
 
-template <int D, int SUM_HALVES>
+template <int D>
 hipError_t launch_fwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
 {
     const int bh = a.B * a.H;
     if (p.step) return launch_kernel(scan_step_kernel<D>, dim3(bh * (D / 32)), dim3(256), stream, a);
     const Work wk = work_of(a, p);
-    const hipError_t e = launch_sums<D, SUM_HALVES>(a, p, wk, false, 0, stream);
+    const hipError_t e = launch_sums<D>(a, p, wk, false, 0, stream);
     if (e != hipSuccess) return e;
     return launch_kernel(scan_out_kernel<D, 2>, dim3(bh * p.nseg), dim3(Cfg<D, 2>::NT), stream, a, wk);
 }
 
-template <int D, int SUM_HALVES, int HALVES>
+template <int D, int HALVES>
 hipError_t launch_bwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
 {
     const int bh = a.B * a.H;
     const Work wk = work_of(a, p);
-    hipError_t e = launch_sums<D, SUM_HALVES>(a, p, wk, true, a.dS0 != nullptr, stream);
+    hipError_t e = launch_sums<D>(a, p, wk, true, a.dS0 != nullptr, stream);
     if (e != hipSuccess) return e;
     e = launch_kernel(scan_grad_kernel<D, HALVES>, dim3(3 * bh * p.nseg), dim3(Cfg<D, HALVES>::NT), stream, a, wk);
     if (e != hipSuccess || a.dla == nullptr) return e;
@@ -955,9 +955,10 @@ size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Segments: enough workgroups for the chip, no more states than that takes.  Time is counted in hundredths of a block of a full chip, which has `per_cu` workgroups
 // on a CU (one alone takes 70 and 60 hundredths of two's and three's); a second part of the sequence costs the sums of the segments (a block half of one), what joins them,
-// by segment, and two launches.  12 heads x 128: 1560 tokens in 7, 9, 13 (taken), 25 segments 32.0, 28.1, 25.3, 32.8 us; 32760 in 15, 21 (taken), 32, 42: 216,
-// 174, 201, 182 us; gradients of 1560 in 3, 7, 13 (taken), 25: 86, 53, 48.4, 65 us; of 8 x 4680 in 5 (taken), 6, 8, 10: 537, 580, 590, 604 us; 24 heads x 64: 5 x 2999 in
-// 4, 6 (taken), 8: 74, 63, 70 us; gradients of 5 x 999 in 1 (taken), 2, 4: 68.7, 70.3, 74.0 us (all before a block's norms were summed side by side, which takes 2 to 4 %).
+// by segment, and two launches.  12 heads x 128: 1560 tokens in 7, 9, 13 (taken), 25 segments 31.4, 27.6, 24.9, 32.7 us; 32760 in 15, 21 (taken), 32, 42: 210,
+// 169, 188, 176 us; gradients of 1560 in 3, 7, 13 (taken), 25: 84, 52.5, 48.5, 64 us; of 8 x 4680 in 5 (taken), 6, 8, 10: 518, 554, 564, 577 us; 24 heads x 64: 5 x 2999 in
+// 4, 6 (taken), 8: 71, 60.4, 67 us; gradients of 5 x 999 in 1 (taken), 2, 4: 61.7, 68.3, 71.9 us.  All pairs have the same number of segments, and some counts of pairs fit
+// the chip badly: 4096 tokens of 96, 128, 192, 256, 257, 320, 384, 448, 512 pairs x 128 take 177, 206, 243, 271, 430, 486, 486, 508, 534 us.
 ScanPlan scan_plan(int B, int H, int L, int D, bool backward)
 {
     ScanPlan p = {};
@@ -993,12 +994,12 @@ ScanPlan scan_plan(int B, int H, int L, int D, bool backward)
 
 hipError_t launch_scan_fwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
 {
-    return a.D == 128 ? launch_fwd<128, 2>(a, p, stream) : launch_fwd<64, 2>(a, p, stream);
+    return a.D == 128 ? launch_fwd<128>(a, p, stream) : launch_fwd<64>(a, p, stream);
 }
 
 hipError_t launch_scan_bwd(const ScanArgs &a, const ScanPlan &p, hipStream_t stream)
 {
-    return a.D == 128 ? launch_bwd<128, 2, 1>(a, p, stream) : launch_bwd<64, 2, 2>(a, p, stream);
+    return a.D == 128 ? launch_bwd<128, 1>(a, p, stream) : launch_bwd<64, 2>(a, p, stream);
 }
 
 }  // namespace arl2
