@@ -406,8 +406,8 @@ arl2_status arl2_scan_fwd(const arl2_scan_desc *desc, const void *q, const void 
  *   dq, dk, dv  device bf16 [B][L][H][D], written (through the normalisation where there is one).
  *   dlog_alpha  device fp32 [B][L][H], written: the gradient of log_alpha as if it had no upper limit; zero at a gate of zero.  NULL: it is not wanted.
  *   dS0       device fp32 [B][H][D][D], written; NULL: it is not wanted.
- * The same ranges hold for features of dout and for the state's gradient.  Where l2_eps is below 1e-14, products dout.v have to be below 2^63 sqrt(l2_eps) too, and the
- * gradients of normalised rows, before the normalisation, below 2^127 l2_eps.
+ * Features of rows and of dout have to be below 2^15 (a row's product with its gradient holds four of them and a decay taken out), states and their gradients below 2^48.
+ * Where l2_eps is below 1e-14, products dout.v have to be below 2^63 sqrt(l2_eps) too, and the gradients of normalised rows, before the normalisation, below 2^127 l2_eps.
  * Of what the matrix cores take, dv and dS0 are rounded as out and S are; dq and dk, whose products with q' and k' add up to dlog_alpha over up to 1024
  * tokens, take the states and what enters them in three bf16 parts (to 2^-25; dlog_alpha is off by 5.5e-6 in the 2-norm at
  * most where it was looked at, by 8.1e-6 in one head, and by 2.1e-5 in one whose gates leave next to nothing of the state).  A NaN or an infinity in a row
