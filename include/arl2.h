@@ -410,7 +410,7 @@ arl2_status arl2_scan_fwd(const arl2_scan_desc *desc, const void *q, const void 
  * Where l2_eps is below 1e-14, products dout.v have to be below 2^63 sqrt(l2_eps) too, and the gradients of normalised rows, before the normalisation, below 2^127 l2_eps.
  * Of what the matrix cores take, dv and dS0 are rounded as out and S are; dq and dk, whose products with q' and k' add up to dlog_alpha over up to 1024
  * tokens, take the states and what enters them in three bf16 parts (to 2^-25; dlog_alpha is off by 5.5e-6 in the 2-norm at
- * most where it was looked at, by 8.1e-6 in one head, and by 2.1e-5 in one whose gates leave next to nothing of the state).  A NaN or an infinity in a row
+ * most where it was looked at, by 8.1e-6 in one head; a sum of such products that cancel, it is off by more of itself where gates leave next to nothing of the state).  A NaN or an infinity in a row
  * reaches gradients of its own stream and head alone, of tokens on either side of it.
  * What is written must overlap neither an input nor what else is written.  Deterministic.
  */

@@ -11,6 +11,7 @@ STATE = R.TWO
 # dlog_alpha: a token adds the state's part of q'.dq' and of k'.dk', and pairs' products that go in and out again as one fp32 value.  The state and what enters it are
 # in three parts (2^-25) and fp32 sums, so that a token's is off by 2^-22 of what a token has to do with the state, at least its product with itself, E's own
 # size or more; up to 1024 such errors add up in directions of their own, by 2^5: 2^-17 of the two in the 2-norm.  Three times that is 2^-15.4: TWO is 2^-15.4.
+# Not for gates that leave next to nothing of the state where dS is given: a token's product with dS, which goes in and out again, has nothing to do with the two.
 GATES = R.TWO
 
 
