@@ -393,8 +393,8 @@ size_t arl2_scan_bwd_workspace_bytes(const arl2_scan_desc *desc);
  * rounded to bf16 once.
  * Features of rows have to be below 2^16, the state below 2^48 (products of three of them have decays taken out, up to 2^64, before fp32 holds them).
  * Up to 8 tokens are computed in fp32 throughout, with the state read and written once.  A NaN or an infinity in
- * a row reaches outputs of the 64 tokens, counted from the first, that it lies in and of later ones, not of earlier blocks; the state keeps it also behind a gate of
- * zero, which multiplies by zero.  Deterministic.
+ * a token's rows or gate reaches outputs of that token and of later ones (in v: that feature alone), and the state, which keeps it also behind a gate of zero, which multiplies by zero.
+ * Deterministic.
  */
 arl2_status arl2_scan_fwd(const arl2_scan_desc *desc, const void *q, const void *k, const void *v, const float *log_alpha,
                           const int32_t *seq_len, const float *S0, void *out, float *S);

@@ -28,6 +28,7 @@ namespace {
 constexpr int kBlock = 64;                    // tokens
 constexpr int kStepTokens = 8;
 constexpr double kLog2e = 1.4426950408889634;
+typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
 constexpr float kZeroGate = -2839.f;           // below: a gate of zero (2^-4095.8, of which fp32 has nothing left), from which the gates' gradients begin anew
 
 enum Mode { kOut, kDq, kDk, kDv, kSum, kSumBack };       // the last two make states and no rows
@@ -75,6 +76,7 @@ struct Scalars {
         float red[D / 32][kBlock][3];
         struct { float later[3][32], earlier[3][32]; } pair;      // of the 32 x 32 pairs of a block: sums of G over s, over u
     };
+    int unclean;                                          // the state has columns of NaNs
 };
 
 __device__ __forceinline__ int tokens_of(const ScanArgs &a, int b)
@@ -133,6 +135,9 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t (&part)[N]
 __device__ __forceinline__ f32x16 mfma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 mfma(u32x4 a, bf16x8 b, f32x16 c) { return mfma(__builtin_bit_cast(bf16x8, a), b, c); }
 
+// Where two bf16 values are an infinity or a NaN: all bits of that half.
+__device__ __forceinline__ uint32_t not_finite(uint32_t two) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(u16x2, two & 0x7fff7fffu) >= (u16x2)0x7f80); }
+
 // Sum with the lane in the other half-wave, without LDS.
 __device__ __forceinline__ float halves_sum(float x)
 {
@@ -173,17 +178,22 @@ struct Walk {
     static constexpr bool HANDS_ON = ROWS && HALVES == 2, IN_PLACE = D == 64;
     static constexpr int LDS_ROWS = (ROWS ? 3 : 2) * C::MAT + (ROWS ? C::PMAT : 0) + (HANDS_ON && !IN_PLACE ? C::NW * 4096 : 0);
 
-    // `lds`: LDS_ROWS bytes.  Segment `seg` of (stream, head) bh.
-    static __device__ __forceinline__ void run(const ScanArgs &a, const Work &wk, int bh, int seg, unsigned char *lds, Scalars<D> &sc)
+    // `lds`: LDS_ROWS bytes.  Segment `seg` of (stream, head) bh.  True (of kOut alone): it is to be walked once more, `careful`.  A token's products with later ones are zeros,
+    // but zero times a NaN is not: a NaN or an infinity in a row of v makes its feature of earlier tokens of its 32 a NaN too, and its column of the state.  Where a state has come
+    // out so, the second walk takes what is not finite in v as zeros, and then that token's feature, the later ones' and the state's column are made NaNs.  (Rows of q and k reach
+    // the products of their own tokens and later ones alone.  To look at v's rows in every block took 3.5 to 4.5 % of the call.)
+    static __device__ __forceinline__ bool run(const ScanArgs &a, const Work &wk, int bh, int seg, unsigned char *lds, Scalars<D> &sc, bool careful = false)
     {
-        int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
+        int tid = threadIdx.x;
+        if (MODE == kOut) asm volatile("" : "+v"(tid), "+s"(bh), "+s"(seg));      // (else the first walk keeps the second one's addresses)
+        int lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), column = HALVES == 1 ? wave : wave % C::NC, half = HALVES == 1 ? 0 : wave / C::NC;
         const int b = bh / a.H, h = bh - b * a.H;
-        const int n = tokens_of(a, b);
+        const int tokens = tokens_of(a, b), n = careful ? __builtin_amdgcn_readfirstlane(tokens) : tokens;     // (behind the first walk's stores no scalar load)
         const int nblk = (n + kBlock - 1) / kBlock;
         const int blk0 = seg * wk.seg, blk1 = min(blk0 + wk.seg, nblk);
         const int nact = max(1, (nblk + wk.seg - 1) / wk.seg);
-        if (seg >= nact) return;                                  // (without tokens the first segment hands its state on)
+        if (seg >= nact) return false;                            // (without tokens the first segment hands its state on)
 
         const uint32_t rs = (uint32_t)a.H * D * 2;                // bytes from token to token
         const size_t stream = (size_t)b * a.L * rs;
@@ -347,6 +357,7 @@ struct Walk {
             fetch(block_at(0));
             fetch_gate(block_at(0));
             if (wave == GW) gates(0);
+            if (MODE == kOut && tid == 0) sc.unclean = 0;
             if (count > 1) fetch_gate(block_at(1));
             lds_barrier();
             if (MODE == kDq && tid == 0 && seg > 0 && a.dla != nullptr) anchor(seg, 1.f);
@@ -377,10 +388,15 @@ struct Walk {
             // tokens of 24 heads x 64 took 76.5 us, so 71.4, of 8 x 4680 tokens of 12 heads x 128 547 and 535.
             __builtin_amdgcn_s_setprio(1);
             norms(GRAD ? gz : gy, gx, buf);
+            if (MODE == kOut && careful)
+#pragma unroll
+                for (int r = 0; r < ROUNDS; ++r)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) gz[r][j] &= ~not_finite(gz[r][j]);
             if (ROWS) stage(gx, lx);
             stage(gy, ly);
             stage(gz, lz);
-            if (i + 1 < count) fetch(block_at(i + 1));
+            if (!careful && i + 1 < count) fetch(block_at(i + 1));
             const bool pairs = __builtin_amdgcn_readfirstlane(sc.pairs[buf]) != 0;
             lds_barrier();
 
@@ -657,6 +673,38 @@ struct Walk {
                     }
                 }
             } else lds_barrier();
+            if (careful && i + 1 < count) fetch(block_at(i + 1));     // (late: registers)
+        }
+
+        if (MODE == kOut && !careful && count > 0) {
+            if (!(st[0][0] == st[0][0])) sc.unclean = 1;          // (what is not finite makes all rows of its column NaNs)
+            lds_barrier();
+            if (__builtin_amdgcn_readfirstlane(sc.unclean) != 0) {
+                lds_barrier();
+                return true;
+            }
+        }
+        if (MODE == kOut && careful) {
+            asm volatile("" : "+v"(l32), "+v"(hh));               // (addresses are made now)
+            __threadfence();                                      // the rows have been written
+            __syncthreads();
+            const size_t column0 = ((size_t)b * a.L * a.H + h) * D + e0 + l32;
+            const int last = min(blk1 * kBlock, n) - 1;
+            bool seen = false;
+            for (int t0 = blk0 * kBlock; t0 <= last; t0 += 8) {   // (the last token as often as it takes to make eight)
+                uint16_t x[8];
+#pragma unroll
+                for (int t = 0; t < 8; ++t) x[t] = ((const uint16_t *)a.v)[column0 + (size_t)min(t0 + t, last) * a.H * D];
+#pragma unroll
+                for (int t = 0; t < 8; ++t) {
+                    seen |= (x[t] & 0x7fff) >= 0x7f80;
+                    if (seen && half == 0 && hh == 0) ((uint16_t *)a.out)[column0 + (size_t)min(t0 + t, last) * a.H * D] = 0x7fc0;
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < C::TPW; ++t)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) st[t][j] = seen ? __builtin_nanf("") : st[t][j];
         }
 
         // ---- the state at the end
@@ -685,6 +733,7 @@ struct Walk {
             if (tid == 0) anchor(nact, sc.fold[0]);
         }
         if (!ROWS && tid == 64 * GW) (MODE == kSum ? wk.decay_forth : wk.decay_back)[(size_t)bh * wk.nseg + seg] = exp2_of(seg_total);
+        return false;
     }
 
     // Product of 16 features of a row with the accumulator that lies over them.
@@ -711,7 +760,19 @@ __global__ __launch_bounds__((Cfg<D, HALVES>::NT), D == 64 ? 3 : 2) void scan_ou
     __shared__ __align__(16) unsigned char lds[W::LDS_ROWS];
     __shared__ __align__(16) Scalars<D> sc;
     const int id = xcd_contiguous_id(blockIdx.x, gridDim.x);
-    W::run(a, wk, id / wk.nseg, id % wk.nseg, lds, sc);
+    if (!W::run(a, wk, id / wk.nseg, id % wk.nseg, lds, sc)) return;
+    // Once more, with the arguments read again: the first walk has no scalar registers left to keep them in (16 x 4096 tokens of 16 heads took 280 us for 269).
+    struct Given { ScanArgs a; Work wk; };                        // (two arguments of like alignment lie so one behind the other)
+    static_assert(alignof(ScanArgs) == alignof(Work) && sizeof(Given) == sizeof(ScanArgs) + sizeof(Work) && sizeof(Given) % 8 == 0, "");
+    const __attribute__((address_space(4))) uint64_t *at = (const __attribute__((address_space(4))) uint64_t *)__builtin_amdgcn_kernarg_segment_ptr();
+    int block = blockIdx.x;
+    asm volatile("" : "+s"(at), "+s"(block));
+    uint64_t words[sizeof(Given) / 8];
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(Given) / 8); ++i) words[i] = at[i];
+    const Given given = __builtin_bit_cast(Given, words);
+    const int unit = xcd_contiguous_id(block, gridDim.x);
+    W::run(given.a, given.wk, unit / given.wk.nseg, unit % given.wk.nseg, lds, sc, true);
 }
 
 // Segments' own states, but for the last of the way forth.  `back`: the way back too, as every second workgroup; the first of the way back only where
